@@ -379,8 +379,7 @@ def _run_own(s):
         D.dtst_product(s["a"], s["sa"], s["b"], s["sb"], s["c"], bias=s["bias"])
         return s["c"]
     if kind == "linear_grad":
-        D.dtst_quantise(s["g"], s["q"], s["sq"])
-        D.dtst_quantise(s["g"], s["qt"], s["sqt"], transpose=True)
+        D.dtst_quantise(s["g"], s["q"], s["sq"], qt=s["qt"], scale_t=s["sqt"])
         D.dtst_product(s["q"], s["sq"], s["wt"], s["swt"], s["g_x"])
         D.dtst_product(s["qt"], s["sqt"], s["xt"], s["sxt"], s["g_w"])
         return {"g_x": s["g_x"], "g_w": s["g_w"]}
