@@ -13,6 +13,10 @@
  *   inverse partial DFT   Sec. V-A Eq. (dtst_inverse)
  *   adjoints              Sec. V-C (backward pass)
  *
+ * and, for models that march fields in time, the operators of a recurrent
+ * block on sequences of latent vectors: RMS norm, 8-bit products, a gated
+ * linear recurrence, and their backward passes.
+ *
  * Conventions shared by every call
  * --------------------------------
  * Dimensions are ordered (x, y, z, t); t is innermost in memory.
@@ -285,6 +289,153 @@ dtst_status dtst_plan_block_info(dtst_plan_t p, size_t* workspace_bytes, int* fu
  * in the array needs clearing: a call reads only entries it wrote before. */
 #define DTST_SCRATCH_BYTES ((size_t)64 << 20)
 dtst_status dtst_forward_noalloc(dtst_plan_t p, const float* x, void* xhat, int accumulate, void* stream);
+
+/* ---- operators on latent sequences --------------------------------------- */
+
+/* What a model that marches fields in time runs on (rows, features) tokens
+ * between the spectral layers: a token is one time step's coefficient vector
+ * (dtst_forward of a plan with one time step per batch entry).  Features are
+ * contiguous; every other axis has a stride.  Independent of any plan; the
+ * calls run on the current device, asynchronous on `stream`, allocate nothing
+ * and launch kernels only.  Operands need the alignment of their type unless
+ * said otherwise.  Outputs share no element with each other or with an input,
+ * except where a call says that they may be the same array.  All arithmetic,
+ * sums and states are in 32 bits; results are rounded once, to nearest even. */
+
+/* Element types. */
+enum {
+  DTST_F32 = 0,
+  DTST_BF16 = 1,
+  DTST_F16 = 2,
+  DTST_E4M3 = 3 /* 8 bits: 4 exponent and 3 fraction bits, no infinity, largest value 448 */
+};
+
+/* 8-bit arrays with scales.  An (R, K) array is R rows of codes (E4M3) of
+ * round_up(K, 128) bytes, the columns past K zero, at a row stride that is a
+ * multiple of 16 bytes on a 16-byte aligned pointer, and R rows of scales, one
+ * byte s for each 128 columns standing for 2^(s - 127), at a row stride that is
+ * a multiple of 4 bytes on a 4-byte aligned pointer.  A value is its code times
+ * its scale.  Powers of two lose no bits, and the matrix cores apply them
+ * inside the product.  The library writes the smallest scale >= 2^-126 that
+ * brings the block's largest magnitude to at most 448 (1 for a block of
+ * zeros), rounds to nearest even, and fills the last four bytes of a row of
+ * scales with 127; the values that are infinite or no number become the code
+ * of no number and do not count for the scale. */
+
+/* RMS norm with the residual's addition, row by row:
+ *   u = x + res,  rounded to the residual's type and stored in sum_out;
+ *   r = 1 / sqrt(mean_c u[c]^2 + eps)  (of u as stored),  rstd = r;
+ *   y[c] = u[c] r weight[c].
+ * x: (rows, cols) of x_type; res and sum_out: res_type, which is x_type or
+ * DTST_F32.  res may be NULL (u = x; sum_out may then be NULL too); sum_out may
+ * be NULL, or res itself (an update in place).  weight: cols fp32.  rstd: rows
+ * fp32, or NULL.  y: x_type, or DTST_E4M3 with `scale` (NULL otherwise); y may
+ * be x itself when the types agree.  Strides ld_* in elements, >= cols.
+ * eps >= 0.  cols <= 32768 (DTST_ERR_UNSUPPORTED above). */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld_x, ld_res, ld_sum, ld_y, ld_scale;
+  int32_t x_type, res_type, y_type;
+  float eps;
+} dtst_norm_desc;
+dtst_status dtst_rms_norm(const dtst_norm_desc* d, const void* x, const void* res, const float* weight, void* sum_out,
+                          void* y, void* scale, float* rstd, void* stream);
+
+/* Backward of dtst_rms_norm from its stored sum u and rstd, with h = u rstd and
+ * t = g_y weight:
+ *   g_u = rstd (t - h mean_c(t h)) + g_sum,   g_weight (+)= sum_rows g_y h.
+ * g_u is the gradient of both x and res.  g_y: x_type; u, g_sum and g_u:
+ * res_type; g_sum, the gradient that reaches sum_out from elsewhere, may be
+ * NULL, and g_u may be g_sum itself.  g_x: the same as g_u in x_type, or NULL.
+ * g_weight: cols fp32, overwritten or (accumulate = 1) added to.  The sum over
+ * rows has a fixed order.  workspace: dtst_rms_norm_adj_workspace bytes. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld_g_y, ld_u, ld_g_sum, ld_g_u, ld_g_x;
+  int32_t x_type, res_type;
+  int32_t accumulate;
+} dtst_norm_adj_desc;
+dtst_status dtst_rms_norm_adj_workspace(int64_t rows, int64_t cols, size_t* bytes);
+dtst_status dtst_rms_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
+                              const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of x, (rows, cols) of `type` at stride ld_x, in 8 bits: q and scale as
+ * a (rows, cols) array, and (or) its transpose, qt and scale_t as a
+ * (cols, rows) array with a scale for each 128 rows of x.  Either pair may be
+ * NULL.  With both, x is read once. */
+typedef struct {
+  int64_t rows, cols;
+  int64_t ld_x, ld_q, ld_scale, ld_qt, ld_scale_t;
+  int32_t type;
+} dtst_quantise_desc;
+dtst_status dtst_quantise(const dtst_quantise_desc* d, const void* x, void* q, void* scale, void* qt, void* scale_t,
+                          void* stream);
+
+/* Product of 8-bit arrays a (m, k) and b (n, k) along their rows:
+ *   c[i,j] = sum_l a[i,l] b[j,l] + bias[j]   (+ c[i,j] with accumulate = 1),
+ * c: (m, n) of c_type (DTST_F32, DTST_BF16 or DTST_F16) at stride ld_c; bias:
+ * n fp32, or NULL.  A linear layer's forward takes b = its weights (out, in);
+ * its data gradient takes the output's gradient and the weights' transpose,
+ * its weight gradient the transposes of the output's gradient and of the
+ * input (dtst_quantise writes both forms).  short_sums = 0: products and sums
+ * are exact to 32 bits (the codes go to the matrix cores as bf16, which holds
+ * them and their scales without loss; what a scale brings below 2^-126 loses
+ * low bits).  short_sums = 1 lets the library take the 8-bit matrix
+ * instruction, up to twice as fast: its sum of eight neighbouring products
+ * keeps 13 bits below the largest of them (1e-5 to 2e-5 of the result on
+ * normally distributed values), the sum of those sums 32 bits.  k and the
+ * strides up to 2^23 (DTST_ERR_UNSUPPORTED above).  workspace: dtst_product_workspace bytes; it
+ * is 0 for most sizes, and then workspace may be NULL. */
+typedef struct {
+  int64_t m, n, k;
+  int64_t ld_a, ld_a_scale, ld_b, ld_b_scale, ld_c;
+  int32_t c_type;
+  int32_t accumulate, short_sums;
+} dtst_product_desc;
+dtst_status dtst_product_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
+dtst_status dtst_product(const dtst_product_desc* d, const void* a, const void* a_scale, const void* b,
+                         const void* b_scale, const float* bias, void* c, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/* Gated linear recurrence along the steps, feature by feature, with the
+ * logistic function s(v) = 1 / (1 + exp(-v)):
+ *   h_t = s(z_t) h_{t-1} + (1 - s(z_t)) v_t,    y_t = h_t o_t s(o_t)
+ * (y_t = h_t without o).  z, v, o, y: (batch, steps, features) of `type`, each
+ * with a stride of batch entries and of steps, so they may be column ranges of
+ * one array.  h_zero: (batch, features) fp32, the state before the first step,
+ * NULL for zero; h_out: (batch, features) fp32, the state after the last, NULL
+ * if not wanted; it may be h_zero itself, which is a serving step with steps =
+ * 1.  lengths: batch int32 on the device, NULL for `steps` each; from
+ * lengths[b] (clamped to 0 .. steps) on, the state stands still, y is zero and
+ * z, v and o are not read.  states: (batch, ceil(steps / DTST_RECURRENCE_SPAN),
+ * features) fp32, the states before steps 0, SPAN, 2 SPAN, ... that the
+ * backward needs, NULL if not wanted.  workspace:
+ * dtst_recurrence_workspace bytes, any contents. */
+#define DTST_RECURRENCE_SPAN 128
+typedef struct {
+  int64_t batch, steps, features;
+  int64_t z_stride[2], v_stride[2], o_stride[2], y_stride[2]; /* of batch entries, of steps */
+  int64_t g_z_stride[2], g_v_stride[2], g_o_stride[2];        /* dtst_recurrence_adj only; y_stride: of g_y there */
+  int32_t type;
+} dtst_recurrence_desc;
+dtst_status dtst_recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type, size_t* bytes);
+dtst_status dtst_recurrence(const dtst_recurrence_desc* d, const void* z, const void* v, const void* o,
+                            const float* h_zero, const int32_t* lengths, void* y, float* h_out, float* states,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward of dtst_recurrence from its inputs and states.  With d_t the
+ * gradient that reaches h_t, d_t = g_y_t o_t s(o_t) + s(z_{t+1}) d_{t+1} and g_h
+ * (the gradient of h_out; NULL for zero) entering at the last step:
+ *   g_z_t = d_t (h_{t-1} - v_t) s(z_t) s(-z_t),   g_v_t = d_t s(-z_t),
+ *   g_o_t = g_y_t h_t s(o_t) (1 + o_t s(-o_t)),   g_hzero = s(z_0) d_0.
+ * g_y, g_z, g_v, g_o are of `type`; g_o NULL without o; g_hzero: (batch,
+ * features) fp32 or NULL, and may be g_h itself.  Gradients are zero past a
+ * sequence's length.  The workspace is dtst_recurrence_workspace bytes. */
+dtst_status dtst_recurrence_adj(const dtst_recurrence_desc* d, const void* z, const void* v, const void* o,
+                                const int32_t* lengths, const float* states, const void* g_y, const float* g_h,
+                                void* g_z, void* g_v, void* g_o, float* g_hzero, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 /* ---- instrumentation ----------------------------------------------------- */
 

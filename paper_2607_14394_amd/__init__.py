@@ -26,6 +26,9 @@ __all__ = [
     "dtst_inverse_block", "dtst_pointwise", "dtst_forward_noalloc", "dtst_profile_enable",
     "dtst_profile_collect", "dtst_plan_block_info", "Schedule", "dtst_desc_schedule", "Plan", "LIB_PATH",
     "PLAN_SPLIT_SCHEDULE", "PLAN_UNFUSED_BLOCK", "SCRATCH_BYTES", "torch_stream",
+    "RECURRENCE_SPAN", "code_columns", "scale_columns", "empty_codes", "recurrence_states_shape", "dtst_rms_norm",
+    "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product", "dtst_product_workspace",
+    "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdtst.so")
@@ -68,6 +71,41 @@ class Schedule(ctypes.Structure):
                  "z_mirrored", "y_parts")]
 
 
+class NormDesc(ctypes.Structure):
+    """dtst_norm_desc."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_res", "ld_sum", "ld_y", "ld_scale")]
+                + [(n, ctypes.c_int32) for n in ("x_type", "res_type", "y_type")] + [("eps", ctypes.c_float)])
+
+
+class NormAdjDesc(ctypes.Structure):
+    """dtst_norm_adj_desc."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_g_y", "ld_u", "ld_g_sum", "ld_g_u", "ld_g_x")]
+                + [(n, ctypes.c_int32) for n in ("x_type", "res_type", "accumulate")])
+
+
+class QuantiseDesc(ctypes.Structure):
+    """dtst_quantise_desc."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_q", "ld_scale", "ld_qt", "ld_scale_t")]
+                + [("type", ctypes.c_int32)])
+
+
+class ProductDesc(ctypes.Structure):
+    """dtst_product_desc."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("m", "n", "k", "ld_a", "ld_a_scale", "ld_b", "ld_b_scale", "ld_c")]
+                + [(n, ctypes.c_int32) for n in ("c_type", "accumulate", "short_sums")])
+
+
+class RecurrenceDesc(ctypes.Structure):
+    """dtst_recurrence_desc."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("batch", "steps", "features")]
+                + [(n + "_stride", ctypes.c_int64 * 2) for n in ("z", "v", "o", "y", "g_z", "g_v", "g_o")]
+                + [("type", ctypes.c_int32)])
+
+
+# DTST_F32 .. DTST_E4M3 of include/dtst.h
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
+RECURRENCE_SPAN = 128        # DTST_RECURRENCE_SPAN of include/dtst.h
+
 # DTST_ROWS_* and DTST_BLOCK_* of include/dtst.h
 ROWS_T_FIRST, ROWS_T_FIRST_Y, ROWS_Z_FIRST, ROWS_Z_FIRST_Y = range(4)
 BLOCK_SEPARATE, BLOCK_CHUNKS, BLOCK_ROW_TASKS = range(3)
@@ -100,6 +138,15 @@ def _load():
         "dtst_inverse_block": [P, VP, VP, VP, VP, VP, SZ, VP],
         "dtst_pointwise": [VP, VP, VP, VP, I64, I64, I64, I64, I, VP],
         "dtst_forward_noalloc": [P, VP, VP, I, VP],
+        "dtst_rms_norm": [VP] * 9,
+        "dtst_rms_norm_adj_workspace": [I64, I64, ctypes.POINTER(SZ)],
+        "dtst_rms_norm_adj": [VP] * 10 + [SZ, VP],
+        "dtst_quantise": [VP] * 7,
+        "dtst_product_workspace": [I64, I64, I64, ctypes.POINTER(SZ)],
+        "dtst_product": [VP] * 8 + [SZ, VP],
+        "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
+        "dtst_recurrence": [VP] * 10 + [SZ, VP],
+        "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -287,6 +334,234 @@ def dtst_pointwise(x, w, bias, y, act=0, stream=None):
 def dtst_mix_wgrad(plan, xhat, g_yhat, g_w_shard, m0, m1, accumulate, stream=None):
     _check(lib.dtst_mix_wgrad(plan, _ptr(xhat), _ptr(g_yhat), _ptr(g_w_shard), int(m0), int(m1), int(accumulate),
                               _stream(stream)))
+
+
+# ---- operators on latent sequences (device tensors) --------------------------
+# Shape, type and device checks here, arithmetic in the library.  A workspace
+# that is not given is allocated for the call.
+
+def code_columns(k):
+    """Columns of the codes of rows of k values."""
+    return (k + 127) // 128 * 128
+
+
+def scale_columns(k):
+    """Columns of the scales of rows of k values."""
+    return ((k + 127) // 128 + 3) // 4 * 4
+
+
+def empty_codes(rows, k, device="cuda"):
+    """Codes (float8_e4m3fn) and scales (float8_e8m0fnu) for rows of k values."""
+    return (torch.empty((rows, code_columns(k)), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((rows, scale_columns(k)), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def recurrence_states_shape(batch, steps, features):
+    return (batch, -(-steps // RECURRENCE_SPAN), features)
+
+
+def _rows(t, shape, name, dtypes):
+    """Row stride of a 2-D tensor on the current device with contiguous rows."""
+    if t.shape != shape or t.dtype not in dtypes or not _here(t):
+        raise ValueError(f"{name}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)} on the current "
+                         f"device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    st = t.stride()
+    if st[1] != 1 and shape[1] > 1 and shape[0]:
+        raise ValueError(f"{name}: columns must be contiguous")
+    # (the stride of a single row is any; one that suits every type)
+    return st[0] if shape[0] > 1 else -(-shape[1] // 16) * 16
+
+
+def _vector(t, n, name, dtype=torch.float32):
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or not _here(t):
+        raise ValueError(f"{name}: need contiguous {dtype} of shape ({n},) on the current device")
+
+
+def _here(t):
+    """Whether t is on the current device."""
+    return t.is_cuda and t.get_device() == torch.cuda.current_device()
+
+
+_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
+_CODES, _SCALES = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu,)
+
+
+def _codes(q, s, rows, k, name):
+    return (_rows(q, (rows, code_columns(k)), name, _CODES),
+            _rows(s, (rows, scale_columns(k)), name + " scale", _SCALES))
+
+
+def _scratch(ws, need, device, stream):
+    """Pointer and bytes of the workspace, and what keeps it until the launch."""
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None and int(stream) != torch_stream():
+            ws.record_stream(torch.cuda.ExternalStream(int(stream)))
+    return _wsargs(ws) + (ws,)
+
+
+def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, eps=1e-6, stream=None):
+    """u = x + res into sum_out, y = u / rms(u) * weight; y in x's type, or
+    codes with their scales.  x, res, sum_out: (rows, cols)."""
+    if x.dim() != 2:
+        raise ValueError("x must be (rows, cols)")
+    shape = rows, cols = tuple(x.shape)
+    tx = (x.dtype,)
+    rt = sum_out.dtype if res is None and sum_out is not None else x.dtype if res is None else res.dtype
+    d = NormDesc(rows, cols, _rows(x, shape, "x", _FLOATS),
+                 0 if res is None else _rows(res, shape, "res", (x.dtype, torch.float32)),
+                 0 if sum_out is None else _rows(sum_out, shape, "sum_out", (rt,)), 0, 0,
+                 _TYPES[x.dtype], _TYPES[rt], _TYPES.get(y.dtype, -1), eps)
+    if scale is not None:
+        d.ld_y, d.ld_scale = _codes(y, scale, rows, cols, "y")
+    else:
+        d.ld_y = _rows(y, shape, "y", tx)
+    _vector(weight, cols, "weight")
+    if rstd is not None:
+        _vector(rstd, rows, "rstd")
+    _check(lib.dtst_rms_norm(ctypes.addressof(d), _ptr(x), _ptr(res), _ptr(weight), _ptr(sum_out), _ptr(y), _ptr(scale),
+                             _ptr(rstd), _stream(stream)))
+
+
+def dtst_rms_norm_adj_workspace(rows, cols) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_rms_norm_adj_workspace(int(rows), int(cols), ctypes.byref(n)))
+    return n.value
+
+
+def dtst_rms_norm_adj(g_y, u, weight, rstd, g_u, g_weight, g_sum=None, g_x=None, accumulate=False, ws=None,
+                      stream=None):
+    """Backward of dtst_rms_norm from its stored sum u and rstd: g_u (of x and
+    res alike; g_x the same in g_y's type) and g_weight."""
+    if g_y.dim() != 2:
+        raise ValueError("g_y must be (rows, cols)")
+    shape = rows, cols = tuple(g_y.shape)
+    tr = (u.dtype,)
+    d = NormAdjDesc(rows, cols, _rows(g_y, shape, "g_y", _FLOATS), _rows(u, shape, "u", (g_y.dtype, torch.float32)),
+                    0 if g_sum is None else _rows(g_sum, shape, "g_sum", tr), _rows(g_u, shape, "g_u", tr),
+                    0 if g_x is None else _rows(g_x, shape, "g_x", (g_y.dtype,)), _TYPES[g_y.dtype], _TYPES[u.dtype],
+                    int(accumulate))
+    _vector(weight, cols, "weight")
+    _vector(g_weight, cols, "g_weight")
+    _vector(rstd, rows, "rstd")
+    p, n, ws = _scratch(ws, dtst_rms_norm_adj_workspace(rows, cols) if ws is None else 0, g_y.device, stream)
+    _check(lib.dtst_rms_norm_adj(ctypes.addressof(d), _ptr(g_y), _ptr(u), _ptr(weight), _ptr(rstd), _ptr(g_sum),
+                                 _ptr(g_u), _ptr(g_x), _ptr(g_weight), p, n, _stream(stream)))
+
+
+def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
+    """Rows of x (rows, cols) as codes and scales into q and scale, and (or)
+    its transpose's rows into qt and scale_t."""
+    if x.dim() != 2:
+        raise ValueError("x must be (rows, cols)")
+    if (q is None) != (scale is None) or (qt is None) != (scale_t is None) or (q is None and qt is None):
+        raise ValueError("need q with scale, or qt with scale_t, or all four")
+    rows, cols = x.shape
+    d = QuantiseDesc(rows, cols, _rows(x, (rows, cols), "x", _FLOATS), 0, 0, 0, 0, _TYPES[x.dtype])
+    if q is not None:
+        d.ld_q, d.ld_scale = _codes(q, scale, rows, cols, "q")
+    if qt is not None:
+        d.ld_qt, d.ld_scale_t = _codes(qt, scale_t, cols, rows, "qt")
+    _check(lib.dtst_quantise(ctypes.addressof(d), _ptr(x), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t),
+                             _stream(stream)))
+
+
+def dtst_product_workspace(m, n, k) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib.dtst_product_workspace(int(m), int(n), int(k), ctypes.byref(b)))
+    return b.value
+
+
+def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_sums=False, ws=None, stream=None):
+    """c = a b^T + bias (+ c): codes a (m, k) and b (n, k) with their scales
+    into c (m, n).  short_sums: allow the 8-bit matrix instruction's sums."""
+    if c.dim() != 2 or a.dim() != 2:
+        raise ValueError("a and c must be (m, k) and (m, n)")
+    m, n = c.shape
+    k = a.shape[1]
+    d = ProductDesc(m, n, k, *_codes(a, a_scale, m, k, "a"), *_codes(b, b_scale, n, k, "b"),
+                    _rows(c, (m, n), "c", _FLOATS), _TYPES[c.dtype], int(accumulate), int(short_sums))
+    if bias is not None:
+        _vector(bias, n, "bias")
+    p, nb, ws = _scratch(ws, dtst_product_workspace(m, n, k) if ws is None else 0, c.device, stream)
+    _check(lib.dtst_product(ctypes.addressof(d), _ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), _ptr(c), p,
+                            nb, _stream(stream)))
+
+
+def dtst_recurrence_workspace(batch, steps, features, dtype) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_recurrence_workspace(int(batch), int(steps), int(features), _TYPES[dtype], ctypes.byref(n)))
+    return n.value
+
+
+def _sequence(t, shape, name, dtype):
+    """Strides of batch entries and steps of a (batch, steps, features) tensor."""
+    if t.shape != shape or t.dtype != dtype or not _here(t):
+        raise ValueError(f"{name}: need {dtype} of shape {tuple(shape)} on the current device, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    st = t.stride()
+    if st[2] != 1 and shape[2] > 1 and t.numel():
+        raise ValueError(f"{name}: features must be contiguous")
+    return st[:2]
+
+
+def _state(t, shape, name):
+    if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or not _here(t):
+        raise ValueError(f"{name}: need contiguous torch.float32 of shape {tuple(shape)} on the current device")
+
+
+def dtst_recurrence(z, v, y, o=None, h0=None, h_out=None, lengths=None, states=None, ws=None, stream=None):
+    """h_t = s(z_t) h_{t-1} + (1 - s(z_t)) v_t, y_t = h_t o_t s(o_t) along the
+    steps of (batch, steps, features); h0, h_out: (batch, features) float32,
+    lengths: (batch,) int32, states: recurrence_states_shape float32."""
+    if z.dim() != 3:
+        raise ValueError("z must be (batch, steps, features)")
+    shape = B, T, F = tuple(z.shape)
+    e = z.dtype
+    if e not in _FLOATS:
+        raise ValueError(f"z: need {' or '.join(str(d) for d in _FLOATS)}")
+    d = RecurrenceDesc(B, T, F, _sequence(z, shape, "z", e), _sequence(v, shape, "v", e),
+                       (0, 0) if o is None else _sequence(o, shape, "o", e), _sequence(y, shape, "y", e))
+    d.type = _TYPES[e]
+    for t, name in ((h0, "h0"), (h_out, "h_out")):
+        if t is not None:
+            _state(t, (B, F), name)
+    if states is not None:
+        _state(states, recurrence_states_shape(B, T, F), "states")
+    if lengths is not None:
+        _vector(lengths, B, "lengths", torch.int32)
+    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e) if ws is None and T > 1 else 0, z.device, stream)
+    _check(lib.dtst_recurrence(ctypes.addressof(d), _ptr(z), _ptr(v), _ptr(o), _ptr(h0), _ptr(lengths), _ptr(y),
+                               _ptr(h_out), _ptr(states), p, n, _stream(stream)))
+
+
+def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None, g_hzero=None, lengths=None, ws=None,
+                        stream=None):
+    """Backward of dtst_recurrence from its inputs and states: g_z, g_v, g_o
+    and, from the gradient g_h of the last state, g_hzero of the first."""
+    if z.dim() != 3:
+        raise ValueError("z must be (batch, steps, features)")
+    shape = B, T, F = tuple(z.shape)
+    e = z.dtype
+    if e not in _FLOATS:
+        raise ValueError(f"z: need {' or '.join(str(d) for d in _FLOATS)}")
+    if (o is None) != (g_o is None):
+        raise ValueError("g_o goes with o")
+    none = (0, 0)
+    d = RecurrenceDesc(B, T, F, _sequence(z, shape, "z", e), _sequence(v, shape, "v", e),
+                       none if o is None else _sequence(o, shape, "o", e), _sequence(g_y, shape, "g_y", e),
+                       _sequence(g_z, shape, "g_z", e), _sequence(g_v, shape, "g_v", e),
+                       none if g_o is None else _sequence(g_o, shape, "g_o", e), _TYPES[e])
+    for t, name in ((g_h, "g_h"), (g_hzero, "g_hzero")):
+        if t is not None:
+            _state(t, (B, F), name)
+    _state(states, recurrence_states_shape(B, T, F), "states")
+    if lengths is not None:
+        _vector(lengths, B, "lengths", torch.int32)
+    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e) if ws is None else 0, z.device, stream)
+    _check(lib.dtst_recurrence_adj(ctypes.addressof(d), _ptr(z), _ptr(v), _ptr(o), _ptr(lengths), _ptr(states),
+                                   _ptr(g_y), _ptr(g_h), _ptr(g_z), _ptr(g_v), _ptr(g_o), _ptr(g_hzero), p, n,
+                                   _stream(stream)))
 
 
 def dtst_profile_enable(on=True):

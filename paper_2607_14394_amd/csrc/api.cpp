@@ -14,6 +14,7 @@
 #include <unordered_set>
 #include <vector>
 
+#include "api_common.h"
 #include "dtst_internal.h"
 
 struct dtst_plan_st {
@@ -24,7 +25,7 @@ struct dtst_plan_st {
 
 namespace {
 
-thread_local std::string g_last_error;
+using namespace dtst;
 
 std::mutex g_plans_mu;
 std::unordered_set<const dtst_plan_st*>& live_plans() {
@@ -32,22 +33,10 @@ std::unordered_set<const dtst_plan_st*>& live_plans() {
   return s;
 }
 
-dtst_status fail(dtst_status s, const std::string& msg) {
-  g_last_error = msg;
-  return s;
-}
-
-dtst_status ok() {
-  g_last_error.clear();
-  return DTST_OK;
-}
-
 bool is_live(const dtst_plan_st* p) {
   std::lock_guard<std::mutex> lk(g_plans_mu);
   return p != nullptr && live_plans().count(p) != 0;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Makes the plan's device current for the duration of a call.
 struct DeviceGuard {
@@ -66,19 +55,8 @@ struct DeviceGuard {
   }
 };
 
-dtst_status device_status(int e, const char* what) {
-  if (e == hipSuccess) return ok();
-  return fail(DTST_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(static_cast<hipError_t>(e)));
-}
-
 dtst_status check_plan(const dtst_plan_st* p) {
   if (!is_live(p)) return fail(DTST_ERR_INVALID_ARG, "plan is null or was destroyed");
-  return DTST_OK;
-}
-
-dtst_status check_ptr(const void* ptr, const char* name) {
-  if (ptr == nullptr) return fail(DTST_ERR_INVALID_ARG, std::string(name) + " is null");
-  if (!aligned16(ptr)) return fail(DTST_ERR_INVALID_ARG, std::string(name) + " is not 16-byte aligned");
   return DTST_OK;
 }
 
@@ -88,72 +66,6 @@ dtst_status check_ws(const dtst_plan_st* p, const void* ws, size_t ws_bytes) {
                                           " bytes, got " + std::to_string(ws_bytes));
   if (p->dv.ws_bytes > 0) return check_ptr(ws, "workspace");
   return DTST_OK;
-}
-
-#define DTST_TRY(expr)                 \
-  do {                                 \
-    dtst_status s_ = (expr);           \
-    if (s_ != DTST_OK) return s_;      \
-  } while (0)
-
-// ---- per-kernel event timing (dtst_profile_enable / dtst_profile_collect) ----
-enum KernelRole { K_FWD_TZ, K_AXIS_FWD_Y, K_AXIS_FWD_X, K_AXIS_INV_X, K_AXIS_INV_Y, K_INV_ZT, K_MIX, K_MIX_H,
-                  K_WGRAD, K_BLOCK, K_FWD_TZY, K_INV_YZT, K_POINTWISE, K_INV_ZT_BLOCK, K_COUNT };
-const char* const kRoleNames[K_COUNT] = {"stream_fwd_tz", "axis_fwd_y", "axis_fwd_x", "axis_inv_x", "axis_inv_y",
-                                         "stream_inv_zt", "mix", "mix_h", "wgrad", "block_epilogue",
-                                         "stream_fwd_tzy", "stream_inv_yzt", "pointwise", "stream_inv_zt_block"};
-
-struct Profiler {
-  std::mutex mu;
-  bool on = false;
-  struct Rec {
-    int role;
-    hipEvent_t a, b;
-  };
-  std::vector<Rec> pending;
-  std::vector<hipEvent_t> pool;
-  double total_ms[K_COUNT] = {};
-  int64_t launches[K_COUNT] = {};
-  hipEvent_t get() {
-    if (!pool.empty()) {
-      hipEvent_t e = pool.back();
-      pool.pop_back();
-      return e;
-    }
-    hipEvent_t e = nullptr;
-    if (hipEventCreate(&e) != hipSuccess) return nullptr;
-    return e;
-  }
-};
-Profiler& prof() {
-  static Profiler p;
-  return p;
-}
-
-// Runs one launcher; when profiling is on, brackets it with events on `stream`.
-template <class F>
-int timed(int role, void* stream, F&& launch) {
-  Profiler& P = prof();
-  bool on;
-  {
-    std::lock_guard<std::mutex> lk(P.mu);
-    on = P.on;
-  }
-  if (!on) return launch();
-  hipEvent_t a, b;
-  {
-    std::lock_guard<std::mutex> lk(P.mu);
-    a = P.get();
-    b = P.get();
-  }
-  if (a == nullptr || b == nullptr) return launch();
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  (void)hipEventRecord(a, s);
-  const int e = launch();
-  (void)hipEventRecord(b, s);
-  std::lock_guard<std::mutex> lk(P.mu);
-  P.pending.push_back({role, a, b});
-  return e;
 }
 
 // Forward-direction chain: streaming t+z, then y (one fused launch when the
@@ -281,7 +193,7 @@ const char* dtst_status_string(dtst_status s) {
   return "DTST_ERR_UNKNOWN";
 }
 
-const char* dtst_last_error(void) { return g_last_error.c_str(); }
+const char* dtst_last_error(void) { return last_error().c_str(); }
 
 dtst_status dtst_desc_validate(const dtst_desc* d) { return validate_ex(d, 0); }
 

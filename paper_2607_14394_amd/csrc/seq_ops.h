@@ -1,0 +1,106 @@
+// Device helpers of the latent-sequence operators: element types, vector
+// access at any alignment, wave reductions, 8-bit codes and their scales.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "dtst.h"
+
+namespace dtst {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+// N elements of T at the alignment of T.  gfx950 takes 16-byte accesses at any
+// alignment of global memory, so odd strides and column ranges keep the wide
+// form.
+template <class T, int N>
+struct pack_of {
+  typedef T raw __attribute__((ext_vector_type(N)));
+  typedef raw type __attribute__((aligned(alignof(T))));
+};
+template <class T, int N>
+using pack_t = typename pack_of<T, N>::type;
+
+// p[0..N) as floats; entries from n on are zero and not read.
+template <int N, class T>
+__device__ __forceinline__ void load_n(const T* p, int64_t n, float (&out)[N]) {
+  if (n >= N) {
+    const pack_t<T, N> v = *reinterpret_cast<const pack_t<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = float(v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = i < n ? float(p[i]) : 0.f;
+  }
+}
+
+template <int N, class T>
+__device__ __forceinline__ void store_n(T* p, int64_t n, const float (&v)[N]) {
+  if (n >= N) {
+    typename pack_of<T, N>::raw r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = T(v[i]);
+    *reinterpret_cast<pack_t<T, N>*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = T(v[i]);
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+
+// The value of lane ^ partner within 16 lanes, rotated by R (1, 2, 4 or 8).
+template <int R>
+__device__ __forceinline__ float row_rotate(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + R, 0xf, 0xf, false));
+}
+
+// Largest of the 16 lanes of a row of lanes.
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, row_rotate<1>(v));
+  v = fmaxf(v, row_rotate<2>(v));
+  v = fmaxf(v, row_rotate<4>(v));
+  return fmaxf(v, row_rotate<8>(v));
+}
+
+// |v|, or zero where v is infinite or no number (those do not count for a
+// block's scale).
+__device__ __forceinline__ float finite_abs(float v) {
+  const float a = fabsf(v);
+  return a <= 3.402823466e38f ? a : 0.f;
+}
+
+// The scale byte of a block whose largest magnitude is amax >= 0: the smallest
+// power of two 2^e, e >= -126, with amax <= 448 * 2^e; 448 = 1.75 * 2^8, so e is
+// amax's exponent less 8, one more when its significand is above 1.75.
+__device__ __forceinline__ uint32_t scale_byte(float amax) {
+  const uint32_t bits = __float_as_uint(amax);
+  const int e = int(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return amax == 0.f ? 127u : uint32_t(e < 1 ? 1 : e);
+}
+
+// 2^-(s - 127), the factor that brings a block's values to code range
+// (s = 1 .. 247, so 2^126 .. 2^-120).
+__device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }
+
+// Four values to four codes, nearest even; what is infinite or no number
+// becomes the code of no number (0x7f).  In range otherwise.
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+  const float nan = __uint_as_float(0x7fc00000u);
+  a = fabsf(a) <= 448.f ? a : nan;
+  b = fabsf(b) <= 448.f ? b : nan;
+  c = fabsf(c) <= 448.f ? c : nan;
+  d = fabsf(d) <= 448.f ? d : nan;
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
+}
+
+}  // namespace dtst
