@@ -331,6 +331,12 @@ bool share(const dtst_recurrence_desc* d, const Sequence& a, const Sequence& b, 
   return pa == pb;
 }
 
+// (one workgroup of 64 lanes a step's features, or of 512 for each 128 steps)
+dtst_status check_recurrence_grid(const dtst_recurrence_desc* d) {
+  const int64_t tiles = d->batch * ((d->features + 63) / 64), spans = (d->steps + 127) / 128;
+  return check_grid(tiles * (spans > 0 ? spans : 1), d->steps <= 1 ? 64 : 512);
+}
+
 dtst_status check_no_share(const dtst_recurrence_desc* d, const Sequence& out, const Sequence& other, int size) {
   if (share(d, out, other, size)) return bad(std::string(out.name) + " and " + other.name + " overlap");
   return DTST_OK;
@@ -356,6 +362,7 @@ dtst_status recurrence(const dtst_recurrence_desc* d, const void* z, const void*
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
   DTST_TRY(check_workspace(workspace, workspace_bytes,
                            recurrence_workspace(d->batch, d->steps, d->features, d->type)));
+  DTST_TRY(check_recurrence_grid(d));
   const int e = timed(K_RECUR, stream, [&] {
     return launch_recurrence(*d, z, v, o, h_zero, lengths, y, h_out, states, workspace, stream);
   });
@@ -388,6 +395,7 @@ dtst_status recurrence_adj(const dtst_recurrence_desc* d, const void* z, const v
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
   DTST_TRY(check_workspace(workspace, workspace_bytes,
                            recurrence_workspace(d->batch, d->steps, d->features, d->type)));
+  DTST_TRY(check_recurrence_grid(d));
   const int e = timed(K_RECUR_ADJ, stream, [&] {
     return launch_recurrence_adj(*d, z, v, o, lengths, states, g_y, g_h, g_z, g_v, g_o, g_hzero, workspace, stream);
   });

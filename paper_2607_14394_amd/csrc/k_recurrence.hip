@@ -1,7 +1,25 @@
 // Gated linear recurrence along the steps and its backward (dtst_recurrence,
 // dtst_recurrence_adj):
 //   h_t = s(z_t) h_{t-1} + s(-z_t) v_t,   y_t = h_t o_t s(o_t).
-// A few operations per value: bound by HBM (z, v, o read, y written).
+//
+// A few operations per value: bound by HBM (z, v, o read and y written once;
+// backward: z, v, o, g_y read and g_z, g_v, g_o written once).  Long sequences
+// of few features have to be divided along the steps to keep the card's loads in
+// flight.  A run of steps maps the state that enters it to the one that leaves
+// it as h -> A h + H (A the product of its gates, H its end from a zero state),
+// and two neighbouring runs compose to such a map.  So a workgroup takes SPAN
+// steps of 128 features: its waves hold 16 steps each in registers (a lane two
+// neighbouring features), form their maps, and meet in LDS; the workgroup
+// publishes its span's map, composes those of the spans before it until it meets
+// one whose leaving state is known already, publishes its own, and runs its
+// steps from the state that enters.  Every value is read once.  The backward runs
+// the same scheme from the last span to the first on d_t's carry,
+// e_{t-1} = s(z_t) (g_t + e_t), g_t = g_y_t o_t s(o_t), and takes the states from
+// the one that the forward kept for each span.
+//
+// Waiting ends: spans are taken by ticket, spans earlier in the chain have
+// earlier tickets, so a workgroup waits only for workgroups that already run,
+// and the earliest of those waits for none.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,13 +31,15 @@ namespace dtst {
 namespace {
 
 constexpr int SPAN = DTST_RECURRENCE_SPAN;
+constexpr int WAVES = 8;
+constexpr int RPW = SPAN / WAVES;  // steps of a wave
 
 // s(x) and s(-x), both to full relative precision (1 - s(x) would lose it).
 // Infinities give 0 and 1, no number gives no number.
 __device__ __forceinline__ void logistic(float x, float& s, float& sn) {
-  const float e = __expf(-fabsf(x)), r = 1.f / (1.f + e);
-  s = x >= 0.f ? r : e * r;
-  sn = x >= 0.f ? e * r : r;
+  const float e = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
+  s = x >= 0.f ? r : er;
+  sn = x >= 0.f ? er : r;
 }
 
 struct Strides {
@@ -31,6 +51,10 @@ struct Args {
   int64_t batch, steps, features;
   Strides z, v, o, y, gz, gv, go;
   const int32_t* lengths;
+  int64_t tiles, feature_tiles;  // tiles = batch * feature_tiles, one a workgroup's features
+  int spans;
+  unsigned long long* maps;  // (tiles, spans, 64 CPL) words of the chain
+  unsigned* ticket;
 };
 
 __device__ __forceinline__ int64_t length_of(const Args& p, int64_t b) {
@@ -39,89 +63,424 @@ __device__ __forceinline__ int64_t length_of(const Args& p, int64_t b) {
   return n < 0 ? 0 : n > p.steps ? p.steps : n;
 }
 
-// One lane a feature of a sequence, step by step.
-template <class T>
-__global__ void __launch_bounds__(64)
-recurrence_serial_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zero, T* y, float* h_out,
-                         float* states) {
-  const int64_t i = int64_t(blockIdx.x) * 64 + threadIdx.x;
-  if (i >= p.batch * p.features) return;
-  const int64_t b = i / p.features, c = i % p.features, n = length_of(p, b);
-  const int64_t spans = (p.steps + SPAN - 1) / SPAN;
-  float h = h_zero ? h_zero[i] : 0.f;
-  for (int64_t t = 0; t < p.steps; ++t) {
-    if (states != nullptr && t % SPAN == 0) states[(b * spans + t / SPAN) * p.features + c] = h;
-    float r = 0.f;
-    if (t < n) {
-      float s, sn, so, son;
-      logistic(float(z[at(p.z, b, t) + c]), s, sn);
-      h = s * h + sn * float(v[at(p.v, b, t) + c]);
-      r = h;
-      if (o != nullptr) {
-        const float ot = float(o[at(p.o, b, t) + c]);
-        logistic(ot, so, son);
-        r = h * ot * so;
-      }
-    }
-    y[at(p.y, b, t) + c] = T(r);
-  }
-  if (h_out != nullptr) h_out[i] = h;
+// A span's map in a word of the chain: A >= 0 with its sign bit set (a word of
+// zeros: not there yet) and H.  A = 0 says that H is the leaving state itself;
+// a product that underflows is kept above zero, so that no number stays one.
+__device__ __forceinline__ unsigned long long map_word(float A, float H) {
+  const unsigned a = (A == 0.f ? 1u : __float_as_uint(A)) | 0x80000000u;
+  return (unsigned long long)(__float_as_uint(H)) << 32 | a;
+}
+__device__ __forceinline__ unsigned long long state_word(float h) {
+  return (unsigned long long)(__float_as_uint(h)) << 32 | 0x80000000u;
+}
+__device__ __forceinline__ void put_word(unsigned long long* p, unsigned long long w) {
+  __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long get_word(const unsigned long long* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Backward: the spans from the last to the first, the states inside a span
-// again from its first.
-template <class T>
-__global__ void __launch_bounds__(64)
-recurrence_adj_serial_kernel(Args p, const T* z, const T* v, const T* o, const float* states, const T* g_y,
-                             const float* g_h, T* g_z, T* g_v, T* g_o, float* g_hzero) {
-  const int64_t i = int64_t(blockIdx.x) * 64 + threadIdx.x;
-  if (i >= p.batch * p.features) return;
-  const int64_t b = i / p.features, c = i % p.features, n = length_of(p, b);
-  const int64_t spans = (p.steps + SPAN - 1) / SPAN;
-  float d = g_h ? g_h[i] : 0.f;
-  for (int64_t k = spans - 1; k >= 0; --k) {
-    float h[SPAN + 1];
-    h[0] = states[(b * spans + k) * p.features + c];
-    const int64_t t0 = k * SPAN, len = p.steps - t0 < SPAN ? p.steps - t0 : SPAN;
-    for (int j = 0; j < len; ++j) {
-      h[j + 1] = h[j];
-      if (t0 + j >= n) continue;
-      float s, sn;
-      logistic(float(z[at(p.z, b, t0 + j) + c]), s, sn);
-      h[j + 1] = s * h[j] + sn * float(v[at(p.v, b, t0 + j) + c]);
-    }
-    for (int j = int(len) - 1; j >= 0; --j) {
-      const int64_t t = t0 + j;
-      float gz = 0.f, gv = 0.f, go = 0.f;
-      if (t < n) {
-        float s, sn;
-        logistic(float(z[at(p.z, b, t) + c]), s, sn);
-        float gy = float(g_y[at(p.y, b, t) + c]);
-        if (o != nullptr) {
-          const float ot = float(o[at(p.o, b, t) + c]);
-          float so, son;
-          logistic(ot, so, son);
-          go = gy * h[j + 1] * so * (1.f + ot * son);
-          gy *= ot * so;
+// The state that enters span k of the chain (k >= 1), for the lane's features:
+// the maps of spans k - 1, k - 2, ... composed until a known state.  words: the
+// lane's first word of span 0; a span's words are `pitch` apart.
+template <int CPL>
+__device__ void look_back(const unsigned long long* words, int64_t pitch, int k, float (&h)[CPL]) {
+  constexpr int AHEAD = 4;
+  float a[CPL];
+  bool done[CPL];
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) a[c] = 1.f, h[c] = 0.f, done[c] = false;
+  int j = k - 1;
+  for (int tries = 0; j >= 0 && tries < (1 << 24); ++tries) {
+    unsigned long long w[AHEAD][CPL];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) w[i][c] = get_word(words + (j - i > 0 ? j - i : 0) * pitch + c);
+    bool there = true, all = false;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      bool valid = true, ended = true;
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) valid = valid && (unsigned(w[i][c]) >> 31) != 0;
+      there = there && !all && j >= 0 && __all(valid);
+      if (there) {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          const float H = __uint_as_float(unsigned(w[i][c] >> 32)), A = __uint_as_float(unsigned(w[i][c]) & 0x7fffffffu);
+          if (!done[c]) h[c] += a[c] * H;
+          a[c] *= A;
+          done[c] = done[c] || unsigned(w[i][c]) == 0x80000000u;
+          ended = ended && done[c];
         }
-        d += gy;
-        gv = d * sn;
-        gz = d * (h[j] - float(v[at(p.v, b, t) + c])) * s * sn;
-        d *= s;
+        all = __all(ended);
+        --j;
       }
-      g_z[at(p.gz, b, t) + c] = T(gz);
-      g_v[at(p.gv, b, t) + c] = T(gv);
-      if (g_o != nullptr) g_o[at(p.go, b, t) + c] = T(go);
     }
+    if (all) return;
+    if (!there) __builtin_amdgcn_s_sleep(1);
   }
-  if (g_hzero != nullptr) g_hzero[i] = d;
+  if (j < 0) return;
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) h[c] = __uint_as_float(0x7fc00000u);  // (never: see above)
 }
 
-Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths) {
-  auto st = [](const int64_t (&s)[2]) { return Strides{s[0], s[1]}; };
-  return Args{d.batch, d.steps, d.features, st(d.z_stride), st(d.v_stride), st(d.o_stride), st(d.y_stride),
-              st(d.g_z_stride), st(d.g_v_stride), st(d.g_o_stride), lengths};
+// What a workgroup works on.
+struct Place {
+  int64_t b, c;  // batch entry, the lane's first feature
+  int64_t tile;
+  int span;      // place in the chain, 0 first
+  bool live;     // the lane stores
+};
+
+// CHAIN: spans by ticket, else one span a sequence (steps <= SPAN).
+template <int CPL, bool CHAIN>
+__device__ __forceinline__ Place place_of(const Args& p, unsigned* slot) {
+  int64_t id = blockIdx.x;
+  if constexpr (CHAIN) {
+    if (threadIdx.x == 0) *slot = atomicAdd(p.ticket, 1u);
+    __syncthreads();
+    id = *slot;
+  }
+  Place q;
+  q.tile = id % p.tiles;
+  q.span = int(id / p.tiles);
+  q.b = q.tile / p.feature_tiles;
+  const int64_t c = (q.tile % p.feature_tiles) * (64 * CPL) + (threadIdx.x & 63) * CPL;
+  // the last lane takes the last CPL features (some twice, to the same result); lanes past it read those, too
+  q.live = c < p.features;
+  q.c = c + CPL <= p.features ? c : p.features - CPL;
+  return q;
 }
+
+template <class T, int CPL>
+using raw_t = typename pack_of<T, CPL>::raw;
+template <class T, int CPL>
+__device__ __forceinline__ raw_t<T, CPL> get(const T* p) {
+  return *reinterpret_cast<const pack_t<T, CPL>*>(p);
+}
+template <class T, int CPL>
+__device__ __forceinline__ void put(T* p, const float (&v)[CPL]) {
+  store_n<CPL>(p, CPL, v);
+}
+
+// R rows a wave.  FULL: all of them are inside the sequence.
+template <class T, int CPL, int R, bool CHAIN>
+__global__ void __launch_bounds__(64 * WAVES)
+recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zero, T* y, float* h_out, float* states) {
+  __shared__ float mapA[WAVES][64 * CPL], mapH[WAVES][64 * CPL], enter[64 * CPL];
+  __shared__ unsigned slot;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const Place q = place_of<CPL, CHAIN>(p, &slot);
+  const int64_t n = length_of(p, q.b), span0 = int64_t(q.span) * SPAN, t0 = span0 + wave * R;
+  if (span0 >= n && !(span0 == 0)) {  // past the end: zeros (n = 0 goes on for the states)
+    for (int i = 0; i < R; ++i)
+      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, {});
+    return;
+  }
+  const int rows = int(n - t0 < 0 ? 0 : n - t0 < R ? n - t0 : R);  // live rows of this wave
+  raw_t<T, CPL> zr[R], vr[R], orw[R];
+  float s[R][CPL], bv[R][CPL];
+  if (rows > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t t = t0 + (i < rows ? i : rows - 1);
+      zr[i] = get<T, CPL>(z + at(p.z, q.b, t) + q.c);
+      vr[i] = get<T, CPL>(v + at(p.v, q.b, t) + q.c);
+    }
+    if (o != nullptr) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int64_t t = t0 + (i < rows ? i : rows - 1);
+        orw[i] = get<T, CPL>(o + at(p.o, q.b, t) + q.c);
+      }
+    }
+  }
+  float A[CPL], H[CPL], h[CPL];
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) A[c] = 1.f, H[c] = 0.f, h[c] = 0.f;
+  if (rows > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        float g, gn;
+        logistic(float(zr[i][c]), g, gn);
+        s[i][c] = i < rows ? g : 1.f;
+        bv[i][c] = i < rows ? gn * float(vr[i][c]) : 0.f;
+        A[c] *= s[i][c];
+        H[c] = s[i][c] * H[c] + bv[i][c];
+      }
+  }
+  // the state that enters this wave's rows
+  if (q.span == 0 && h_zero != nullptr) {
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) h[c] = h_zero[q.b * p.features + q.c + c];
+  }
+  if (waves > 1) {
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c];
+    __syncthreads();
+    if constexpr (CHAIN) {
+      if (wave == 0) {
+        float tA[CPL], tH[CPL];
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          tA[c] = A[c], tH[c] = H[c];
+          for (int i = 1; i < waves; ++i) {
+            const float a = mapA[i][lane * CPL + c];
+            tH[c] = a * tH[c] + mapH[i][lane * CPL + c];
+            tA[c] *= a;
+          }
+        }
+        const int64_t pitch = 64 * CPL;
+        unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
+        if (q.span > 0) {
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) put_word(words + q.span * pitch + c, map_word(tA[c], tH[c]));
+          look_back<CPL>(words, pitch, q.span, h);
+        }
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          put_word(words + q.span * pitch + c, state_word(tA[c] * h[c] + tH[c]));
+          enter[lane * CPL + c] = h[c];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) h[c] = enter[lane * CPL + c];
+    }
+  }
+  if (states != nullptr && wave == 0 && q.live) put<float, CPL>(states + (q.b * p.spans + q.span) * p.features + q.c, h);
+#pragma unroll
+  for (int c = 0; c < CPL; ++c)
+    for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
+  if (rows > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float r[CPL];
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        h[c] = s[i][c] * h[c] + bv[i][c];
+        r[c] = h[c];
+        if (o != nullptr) {
+          const float x = float(orw[i][c]);
+          float so, son;
+          logistic(x, so, son);
+          r[c] *= x * so;
+        }
+        if (i >= rows) r[c] = 0.f;
+      }
+      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, r);
+    }
+  } else {
+    for (int i = 0; i < R; ++i)
+      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, {});
+  }
+  // the wave of the last live step (the first wave where there is none) has the state that leaves
+  if (q.live && (n == 0 ? wave == 0 : rows > 0 && t0 + rows == n)) {
+    if (h_out != nullptr) put<float, CPL>(h_out + q.b * p.features + q.c, h);
+    if (states != nullptr)
+      for (int k = q.span + 1; k < p.spans; ++k) put<float, CPL>(states + (q.b * p.spans + k) * p.features + q.c, h);
+  }
+}
+
+// The backward; spans of the chain count from the last live one.
+template <class T, int CPL, int R, bool CHAIN>
+__global__ void __launch_bounds__(64 * WAVES)
+recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* states, const T* g_y, const float* g_h,
+                      T* g_z, T* g_v, T* g_o, float* g_hzero) {
+  __shared__ float mapA[WAVES][64 * CPL], mapH[WAVES][64 * CPL], mapG[WAVES][64 * CPL], enter[64 * CPL];
+  __shared__ unsigned slot;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const Place q = place_of<CPL, CHAIN>(p, &slot);
+  const int64_t n = length_of(p, q.b);
+  const int live_spans = int((n + SPAN - 1) / SPAN);
+  const int place = q.span;                                                       // in the chain, while it is live
+  const int span = place < live_spans ? live_spans - 1 - place : place;           // of the sequence
+  const int64_t span0 = int64_t(span) * SPAN, t0 = span0 + wave * R;
+  if (place >= live_spans) {
+    for (int i = 0; i < R; ++i) {
+      const int64_t t = t0 + i;
+      if (t < p.steps && q.live) {
+        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, {});
+        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, {});
+        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, {});
+      }
+    }
+    if (n == 0 && place == 0 && wave == 0 && q.live && g_hzero != nullptr) {
+      float e[CPL];
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) e[c] = g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
+      put<float, CPL>(g_hzero + q.b * p.features + q.c, e);
+    }
+    return;
+  }
+  const int rows = int(n - t0 < 0 ? 0 : n - t0 < R ? n - t0 : R);
+  raw_t<T, CPL> zr[R], vr[R], orw[R], gr[R];
+  float s[R][CPL], sn[R][CPL], prev[R][CPL];
+  float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL];
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) {
+    h[c] = states[(q.b * p.spans + span) * p.features + q.c + c];
+    e[c] = place == 0 && g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
+    A[c] = 1.f, H[c] = 0.f, G[c] = 0.f;
+  }
+  if (rows > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t t = t0 + (i < rows ? i : rows - 1);
+      zr[i] = get<T, CPL>(z + at(p.z, q.b, t) + q.c);
+      vr[i] = get<T, CPL>(v + at(p.v, q.b, t) + q.c);
+      gr[i] = get<T, CPL>(g_y + at(p.y, q.b, t) + q.c);
+    }
+    if (o != nullptr) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int64_t t = t0 + (i < rows ? i : rows - 1);
+        orw[i] = get<T, CPL>(o + at(p.o, q.b, t) + q.c);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        float g, gn;
+        logistic(float(zr[i][c]), g, gn);
+        s[i][c] = i < rows ? g : 1.f;
+        sn[i][c] = i < rows ? gn : 0.f;
+        A[c] *= s[i][c];
+        H[c] = s[i][c] * H[c] + (i < rows ? gn * float(vr[i][c]) : 0.f);
+      }
+#pragma unroll
+    for (int i = R - 1; i >= 0; --i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        float g = float(gr[i][c]);
+        if (o != nullptr) {
+          const float x = float(orw[i][c]);
+          float so, son;
+          logistic(x, so, son);
+          g *= x * so;
+        }
+        G[c] = s[i][c] * ((i < rows ? g : 0.f) + G[c]);
+      }
+  }
+  if (waves > 1) {
+#pragma unroll
+    for (int c = 0; c < CPL; ++c)
+      mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c], mapG[wave][lane * CPL + c] = G[c];
+    __syncthreads();
+    if constexpr (CHAIN) {
+      if (wave == 0) {
+        float tA[CPL], tG[CPL];
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          tA[c] = 1.f, tG[c] = 0.f;
+          for (int i = waves - 1; i >= 0; --i) {
+            const float a = mapA[i][lane * CPL + c];
+            tG[c] = a * tG[c] + mapG[i][lane * CPL + c];
+            tA[c] *= a;
+          }
+        }
+        const int64_t pitch = 64 * CPL;
+        unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
+        if (place > 0) {
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) put_word(words + place * pitch + c, map_word(tA[c], tG[c]));
+          look_back<CPL>(words, pitch, place, e);
+        }
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          put_word(words + place * pitch + c, state_word(tA[c] * e[c] + tG[c]));
+          enter[lane * CPL + c] = e[c];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) e[c] = enter[lane * CPL + c];
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) {
+    for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
+    for (int i = waves - 1; i > wave; --i) e[c] = mapA[i][lane * CPL + c] * e[c] + mapG[i][lane * CPL + c];
+  }
+  if (rows > 0) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        prev[i][c] = h[c];
+        h[c] = s[i][c] * h[c] + (i < rows ? sn[i][c] * float(vr[i][c]) : 0.f);
+      }
+#pragma unroll
+    for (int i = R - 1; i >= 0; --i) {
+      float gz[CPL], gv[CPL], go[CPL];
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        const float vv = float(vr[i][c]);
+        float g = float(gr[i][c]);
+        go[c] = 0.f;
+        if (o != nullptr) {
+          const float x = float(orw[i][c]), ht = s[i][c] * prev[i][c] + sn[i][c] * vv;
+          float so, son;
+          logistic(x, so, son);
+          go[c] = g * ht * so * (1.f + x * son);
+          g *= x * so;
+        }
+        const float d = g + e[c];
+        gv[c] = d * sn[i][c];
+        gz[c] = gv[c] * s[i][c] * (prev[i][c] - vv);
+        if (i < rows) {
+          e[c] = s[i][c] * d;
+        } else {
+          gz[c] = gv[c] = go[c] = 0.f;
+        }
+      }
+      const int64_t t = t0 + i;
+      if (t < p.steps && q.live) {
+        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, gz);
+        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, gv);
+        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, go);
+      }
+    }
+  } else {
+    for (int i = 0; i < R; ++i) {
+      const int64_t t = t0 + i;
+      if (t < p.steps && q.live) {
+        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, {});
+        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, {});
+        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, {});
+      }
+    }
+  }
+  if (span == 0 && wave == 0 && q.live && g_hzero != nullptr) put<float, CPL>(g_hzero + q.b * p.features + q.c, e);
+}
+
+// h_out = h_zero (g_hzero = g_h) where there are no steps.
+__global__ void __launch_bounds__(256) copy_state_kernel(const float* in, float* out, int64_t n) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n) out[i] = in != nullptr ? in[i] : 0.f;
+}
+
+// The chain's words and its ticket start from zero.
+__global__ void __launch_bounds__(256) clear_kernel(uint4* p, int64_t n) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n) p[i] = uint4{0, 0, 0, 0};
+}
+
+Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths, int cpl) {
+  auto st = [](const int64_t (&s)[2]) { return Strides{s[0], s[1]}; };
+  Args p{d.batch, d.steps, d.features, st(d.z_stride), st(d.v_stride), st(d.o_stride), st(d.y_stride),
+         st(d.g_z_stride), st(d.g_v_stride), st(d.g_o_stride), lengths, 0, 0, 0, nullptr, nullptr};
+  p.feature_tiles = (d.features + 64 * cpl - 1) / (64 * cpl);
+  p.tiles = p.feature_tiles * d.batch;
+  p.spans = int((d.steps + SPAN - 1) / SPAN);
+  return p;
+}
+
+int lanes_features(int64_t features) { return features >= 2 ? 2 : 1; }
 
 template <class F>
 int by_type(int type, F&& f) {
@@ -130,33 +489,80 @@ int by_type(int type, F&& f) {
   return f(f16_t());
 }
 
+int copy_state(const float* in, float* out, int64_t n, hipStream_t s) {
+  if (out == nullptr || out == in) return hipSuccess;
+  hipLaunchKernelGGL(copy_state_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, s, in, out, n);
+  return hipGetLastError();
+}
+
+// Clears the chain, then calls f(R, CHAIN, workgroups, threads): steps a wave
+// by how many there are (one step holds one row's registers and loads), spans
+// by ticket where a sequence has several.
+template <class F>
+int with_form(Args& p, int cpl, void* workspace, hipStream_t s, F&& f) {
+  using std::integral_constant;
+  if (p.spans > 1) {
+    const int64_t bytes = 64 + p.tiles * p.spans * 64 * cpl * 8;
+    p.ticket = static_cast<unsigned*>(workspace);
+    p.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 64);
+    hipLaunchKernelGGL(clear_kernel, dim3(unsigned((bytes / 16 + 255) / 256)), dim3(256), 0, s,
+                       static_cast<uint4*>(workspace), bytes / 16);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return f(integral_constant<int, RPW>(), integral_constant<bool, true>(), unsigned(p.tiles * p.spans), 64 * WAVES);
+  }
+  if (p.steps == 1) return f(integral_constant<int, 1>(), integral_constant<bool, false>(), unsigned(p.tiles), 64);
+  return f(integral_constant<int, RPW>(), integral_constant<bool, false>(), unsigned(p.tiles),
+           64 * int((p.steps + RPW - 1) / RPW));
+}
+
 }  // namespace
 
-size_t recurrence_workspace(int64_t, int64_t, int64_t, int) { return 0; }
+size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int) {
+  if (steps <= SPAN) return 0;
+  const int64_t w = 64 * lanes_features(features);
+  return 64 + size_t(batch * ((features + w - 1) / w)) * ((steps + SPAN - 1) / SPAN) * w * 8;
+}
 
 int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o, const float* h_zero,
-                      const int32_t* lengths, void* y, float* h_out, float* states, void*, void* stream) {
+                      const int32_t* lengths, void* y, float* h_out, float* states, void* workspace, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d.steps == 0) return copy_state(h_zero, h_out, d.batch * d.features, s);
   return by_type(d.type, [&](auto t) {
     using T = decltype(t);
-    const unsigned blocks = unsigned((d.batch * d.features + 63) / 64);
-    hipLaunchKernelGGL(recurrence_serial_kernel<T>, dim3(blocks), dim3(64), 0, static_cast<hipStream_t>(stream),
-                       args_of(d, lengths), static_cast<const T*>(z), static_cast<const T*>(v),
-                       static_cast<const T*>(o), h_zero, static_cast<T*>(y), h_out, states);
-    return int(hipGetLastError());
+    const auto run = [&](auto cpl) {
+      constexpr int CPL = decltype(cpl)::value;
+      Args p = args_of(d, lengths, CPL);
+      return with_form(p, CPL, workspace, s, [&](auto r, auto chain, unsigned groups, int threads) {
+        hipLaunchKernelGGL((recurrence_kernel<T, CPL, decltype(r)::value, decltype(chain)::value>), dim3(groups),
+                           dim3(threads), 0, s, p, static_cast<const T*>(z), static_cast<const T*>(v),
+                           static_cast<const T*>(o), h_zero, static_cast<T*>(y), h_out, states);
+        return int(hipGetLastError());
+      });
+    };
+    return lanes_features(d.features) == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
   });
 }
 
 int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o,
                           const int32_t* lengths, const float* states, const void* g_y, const float* g_h, void* g_z,
-                          void* g_v, void* g_o, float* g_hzero, void*, void* stream) {
+                          void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d.steps == 0) return copy_state(g_h, g_hzero, d.batch * d.features, s);
   return by_type(d.type, [&](auto t) {
     using T = decltype(t);
-    const unsigned blocks = unsigned((d.batch * d.features + 63) / 64);
-    hipLaunchKernelGGL(recurrence_adj_serial_kernel<T>, dim3(blocks), dim3(64), 0, static_cast<hipStream_t>(stream),
-                       args_of(d, lengths), static_cast<const T*>(z), static_cast<const T*>(v),
-                       static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h, static_cast<T*>(g_z),
-                       static_cast<T*>(g_v), static_cast<T*>(g_o), g_hzero);
-    return int(hipGetLastError());
+    const auto run = [&](auto cpl) {
+      constexpr int CPL = decltype(cpl)::value;
+      Args p = args_of(d, lengths, CPL);
+      return with_form(p, CPL, workspace, s, [&](auto r, auto chain, unsigned groups, int threads) {
+        hipLaunchKernelGGL((recurrence_adj_kernel<T, CPL, decltype(r)::value, decltype(chain)::value>), dim3(groups),
+                           dim3(threads), 0, s, p, static_cast<const T*>(z), static_cast<const T*>(v),
+                           static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h, static_cast<T*>(g_z),
+                           static_cast<T*>(g_v), static_cast<T*>(g_o), g_hzero);
+        return int(hipGetLastError());
+      });
+    };
+    return lanes_features(d.features) == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
   });
 }
 

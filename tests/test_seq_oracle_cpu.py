@@ -189,7 +189,7 @@ def test_product_of_nothing_is_done():
     assert product_call(m=0, a=None)[0] == 0 and product_call(n=0, b=None)[0] == 0
 
 
-def recur_call(z=P, v=P * 2, o=P * 3, h0=None, n=None, y=P * 4, h=None, st=None, ws=P * 8, nws=1 << 20, fn="dtst_recurrence", **kw):
+def recur_call(z=P, v=P * 2, o=P * 3, h0=None, n=None, y=P * 4, h=None, st=None, ws=P * 8, nws=1 << 30, fn="dtst_recurrence", **kw):
     f = dict(batch=2, steps=300, features=16, type=1)
     f.update({k + "_stride": (4800, 16) for k in ("z", "v", "o", "y", "g_z", "g_v", "g_o")})
     f.update(kw)
@@ -204,7 +204,7 @@ def recur_call(z=P, v=P * 2, o=P * 3, h0=None, n=None, y=P * 4, h=None, st=None,
     (dict(batch=-1), 1, "batch"), (dict(steps=-1), 1, "steps"), (dict(type=3), 1, "type"), (dict(z=None), 1, "z is null"),
     (dict(z=P + 1), 1, "aligned"), (dict(z_stride=(4800, 15)), 1, "strides of z"), (dict(v_stride=(-4800, 16)), 1, "strides of v"),
     (dict(y_stride=(160, 16)), 1, "rows of y"), (dict(y=P), 1, "overlap"), (dict(h0=P + 2), 1, "aligned"),
-    (dict(batch=1 << 40, steps=1 << 40), 1, "overflow"), (dict(o_stride=(1 << 60, 16)), 1, "too large"),
+    (dict(batch=1 << 40, steps=1 << 40), 1, "overflow"), (dict(nws=64), 1, "workspace"), (dict(ws=None), 1, "workspace"), (dict(o_stride=(1 << 60, 16)), 1, "too large"),
 ])
 def test_recurrence_refusals(kw, code, word):
     st, msg = recur_call(**kw)
