@@ -8,7 +8,7 @@ import pytest
 
 from gpu_common import say, torch_gpu
 from oracle import seq_oracle as S
-from seq_common import dtype, f64, near, outside, rounded, strided
+from seq_common import HALF_STEP, dtype, f64, near, outside, rounded, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -37,7 +37,7 @@ SIZES = [(1, 1, 128), (1, 100, 1000), (2, 64, 512), (3, 300, 640), (4, 4608, 256
          (16, 16, 1), (17, 65, 513), (31, 256, 1024), (33, 127, 384), (63, 255, 130), (64, 64, 4096), (65, 257, 200),
          (100, 1000, 1900), (127, 129, 1152), (128, 128, 128), (129, 513, 896), (200, 1, 700), (255, 300, 1024),
          (256, 256, 256), (257, 255, 520), (500, 700, 300), (513, 640, 128), (777, 1000, 1900), (1025, 1030, 512),
-         (1300, 2100, 640), (2048, 2048, 1024)]
+         (1300, 2100, 640), (2048, 2048, 1024), (3500, 3700, 256)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -64,6 +64,37 @@ def test_product(m, n, k):
     base, basev = rounded(torch, rng.randn(m, n), "f32")
     D.dtst_product(a, sa, b, sb, base, accumulate=True)
     near((f64(base) - basev) / size, ref / size, "f32", "accumulate", arithmetic=2e-5, rms=1.0)
+
+
+# The 8-bit instruction's sum of eight neighbouring products keeps 13 bits below
+# the largest: each of the eight loses less than 2^-13 of it, so a result's error
+# is below the sum over its eights of 8 * 2^-13 of their largest product; beside
+# the bar of the 32-bit sums.
+@pytest.mark.parametrize("m,n,k", SIZES + [(3000, 4200, 300), (4096, 3600, 1152)])
+def test_short_sums(m, n, k):
+    torch, D = lib()
+    rng = np.random.RandomState(m + n + k)
+    a, sa, av = codes(torch, D, operand(rng, m, k))
+    b, sb, bv = codes(torch, D, operand(rng, n, k))
+    bias, biasv = rounded(torch, rng.randn(n), "f32")
+    say(f"[short sums] {m} x {n} x {k}")
+    rows, cols = rng.permutation(m)[:150], rng.permutation(n)[:150]     # sampled where there are many
+    rows[0], cols[0] = m - 1, n - 1
+    ra, rb = av[rows], bv[cols]
+    ref = S.product(ra, rb, biasv[cols])
+    size = np.sqrt((ra ** 2).sum(axis=1)[:, None] * (rb ** 2).sum(axis=1)[None, :])
+    lost = np.zeros_like(ref)
+    for i in range(0, ra.shape[1], 8):
+        lost += 2.0 ** -10 * (np.abs(ra[:, None, i:i + 8]) * np.abs(rb[None, :, i:i + 8])).max(axis=2)
+    for t in ("bf16", "f32"):
+        c = torch.full((m, n), float("nan"), device="cuda").to(dtype(torch, t))
+        D.dtst_product(a, sa, b, sb, c, bias=bias, short_sums=True)
+        got = f64(c)[np.ix_(rows, cols)]
+        assert not np.isnan(f64(c)).any()
+        tol = HALF_STEP[t] * np.abs(ref) * (1 + 1e-5) + 1e-5 * (np.abs(ref) + size) + lost
+        worst = (np.abs(got - ref) / tol).max()
+        say(f"  {t}: up to {worst:.2f} of the bar")
+        assert worst <= 1
 
 
 @pytest.mark.parametrize("m,n,k", [(5, 70, 300), (70, 90, 700), (300, 520, 256)])
