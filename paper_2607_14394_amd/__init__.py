@@ -11,7 +11,9 @@ loudly when it is missing -- there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 
 # torch ships its own HIP runtime under the same soname (libamdhip64.so.7).
 # Loading torch first makes libdtst.so bind to that one copy; loading
@@ -71,36 +73,13 @@ class Schedule(ctypes.Structure):
                  "z_mirrored", "y_parts")]
 
 
-class NormDesc(ctypes.Structure):
-    """dtst_norm_desc."""
-    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_res", "ld_sum", "ld_y", "ld_scale")]
-                + [(n, ctypes.c_int32) for n in ("x_type", "res_type", "y_type")] + [("eps", ctypes.c_float)])
-
-
-class NormAdjDesc(ctypes.Structure):
-    """dtst_norm_adj_desc."""
-    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_g_y", "ld_u", "ld_g_sum", "ld_g_u", "ld_g_x")]
-                + [(n, ctypes.c_int32) for n in ("x_type", "res_type", "accumulate")])
-
-
-class QuantiseDesc(ctypes.Structure):
-    """dtst_quantise_desc."""
-    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_q", "ld_scale", "ld_qt", "ld_scale_t")]
-                + [("type", ctypes.c_int32)])
-
-
-class ProductDesc(ctypes.Structure):
-    """dtst_product_desc."""
-    _fields_ = ([(n, ctypes.c_int64) for n in ("m", "n", "k", "ld_a", "ld_a_scale", "ld_b", "ld_b_scale", "ld_c")]
-                + [(n, ctypes.c_int32) for n in ("c_type", "accumulate", "short_sums")])
-
-
-class RecurrenceDesc(ctypes.Structure):
-    """dtst_recurrence_desc."""
-    _fields_ = ([(n, ctypes.c_int64) for n in ("batch", "steps", "features")]
-                + [(n + "_stride", ctypes.c_int64 * 2) for n in ("z", "v", "o", "y", "g_z", "g_v", "g_o")]
-                + [("type", ctypes.c_int32)])
-
+# The descriptors of the latent-sequence operators, packed in the layout of
+# include/dtst.h (a ctypes.Structure takes three times as long to fill).
+NORM_DESC = struct.Struct("@7q3if")
+NORM_ADJ_DESC = struct.Struct("@7q3i4x")
+QUANTISE_DESC = struct.Struct("@7qi4x")
+PRODUCT_DESC = struct.Struct("@8q3i4x")
+RECURRENCE_DESC = struct.Struct("@17qi4x")
 
 # DTST_F32 .. DTST_E4M3 of include/dtst.h
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
@@ -360,44 +339,50 @@ def recurrence_states_shape(batch, steps, features):
     return (batch, -(-steps // RECURRENCE_SPAN), features)
 
 
-def _rows(t, shape, name, dtypes):
-    """Row stride of a 2-D tensor on the current device with contiguous rows."""
-    if t.shape != shape or t.dtype not in dtypes or not _here(t):
+def _device():
+    """The current device (-2 without one: no tensor is there)."""
+    try:
+        return torch._C._cuda_getDevice()
+    except (RuntimeError, AttributeError):
+        return -2
+
+
+def _rows(t, shape, name, dtypes, dev):
+    """Row stride of a 2-D tensor on device dev with contiguous rows."""
+    if t.shape != shape or t.dtype not in dtypes or t.get_device() != dev:
         raise ValueError(f"{name}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)} on the current "
                          f"device, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    st = t.stride()
-    if st[1] != 1 and shape[1] > 1 and shape[0]:
+    rows, cols = shape
+    s0, s1 = t.stride()
+    if s1 != 1 and cols > 1 and rows:
         raise ValueError(f"{name}: columns must be contiguous")
     # (the stride of a single row is any; one that suits every type)
-    return st[0] if shape[0] > 1 else -(-shape[1] // 16) * 16
+    return s0 if rows > 1 else -(-cols // 16) * 16
 
 
-def _vector(t, n, name, dtype=torch.float32):
-    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or not _here(t):
+def _vector(t, n, name, dev, dtype=torch.float32):
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError(f"{name}: need contiguous {dtype} of shape ({n},) on the current device")
-
-
-def _here(t):
-    """Whether t is on the current device."""
-    return t.is_cuda and t.get_device() == torch.cuda.current_device()
 
 
 _FLOATS = (torch.float32, torch.bfloat16, torch.float16)
 _CODES, _SCALES = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu,)
 
 
-def _codes(q, s, rows, k, name):
-    return (_rows(q, (rows, code_columns(k)), name, _CODES),
-            _rows(s, (rows, scale_columns(k)), name + " scale", _SCALES))
+def _codes(q, s, rows, k, name, dev):
+    return (_rows(q, (rows, code_columns(k)), name, _CODES, dev),
+            _rows(s, (rows, scale_columns(k)), name + " scale", _SCALES, dev))
 
 
 def _scratch(ws, need, device, stream):
     """Pointer and bytes of the workspace, and what keeps it until the launch."""
-    if ws is None and need:
+    if ws is None:
+        if not need:
+            return None, 0, None
         ws = torch.empty(need, dtype=torch.uint8, device=device)
         if stream is not None and int(stream) != torch_stream():
             ws.record_stream(torch.cuda.ExternalStream(int(stream)))
-    return _wsargs(ws) + (ws,)
+    return ws.data_ptr(), ws.nbytes, ws
 
 
 def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, eps=1e-6, stream=None):
@@ -405,24 +390,26 @@ def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, e
     codes with their scales.  x, res, sum_out: (rows, cols)."""
     if x.dim() != 2:
         raise ValueError("x must be (rows, cols)")
-    shape = rows, cols = tuple(x.shape)
-    tx = (x.dtype,)
-    rt = sum_out.dtype if res is None and sum_out is not None else x.dtype if res is None else res.dtype
-    d = NormDesc(rows, cols, _rows(x, shape, "x", _FLOATS),
-                 0 if res is None else _rows(res, shape, "res", (x.dtype, torch.float32)),
-                 0 if sum_out is None else _rows(sum_out, shape, "sum_out", (rt,)), 0, 0,
-                 _TYPES[x.dtype], _TYPES[rt], _TYPES.get(y.dtype, -1), eps)
+    shape = rows, cols = x.shape
+    dev, tx = _device(), x.dtype
+    rt = res.dtype if res is not None else tx if sum_out is None else sum_out.dtype
+    ld_x = _rows(x, shape, "x", _FLOATS, dev)
+    ld_res = 0 if res is None else _rows(res, shape, "res", (tx, torch.float32), dev)
+    ld_sum = 0 if sum_out is None else _rows(sum_out, shape, "sum_out", (rt,), dev)
     if scale is not None:
-        d.ld_y, d.ld_scale = _codes(y, scale, rows, cols, "y")
+        ld_y, ld_scale = _codes(y, scale, rows, cols, "y", dev)
     else:
-        d.ld_y = _rows(y, shape, "y", tx)
-    _vector(weight, cols, "weight")
+        ld_y, ld_scale = _rows(y, shape, "y", (tx,), dev), 0
+    _vector(weight, cols, "weight", dev)
     if rstd is not None:
-        _vector(rstd, rows, "rstd")
-    _check(lib.dtst_rms_norm(ctypes.addressof(d), _ptr(x), _ptr(res), _ptr(weight), _ptr(sum_out), _ptr(y), _ptr(scale),
+        _vector(rstd, rows, "rstd", dev)
+    _check(lib.dtst_rms_norm(NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt],
+                                            _TYPES[y.dtype], eps),
+                             x.data_ptr(), _ptr(res), weight.data_ptr(), _ptr(sum_out), y.data_ptr(), _ptr(scale),
                              _ptr(rstd), _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def dtst_rms_norm_adj_workspace(rows, cols) -> int:
     n = ctypes.c_size_t(0)
     _check(lib.dtst_rms_norm_adj_workspace(int(rows), int(cols), ctypes.byref(n)))
@@ -435,18 +422,19 @@ def dtst_rms_norm_adj(g_y, u, weight, rstd, g_u, g_weight, g_sum=None, g_x=None,
     res alike; g_x the same in g_y's type) and g_weight."""
     if g_y.dim() != 2:
         raise ValueError("g_y must be (rows, cols)")
-    shape = rows, cols = tuple(g_y.shape)
-    tr = (u.dtype,)
-    d = NormAdjDesc(rows, cols, _rows(g_y, shape, "g_y", _FLOATS), _rows(u, shape, "u", (g_y.dtype, torch.float32)),
-                    0 if g_sum is None else _rows(g_sum, shape, "g_sum", tr), _rows(g_u, shape, "g_u", tr),
-                    0 if g_x is None else _rows(g_x, shape, "g_x", (g_y.dtype,)), _TYPES[g_y.dtype], _TYPES[u.dtype],
-                    int(accumulate))
-    _vector(weight, cols, "weight")
-    _vector(g_weight, cols, "g_weight")
-    _vector(rstd, rows, "rstd")
-    p, n, ws = _scratch(ws, dtst_rms_norm_adj_workspace(rows, cols) if ws is None else 0, g_y.device, stream)
-    _check(lib.dtst_rms_norm_adj(ctypes.addressof(d), _ptr(g_y), _ptr(u), _ptr(weight), _ptr(rstd), _ptr(g_sum),
-                                 _ptr(g_u), _ptr(g_x), _ptr(g_weight), p, n, _stream(stream)))
+    shape = rows, cols = g_y.shape
+    dev, tx, tr = _device(), g_y.dtype, (u.dtype,)
+    d = NORM_ADJ_DESC.pack(rows, cols, _rows(g_y, shape, "g_y", _FLOATS, dev),
+                           _rows(u, shape, "u", (tx, torch.float32), dev),
+                           0 if g_sum is None else _rows(g_sum, shape, "g_sum", tr, dev),
+                           _rows(g_u, shape, "g_u", tr, dev), 0 if g_x is None else _rows(g_x, shape, "g_x", (tx,), dev),
+                           _TYPES[tx], _TYPES[u.dtype], int(accumulate))
+    _vector(weight, cols, "weight", dev)
+    _vector(g_weight, cols, "g_weight", dev)
+    _vector(rstd, rows, "rstd", dev)
+    p, n, ws = _scratch(ws, dtst_rms_norm_adj_workspace(rows, cols), g_y.device, stream)
+    _check(lib.dtst_rms_norm_adj(d, g_y.data_ptr(), u.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(g_sum),
+                                 g_u.data_ptr(), _ptr(g_x), g_weight.data_ptr(), p, n, _stream(stream)))
 
 
 def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
@@ -457,15 +445,15 @@ def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
     if (q is None) != (scale is None) or (qt is None) != (scale_t is None) or (q is None and qt is None):
         raise ValueError("need q with scale, or qt with scale_t, or all four")
     rows, cols = x.shape
-    d = QuantiseDesc(rows, cols, _rows(x, (rows, cols), "x", _FLOATS), 0, 0, 0, 0, _TYPES[x.dtype])
-    if q is not None:
-        d.ld_q, d.ld_scale = _codes(q, scale, rows, cols, "q")
-    if qt is not None:
-        d.ld_qt, d.ld_scale_t = _codes(qt, scale_t, cols, rows, "qt")
-    _check(lib.dtst_quantise(ctypes.addressof(d), _ptr(x), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t),
-                             _stream(stream)))
+    dev = _device()
+    ld_x = _rows(x, (rows, cols), "x", _FLOATS, dev)
+    ld_q, ld_s = (0, 0) if q is None else _codes(q, scale, rows, cols, "q", dev)
+    ld_qt, ld_st = (0, 0) if qt is None else _codes(qt, scale_t, cols, rows, "qt", dev)
+    _check(lib.dtst_quantise(QUANTISE_DESC.pack(rows, cols, ld_x, ld_q, ld_s, ld_qt, ld_st, _TYPES[x.dtype]),
+                             x.data_ptr(), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def dtst_product_workspace(m, n, k) -> int:
     b = ctypes.c_size_t(0)
     _check(lib.dtst_product_workspace(int(m), int(n), int(k), ctypes.byref(b)))
@@ -479,34 +467,38 @@ def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_s
         raise ValueError("a and c must be (m, k) and (m, n)")
     m, n = c.shape
     k = a.shape[1]
-    d = ProductDesc(m, n, k, *_codes(a, a_scale, m, k, "a"), *_codes(b, b_scale, n, k, "b"),
-                    _rows(c, (m, n), "c", _FLOATS), _TYPES[c.dtype], int(accumulate), int(short_sums))
+    dev = _device()
+    ld_a, ld_sa = _codes(a, a_scale, m, k, "a", dev)
+    ld_b, ld_sb = _codes(b, b_scale, n, k, "b", dev)
+    d = PRODUCT_DESC.pack(m, n, k, ld_a, ld_sa, ld_b, ld_sb, _rows(c, (m, n), "c", _FLOATS, dev), _TYPES[c.dtype],
+                          int(accumulate), int(short_sums))
     if bias is not None:
-        _vector(bias, n, "bias")
-    p, nb, ws = _scratch(ws, dtst_product_workspace(m, n, k) if ws is None else 0, c.device, stream)
-    _check(lib.dtst_product(ctypes.addressof(d), _ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), _ptr(c), p,
-                            nb, _stream(stream)))
+        _vector(bias, n, "bias", dev)
+    p, nb, ws = _scratch(ws, dtst_product_workspace(m, n, k), c.device, stream)
+    _check(lib.dtst_product(d, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias),
+                            c.data_ptr(), p, nb, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=1024)
 def dtst_recurrence_workspace(batch, steps, features, dtype) -> int:
     n = ctypes.c_size_t(0)
     _check(lib.dtst_recurrence_workspace(int(batch), int(steps), int(features), _TYPES[dtype], ctypes.byref(n)))
     return n.value
 
 
-def _sequence(t, shape, name, dtype):
+def _sequence(t, shape, name, dtype, dev):
     """Strides of batch entries and steps of a (batch, steps, features) tensor."""
-    if t.shape != shape or t.dtype != dtype or not _here(t):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
         raise ValueError(f"{name}: need {dtype} of shape {tuple(shape)} on the current device, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
-    st = t.stride()
-    if st[2] != 1 and shape[2] > 1 and t.numel():
+    sb, st, sf = t.stride()
+    if sf != 1 and shape[2] > 1 and t.numel():
         raise ValueError(f"{name}: features must be contiguous")
-    return st[:2]
+    return sb, st
 
 
-def _state(t, shape, name):
-    if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or not _here(t):
+def _state(t, shape, name, dev):
+    if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError(f"{name}: need contiguous torch.float32 of shape {tuple(shape)} on the current device")
 
 
@@ -516,22 +508,23 @@ def dtst_recurrence(z, v, y, o=None, h0=None, h_out=None, lengths=None, states=N
     lengths: (batch,) int32, states: recurrence_states_shape float32."""
     if z.dim() != 3:
         raise ValueError("z must be (batch, steps, features)")
-    shape = B, T, F = tuple(z.shape)
-    e = z.dtype
+    shape = B, T, F = z.shape
+    e, dev = z.dtype, _device()
     if e not in _FLOATS:
         raise ValueError(f"z: need {' or '.join(str(d) for d in _FLOATS)}")
-    d = RecurrenceDesc(B, T, F, _sequence(z, shape, "z", e), _sequence(v, shape, "v", e),
-                       (0, 0) if o is None else _sequence(o, shape, "o", e), _sequence(y, shape, "y", e))
-    d.type = _TYPES[e]
-    for t, name in ((h0, "h0"), (h_out, "h_out")):
-        if t is not None:
-            _state(t, (B, F), name)
+    d = RECURRENCE_DESC.pack(B, T, F, *_sequence(z, shape, "z", e, dev), *_sequence(v, shape, "v", e, dev),
+                             *((0, 0) if o is None else _sequence(o, shape, "o", e, dev)),
+                             *_sequence(y, shape, "y", e, dev), 0, 0, 0, 0, 0, 0, _TYPES[e])
+    if h0 is not None:
+        _state(h0, (B, F), "h0", dev)
+    if h_out is not None:
+        _state(h_out, (B, F), "h_out", dev)
     if states is not None:
-        _state(states, recurrence_states_shape(B, T, F), "states")
+        _state(states, recurrence_states_shape(B, T, F), "states", dev)
     if lengths is not None:
-        _vector(lengths, B, "lengths", torch.int32)
-    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e) if ws is None and T > 1 else 0, z.device, stream)
-    _check(lib.dtst_recurrence(ctypes.addressof(d), _ptr(z), _ptr(v), _ptr(o), _ptr(h0), _ptr(lengths), _ptr(y),
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
+    _check(lib.dtst_recurrence(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(h0), _ptr(lengths), y.data_ptr(),
                                _ptr(h_out), _ptr(states), p, n, _stream(stream)))
 
 
@@ -541,27 +534,29 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     and, from the gradient g_h of the last state, g_hzero of the first."""
     if z.dim() != 3:
         raise ValueError("z must be (batch, steps, features)")
-    shape = B, T, F = tuple(z.shape)
-    e = z.dtype
+    shape = B, T, F = z.shape
+    e, dev = z.dtype, _device()
     if e not in _FLOATS:
         raise ValueError(f"z: need {' or '.join(str(d) for d in _FLOATS)}")
     if (o is None) != (g_o is None):
         raise ValueError("g_o goes with o")
     none = (0, 0)
-    d = RecurrenceDesc(B, T, F, _sequence(z, shape, "z", e), _sequence(v, shape, "v", e),
-                       none if o is None else _sequence(o, shape, "o", e), _sequence(g_y, shape, "g_y", e),
-                       _sequence(g_z, shape, "g_z", e), _sequence(g_v, shape, "g_v", e),
-                       none if g_o is None else _sequence(g_o, shape, "g_o", e), _TYPES[e])
-    for t, name in ((g_h, "g_h"), (g_hzero, "g_hzero")):
-        if t is not None:
-            _state(t, (B, F), name)
-    _state(states, recurrence_states_shape(B, T, F), "states")
+    d = RECURRENCE_DESC.pack(B, T, F, *_sequence(z, shape, "z", e, dev), *_sequence(v, shape, "v", e, dev),
+                             *(none if o is None else _sequence(o, shape, "o", e, dev)),
+                             *_sequence(g_y, shape, "g_y", e, dev), *_sequence(g_z, shape, "g_z", e, dev),
+                             *_sequence(g_v, shape, "g_v", e, dev),
+                             *(none if g_o is None else _sequence(g_o, shape, "g_o", e, dev)), _TYPES[e])
+    if g_h is not None:
+        _state(g_h, (B, F), "g_h", dev)
+    if g_hzero is not None:
+        _state(g_hzero, (B, F), "g_hzero", dev)
+    _state(states, recurrence_states_shape(B, T, F), "states", dev)
     if lengths is not None:
-        _vector(lengths, B, "lengths", torch.int32)
-    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e) if ws is None else 0, z.device, stream)
-    _check(lib.dtst_recurrence_adj(ctypes.addressof(d), _ptr(z), _ptr(v), _ptr(o), _ptr(lengths), _ptr(states),
-                                   _ptr(g_y), _ptr(g_h), _ptr(g_z), _ptr(g_v), _ptr(g_o), _ptr(g_hzero), p, n,
-                                   _stream(stream)))
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
+    _check(lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
+                                   g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o), _ptr(g_hzero),
+                                   p, n, _stream(stream)))
 
 
 def dtst_profile_enable(on=True):

@@ -224,7 +224,7 @@ dtst_status quantise(const dtst_quantise_desc* d, const void* x, void* q, void* 
   if (q) DTST_TRY(check_codes(aq, as));
   if (qt) DTST_TRY(check_codes(at, ast));
   DTST_TRY(check_extent(d->rows, (d->cols + 127) / 128, "x"));
-  DTST_TRY(check_grid(((d->rows + 127) / 128) * ((d->cols + 127) / 128), 256));
+  DTST_TRY(check_grid((d->rows + 15) * ((d->cols + 127) / 128) / 16 + 1, 256));
   const Array* all[] = {&ax, &aq, &as, &at, &ast};
   for (int i = 1; i < 5; ++i)
     for (int j = 0; j < i; ++j) DTST_TRY(check_apart(*all[i], *all[j], false));

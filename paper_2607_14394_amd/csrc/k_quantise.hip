@@ -2,10 +2,12 @@
 // 128 values (dtst_quantise).  Bound by HBM: x is read once, codes are written
 // once.
 //
-// A workgroup takes 128 x 128 values.  For the rows' form, 16 lanes hold a
-// row's block of 128, eight neighbouring columns each, and its scale is a
-// maximum within a row of lanes.  For the transposed form the tile goes through
-// LDS: a lane then holds 8 rows of a column, and 16 lanes its 128.
+// In both forms 16 lanes hold a row's block of 128 columns, eight neighbouring
+// columns each; the row's scale is a maximum within a row of lanes.  For the
+// transposed form a workgroup takes 128 x 128 values, a lane 8 x 8 of them: the
+// columns' scales are maxima over a lane's rows, lanes and waves, and a lane's
+// codes of 8 rows of a column go to LDS as one word, from which each column's 128
+// codes are written as one line.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -15,10 +17,6 @@
 
 namespace dtst {
 namespace {
-
-// LDS pitch of a tile row in floats: the transposed read takes 8 rows of one
-// column per lane, 16 lanes a column and 4 columns a wave.
-constexpr int PITCH = 129;
 
 __device__ __forceinline__ uint32_t code_block(const float (&v)[8], uint2& q) {
   float m = 0.f;
@@ -39,62 +37,98 @@ __device__ __forceinline__ void put_scale(uint8_t* row, int64_t block, int64_t b
     for (int64_t b = blocks; b < (blocks + 3) / 4 * 4; ++b) row[b] = 127;
 }
 
-template <class T, bool ROWS, bool COLS>
+// Rows alone: a block of 128 for every 16 lanes.
+template <class T>
 __global__ void __launch_bounds__(256)
-quantise_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, uint8_t* scale, uint8_t* qt,
-                uint8_t* scale_t, int col_tiles) {
-  __shared__ float tile[COLS ? 128 * PITCH : 1];
+quantise_rows_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, uint8_t* scale, uint32_t col_blocks) {
+  const uint32_t id = blockIdx.x * 16 + (threadIdx.x >> 4), part = threadIdx.x & 15;
+  const uint32_t block = id % col_blocks;
+  const int64_t row = id / col_blocks, c = int64_t(block) * 128 + part * 8;
+  if (row >= d.rows) return;  // (all 16 lanes of the block)
+  float v[8];
+  load_n<8>(x + row * d.ld_x + c, d.cols - c, v);
+  uint2 codes;
+  const uint32_t s = code_block(v, codes);
+  *reinterpret_cast<uint2*>(q + row * d.ld_q + c) = codes;
+  if (part == 0) put_scale(scale + row * d.ld_scale, block, col_blocks, s);
+}
+
+template <class T, bool ROWS>
+__global__ void __launch_bounds__(256)
+quantise_cols_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, uint8_t* scale, uint8_t* qt,
+                     uint8_t* scale_t, int col_tiles) {
+  __shared__ uint2 codes[128][16];   // 8 codes of a column each, word w of column c at w ^ (c / 8)
+  __shared__ float top[4][128];
   const int64_t rt = blockIdx.x / col_tiles, ct = blockIdx.x % col_tiles;
-  const int sub = threadIdx.x >> 4, part = threadIdx.x & 15;  // 16 rows at a time, 16 lanes a row
+  const int sub = threadIdx.x >> 4, part = threadIdx.x & 15, wave = threadIdx.x >> 6;  // rows 8 sub .., columns 8 part ..
   const int64_t c = ct * 128 + part * 8;
   const int64_t col_blocks = (d.cols + 127) / 128, row_blocks = (d.rows + 127) / 128;
+  float v[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int lr = i * 16 + sub;
-    const int64_t row = rt * 128 + lr;
-    float v[8];
-    load_n<8>(x + row * d.ld_x + c, row < d.rows ? d.cols - c : 0, v);
-    if constexpr (ROWS) {
-      uint2 codes;
-      const uint32_t s = code_block(v, codes);
+    const int64_t row = rt * 128 + sub * 8 + i;
+    load_n<8>(x + row * d.ld_x + c, row < d.rows ? d.cols - c : 0, v[i]);
+  }
+  float m[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    m[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[j] = fmaxf(m[j], finite_abs(v[i][j]));
+    m[j] = fmaxf(m[j], __shfl_xor(m[j], 16, 64));
+    m[j] = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
+    if ((threadIdx.x & 48) == 0) top[wave][part * 8 + j] = m[j];
+  }
+  if constexpr (ROWS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = rt * 128 + sub * 8 + i;
+      uint2 r;
+      const uint32_t s = code_block(v[i], r);
       if (row < d.rows) {
-        *reinterpret_cast<uint2*>(q + row * d.ld_q + c) = codes;
+        *reinterpret_cast<uint2*>(q + row * d.ld_q + c) = r;
         if (part == 0) put_scale(scale + row * d.ld_scale, ct, col_blocks, s);
       }
     }
-    if constexpr (COLS) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) tile[lr * PITCH + part * 8 + j] = v[j];
-    }
   }
-  if constexpr (COLS) {
-    __syncthreads();
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int lc = i * 16 + sub;
-      const int64_t col = ct * 128 + lc;
-      float v[8];
+  for (int j = 0; j < 8; ++j) {
+    const int lc = part * 8 + j;
+    const uint32_t s = scale_byte(fmaxf(fmaxf(top[0][lc], top[1][lc]), fmaxf(top[2][lc], top[3][lc])));
+    const float inv = scale_inverse(s);
+    uint2 r;
+    r.x = to_codes(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv);
+    r.y = to_codes(v[4][j] * inv, v[5][j] * inv, v[6][j] * inv, v[7][j] * inv);
+    codes[lc][sub ^ part] = r;
+    if (sub == 0 && c + j < d.cols) put_scale(scale_t + (c + j) * d.ld_scale_t, rt, row_blocks, s);
+  }
+  __syncthreads();
+  // 8 lanes a column, two words each
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = tile[(part * 8 + j) * PITCH + lc];
-      uint2 codes;
-      const uint32_t s = code_block(v, codes);
-      if (col < d.cols) {
-        *reinterpret_cast<uint2*>(qt + col * d.ld_qt + rt * 128 + part * 8) = codes;
-        if (part == 0) put_scale(scale_t + col * d.ld_scale_t, rt, row_blocks, s);
-      }
-    }
+  for (int i = 0; i < 4; ++i) {
+    const int lc = i * 32 + (threadIdx.x >> 3), pair = threadIdx.x & 7, p = lc >> 3;
+    const uint4 two = *reinterpret_cast<const uint4*>(&codes[lc][(pair ^ (p >> 1)) * 2]);
+    const int64_t col = ct * 128 + lc;
+    if (col < d.cols)
+      *reinterpret_cast<uint4*>(qt + col * d.ld_qt + rt * 128 + pair * 16) =
+          (p & 1) ? uint4{two.z, two.w, two.x, two.y} : two;
   }
 }
 
 template <class T>
 int launch(const dtst_quantise_desc& d, const void* x, void* q, void* scale, void* qt, void* scale_t, hipStream_t s) {
   const int64_t ct = (d.cols + 127) / 128, rt = (d.rows + 127) / 128;
-  auto* fn = q == nullptr ? quantise_kernel<T, false, true>
-             : qt == nullptr ? quantise_kernel<T, true, false>
-                             : quantise_kernel<T, true, true>;
-  hipLaunchKernelGGL(fn, dim3(unsigned(ct * rt)), dim3(256), 0, s, d, static_cast<const T*>(x),
-                     static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale), static_cast<uint8_t*>(qt),
-                     static_cast<uint8_t*>(scale_t), int(ct));
+  const T* xt = static_cast<const T*>(x);
+  uint8_t *q8 = static_cast<uint8_t*>(q), *s8 = static_cast<uint8_t*>(scale);
+  if (qt == nullptr) {
+    hipLaunchKernelGGL(quantise_rows_kernel<T>, dim3(unsigned((d.rows * ct + 15) / 16)), dim3(256), 0, s, d, xt, q8, s8,
+                       uint32_t(ct));
+  } else {
+    auto* fn = q == nullptr ? quantise_cols_kernel<T, false> : quantise_cols_kernel<T, true>;
+    hipLaunchKernelGGL(fn, dim3(unsigned(ct * rt)), dim3(256), 0, s, d, xt, q8, s8, static_cast<uint8_t*>(qt),
+                       static_cast<uint8_t*>(scale_t), int(ct));
+  }
   return hipGetLastError();
 }
 

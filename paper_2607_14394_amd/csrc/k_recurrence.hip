@@ -23,6 +23,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "seq_internal.h"
 #include "seq_ops.h"
@@ -34,13 +35,18 @@ constexpr int SPAN = DTST_RECURRENCE_SPAN;
 constexpr int WAVES = 8;
 constexpr int RPW = SPAN / WAVES;  // steps of a wave
 
-// s(x) and s(-x), both to full relative precision (1 - s(x) would lose it).
-// Infinities give 0 and 1, no number gives no number.
+// exp(-x)
+__device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
+
+// s(x) and s(-x), both to full relative precision (1 - s(x) would lose that of a
+// small s(-x), and 1 / (1 + exp(x)) costs two more transcendentals).  Infinities
+// give 0 and 1, no number gives no number.
 __device__ __forceinline__ void logistic(float x, float& s, float& sn) {
-  const float e = __expf(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-  s = x >= 0.f ? r : er;
-  sn = x >= 0.f ? er : r;
+  const float e = exp_minus(x);
+  s = __builtin_amdgcn_rcpf(1.f + e);
+  sn = x < 0.f ? 1.f - s : e * s;
 }
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + exp_minus(x)); }
 
 struct Strides {
   int64_t b, t;
@@ -140,7 +146,7 @@ __device__ __forceinline__ Place place_of(const Args& p, unsigned* slot) {
   if constexpr (CHAIN) {
     if (threadIdx.x == 0) *slot = atomicAdd(p.ticket, 1u);
     __syncthreads();
-    id = *slot;
+    id = uint32_t(__builtin_amdgcn_readfirstlane(int(*slot)));  // (one for all: addresses stay in scalar registers)
   }
   Place q;
   q.tile = id % p.tiles;
@@ -170,7 +176,7 @@ __global__ void __launch_bounds__(64 * WAVES)
 recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zero, T* y, float* h_out, float* states) {
   __shared__ float mapA[WAVES][64 * CPL], mapH[WAVES][64 * CPL], enter[64 * CPL];
   __shared__ unsigned slot;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const Place q = place_of<CPL, CHAIN>(p, &slot);
   const int64_t n = length_of(p, q.b), span0 = int64_t(q.span) * SPAN, t0 = span0 + wave * R;
   if (span0 >= n && !(span0 == 0)) {  // past the end: zeros (n = 0 goes on for the states)
@@ -204,10 +210,21 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < CPL; ++c) {
-        float g, gn;
-        logistic(float(zr[i][c]), g, gn);
-        s[i][c] = i < rows ? g : 1.f;
-        bv[i][c] = i < rows ? gn * float(vr[i][c]) : 0.f;
+        float gn;
+        logistic(float(zr[i][c]), s[i][c], gn);
+        bv[i][c] = gn * float(vr[i][c]);
+      }
+    if (rows < R) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int c = 0; c < CPL; ++c)
+          if (i >= rows) s[i][c] = 1.f, bv[i][c] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
         A[c] *= s[i][c];
         H[c] = s[i][c] * H[c] + bv[i][c];
       }
@@ -255,7 +272,7 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
 #pragma unroll
   for (int c = 0; c < CPL; ++c)
     for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
-  if (rows > 0) {
+  const auto run = [&](auto full) {  // full: all rows are live
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       float r[CPL];
@@ -265,14 +282,17 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
         r[c] = h[c];
         if (o != nullptr) {
           const float x = float(orw[i][c]);
-          float so, son;
-          logistic(x, so, son);
-          r[c] *= x * so;
+          r[c] *= x * logistic(x);
         }
-        if (i >= rows) r[c] = 0.f;
+        if (!full.value && i >= rows) r[c] = 0.f;
       }
-      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, r);
+      if (q.live && (full.value || t0 + i < p.steps)) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, r);
     }
+  };
+  if (rows == R) {
+    run(std::true_type());
+  } else if (rows > 0) {
+    run(std::false_type());
   } else {
     for (int i = 0; i < R; ++i)
       if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, {});
@@ -292,7 +312,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
                       T* g_z, T* g_v, T* g_o, float* g_hzero) {
   __shared__ float mapA[WAVES][64 * CPL], mapH[WAVES][64 * CPL], mapG[WAVES][64 * CPL], enter[64 * CPL];
   __shared__ unsigned slot;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const Place q = place_of<CPL, CHAIN>(p, &slot);
   const int64_t n = length_of(p, q.b);
   const int live_spans = int((n + SPAN - 1) / SPAN);
@@ -318,7 +338,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
   }
   const int rows = int(n - t0 < 0 ? 0 : n - t0 < R ? n - t0 : R);
   raw_t<T, CPL> zr[R], vr[R], orw[R], gr[R];
-  float s[R][CPL], sn[R][CPL], prev[R][CPL];
+  float s[R][CPL], sn[R][CPL], b[R][CPL], g[R][CPL];  // b: then the state before the row
   float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) {
@@ -345,26 +365,32 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < CPL; ++c) {
-        float g, gn;
-        logistic(float(zr[i][c]), g, gn);
-        s[i][c] = i < rows ? g : 1.f;
-        sn[i][c] = i < rows ? gn : 0.f;
+        logistic(float(zr[i][c]), s[i][c], sn[i][c]);
+        b[i][c] = sn[i][c] * float(vr[i][c]);
+        g[i][c] = float(gr[i][c]);
+        if (o != nullptr) {
+          const float x = float(orw[i][c]);
+          g[i][c] *= x * logistic(x);
+        }
+      }
+    if (rows < R) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int c = 0; c < CPL; ++c)
+          if (i >= rows) s[i][c] = 1.f, sn[i][c] = b[i][c] = g[i][c] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
         A[c] *= s[i][c];
-        H[c] = s[i][c] * H[c] + (i < rows ? gn * float(vr[i][c]) : 0.f);
+        H[c] = s[i][c] * H[c] + b[i][c];
       }
 #pragma unroll
     for (int i = R - 1; i >= 0; --i)
 #pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        float g = float(gr[i][c]);
-        if (o != nullptr) {
-          const float x = float(orw[i][c]);
-          float so, son;
-          logistic(x, so, son);
-          g *= x * so;
-        }
-        G[c] = s[i][c] * ((i < rows ? g : 0.f) + G[c]);
-      }
+      for (int c = 0; c < CPL; ++c) G[c] = s[i][c] * (g[i][c] + G[c]);
   }
   if (waves > 1) {
 #pragma unroll
@@ -406,13 +432,14 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
     for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
     for (int i = waves - 1; i > wave; --i) e[c] = mapA[i][lane * CPL + c] * e[c] + mapG[i][lane * CPL + c];
   }
-  if (rows > 0) {
+  const auto run = [&](auto full) {  // full: all rows are live
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < CPL; ++c) {
-        prev[i][c] = h[c];
-        h[c] = s[i][c] * h[c] + (i < rows ? sn[i][c] * float(vr[i][c]) : 0.f);
+        const float next = s[i][c] * h[c] + b[i][c];
+        b[i][c] = h[c];
+        h[c] = next;
       }
 #pragma unroll
     for (int i = R - 1; i >= 0; --i) {
@@ -420,31 +447,29 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
 #pragma unroll
       for (int c = 0; c < CPL; ++c) {
         const float vv = float(vr[i][c]);
-        float g = float(gr[i][c]);
         go[c] = 0.f;
         if (o != nullptr) {
-          const float x = float(orw[i][c]), ht = s[i][c] * prev[i][c] + sn[i][c] * vv;
-          float so, son;
-          logistic(x, so, son);
-          go[c] = g * ht * so * (1.f + x * son);
-          g *= x * so;
+          const float x = float(orw[i][c]), so = logistic(x);
+          go[c] = float(gr[i][c]) * (s[i][c] * b[i][c] + sn[i][c] * vv) * (so + x * so * (1.f - so));
         }
-        const float d = g + e[c];
+        const float d = g[i][c] + e[c];
         gv[c] = d * sn[i][c];
-        gz[c] = gv[c] * s[i][c] * (prev[i][c] - vv);
-        if (i < rows) {
-          e[c] = s[i][c] * d;
-        } else {
-          gz[c] = gv[c] = go[c] = 0.f;
-        }
+        gz[c] = gv[c] * s[i][c] * (b[i][c] - vv);
+        e[c] = s[i][c] * d;
+        if (!full.value && i >= rows) gz[c] = gv[c] = go[c] = 0.f;
       }
       const int64_t t = t0 + i;
-      if (t < p.steps && q.live) {
+      if (q.live && (full.value || t < p.steps)) {
         put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, gz);
         put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, gv);
         if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, go);
       }
     }
+  };
+  if (rows == R) {
+    run(std::true_type());
+  } else if (rows > 0) {
+    run(std::false_type());
   } else {
     for (int i = 0; i < R; ++i) {
       const int64_t t = t0 + i;

@@ -2,8 +2,6 @@
 differences, 8-bit rounding against torch's conversion, and the binding's
 argument checks (no GPU needed)."""
 
-import ctypes
-
 import numpy as np
 import pytest
 import torch
@@ -102,8 +100,8 @@ def norm_call(x=P, res=None, w=P * 2, s=None, y=P * 3, scale=None, rstd=None, **
     f = dict(rows=4, cols=64, ld_x=64, ld_res=64, ld_sum=64, ld_y=128, ld_scale=4, x_type=1, res_type=1, y_type=1,
              eps=1e-6)
     f.update(kw)
-    d = D.NormDesc(**f)
-    return status(D.lib.dtst_rms_norm, ctypes.addressof(d), x, res, w, s, y, scale, rstd, None)
+    d = D.NORM_DESC.pack(*f.values())
+    return status(D.lib.dtst_rms_norm, d, x, res, w, s, y, scale, rstd, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
@@ -131,8 +129,8 @@ def test_norm_of_no_rows_is_done():
 def adj_call(gy=P, u=P * 2, w=P * 3, r=P * 4, gs=None, gu=P * 5, gx=None, gw=P * 6, ws=P * 7, nws=1 << 16, **kw):
     f = dict(rows=4, cols=64, ld_g_y=64, ld_u=64, ld_g_sum=64, ld_g_u=64, ld_g_x=64, x_type=1, res_type=0, accumulate=0)
     f.update(kw)
-    d = D.NormAdjDesc(**f)
-    return status(D.lib.dtst_rms_norm_adj, ctypes.addressof(d), gy, u, w, r, gs, gu, gx, gw, ws, nws, None)
+    d = D.NORM_ADJ_DESC.pack(*f.values())
+    return status(D.lib.dtst_rms_norm_adj, d, gy, u, w, r, gs, gu, gx, gw, ws, nws, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
@@ -150,8 +148,8 @@ def test_norm_adj_refusals(kw, code, word):
 def quantise_call(x=P, q=P * 2, s=P * 3, qt=None, st=None, **kw):
     f = dict(rows=4, cols=200, ld_x=200, ld_q=256, ld_scale=4, ld_qt=128, ld_scale_t=4, type=1)
     f.update(kw)
-    d = D.QuantiseDesc(**f)
-    return status(D.lib.dtst_quantise, ctypes.addressof(d), x, q, s, qt, st, None)
+    d = D.QUANTISE_DESC.pack(*f.values())
+    return status(D.lib.dtst_quantise, d, x, q, s, qt, st, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
@@ -169,8 +167,8 @@ def test_quantise_refusals(kw, code, word):
 def product_call(a=P, sa=P * 2, b=P * 3, sb=P * 4, bias=None, c=P * 5, ws=None, nws=0, **kw):
     f = dict(m=70, n=80, k=200, ld_a=256, ld_a_scale=4, ld_b=256, ld_b_scale=4, ld_c=80, c_type=1, accumulate=0, short_sums=0)
     f.update(kw)
-    d = D.ProductDesc(**f)
-    return status(D.lib.dtst_product, ctypes.addressof(d), a, sa, b, sb, bias, c, ws, nws, None)
+    d = D.PRODUCT_DESC.pack(*f.values())
+    return status(D.lib.dtst_product, d, a, sa, b, sb, bias, c, ws, nws, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
@@ -190,14 +188,18 @@ def test_product_of_nothing_is_done():
 
 
 def recur_call(z=P, v=P * 2, o=P * 3, h0=None, n=None, y=P * 4, h=None, st=None, ws=P * 8, nws=1 << 30, fn="dtst_recurrence", **kw):
-    f = dict(batch=2, steps=300, features=16, type=1)
+    f = dict(batch=2, steps=300, features=16)
     f.update({k + "_stride": (4800, 16) for k in ("z", "v", "o", "y", "g_z", "g_v", "g_o")})
+    f.update(type=1)
     f.update(kw)
-    d = D.RecurrenceDesc(**f)
+    flat = []
+    for x in f.values():
+        flat += list(x) if isinstance(x, tuple) else [x]
+    d = D.RECURRENCE_DESC.pack(*flat)
     if fn == "dtst_recurrence":
-        return status(D.lib.dtst_recurrence, ctypes.addressof(d), z, v, o, h0, n, y, h, st, ws, nws, None)
+        return status(D.lib.dtst_recurrence, d, z, v, o, h0, n, y, h, st, ws, nws, None)
     gz, gv, go = kw.get("out", (P * 5, P * 6, P * 7))
-    return status(D.lib.dtst_recurrence_adj, ctypes.addressof(d), z, v, o, n, st, y, h0, gz, gv, go, h, ws, nws, None)
+    return status(D.lib.dtst_recurrence_adj, d, z, v, o, n, st, y, h0, gz, gv, go, h, ws, nws, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
