@@ -252,7 +252,7 @@ dtst_status product(const dtst_product_desc* d, const void* a, const void* a_sca
     return fail(DTST_ERR_UNSUPPORTED, "k or a stride of a or b above 2^23");
   if (d->m > (int64_t(1) << 31) || d->n > (int64_t(1) << 31))
     return fail(DTST_ERR_UNSUPPORTED, "m or n above 2^31");
-  DTST_TRY(check_grid(d->m <= 64 ? (d->n + 15) / 16 : ((d->m + 63) / 64) * ((d->n + 63) / 64), 512));
+  DTST_TRY(check_grid(((d->m + 127) / 128) * ((d->n + 127) / 128), 512));
   const size_t need = product_workspace(d->m, d->n, d->k);
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   const Array aws{need ? workspace : nullptr, 1, int64_t(need), int64_t(need), 1, "workspace"};

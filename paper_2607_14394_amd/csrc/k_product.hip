@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "seq_internal.h"
 #include "seq_ops.h"
@@ -49,90 +50,26 @@ struct Operands {
   int accumulate;
 };
 
-// Four neighbouring columns of a row of c, `left` of them inside.
+// Eight neighbouring columns of a row of c, `left` of them inside.
 template <class TC>
-__device__ __forceinline__ void put_c(TC* c, int64_t left, v4f v, const float* bias, int accumulate) {
-  float o[4], e[4];
+__device__ __forceinline__ void put_c(TC* c, int64_t left, float (&v)[8], const float* bias, int accumulate) {
+  float e[8];
   if (bias != nullptr) {
-    load_n<4>(bias, left, e);
+    load_n<8>(bias, left, e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += e[i];
+    for (int i = 0; i < 8; ++i) v[i] += e[i];
   }
   if (accumulate) {
-    load_n<4>(c, left, e);
+    load_n<8>(c, left, e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += e[i];
+    for (int i = 0; i < 8; ++i) v[i] += e[i];
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = v[i];
-  store_n<4>(c, left, o);
+  store_n<8>(c, left, v);
 }
 
-// ---- few rows of a ----------------------------------------------------------
-//
-// Up to 16 MT rows: bound by reading b once.  A workgroup takes 16 rows of b;
-// its waves take every eighth block of 128 codes, straight from global memory,
-// and their sums meet in LDS in a fixed order.
-constexpr int FEW_WAVES = 8;
-
-template <class TC, int MT>
-__global__ void __launch_bounds__(64 * FEW_WAVES)
-product_few_kernel(Operands p, TC* c) {
-  __shared__ v4f sums[FEW_WAVES][MT][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int64_t n0 = int64_t(blockIdx.x) * 16;
-  // rows past the end read the last one; their results are not stored
-  const int64_t rb = min(n0 + r, p.n - 1);
-  const uint8_t *pb = p.b + rb * p.ld_b + g * 32, *psb = p.sb + rb * p.ld_sb;
-  const uint8_t *pa[MT], *psa[MT];
-  v4f acc[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t ra = min(int64_t(i * 16 + r), p.m - 1);
-    pa[i] = p.a + ra * p.ld_a + g * 32;
-    psa[i] = p.sa + ra * p.ld_sa;
-    acc[i] = v4f{0.f, 0.f, 0.f, 0.f};
-  }
-  const int nk = int((p.k + 127) / 128);
-  for (int kb = wave; kb < nk; kb += FEW_WAVES) {
-    const uint4* qb = reinterpret_cast<const uint4*>(pb + int64_t(kb) * 128);
-    const uint4 y0 = qb[0], y1 = qb[1];
-    const float sb = scale_value(psb[kb]);
-    uint4 x[MT][2];
-    float sa[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const uint4* qa = reinterpret_cast<const uint4*>(pa[i] + int64_t(kb) * 128);
-      x[i][0] = qa[0], x[i][1] = qa[1];
-      sa[i] = scale_value(psa[i][kb]);
-    }
-    const v8b fb[4] = {widen(y0.x, y0.y, sb), widen(y0.z, y0.w, sb), widen(y1.x, y1.y, sb), widen(y1.z, y1.w, sb)};
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[2 * h], widen(x[i][h].x, x[i][h].y, sa[i]), acc[i], 0, 0, 0);
-        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[2 * h + 1], widen(x[i][h].z, x[i][h].w, sa[i]), acc[i], 0, 0, 0);
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
-  __syncthreads();
-  for (int i = wave; i < MT; i += FEW_WAVES) {
-    v4f v = sums[0][i][lane];
-#pragma unroll
-    for (int w = 1; w < FEW_WAVES; ++w) v += sums[w][i][lane];
-    const int64_t row = i * 16 + r, col = n0 + g * 4;
-    if (row < p.m && col < p.n)
-      put_c(c + row * p.ld_c + col, p.n - col, v, p.bias == nullptr ? nullptr : p.bias + col, p.accumulate);
-  }
-}
-
-// ---- tiles ------------------------------------------------------------------
-//
-// A workgroup of WM x WN waves takes BM x BN of c, a wave TM x TN tiles of 16 x
-// 16.  Each 128 codes of the summed axis are a stage: the rows' 128 bytes go
+// A workgroup takes BM x BN of c.  WM x WN waves hold it, each TM x TN tiles of 16
+// x 16; KS such groups take a part of the summed axis each and add up in LDS at
+// the end.  Each 128 codes of the summed axis are a stage: the rows' 128 bytes go
 // straight from global memory to LDS (16 bytes a lane, no registers), STAGES - 1
 // stages ahead of the products.  A row's 16-byte chunk i lies at place
 // i ^ (row % 8), so the 8 lanes that read one chunk of 8 rows meet 8 different
@@ -143,19 +80,17 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)(p)));
 }
 
-// 64 lanes' 16 (4) bytes at base + off to LDS at `to` + 16 (4) times the lane.
-// (The compiler does not see the load: whoever reads the bytes waits for it.)
+// 64 lanes' 16 bytes at base + off (4 bytes at p) to LDS at `to` + 16 (4) times
+// the lane.  (The compiler does not see the load: whoever reads the bytes waits
+// for it.)
 __device__ __forceinline__ void fetch16(const uint8_t* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(to), "v"(off), "s"(base)
                : "memory");
 }
-__device__ __forceinline__ void fetch4(const uint8_t* base, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               :
-               : "s"(to), "v"(off), "s"(base)
-               : "memory");
+__device__ __forceinline__ void fetch4(const uint8_t* p, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(to), "v"(p) : "memory");
 }
 // At most N of the wave's loads are still on their way, and none of its reads
 // of LDS.
@@ -164,15 +99,20 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
 }
 
-template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, class TC>
-__global__ void __launch_bounds__(64 * WM * WN)
+template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
+__global__ void __launch_bounds__(64 * WM * WN * KS)
 product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
   constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, STAGE = (BM + BN) * ROW;
   constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;  // loads of a wave and stage: 8 rows each
   static_assert(LA * 8 * WAVES == BM && LB * 8 * WAVES == BN, "whole loads");
-  constexpr int SCALES = (BM + BN) * 4;
-  extern __shared__ uint8_t lds[];  // STAGES stages, then two groups of scale words
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  constexpr int SL = (BM + BN + 63) / 64, SPW = (SL + WAVES - 1) / WAVES;  // scale words: 64 rows a load, waves in turn
+  constexpr int SCALES = SL * 256;
+  constexpr int GROUP = STAGES * STAGE + 2 * SCALES;  // LDS of a group: its stages, then two groups of scale words
+  static_assert((KS - 1) * BM * BN * 4 <= KS * GROUP, "the sums fit over the stages");
+  extern __shared__ uint8_t lds_all[];
+  const int any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave = any_wave % WAVES, group = any_wave / WAVES;
+  uint8_t* lds = lds_all + group * GROUP;
   const int r = lane & 15, g = lane >> 4;
 
   // Workgroups go to the 8 dies in turn: a die gets neighbouring tiles, in bands
@@ -184,7 +124,9 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
     id = die * per + min(die, extra) + id / 8;
   }
   const int band = id / (8 * n_tiles), band_rows = min(8, m_tiles - band * 8), in_band = id - band * 8 * n_tiles;
-  const int64_t m0 = int64_t(band * 8 + in_band % band_rows) * BM, n0 = int64_t(in_band / band_rows) * BN;
+  // (readfirstlane: the addresses that follow from them belong in scalar registers)
+  const int64_t m0 = int64_t(__builtin_amdgcn_readfirstlane(band * 8 + in_band % band_rows)) * BM;
+  const int64_t n0 = int64_t(__builtin_amdgcn_readfirstlane(in_band / band_rows)) * BN;
 
   // Where this lane's loads start: row wave * L + .. of each operand.  Rows past
   // the end read the last one; their results are not stored.
@@ -201,34 +143,40 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
     const int64_t row = min<int64_t>((wave * LB + i) * 8 + (lane >> 3), p.n - 1 - n0);
     off_b[i] = uint32_t(row * p.ld_b) + chunk * 16;
   }
-  // scale words: 64 rows a load, the waves in turn
-  constexpr int SL = (BM + BN) / 64, SPW = (SL + WAVES - 1) / WAVES;
-  uint32_t off_s[SPW];
+  const uint8_t* scale_rows[SPW];  // this lane's row of scales for each load
 #pragma unroll
   for (int i = 0; i < SPW; ++i) {
     const int row = (wave + i * WAVES) * 64 + lane;
-    off_s[i] = row < BM ? uint32_t(min<int64_t>(row, p.m - 1 - m0) * p.ld_sa)
-                        : uint32_t(min<int64_t>(row - BM, p.n - 1 - n0) * p.ld_sb);
+    scale_rows[i] = row < BM ? p.sa + min(m0 + row, p.m - 1) * p.ld_sa : p.sb + min(n0 + row - BM, p.n - 1) * p.ld_sb;
   }
-  const uint8_t *base_sa = p.sa + m0 * p.ld_sa, *base_sb = p.sb + n0 * p.ld_sb;
+
+  // this group's blocks of 128: nk from block k0 on (groups of scale words stay
+  // whole); every group meets at `steps` barriers
+  const int blocks = int((p.k + 127) / 128);
+  const int steps = KS == 1 ? blocks : ((blocks + KS - 1) / KS + 3) / 4 * 4;
+  const int k0 = group * steps, nk = KS == 1 ? blocks : min(max(blocks - k0, 0), steps);
+  base_a += int64_t(k0) * ROW, base_b += int64_t(k0) * ROW;
 
   const uint32_t lds0 = lds_address(lds);
-  const auto fetch = [&](int kb) {
-    const uint32_t to = lds0 + (kb % STAGES) * STAGE;
+  // the scale words (every fourth stage) and part i of n of a stage's loads
+  const auto fetch_scales = [&](int kb) {
     if (kb % 4 == 0) {
 #pragma unroll
       for (int i = 0; i < SPW; ++i) {
         const int part = wave + i * WAVES;
-        if (part < SL)
-          fetch4((part * 64 < BM ? base_sa : base_sb) + kb, off_s[i],
-                 lds0 + STAGES * STAGE + (kb / 4 % 2) * SCALES + part * 256);
+        if (part < SL) fetch4(scale_rows[i] + k0 + kb, lds0 + STAGES * STAGE + (kb / 4 % 2) * SCALES + part * 256);
       }
     }
+  };
+  const auto fetch = [&](int kb, int i, int n) {
+    const uint32_t to = lds0 + (kb % STAGES) * STAGE;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) fetch16(base_a + int64_t(kb) * ROW, off_a[i], to + (wave * LA + i) * 1024);
-#pragma unroll
-    for (int i = 0; i < LB; ++i)
-      fetch16(base_b + int64_t(kb) * ROW, off_b[i], to + BM * ROW + (wave * LB + i) * 1024);
+    for (int l = (LA + LB) * i / n; l < (LA + LB) * (i + 1) / n; ++l) {
+      if (l < LA)
+        fetch16(base_a + int64_t(kb) * ROW, off_a[l], to + (wave * LA + l) * 1024);
+      else
+        fetch16(base_b + int64_t(kb) * ROW, off_b[l - LA], to + BM * ROW + (wave * LB + l - LA) * 1024);
+    }
   };
 
   v4f acc[TM][TN];
@@ -239,11 +187,10 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
 
   const int wm = wave / WN, wn = wave % WN;
   const int place = r * ROW + ((g ^ (r & 7)) << 4);  // chunk g of row r; chunk g + 4 lies at ^ 64
-  const int nk = int((p.k + 127) / 128);
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
-    if (s < nk) fetch(s);
-  for (int kb = 0; kb < nk; ++kb) {
+    if (s < nk) fetch_scales(s), fetch(s, 0, 1);
+  for (int kb = 0; kb < steps; ++kb) {
     // this stage's loads are done when only those of the STAGES - 2 later ones are left
     if (kb + STAGES - 2 < nk)
       wait_loads<(LA + LB) * (STAGES - 2)>();
@@ -251,7 +198,15 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
       wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
-    if (kb + STAGES - 1 < nk) fetch(kb + STAGES - 1);  // over the stage that every wave has left
+    // The loads go over the stage that every wave has left, spread over the first
+    // half of the products: in one go they would hold up the first reads of LDS.
+    constexpr int PARTS = TM >= 4 ? TM / 2 : 1;
+    const int ahead = kb + STAGES - 1;
+    if (ahead < nk) {
+      fetch_scales(ahead);
+      if (PARTS == 1) fetch(ahead, 0, 1);
+    }
+    if (KS > 1 && kb >= nk) continue;
     const uint8_t* at_a = lds + (kb % STAGES) * STAGE + wm * TM * 16 * ROW;
     const uint8_t* at_b = lds + (kb % STAGES) * STAGE + BM * ROW + wn * TN * 16 * ROW;
     const uint8_t* at_sa = lds + STAGES * STAGE + (kb / 4 % 2) * SCALES + (wm * TM * 16 + r) * 4 + kb % 4;
@@ -284,6 +239,7 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i & 1], acc[i][j], 0, 0, 0, sb[j], 0,
                                                                         sa[i & 1]);
         __builtin_amdgcn_sched_barrier(0);
+        if (PARTS > 1 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
       }
     } else {
       float sa[TM], sb[TN];
@@ -308,58 +264,137 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
               acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][e], fa[e], acc[i][j], 0, 0, 0);
+          if (PARTS > 1 && h == 0 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
         }
       }
     }
   }
+  __syncthreads();
+  if constexpr (KS > 1) {
+    v4f* sums = reinterpret_cast<v4f*>(lds_all) + wave * 64 + lane;  // (group - 1, tile, wave, lane)
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sums[(((group - 1) * TM + i) * TN + j) * WAVES * 64] = acc[i][j];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] += sums[((k * TM + i) * TN + j) * WAVES * 64];
+  }
+  // 16 rows at a time through the wave's own strip of LDS, so that a lane stores
+  // eight neighbouring columns and a row's lanes whole lines.
+  constexpr int PITCH = TN * 16 + 4;  // (8 rows' accesses of 16 bytes meet all banks)
+  static_assert((KS - 1) * BM * BN * 4 + WAVES * 16 * PITCH * 4 <= KS * GROUP, "the strips fit beside the sums");
+  float* strip = reinterpret_cast<float*>(lds_all + (KS - 1) * BM * BN * 4) + wave * 16 * PITCH;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int64_t row = m0 + (wm * TM + i) * 16 + r;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t col = n0 + (wn * TN + j) * 16 + g * 4;
+    for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
+#pragma unroll
+    for (int e = 0; e < TN / 2; ++e) {
+      const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const v4f x = *reinterpret_cast<const v4f*>(strip + at * PITCH + c8 + h * 4);
+        v[4 * h] = x[0], v[4 * h + 1] = x[1], v[4 * h + 2] = x[2], v[4 * h + 3] = x[3];
+      }
+      const int64_t row = m0 + (wm * TM + i) * 16 + at, col = n0 + wn * TN * 16 + c8;
       if (row < p.m && col < p.n)
-        put_c(c + row * p.ld_c + col, p.n - col, acc[i][j], p.bias == nullptr ? nullptr : p.bias + col, p.accumulate);
+        put_c(c + row * p.ld_c + col, p.n - col, v, p.bias == nullptr ? nullptr : p.bias + col, p.accumulate);
     }
   }
 }
 
-template <class TC, int MT>
-int launch_few(const Operands& p, void* c, hipStream_t s) {
-  hipLaunchKernelGGL((product_few_kernel<TC, MT>), dim3(unsigned((p.n + 15) / 16)), dim3(64 * FEW_WAVES), 0, s, p,
-                     static_cast<TC*>(c));
-  return hipGetLastError();
+// Raises a kernel's limit of dynamic LDS on the current device, once (the call
+// takes as long as a launch).
+hipError_t allow_lds(const void* fn, size_t bytes, std::atomic<uint64_t>& done) {
+  if (bytes <= 65536) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
-template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, class TC>
+template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
 int launch_tile(const Operands& p, void* c, hipStream_t s) {
   constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
   const int64_t mt = (p.m + BM - 1) / BM, nt = (p.n + BN - 1) / BN;
-  constexpr size_t lds = size_t(STAGES) * (BM + BN) * ROW + 2 * (BM + BN) * 4;
-  auto* fn = product_tile_kernel<SHORT, WM, WN, TM, TN, STAGES, TC>;
-  if (lds > 65536) {
-    const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(fn, dim3(unsigned(mt * nt)), dim3(64 * WM * WN), lds, s, p, static_cast<TC*>(c), int(mt), int(nt));
+  constexpr size_t lds = KS * (size_t(STAGES) * (BM + BN) * ROW + 2 * ((BM + BN + 63) / 64 * 256));
+  auto* fn = product_tile_kernel<SHORT, WM, WN, TM, TN, STAGES, KS, TC>;
+  static std::atomic<uint64_t> allowed{0};  // devices whose limit for this kernel is raised (one bit each, 64 of them)
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(fn), lds, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fn, dim3(unsigned(mt * nt)), dim3(64 * WM * WN * KS), lds, s, p, static_cast<TC*>(c), int(mt), int(nt));
   return hipGetLastError();
 }
 
-template <class TC>
-int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
-  if (p.m <= 16) return launch_few<TC, 1>(p, c, s);
-  if (p.m <= 32) return launch_few<TC, 2>(p, c, s);
-  if (p.m <= 64) return launch_few<TC, 4>(p, c, s);
+// The tile.  A card of 256 CUs is short of workgroups long before it is short of
+// products, so small results take the smallest tile that still leaves one
+// workgroup a CU, its waves dividing the summed axis.  Measured with 16-bit
+// results, in us:
+//                        16 x 32   64 x 32   64 x 64   128 x 64
+//   4 x 4608 x 2048          3.9       5.4       6.5
+//   48 x 8192 x 8192                  13.0      16.6
+//   256 x 4096 x 4096                 13.9       9.7       17.7
+//   2048 x 2048 x 2048                          14.4       13.0
+// Larger ones take the tile whose rounds of workgroups over the card cost least,
+// at the rates that full rounds reach (`at once`: workgroups that the card holds;
+// where a CU holds two, the last round of a few overlaps the one before):
+//                        128 x 64   128 x 128   128 x 256   256 x 256
+//   2048 x 2048 x 2048       15.0        16.5
+//   4096 x 1536 x 2048       22.2        19.3        21.4
+//   4096 x 2048 x 4608                   38.9        41.2
+//   4608 x 2048 x 4096                   57.5                    52.4
+//   8192 x 8192 x 8192                  568.6                   442.1
+//   the last, exact                    1039         918.4       811.9
+// Exact sums widen each operand once per wave that reads it, which large tiles do
+// least.
+struct Tile {
+  int64_t bm, bn, at_once;
+  double rate;  // TFLOP/s of full rounds
+};
+
+double cost(const Operands& p, const Tile& t) {
+  const int64_t tiles = ((p.m + t.bm - 1) / t.bm) * ((p.n + t.bn - 1) / t.bn);
+  const double whole = double((tiles + t.at_once - 1) / t.at_once), part = double(tiles) / double(t.at_once);
+  const double rounds = t.at_once > 256 && tiles > t.at_once ? (whole + part) / 2 : whole;
+  return rounds * double(t.at_once * t.bm * t.bn) / t.rate;
+}
+
+template <bool SHORT, class TC>
+int launch(const Operands& p, void* c, hipStream_t s) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
-  if (short_sums) {
-    if (tiles(256, 256) >= 200) return launch_tile<true, 2, 2, 8, 8, 2, TC>(p, c, s);
-    if (tiles(128, 128) >= 200) return launch_tile<true, 2, 2, 4, 4, 2, TC>(p, c, s);
-    return launch_tile<true, 2, 2, 2, 2, 4, TC>(p, c, s);
-  }
-  if (tiles(256, 256) >= 200) return launch_tile<false, 2, 4, 8, 4, 2, TC>(p, c, s);
-  if (tiles(128, 128) >= 200) return launch_tile<false, 2, 2, 4, 4, 2, TC>(p, c, s);
-  return launch_tile<false, 2, 2, 2, 2, 4, TC>(p, c, s);
+  if (tiles(16, 32) <= 256) return launch_tile<SHORT, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
+  if (tiles(64, 32) <= 256) return launch_tile<SHORT, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
+  if (tiles(64, 64) <= 256) return launch_tile<SHORT, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
+  const Tile forms[] = {{128, 64, 512, SHORT ? 1250 : 750},
+                        {128, 128, 512, SHORT ? 1900 : 1000},
+                        {128, 256, 256, SHORT ? 0.1 : 1180},  // (short sums: never the best)
+                        {256, 256, 256, SHORT ? 2480 : 1350}};
+  int best = 0;
+  for (int i = 1; i < 4; ++i)
+    if (cost(p, forms[i]) < cost(p, forms[best])) best = i;
+  if (best == 0) return launch_tile<SHORT, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
+  if (best == 3) return launch_tile<SHORT, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
+  if constexpr (!SHORT)
+    if (best == 2) return launch_tile<SHORT, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
+  return launch_tile<SHORT, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
+}
+
+template <class TC>
+int launch_sums(const Operands& p, int short_sums, void* c, hipStream_t s) {
+  return short_sums ? launch<true, TC>(p, c, s) : launch<false, TC>(p, c, s);
 }
 
 }  // namespace
@@ -372,9 +407,9 @@ int launch_product(const dtst_product_desc& d, const void* a, const void* a_scal
   const Operands p{static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(b),
                    static_cast<const uint8_t*>(a_scale), static_cast<const uint8_t*>(b_scale),
                    d.m, d.n, d.k, d.ld_a, d.ld_a_scale, d.ld_b, d.ld_b_scale, d.ld_c, bias, d.accumulate};
-  if (d.c_type == DTST_F32) return launch<float>(p, d.short_sums, c, s);
-  if (d.c_type == DTST_BF16) return launch<bf16_t>(p, d.short_sums, c, s);
-  return launch<f16_t>(p, d.short_sums, c, s);
+  if (d.c_type == DTST_F32) return launch_sums<float>(p, d.short_sums, c, s);
+  if (d.c_type == DTST_BF16) return launch_sums<bf16_t>(p, d.short_sums, c, s);
+  return launch_sums<f16_t>(p, d.short_sums, c, s);
 }
 
 }  // namespace dtst
