@@ -347,17 +347,27 @@ def _device():
         return -2
 
 
+def _on(stream, dev):
+    """The stream of a call on device dev."""
+    if stream is not None:
+        return int(stream)
+    return _raw_stream(dev) if _raw_stream is not None else torch_stream()
+
+
+def _refuse(t, shape, name, dtypes):
+    raise ValueError(f"{name}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)} with contiguous rows on "
+                     f"the current device, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+# (The checks of a call are a third of its time on the host: each reads a tensor's properties once.)
 def _rows(t, shape, name, dtypes, dev):
     """Row stride of a 2-D tensor on device dev with contiguous rows."""
-    if t.shape != shape or t.dtype not in dtypes or t.get_device() != dev:
-        raise ValueError(f"{name}: need {' or '.join(str(d) for d in dtypes)} of shape {tuple(shape)} on the current "
-                         f"device, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    rows, cols = shape
-    s0, s1 = t.stride()
-    if s1 != 1 and cols > 1 and rows:
-        raise ValueError(f"{name}: columns must be contiguous")
-    # (the stride of a single row is any; one that suits every type)
-    return s0 if rows > 1 else -(-cols // 16) * 16
+    if t.shape == shape and t.dtype in dtypes and t.get_device() == dev:
+        rows, cols = shape
+        s0, s1 = t.stride()
+        if s1 == 1 or cols == 1 or rows == 0:
+            return s0 if rows > 1 else cols + 15 & -16  # (that of a single row is any; one that suits every type)
+    _refuse(t, shape, name, dtypes)
 
 
 def _vector(t, n, name, dev, dtype=torch.float32):
@@ -366,12 +376,22 @@ def _vector(t, n, name, dev, dtype=torch.float32):
 
 
 _FLOATS = (torch.float32, torch.bfloat16, torch.float16)
-_CODES, _SCALES = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu,)
+_CODE, _SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 def _codes(q, s, rows, k, name, dev):
-    return (_rows(q, (rows, code_columns(k)), name, _CODES, dev),
-            _rows(s, (rows, scale_columns(k)), name + " scale", _SCALES, dev))
+    """Row strides of codes and scales."""
+    kq = k + 127 & -128
+    ks = (kq >> 7) + 3 & -4
+    if (q.shape == (rows, kq) and s.shape == (rows, ks) and q.dtype is _CODE and s.dtype is _SCALE
+            and q.get_device() == dev and s.get_device() == dev):
+        if rows <= 1:
+            return kq, ks
+        (q0, q1), (s0, s1) = q.stride(), s.stride()
+        if q1 == 1 and s1 == 1:
+            return q0, s0
+    _refuse(q, (rows, kq), name, (_CODE,)) if q.shape != (rows, kq) or q.dtype is not _CODE or q.stride(-1) != 1 or (
+        q.get_device() != dev) else _refuse(s, (rows, ks), name + " scale", (_SCALE,))
 
 
 def _scratch(ws, need, device, stream):
@@ -406,7 +426,7 @@ def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, e
     _check(lib.dtst_rms_norm(NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt],
                                             _TYPES[y.dtype], eps),
                              x.data_ptr(), _ptr(res), weight.data_ptr(), _ptr(sum_out), y.data_ptr(), _ptr(scale),
-                             _ptr(rstd), _stream(stream)))
+                             _ptr(rstd), _on(stream, dev)))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -434,7 +454,7 @@ def dtst_rms_norm_adj(g_y, u, weight, rstd, g_u, g_weight, g_sum=None, g_x=None,
     _vector(rstd, rows, "rstd", dev)
     p, n, ws = _scratch(ws, dtst_rms_norm_adj_workspace(rows, cols), g_y.device, stream)
     _check(lib.dtst_rms_norm_adj(d, g_y.data_ptr(), u.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(g_sum),
-                                 g_u.data_ptr(), _ptr(g_x), g_weight.data_ptr(), p, n, _stream(stream)))
+                                 g_u.data_ptr(), _ptr(g_x), g_weight.data_ptr(), p, n, _on(stream, dev)))
 
 
 def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
@@ -450,7 +470,7 @@ def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
     ld_q, ld_s = (0, 0) if q is None else _codes(q, scale, rows, cols, "q", dev)
     ld_qt, ld_st = (0, 0) if qt is None else _codes(qt, scale_t, cols, rows, "qt", dev)
     _check(lib.dtst_quantise(QUANTISE_DESC.pack(rows, cols, ld_x, ld_q, ld_s, ld_qt, ld_st, _TYPES[x.dtype]),
-                             x.data_ptr(), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _stream(stream)))
+                             x.data_ptr(), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _on(stream, dev)))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -476,7 +496,7 @@ def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_s
         _vector(bias, n, "bias", dev)
     p, nb, ws = _scratch(ws, dtst_product_workspace(m, n, k), c.device, stream)
     _check(lib.dtst_product(d, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias),
-                            c.data_ptr(), p, nb, _stream(stream)))
+                            c.data_ptr(), p, nb, _on(stream, dev)))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -488,13 +508,11 @@ def dtst_recurrence_workspace(batch, steps, features, dtype) -> int:
 
 def _sequence(t, shape, name, dtype, dev):
     """Strides of batch entries and steps of a (batch, steps, features) tensor."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
-        raise ValueError(f"{name}: need {dtype} of shape {tuple(shape)} on the current device, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
-    sb, st, sf = t.stride()
-    if sf != 1 and shape[2] > 1 and t.numel():
-        raise ValueError(f"{name}: features must be contiguous")
-    return sb, st
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+        sb, st, sf = t.stride()
+        if sf == 1 or shape[2] == 1 or t.numel() == 0:
+            return sb, st
+    _refuse(t, shape, name, (dtype,))
 
 
 def _state(t, shape, name, dev):
@@ -525,7 +543,7 @@ def dtst_recurrence(z, v, y, o=None, h0=None, h_out=None, lengths=None, states=N
         _vector(lengths, B, "lengths", dev, torch.int32)
     p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
     _check(lib.dtst_recurrence(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(h0), _ptr(lengths), y.data_ptr(),
-                               _ptr(h_out), _ptr(states), p, n, _stream(stream)))
+                               _ptr(h_out), _ptr(states), p, n, _on(stream, dev)))
 
 
 def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None, g_hzero=None, lengths=None, ws=None,
@@ -556,7 +574,7 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
     _check(lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
                                    g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o), _ptr(g_hzero),
-                                   p, n, _stream(stream)))
+                                   p, n, _on(stream, dev)))
 
 
 def dtst_profile_enable(on=True):

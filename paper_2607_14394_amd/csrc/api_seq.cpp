@@ -292,6 +292,7 @@ dtst_status check_sequence_sizes(const dtst_recurrence_desc* d) {
   if (d == nullptr) return bad("descriptor is null");
   if (d->batch < 0 || d->steps < 0 || d->features < 0) return bad("need batch, steps and features >= 0");
   if (!is_float_type(d->type)) return bad("type must be DTST_F32, DTST_BF16 or DTST_F16");
+  if (d->features > (int64_t(1) << 28)) return fail(DTST_ERR_UNSUPPORTED, "features above 2^28");
   int64_t n = 0;
   if (__builtin_mul_overflow(d->batch, d->steps, &n) || __builtin_mul_overflow(n, d->features, &n) || n > kMost ||
       __builtin_mul_overflow(d->batch, d->features, &n) || n > kMost)

@@ -133,10 +133,9 @@ __device__ void look_back(const unsigned long long* words, int64_t pitch, int k,
 
 // What a workgroup works on.
 struct Place {
-  int64_t b, c;  // batch entry, the lane's first feature
-  int64_t tile;
-  int span;      // place in the chain, 0 first
-  bool live;     // the lane stores
+  int64_t b, tile;  // batch entry
+  int span;         // place in the chain, 0 first
+  uint32_t c;       // the lane's first feature
 };
 
 // CHAIN: spans by ticket, else one span a sequence (steps <= SPAN).
@@ -152,26 +151,55 @@ __device__ __forceinline__ Place place_of(const Args& p, unsigned* slot) {
   q.tile = id % p.tiles;
   q.span = int(id / p.tiles);
   q.b = q.tile / p.feature_tiles;
-  const int64_t c = (q.tile % p.feature_tiles) * (64 * CPL) + (threadIdx.x & 63) * CPL;
-  // the last lane takes the last CPL features (some twice, to the same result); lanes past it read those, too
-  q.live = c < p.features;
-  q.c = c + CPL <= p.features ? c : p.features - CPL;
+  // Lanes past the end take the last CPL features too, with the same results:
+  // they store the same values to the same places, so no lane is masked.
+  const uint32_t c = uint32_t(q.tile % p.feature_tiles) * (64 * CPL) + (threadIdx.x & 63) * CPL;
+  q.c = min(c, uint32_t(p.features) - CPL);
   return q;
 }
 
 template <class T, int CPL>
 using raw_t = typename pack_of<T, CPL>::raw;
+
+// The lane's features of a row.  (Scalar row address, 32-bit lane offset.)
 template <class T, int CPL>
-__device__ __forceinline__ raw_t<T, CPL> get(const T* p) {
-  return *reinterpret_cast<const pack_t<T, CPL>*>(p);
+__device__ __forceinline__ raw_t<T, CPL> get(const T* row, uint32_t c) {
+  return *reinterpret_cast<const pack_t<T, CPL>*>(reinterpret_cast<const char*>(row) + uint32_t(c * sizeof(T)));
 }
 template <class T, int CPL>
-__device__ __forceinline__ void put(T* p, const float (&v)[CPL]) {
-  store_n<CPL>(p, CPL, v);
+__device__ __forceinline__ void put(T* row, uint32_t c, const float (&v)[CPL]) {
+  store_n<CPL>(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + uint32_t(c * sizeof(T))), CPL, v);
 }
 
-// R rows a wave.  FULL: all of them are inside the sequence.
-template <class T, int CPL, int R, bool CHAIN>
+// A value that the compiler cannot tell from a new one.
+template <class V>
+__device__ __forceinline__ void hide(V& v) {
+  uint32_t w = 0;
+  static_assert(sizeof(V) <= 4, "one register");
+  __builtin_memcpy(&w, &v, sizeof(V));
+  asm volatile("" : "+v"(w));
+  __builtin_memcpy(&v, &w, sizeof(V));
+}
+
+// R rows of an array from row t on, one load each; past `rows` the last of them again.
+template <bool FULL, class T, int CPL, int R>
+__device__ __forceinline__ void get_rows(const T* p, Strides s, int64_t b, int64_t t, uint32_t c, int rows,
+                                         raw_t<T, CPL> (&out)[R]) {
+  const T* row = p + at(s, b, t);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    out[i] = get<T, CPL>(row, c);
+    if (FULL || i + 1 < rows) row += s.t;
+  }
+}
+
+template <class T, int CPL>
+__device__ __forceinline__ void put_zeros(T* p, Strides s, int64_t b, int64_t t, int64_t end, uint32_t c) {
+  for (; t < end; ++t) put<T, CPL>(p + at(s, b, t), c, {});
+}
+
+// R rows a wave.  GATED: with o.
+template <class T, int CPL, int R, bool CHAIN, bool GATED>
 __global__ void __launch_bounds__(64 * WAVES)
 recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zero, T* y, float* h_out, float* states) {
   __shared__ float mapA[WAVES][64 * CPL], mapH[WAVES][64 * CPL], enter[64 * CPL];
@@ -179,134 +207,117 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const Place q = place_of<CPL, CHAIN>(p, &slot);
   const int64_t n = length_of(p, q.b), span0 = int64_t(q.span) * SPAN, t0 = span0 + wave * R;
-  if (span0 >= n && !(span0 == 0)) {  // past the end: zeros (n = 0 goes on for the states)
-    for (int i = 0; i < R; ++i)
-      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, {});
+  const int64_t end = min(t0 + R, p.steps);
+  if (span0 >= n && q.span > 0) {  // past the end (the first span goes on for the states)
+    put_zeros<T, CPL>(y, p.y, q.b, t0, end, q.c);
     return;
   }
-  const int rows = int(n - t0 < 0 ? 0 : n - t0 < R ? n - t0 : R);  // live rows of this wave
-  raw_t<T, CPL> zr[R], vr[R], orw[R];
-  float s[R][CPL], bv[R][CPL];
-  if (rows > 0) {
+  const int rows = int(max<int64_t>(0, min<int64_t>(n - t0, R)));  // live rows of this wave
+  const auto body = [&](auto full_) {  // full: all rows of all waves are live
+    constexpr bool FULL = decltype(full_)::value;
+    raw_t<T, CPL> zr[R], vr[R], orw[R];
+    float s[R][CPL], bv[R][CPL];
+    float A[CPL], H[CPL], h[CPL];
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int64_t t = t0 + (i < rows ? i : rows - 1);
-      zr[i] = get<T, CPL>(z + at(p.z, q.b, t) + q.c);
-      vr[i] = get<T, CPL>(v + at(p.v, q.b, t) + q.c);
+    for (int c = 0; c < CPL; ++c) A[c] = 1.f, H[c] = 0.f, h[c] = 0.f;
+    if (FULL || rows > 0) {
+      get_rows<FULL, T, CPL, R>(z, p.z, q.b, t0, q.c, rows, zr);
+      get_rows<FULL, T, CPL, R>(v, p.v, q.b, t0, q.c, rows, vr);
+      if constexpr (GATED) get_rows<FULL, T, CPL, R>(o, p.o, q.b, t0, q.c, rows, orw);
     }
-    if (o != nullptr) {
+    if (q.span == 0 && h_zero != nullptr) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int64_t t = t0 + (i < rows ? i : rows - 1);
-        orw[i] = get<T, CPL>(o + at(p.o, q.b, t) + q.c);
-      }
+      for (int c = 0; c < CPL; ++c) h[c] = h_zero[q.b * p.features + q.c + c];
     }
-  }
-  float A[CPL], H[CPL], h[CPL];
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) A[c] = 1.f, H[c] = 0.f, h[c] = 0.f;
-  if (rows > 0) {
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        float gn;
-        logistic(float(zr[i][c]), s[i][c], gn);
-        bv[i][c] = gn * float(vr[i][c]);
-      }
-    if (rows < R) {
+    if (FULL || rows > 0) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int c = 0; c < CPL; ++c)
-          if (i >= rows) s[i][c] = 1.f, bv[i][c] = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        A[c] *= s[i][c];
-        H[c] = s[i][c] * H[c] + bv[i][c];
-      }
-  }
-  // the state that enters this wave's rows
-  if (q.span == 0 && h_zero != nullptr) {
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) h[c] = h_zero[q.b * p.features + q.c + c];
-  }
-  if (waves > 1) {
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c];
-    __syncthreads();
-    if constexpr (CHAIN) {
-      if (wave == 0) {
-        float tA[CPL], tH[CPL];
-#pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          tA[c] = A[c], tH[c] = H[c];
-          for (int i = 1; i < waves; ++i) {
-            const float a = mapA[i][lane * CPL + c];
-            tH[c] = a * tH[c] + mapH[i][lane * CPL + c];
-            tA[c] *= a;
+          float gn;
+          logistic(float(zr[i][c]), s[i][c], gn);
+          bv[i][c] = gn * float(vr[i][c]);
+          if (!FULL && i >= rows) s[i][c] = 1.f, bv[i][c] = 0.f;
+          A[c] *= s[i][c];
+          H[c] = s[i][c] * H[c] + bv[i][c];
+        }
+    }
+    // the state that enters this wave's rows
+    if (waves > 1) {
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c];
+      __syncthreads();
+      if constexpr (CHAIN) {
+        if (wave == 0) {
+          float tA[CPL], tH[CPL];
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) {
+            tA[c] = A[c], tH[c] = H[c];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) {
+              const float a = mapA[i][lane * CPL + c];
+              tH[c] = a * tH[c] + mapH[i][lane * CPL + c];
+              tA[c] *= a;
+            }
+          }
+          const int64_t pitch = 64 * CPL;
+          unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
+          if (q.span > 0) {
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) put_word(words + q.span * pitch + c, map_word(tA[c], tH[c]));
+            look_back<CPL>(words, pitch, q.span, h);
+          }
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) {
+            put_word(words + q.span * pitch + c, state_word(tA[c] * h[c] + tH[c]));
+            enter[lane * CPL + c] = h[c];
           }
         }
-        const int64_t pitch = 64 * CPL;
-        unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
-        if (q.span > 0) {
+        __syncthreads();
 #pragma unroll
-          for (int c = 0; c < CPL; ++c) put_word(words + q.span * pitch + c, map_word(tA[c], tH[c]));
-          look_back<CPL>(words, pitch, q.span, h);
-        }
+        for (int c = 0; c < CPL; ++c) h[c] = enter[lane * CPL + c];
+      }
+    }
+    if (states != nullptr && wave == 0) put<float, CPL>(states + (q.b * p.spans + q.span) * p.features, q.c, h);
+    for (int i = 0; i < wave; ++i)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
+    T* row = y + at(p.y, q.b, t0);
+    if (FULL || rows > 0) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if (!FULL && i >= rows) break;
+        float r[CPL];
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          put_word(words + q.span * pitch + c, state_word(tA[c] * h[c] + tH[c]));
-          enter[lane * CPL + c] = h[c];
+          h[c] = s[i][c] * h[c] + bv[i][c];
+          r[c] = h[c];
+          if constexpr (GATED) {
+            const float x = float(orw[i][c]);
+            r[c] *= x * logistic(x);
+          }
         }
+        put<T, CPL>(row, q.c, r);
+        row += p.y.t;
       }
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) h[c] = enter[lane * CPL + c];
     }
-  }
-  if (states != nullptr && wave == 0 && q.live) put<float, CPL>(states + (q.b * p.spans + q.span) * p.features + q.c, h);
-#pragma unroll
-  for (int c = 0; c < CPL; ++c)
-    for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
-  const auto run = [&](auto full) {  // full: all rows are live
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      float r[CPL];
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        h[c] = s[i][c] * h[c] + bv[i][c];
-        r[c] = h[c];
-        if (o != nullptr) {
-          const float x = float(orw[i][c]);
-          r[c] *= x * logistic(x);
-        }
-        if (!full.value && i >= rows) r[c] = 0.f;
-      }
-      if (q.live && (full.value || t0 + i < p.steps)) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, r);
+    if (!FULL) put_zeros<T, CPL>(y, p.y, q.b, t0 + rows, end, q.c);
+    // the wave of the last live step (the first wave where there is none) has the state that leaves
+    if (n == 0 ? wave == 0 : rows > 0 && t0 + rows == n) {
+      if (h_out != nullptr) put<float, CPL>(h_out + q.b * p.features, q.c, h);
+      if (states != nullptr)
+        for (int k = q.span + 1; k < p.spans; ++k)
+          put<float, CPL>(states + (q.b * p.spans + k) * p.features, q.c, h);
     }
   };
-  if (rows == R) {
-    run(std::true_type());
-  } else if (rows > 0) {
-    run(std::false_type());
-  } else {
-    for (int i = 0; i < R; ++i)
-      if (t0 + i < p.steps && q.live) put<T, CPL>(y + at(p.y, q.b, t0 + i) + q.c, {});
-  }
-  // the wave of the last live step (the first wave where there is none) has the state that leaves
-  if (q.live && (n == 0 ? wave == 0 : rows > 0 && t0 + rows == n)) {
-    if (h_out != nullptr) put<float, CPL>(h_out + q.b * p.features + q.c, h);
-    if (states != nullptr)
-      for (int k = q.span + 1; k < p.spans; ++k) put<float, CPL>(states + (q.b * p.spans + k) * p.features + q.c, h);
-  }
+  if (span0 + waves * R <= n)
+    body(std::true_type());
+  else
+    body(std::false_type());
 }
 
 // The backward; spans of the chain count from the last live one.
-template <class T, int CPL, int R, bool CHAIN>
+template <class T, int CPL, int R, bool CHAIN, bool GATED>
 __global__ void __launch_bounds__(64 * WAVES)
 recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* states, const T* g_y, const float* g_h,
                       T* g_z, T* g_v, T* g_o, float* g_hzero) {
@@ -316,171 +327,158 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
   const Place q = place_of<CPL, CHAIN>(p, &slot);
   const int64_t n = length_of(p, q.b);
   const int live_spans = int((n + SPAN - 1) / SPAN);
-  const int place = q.span;                                                       // in the chain, while it is live
-  const int span = place < live_spans ? live_spans - 1 - place : place;           // of the sequence
-  const int64_t span0 = int64_t(span) * SPAN, t0 = span0 + wave * R;
+  const int place = q.span;                                              // in the chain, while it is live
+  const int span = place < live_spans ? live_spans - 1 - place : place;  // of the sequence
+  const int64_t span0 = int64_t(span) * SPAN, t0 = span0 + wave * R, end = min(t0 + R, p.steps);
+  const auto zeros_from = [&](int64_t t) {
+    put_zeros<T, CPL>(g_z, p.gz, q.b, t, end, q.c);
+    put_zeros<T, CPL>(g_v, p.gv, q.b, t, end, q.c);
+    if constexpr (GATED) put_zeros<T, CPL>(g_o, p.go, q.b, t, end, q.c);
+  };
   if (place >= live_spans) {
-    for (int i = 0; i < R; ++i) {
-      const int64_t t = t0 + i;
-      if (t < p.steps && q.live) {
-        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, {});
-        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, {});
-        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, {});
-      }
-    }
-    if (n == 0 && place == 0 && wave == 0 && q.live && g_hzero != nullptr) {
+    zeros_from(t0);
+    if (n == 0 && place == 0 && wave == 0 && g_hzero != nullptr) {
       float e[CPL];
 #pragma unroll
       for (int c = 0; c < CPL; ++c) e[c] = g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
-      put<float, CPL>(g_hzero + q.b * p.features + q.c, e);
+      put<float, CPL>(g_hzero + q.b * p.features, q.c, e);
     }
     return;
   }
-  const int rows = int(n - t0 < 0 ? 0 : n - t0 < R ? n - t0 : R);
-  raw_t<T, CPL> zr[R], vr[R], orw[R], gr[R];
-  float s[R][CPL], sn[R][CPL], b[R][CPL], g[R][CPL];  // b: then the state before the row
-  float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL];
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) {
-    h[c] = states[(q.b * p.spans + span) * p.features + q.c + c];
-    e[c] = place == 0 && g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
-    A[c] = 1.f, H[c] = 0.f, G[c] = 0.f;
-  }
-  if (rows > 0) {
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int64_t t = t0 + (i < rows ? i : rows - 1);
-      zr[i] = get<T, CPL>(z + at(p.z, q.b, t) + q.c);
-      vr[i] = get<T, CPL>(v + at(p.v, q.b, t) + q.c);
-      gr[i] = get<T, CPL>(g_y + at(p.y, q.b, t) + q.c);
-    }
-    if (o != nullptr) {
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int64_t t = t0 + (i < rows ? i : rows - 1);
-        orw[i] = get<T, CPL>(o + at(p.o, q.b, t) + q.c);
-      }
+  const int rows = int(max<int64_t>(0, min<int64_t>(n - t0, R)));
+  const auto body = [&](auto full_) {  // full: all rows of all waves are live
+    constexpr bool FULL = decltype(full_)::value;
+    raw_t<T, CPL> zr[R], vr[R], orw[R], gr[R];
+    float s[R][CPL], sn[R][CPL], b[R][CPL];  // b: then the state before the row
+    float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL];
+    if (FULL || rows > 0) {
+      get_rows<FULL, T, CPL, R>(z, p.z, q.b, t0, q.c, rows, zr);
+      get_rows<FULL, T, CPL, R>(v, p.v, q.b, t0, q.c, rows, vr);
+      get_rows<FULL, T, CPL, R>(g_y, p.y, q.b, t0, q.c, rows, gr);
+      if constexpr (GATED) get_rows<FULL, T, CPL, R>(o, p.o, q.b, t0, q.c, rows, orw);
     }
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        logistic(float(zr[i][c]), s[i][c], sn[i][c]);
-        b[i][c] = sn[i][c] * float(vr[i][c]);
-        g[i][c] = float(gr[i][c]);
-        if (o != nullptr) {
-          const float x = float(orw[i][c]);
-          g[i][c] *= x * logistic(x);
-        }
-      }
-    if (rows < R) {
+    for (int c = 0; c < CPL; ++c) {
+      h[c] = states[(q.b * p.spans + span) * p.features + q.c + c];
+      e[c] = place == 0 && g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
+      A[c] = 1.f, H[c] = 0.f, G[c] = 0.f;
+    }
+    if (FULL || rows > 0) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int c = 0; c < CPL; ++c)
-          if (i >= rows) s[i][c] = 1.f, sn[i][c] = b[i][c] = g[i][c] = 0.f;
-    }
+        for (int c = 0; c < CPL; ++c) {
+          logistic(float(zr[i][c]), s[i][c], sn[i][c]);
+          b[i][c] = sn[i][c] * float(vr[i][c]);
+          if (!FULL && i >= rows) s[i][c] = 1.f, sn[i][c] = b[i][c] = 0.f;
+          A[c] *= s[i][c];
+          H[c] = s[i][c] * H[c] + b[i][c];
+        }
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        A[c] *= s[i][c];
-        H[c] = s[i][c] * H[c] + b[i][c];
-      }
-#pragma unroll
-    for (int i = R - 1; i >= 0; --i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) G[c] = s[i][c] * (g[i][c] + G[c]);
-  }
-  if (waves > 1) {
-#pragma unroll
-    for (int c = 0; c < CPL; ++c)
-      mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c], mapG[wave][lane * CPL + c] = G[c];
-    __syncthreads();
-    if constexpr (CHAIN) {
-      if (wave == 0) {
-        float tA[CPL], tG[CPL];
+      for (int i = R - 1; i >= 0; --i) {
+        if (!FULL && i >= rows) continue;
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          tA[c] = 1.f, tG[c] = 0.f;
-          for (int i = waves - 1; i >= 0; --i) {
-            const float a = mapA[i][lane * CPL + c];
-            tG[c] = a * tG[c] + mapG[i][lane * CPL + c];
-            tA[c] *= a;
+          float g = float(gr[i][c]);
+          if constexpr (GATED) {
+            const float x = float(orw[i][c]);
+            g *= x * logistic(x);
+          }
+          G[c] = s[i][c] * (g + G[c]);
+        }
+      }
+      // (o's logistic is taken again below: kept, its 32 registers spill)
+      if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) hide(orw[i]);
+      }
+    }
+    if (waves > 1) {
+#pragma unroll
+      for (int c = 0; c < CPL; ++c)
+        mapA[wave][lane * CPL + c] = A[c], mapH[wave][lane * CPL + c] = H[c], mapG[wave][lane * CPL + c] = G[c];
+      __syncthreads();
+      if constexpr (CHAIN) {
+        if (wave == 0) {
+          float tA[CPL], tG[CPL];
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) {
+            tA[c] = 1.f, tG[c] = 0.f;
+#pragma unroll
+            for (int i = WAVES - 1; i >= 0; --i) {
+              const float a = mapA[i][lane * CPL + c];
+              tG[c] = a * tG[c] + mapG[i][lane * CPL + c];
+              tA[c] *= a;
+            }
+          }
+          const int64_t pitch = 64 * CPL;
+          unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
+          if (place > 0) {
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) put_word(words + place * pitch + c, map_word(tA[c], tG[c]));
+            look_back<CPL>(words, pitch, place, e);
+          }
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) {
+            put_word(words + place * pitch + c, state_word(tA[c] * e[c] + tG[c]));
+            enter[lane * CPL + c] = e[c];
           }
         }
-        const int64_t pitch = 64 * CPL;
-        unsigned long long* words = p.maps + q.tile * p.spans * pitch + lane * CPL;
-        if (place > 0) {
+        __syncthreads();
 #pragma unroll
-          for (int c = 0; c < CPL; ++c) put_word(words + place * pitch + c, map_word(tA[c], tG[c]));
-          look_back<CPL>(words, pitch, place, e);
-        }
+        for (int c = 0; c < CPL; ++c) e[c] = enter[lane * CPL + c];
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) {
+      for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
+      for (int i = waves - 1; i > wave; --i) e[c] = mapA[i][lane * CPL + c] * e[c] + mapG[i][lane * CPL + c];
+    }
+    if (FULL || rows > 0) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          put_word(words + place * pitch + c, state_word(tA[c] * e[c] + tG[c]));
-          enter[lane * CPL + c] = e[c];
+          const float next = s[i][c] * h[c] + b[i][c];
+          b[i][c] = h[c];
+          h[c] = next;
+        }
+      T *rz = g_z + at(p.gz, q.b, t0 + rows), *rv = g_v + at(p.gv, q.b, t0 + rows);
+      T* ro = GATED ? g_o + at(p.go, q.b, t0 + rows) : nullptr;
+#pragma unroll
+      for (int i = R - 1; i >= 0; --i) {
+        if (!FULL && i >= rows) continue;  // (such a row leaves e as it is)
+        float gz[CPL], gv[CPL], go[CPL];
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+          const float vv = float(vr[i][c]);
+          float g = float(gr[i][c]);
+          if constexpr (GATED) {
+            const float x = float(orw[i][c]), so = logistic(x), xs = x * so;
+            go[c] = g * (s[i][c] * b[i][c] + sn[i][c] * vv) * (so + xs * (1.f - so));
+            g *= xs;
+          }
+          const float d = g + e[c];
+          gv[c] = d * sn[i][c];
+          e[c] = s[i][c] * d;
+          gz[c] = gv[c] * s[i][c] * (b[i][c] - vv);
+        }
+        rz -= p.gz.t, rv -= p.gv.t;
+        put<T, CPL>(rz, q.c, gz);
+        put<T, CPL>(rv, q.c, gv);
+        if constexpr (GATED) {
+          ro -= p.go.t;
+          put<T, CPL>(ro, q.c, go);
         }
       }
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) e[c] = enter[lane * CPL + c];
     }
-  }
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) {
-    for (int i = 0; i < wave; ++i) h[c] = mapA[i][lane * CPL + c] * h[c] + mapH[i][lane * CPL + c];
-    for (int i = waves - 1; i > wave; --i) e[c] = mapA[i][lane * CPL + c] * e[c] + mapG[i][lane * CPL + c];
-  }
-  const auto run = [&](auto full) {  // full: all rows are live
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        const float next = s[i][c] * h[c] + b[i][c];
-        b[i][c] = h[c];
-        h[c] = next;
-      }
-#pragma unroll
-    for (int i = R - 1; i >= 0; --i) {
-      float gz[CPL], gv[CPL], go[CPL];
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        const float vv = float(vr[i][c]);
-        go[c] = 0.f;
-        if (o != nullptr) {
-          const float x = float(orw[i][c]), so = logistic(x);
-          go[c] = float(gr[i][c]) * (s[i][c] * b[i][c] + sn[i][c] * vv) * (so + x * so * (1.f - so));
-        }
-        const float d = g[i][c] + e[c];
-        gv[c] = d * sn[i][c];
-        gz[c] = gv[c] * s[i][c] * (b[i][c] - vv);
-        e[c] = s[i][c] * d;
-        if (!full.value && i >= rows) gz[c] = gv[c] = go[c] = 0.f;
-      }
-      const int64_t t = t0 + i;
-      if (q.live && (full.value || t < p.steps)) {
-        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, gz);
-        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, gv);
-        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, go);
-      }
-    }
+    if (!FULL) zeros_from(t0 + rows);
+    if (span == 0 && wave == 0 && g_hzero != nullptr) put<float, CPL>(g_hzero + q.b * p.features, q.c, e);
   };
-  if (rows == R) {
-    run(std::true_type());
-  } else if (rows > 0) {
-    run(std::false_type());
-  } else {
-    for (int i = 0; i < R; ++i) {
-      const int64_t t = t0 + i;
-      if (t < p.steps && q.live) {
-        put<T, CPL>(g_z + at(p.gz, q.b, t) + q.c, {});
-        put<T, CPL>(g_v + at(p.gv, q.b, t) + q.c, {});
-        if (g_o != nullptr) put<T, CPL>(g_o + at(p.go, q.b, t) + q.c, {});
-      }
-    }
-  }
-  if (span == 0 && wave == 0 && q.live && g_hzero != nullptr) put<float, CPL>(g_hzero + q.b * p.features + q.c, e);
+  if (span0 + waves * R <= n)
+    body(std::true_type());
+  else
+    body(std::false_type());
 }
 
 // h_out = h_zero (g_hzero = g_h) where there are no steps.
@@ -489,10 +487,13 @@ __global__ void __launch_bounds__(256) copy_state_kernel(const float* in, float*
   if (i < n) out[i] = in != nullptr ? in[i] : 0.f;
 }
 
-// The chain's words and its ticket start from zero.
+// The chain's words and its ticket start from zero.  (Four stores a thread: a
+// kernel, as a recorded memset does not replay rightly.)
 __global__ void __launch_bounds__(256) clear_kernel(uint4* p, int64_t n) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (i < n) p[i] = uint4{0, 0, 0, 0};
+  const int64_t i = int64_t(blockIdx.x) * 1024 + threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i + j * 256 < n) p[i + j * 256] = uint4{0, 0, 0, 0};
 }
 
 Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths, int cpl) {
@@ -505,13 +506,15 @@ Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths, int cpl) {
   return p;
 }
 
-int lanes_features(int64_t features) { return features >= 2 ? 2 : 1; }
+// Features of a lane: two 16-bit ones make a word; 32-bit ones are a word each
+// (two of them would hold the backward's arrays in more registers than there are).
+int lane_features(int type, int64_t features) { return type != DTST_F32 && features >= 2 ? 2 : 1; }
 
 template <class F>
 int by_type(int type, F&& f) {
-  if (type == DTST_F32) return f(float());
-  if (type == DTST_BF16) return f(bf16_t());
-  return f(f16_t());
+  if (type == DTST_F32) return f(float(), std::integral_constant<int, 1>());
+  if (type == DTST_BF16) return f(bf16_t(), std::integral_constant<int, 2>());
+  return f(f16_t(), std::integral_constant<int, 2>());
 }
 
 int copy_state(const float* in, float* out, int64_t n, hipStream_t s) {
@@ -520,32 +523,44 @@ int copy_state(const float* in, float* out, int64_t n, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Clears the chain, then calls f(R, CHAIN, workgroups, threads): steps a wave
-// by how many there are (one step holds one row's registers and loads), spans
-// by ticket where a sequence has several.
+// Clears the chain's words and ticket where there is one, then calls
+// f(args, element, CPL, R, CHAIN, GATED, workgroups, threads): spans by ticket
+// where a sequence has several; one row a wave for one step (its registers and
+// loads are then one row's).
 template <class F>
-int with_form(Args& p, int cpl, void* workspace, hipStream_t s, F&& f) {
+int by_form(const dtst_recurrence_desc& d, const int32_t* lengths, bool with_o, void* workspace, hipStream_t s, F&& f) {
   using std::integral_constant;
-  if (p.spans > 1) {
-    const int64_t bytes = 64 + p.tiles * p.spans * 64 * cpl * 8;
-    p.ticket = static_cast<unsigned*>(workspace);
-    p.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 64);
-    hipLaunchKernelGGL(clear_kernel, dim3(unsigned((bytes / 16 + 255) / 256)), dim3(256), 0, s,
-                       static_cast<uint4*>(workspace), bytes / 16);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    return f(integral_constant<int, RPW>(), integral_constant<bool, true>(), unsigned(p.tiles * p.spans), 64 * WAVES);
-  }
-  if (p.steps == 1) return f(integral_constant<int, 1>(), integral_constant<bool, false>(), unsigned(p.tiles), 64);
-  return f(integral_constant<int, RPW>(), integral_constant<bool, false>(), unsigned(p.tiles),
-           64 * int((p.steps + RPW - 1) / RPW));
+  using std::false_type;
+  using std::true_type;
+  return by_type(d.type, [&](auto t, auto wide) {
+    const auto rest = [&](auto cpl, auto gated) {
+      Args p = args_of(d, lengths, cpl.value);
+      if (p.spans > 1) {
+        const int64_t bytes = 64 + p.tiles * p.spans * 64 * cpl.value * 8;
+        p.ticket = static_cast<unsigned*>(workspace);
+        p.maps = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 64);
+        hipLaunchKernelGGL(clear_kernel, dim3(unsigned((bytes / 16 + 1023) / 1024)), dim3(256), 0, s,
+                           static_cast<uint4*>(workspace), bytes / 16);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return int(e);
+        return f(p, t, cpl, integral_constant<int, RPW>(), true_type(), gated, unsigned(p.tiles * p.spans), 64 * WAVES);
+      }
+      if (p.steps == 1)
+        return f(p, t, cpl, integral_constant<int, 1>(), false_type(), gated, unsigned(p.tiles), 64);
+      return f(p, t, cpl, integral_constant<int, RPW>(), false_type(), gated, unsigned(p.tiles),
+               64 * int((p.steps + RPW - 1) / RPW));
+    };
+    const auto with_gate = [&](auto cpl) { return with_o ? rest(cpl, true_type()) : rest(cpl, false_type()); };
+    if (lane_features(d.type, d.features) == wide.value) return with_gate(wide);
+    return with_gate(integral_constant<int, 1>());
+  });
 }
 
 }  // namespace
 
-size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int) {
+size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type) {
   if (steps <= SPAN) return 0;
-  const int64_t w = 64 * lanes_features(features);
+  const int64_t w = 64 * lane_features(type, features);
   return 64 + size_t(batch * ((features + w - 1) / w)) * ((steps + SPAN - 1) / SPAN) * w * 8;
 }
 
@@ -553,20 +568,16 @@ int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* 
                       const int32_t* lengths, void* y, float* h_out, float* states, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.steps == 0) return copy_state(h_zero, h_out, d.batch * d.features, s);
-  return by_type(d.type, [&](auto t) {
-    using T = decltype(t);
-    const auto run = [&](auto cpl) {
-      constexpr int CPL = decltype(cpl)::value;
-      Args p = args_of(d, lengths, CPL);
-      return with_form(p, CPL, workspace, s, [&](auto r, auto chain, unsigned groups, int threads) {
-        hipLaunchKernelGGL((recurrence_kernel<T, CPL, decltype(r)::value, decltype(chain)::value>), dim3(groups),
-                           dim3(threads), 0, s, p, static_cast<const T*>(z), static_cast<const T*>(v),
-                           static_cast<const T*>(o), h_zero, static_cast<T*>(y), h_out, states);
-        return int(hipGetLastError());
-      });
-    };
-    return lanes_features(d.features) == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
-  });
+  return by_form(d, lengths, o != nullptr, workspace, s,
+                 [&](const Args& p, auto t, auto cpl, auto r, auto chain, auto gated, unsigned groups, int threads) {
+                   using T = decltype(t);
+                   hipLaunchKernelGGL((recurrence_kernel<T, decltype(cpl)::value, decltype(r)::value,
+                                                         decltype(chain)::value, decltype(gated)::value>),
+                                      dim3(groups), dim3(threads), 0, s, p, static_cast<const T*>(z),
+                                      static_cast<const T*>(v), static_cast<const T*>(o), h_zero, static_cast<T*>(y),
+                                      h_out, states);
+                   return int(hipGetLastError());
+                 });
 }
 
 int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o,
@@ -574,21 +585,17 @@ int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const vo
                           void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.steps == 0) return copy_state(g_h, g_hzero, d.batch * d.features, s);
-  return by_type(d.type, [&](auto t) {
-    using T = decltype(t);
-    const auto run = [&](auto cpl) {
-      constexpr int CPL = decltype(cpl)::value;
-      Args p = args_of(d, lengths, CPL);
-      return with_form(p, CPL, workspace, s, [&](auto r, auto chain, unsigned groups, int threads) {
-        hipLaunchKernelGGL((recurrence_adj_kernel<T, CPL, decltype(r)::value, decltype(chain)::value>), dim3(groups),
-                           dim3(threads), 0, s, p, static_cast<const T*>(z), static_cast<const T*>(v),
-                           static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h, static_cast<T*>(g_z),
-                           static_cast<T*>(g_v), static_cast<T*>(g_o), g_hzero);
-        return int(hipGetLastError());
-      });
-    };
-    return lanes_features(d.features) == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
-  });
+  return by_form(d, lengths, o != nullptr, workspace, s,
+                 [&](const Args& p, auto t, auto cpl, auto r, auto chain, auto gated, unsigned groups, int threads) {
+                   using T = decltype(t);
+                   hipLaunchKernelGGL((recurrence_adj_kernel<T, decltype(cpl)::value, decltype(r)::value,
+                                                             decltype(chain)::value, decltype(gated)::value>),
+                                      dim3(groups), dim3(threads), 0, s, p, static_cast<const T*>(z),
+                                      static_cast<const T*>(v), static_cast<const T*>(o), states,
+                                      static_cast<const T*>(g_y), g_h, static_cast<T*>(g_z), static_cast<T*>(g_v),
+                                      static_cast<T*>(g_o), g_hzero);
+                   return int(hipGetLastError());
+                 });
 }
 
 }  // namespace dtst
