@@ -100,18 +100,10 @@ rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __res
         for (int j = 0; j < VEC; ++j)
           if (c + j >= cols) u[i][j] = 0.f;
       }
-      float m = 0.f;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) m = fmaxf(m, finite_abs(u[i][j]));
-      const uint32_t s = scale_byte(row_max(m));
-      const float inv = scale_inverse(s);
+      uint2 q;
+      const uint32_t s = code_block(u[i], q);
       const int64_t padded = (cols + 127) / 128 * 128, blocks = padded / 128;
-      if (c < padded) {
-        uint2 q;
-        q.x = to_codes(u[i][0] * inv, u[i][1] * inv, u[i][2] * inv, u[i][3] * inv);
-        q.y = to_codes(u[i][4] * inv, u[i][5] * inv, u[i][6] * inv, u[i][7] * inv);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(y) + row * d.ld_y + c) = q;
-      }
+      if (c < padded) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(y) + row * d.ld_y + c) = q;
       // a byte for each block, and for the rest of the row's last four
       if ((lane & 15) == 0 && c / 128 < (blocks + 3) / 4 * 4)
         scale[row * d.ld_scale + c / 128] = c < padded ? uint8_t(s) : uint8_t(127);

@@ -297,8 +297,9 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
 #pragma unroll
-    for (int e = 0; e < TN / 2; ++e) {
+    for (int e = 0; e < (TN + 1) / 2; ++e) {
       const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
+      if (TN % 2 != 0 && at >= 16) continue;
       float v[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -349,17 +350,20 @@ int launch_tile(const Operands& p, void* c, hipStream_t s) {
 //   256 x 4096 x 4096                 13.9       9.7       17.7
 //   2048 x 2048 x 2048                          14.4       13.0
 // Larger ones take the tile whose rounds of workgroups over the card cost least,
-// at the rates that full rounds reach (`at once`: workgroups that the card holds;
+// at the rates that full rounds reach (at_once: workgroups that the card holds;
 // where a CU holds two, the last round of a few overlaps the one before):
-//                        128 x 64   128 x 128   128 x 256   256 x 256
-//   2048 x 2048 x 2048       15.0        16.5
-//   4096 x 1536 x 2048       22.2        19.3        21.4
-//   4096 x 2048 x 4608                   38.9        41.2
-//   4608 x 2048 x 4096                   57.5                    52.4
-//   8192 x 8192 x 8192                  568.6                   442.1
-//   the last, exact                    1039         918.4       811.9
-// Exact sums widen each operand once per wave that reads it, which large tiles do
-// least.
+//                       128 x 64  128 x 128  128 x 192  192 x 192  192 x 256  256 x 256
+//   2048 x 2048 x 2048      15.0       16.5
+//   4096 x 1536 x 2048      22.2       18.5       18.0       20.7
+//   4096 x 2048 x 4608                 39.5                  41.2       43.6
+//   3000 x 3000 x 2944                                       29.4       30.4       36.8
+//   4608 x 2048 x 4096                 54.8                             40.3       48.3
+//   8192 x 8192 x 8192                  554                              511        437
+// and with exact sums, which widen each operand once per wave that reads it, what
+// large tiles do least (128 x 256 in place of 128 x 64):
+//   4096 x 2048 x 4608      68.4       77.8                  74.3       87.6
+//   4608 x 2048 x 4096                 96.3       93.8                  79.5       96.5
+//   8192 x 8192 x 8192       918       1039                              927        812
 struct Tile {
   int64_t bm, bn, at_once;
   double rate;  // TFLOP/s of full rounds
@@ -378,18 +382,24 @@ int launch(const Operands& p, void* c, hipStream_t s) {
   if (tiles(16, 32) <= 256) return launch_tile<SHORT, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
   if (tiles(64, 32) <= 256) return launch_tile<SHORT, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
   if (tiles(64, 64) <= 256) return launch_tile<SHORT, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
-  const Tile forms[] = {{128, 64, 512, SHORT ? 1250 : 750},
-                        {128, 128, 512, SHORT ? 1900 : 1000},
-                        {128, 256, 256, SHORT ? 0.1 : 1180},  // (short sums: never the best)
-                        {256, 256, 256, SHORT ? 2480 : 1350}};
+  const Tile forms[] = {{128, 64, 512, SHORT ? 1250 : 740},   {128, 128, 512, SHORT ? 1850 : 1000},
+                        {128, 192, 256, SHORT ? 1650 : 950},  {192, 192, 256, SHORT ? 1950 : 1100},
+                        {192, 256, 256, SHORT ? 2420 : 1300}, {256, 256, 256, SHORT ? 2500 : 1340},
+                        {128, 256, 256, 1140}};
   int best = 0;
-  for (int i = 1; i < 4; ++i)
+  for (int i = 1; i < (SHORT ? 6 : 7); ++i)
     if (cost(p, forms[i]) < cost(p, forms[best])) best = i;
-  if (best == 0) return launch_tile<SHORT, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
-  if (best == 3) return launch_tile<SHORT, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
-  if constexpr (!SHORT)
-    if (best == 2) return launch_tile<SHORT, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
-  return launch_tile<SHORT, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
+  switch (best) {
+    case 0: return launch_tile<SHORT, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
+    case 1: return launch_tile<SHORT, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
+    case 2: return launch_tile<SHORT, 2, 4, 4, 3, 2, 1, TC>(p, c, s);
+    case 3: return launch_tile<SHORT, 2, 4, 6, 3, 2, 1, TC>(p, c, s);
+    case 4: return launch_tile<SHORT, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
+    case 5: return launch_tile<SHORT, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
+    default:
+      if constexpr (!SHORT) return launch_tile<SHORT, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
+      return hipErrorInvalidValue;
+  }
 }
 
 template <class TC>

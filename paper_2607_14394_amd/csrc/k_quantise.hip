@@ -18,17 +18,6 @@
 namespace dtst {
 namespace {
 
-__device__ __forceinline__ uint32_t code_block(const float (&v)[8], uint2& q) {
-  float m = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(v[j]));
-  const uint32_t s = scale_byte(row_max(m));
-  const float inv = scale_inverse(s);
-  q.x = to_codes(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-  q.y = to_codes(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
-  return s;
-}
-
 // Scale byte `block` of a row of scales, and after the last one the bytes up to
 // a multiple of four.
 __device__ __forceinline__ void put_scale(uint8_t* row, int64_t block, int64_t blocks, uint32_t s) {
@@ -44,11 +33,11 @@ quantise_rows_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, 
   const uint32_t id = blockIdx.x * 16 + (threadIdx.x >> 4), part = threadIdx.x & 15;
   const uint32_t block = id % col_blocks;
   const int64_t row = id / col_blocks, c = int64_t(block) * 128 + part * 8;
-  if (row >= d.rows) return;  // (all 16 lanes of the block)
   float v[8];
-  load_n<8>(x + row * d.ld_x + c, d.cols - c, v);
+  load_n<8>(x + row * d.ld_x + c, row < d.rows ? d.cols - c : 0, v);
   uint2 codes;
   const uint32_t s = code_block(v, codes);
+  if (row >= d.rows) return;
   *reinterpret_cast<uint2*>(q + row * d.ld_q + c) = codes;
   if (part == 0) put_scale(scale + row * d.ld_scale, block, col_blocks, s);
 }
@@ -63,18 +52,45 @@ quantise_cols_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, 
   const int sub = threadIdx.x >> 4, part = threadIdx.x & 15, wave = threadIdx.x >> 6;  // rows 8 sub .., columns 8 part ..
   const int64_t c = ct * 128 + part * 8;
   const int64_t col_blocks = (d.cols + 127) / 128, row_blocks = (d.rows + 127) / 128;
-  float v[8][8];
+  // (kept as loaded: as 64 floats they would cost a third of the waves)
+  typename pack_of<T, 8>::raw v[8];
+  if (rt * 128 + 128 <= d.rows && ct * 128 + 128 <= d.cols) {
+    const T* at = x + (rt * 128 + sub * 8) * d.ld_x + c;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t row = rt * 128 + sub * 8 + i;
-    load_n<8>(x + row * d.ld_x + c, row < d.rows ? d.cols - c : 0, v[i]);
+    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const pack_t<T, 8>*>(at + i * d.ld_x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = rt * 128 + sub * 8 + i;
+      float f[8];
+      load_n<8>(x + row * d.ld_x + c, row < d.rows ? d.cols - c : 0, f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = T(f[j]);
+    }
   }
+  const auto column = [&](int j, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = float(v[i][j]);
+  };
   float m[8];
+  bool infinite = false;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    m[j] = 0.f;
+    float f[8];
+    column(j, f);
+    m[j] = max_abs(f);
+    infinite = infinite || is_infinite(m[j]);
+  }
+  if (__any(infinite)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m[j] = fmaxf(m[j], finite_abs(v[i][j]));
+    for (int j = 0; j < 8; ++j) {
+      float f[8];
+      column(j, f);
+      m[j] = max_finite_abs(f);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
     m[j] = fmaxf(m[j], __shfl_xor(m[j], 16, 64));
     m[j] = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
     if ((threadIdx.x & 48) == 0) top[wave][part * 8 + j] = m[j];
@@ -83,8 +99,11 @@ quantise_cols_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = rt * 128 + sub * 8 + i;
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = float(v[i][j]);
       uint2 r;
-      const uint32_t s = code_block(v[i], r);
+      const uint32_t s = code_block(f, r);
       if (row < d.rows) {
         *reinterpret_cast<uint2*>(q + row * d.ld_q + c) = r;
         if (part == 0) put_scale(scale + row * d.ld_scale, ct, col_blocks, s);
@@ -97,9 +116,11 @@ quantise_cols_kernel(dtst_quantise_desc d, const T* __restrict__ x, uint8_t* q, 
     const int lc = part * 8 + j;
     const uint32_t s = scale_byte(fmaxf(fmaxf(top[0][lc], top[1][lc]), fmaxf(top[2][lc], top[3][lc])));
     const float inv = scale_inverse(s);
+    float f[8];
+    column(j, f);
     uint2 r;
-    r.x = to_codes(v[0][j] * inv, v[1][j] * inv, v[2][j] * inv, v[3][j] * inv);
-    r.y = to_codes(v[4][j] * inv, v[5][j] * inv, v[6][j] * inv, v[7][j] * inv);
+    r.x = to_codes(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+    r.y = to_codes(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
     codes[lc][sub ^ part] = r;
     if (sub == 0 && c + j < d.cols) put_scale(scale_t + (c + j) * d.ld_scale_t, rt, row_blocks, s);
   }

@@ -506,15 +506,15 @@ Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths, int cpl) {
   return p;
 }
 
-// Features of a lane: two 16-bit ones make a word; 32-bit ones are a word each
-// (two of them would hold the backward's arrays in more registers than there are).
-int lane_features(int type, int64_t features) { return type != DTST_F32 && features >= 2 ? 2 : 1; }
+// Features of a lane: two, one where there is only one, and in the backward one
+// of 32 bits (two would hold more registers than there are).
+int lane_features(int type, int64_t features, bool adj) { return features >= 2 && !(adj && type == DTST_F32) ? 2 : 1; }
 
 template <class F>
 int by_type(int type, F&& f) {
-  if (type == DTST_F32) return f(float(), std::integral_constant<int, 1>());
-  if (type == DTST_BF16) return f(bf16_t(), std::integral_constant<int, 2>());
-  return f(f16_t(), std::integral_constant<int, 2>());
+  if (type == DTST_F32) return f(float());
+  if (type == DTST_BF16) return f(bf16_t());
+  return f(f16_t());
 }
 
 int copy_state(const float* in, float* out, int64_t n, hipStream_t s) {
@@ -527,12 +527,12 @@ int copy_state(const float* in, float* out, int64_t n, hipStream_t s) {
 // f(args, element, CPL, R, CHAIN, GATED, workgroups, threads): spans by ticket
 // where a sequence has several; one row a wave for one step (its registers and
 // loads are then one row's).
-template <class F>
+template <bool ADJ, class F>
 int by_form(const dtst_recurrence_desc& d, const int32_t* lengths, bool with_o, void* workspace, hipStream_t s, F&& f) {
   using std::integral_constant;
   using std::false_type;
   using std::true_type;
-  return by_type(d.type, [&](auto t, auto wide) {
+  return by_type(d.type, [&](auto t) {
     const auto rest = [&](auto cpl, auto gated) {
       Args p = args_of(d, lengths, cpl.value);
       if (p.spans > 1) {
@@ -551,7 +551,8 @@ int by_form(const dtst_recurrence_desc& d, const int32_t* lengths, bool with_o, 
                64 * int((p.steps + RPW - 1) / RPW));
     };
     const auto with_gate = [&](auto cpl) { return with_o ? rest(cpl, true_type()) : rest(cpl, false_type()); };
-    if (lane_features(d.type, d.features) == wide.value) return with_gate(wide);
+    if constexpr (!(ADJ && std::is_same_v<decltype(t), float>))
+      if (lane_features(d.type, d.features, ADJ) == 2) return with_gate(integral_constant<int, 2>());
     return with_gate(integral_constant<int, 1>());
   });
 }
@@ -560,7 +561,8 @@ int by_form(const dtst_recurrence_desc& d, const int32_t* lengths, bool with_o, 
 
 size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type) {
   if (steps <= SPAN) return 0;
-  const int64_t w = 64 * lane_features(type, features);
+  // (the forward's, which is no smaller than the backward's)
+  const int64_t w = 64 * lane_features(type, features, false);
   return 64 + size_t(batch * ((features + w - 1) / w)) * ((steps + SPAN - 1) / SPAN) * w * 8;
 }
 
@@ -568,7 +570,7 @@ int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* 
                       const int32_t* lengths, void* y, float* h_out, float* states, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.steps == 0) return copy_state(h_zero, h_out, d.batch * d.features, s);
-  return by_form(d, lengths, o != nullptr, workspace, s,
+  return by_form<false>(d, lengths, o != nullptr, workspace, s,
                  [&](const Args& p, auto t, auto cpl, auto r, auto chain, auto gated, unsigned groups, int threads) {
                    using T = decltype(t);
                    hipLaunchKernelGGL((recurrence_kernel<T, decltype(cpl)::value, decltype(r)::value,
@@ -585,7 +587,7 @@ int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const vo
                           void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.steps == 0) return copy_state(g_h, g_hzero, d.batch * d.features, s);
-  return by_form(d, lengths, o != nullptr, workspace, s,
+  return by_form<true>(d, lengths, o != nullptr, workspace, s,
                  [&](const Args& p, auto t, auto cpl, auto r, auto chain, auto gated, unsigned groups, int threads) {
                    using T = decltype(t);
                    hipLaunchKernelGGL((recurrence_adj_kernel<T, decltype(cpl)::value, decltype(r)::value,

@@ -71,12 +71,23 @@ __device__ __forceinline__ float row_max(float v) {
   return fmaxf(v, row_rotate<8>(v));
 }
 
-// |v|, or zero where v is infinite or no number (those do not count for a
-// block's scale).
-__device__ __forceinline__ float finite_abs(float v) {
-  const float a = fabsf(v);
-  return a <= 3.402823466e38f ? a : 0.f;
+// Largest magnitude of a lane's values; no numbers do not count, infinities do.
+template <int N>
+__device__ __forceinline__ float max_abs(const float (&v)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(v[i]));
+  return m;
 }
+// The same of the finite values alone.
+template <int N>
+__device__ float max_finite_abs(const float (&v)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(v[i]) <= 3.402823466e38f ? fabsf(v[i]) : 0.f);
+  return m;
+}
+__device__ __forceinline__ bool is_infinite(float m) { return m > 3.402823466e38f; }
 
 // The scale byte of a block whose largest magnitude is amax >= 0: the smallest
 // power of two 2^e, e >= -126, with amax <= 448 * 2^e; 448 = 1.75 * 2^8, so e is
@@ -91,16 +102,23 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
 // (s = 1 .. 247, so 2^126 .. 2^-120).
 __device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }
 
-// Four values to four codes, nearest even; what is infinite or no number
-// becomes the code of no number (0x7f).  In range otherwise.
+// Four values of at most 448, infinities or no numbers to four codes, nearest
+// even; the conversion makes the last two the code of no number.
 __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
-  const float nan = __uint_as_float(0x7fc00000u);
-  a = fabsf(a) <= 448.f ? a : nan;
-  b = fabsf(b) <= 448.f ? b : nan;
-  c = fabsf(c) <= 448.f ? c : nan;
-  d = fabsf(d) <= 448.f ? d : nan;
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
+}
+
+// A block of 128 values, eight a lane in 16 lanes: the lane's codes, and the
+// block's scale byte.  (All lanes of the wave take part.)
+__device__ __forceinline__ uint32_t code_block(const float (&v)[8], uint2& q) {
+  float m = row_max(max_abs(v));
+  if (__any(is_infinite(m))) m = row_max(max_finite_abs(v));
+  const uint32_t s = scale_byte(m);
+  const float inv = scale_inverse(s);
+  q.x = to_codes(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  q.y = to_codes(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+  return s;
 }
 
 }  // namespace dtst
