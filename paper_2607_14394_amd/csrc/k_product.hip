@@ -50,23 +50,6 @@ struct Operands {
   int accumulate;
 };
 
-// Eight neighbouring columns of a row of c, `left` of them inside.
-template <class TC>
-__device__ __forceinline__ void put_c(TC* c, int64_t left, float (&v)[8], const float* bias, int accumulate) {
-  float e[8];
-  if (bias != nullptr) {
-    load_n<8>(bias, left, e);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += e[i];
-  }
-  if (accumulate) {
-    load_n<8>(c, left, e);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += e[i];
-  }
-  store_n<8>(c, left, v);
-}
-
 // A workgroup takes BM x BN of c.  WM x WN waves hold it, each TM x TN tiles of 16
 // x 16; KS such groups take a part of the summed axis each and add up in LDS at
 // the end.  Each 128 codes of the summed axis are a stage: the rows' 128 bytes go
@@ -292,23 +275,44 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
   constexpr int PITCH = TN * 16 + 4;  // (8 rows' accesses of 16 bytes meet all banks)
   static_assert((KS - 1) * BM * BN * 4 + WAVES * 16 * PITCH * 4 <= KS * GROUP, "the strips fit beside the sums");
   float* strip = reinterpret_cast<float*>(lds_all + (KS - 1) * BM * BN * 4) + wave * 16 * PITCH;
+  constexpr int PARTS_C = (TN + 1) / 2;  // eights of a strip's columns that a lane takes
+  float bias[PARTS_C][8];                // (read once: inside the loop each read would hold up a store)
+#pragma unroll
+  for (int e = 0; e < PARTS_C; ++e) {
+    const int64_t col = n0 + wn * TN * 16 + (e * 64 + lane) % (TN * 2) * 8;
+    if (p.bias != nullptr) {
+      load_n<8>(p.bias + col, p.n - col, bias[e]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 8; ++h) bias[e][h] = 0.f;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
 #pragma unroll
-    for (int e = 0; e < (TN + 1) / 2; ++e) {
+    for (int e = 0; e < PARTS_C; ++e) {
       const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
       if (TN % 2 != 0 && at >= 16) continue;
       float v[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const v4f x = *reinterpret_cast<const v4f*>(strip + at * PITCH + c8 + h * 4);
-        v[4 * h] = x[0], v[4 * h + 1] = x[1], v[4 * h + 2] = x[2], v[4 * h + 3] = x[3];
+#pragma unroll
+        for (int l = 0; l < 4; ++l) v[4 * h + l] = x[l] + bias[e][4 * h + l];
       }
       const int64_t row = m0 + (wm * TM + i) * 16 + at, col = n0 + wn * TN * 16 + c8;
-      if (row < p.m && col < p.n)
-        put_c(c + row * p.ld_c + col, p.n - col, v, p.bias == nullptr ? nullptr : p.bias + col, p.accumulate);
+      if (row < p.m && col < p.n) {
+        TC* to = c + row * p.ld_c + col;
+        if (p.accumulate) {
+          float old[8];
+          load_n<8>(to, p.n - col, old);
+#pragma unroll
+          for (int h = 0; h < 8; ++h) v[h] += old[h];
+        }
+        store_n<8>(to, p.n - col, v);
+      }
     }
   }
 }
