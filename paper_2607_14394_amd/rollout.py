@@ -1,0 +1,208 @@
+"""Marching fields in time past a plan's window: every time step's retained
+coefficients (one batch entry of a plan with a single time step) are a token,
+residual blocks with a gated linear recurrence run over the sequence of tokens,
+and the result is expanded back onto the shard.
+
+    u = x + residual;  n = rms norm of u;  z | v | o = n W_in^T + b
+    y = recurrence(z, v, o);  x' = y W_out^T;  residual' = u
+
+Orchestration only: every step is a call of the DTST library
+(``dtst_rms_norm``, ``dtst_quantise``, ``dtst_product``, ``dtst_recurrence``,
+their backward calls, and the plan's transforms), apart from the last residual's
+addition and the sum of a bias' gradient.  Weights are kept in 8 bits with their
+transposes, as the backward needs them; the masters stay with the caller.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from . import (Plan, dtst_product, dtst_quantise, dtst_recurrence, dtst_recurrence_adj, dtst_rms_norm,
+               dtst_rms_norm_adj, empty_codes, recurrence_states_shape)
+
+
+class _Weights:
+    """A linear layer's weights (out, in) as codes, along both axes."""
+
+    def __init__(self, w):
+        out, k = w.shape
+        self.shape = (out, k)
+        self.rows, self.cols = empty_codes(out, k, w.device), empty_codes(k, out, w.device)
+        self.set(w)
+
+    def set(self, w):
+        dtst_quantise(w, *self.rows, qt=self.cols[0], scale_t=self.cols[1])
+
+
+class LatentBlock:
+    """One residual block of width W with F recurrent features.  norm: (W,)
+    float32; w_in: (3 F, W); b_in: (3 F,) float32; w_out: (W, F)."""
+
+    def __init__(self, norm, w_in, b_in, w_out, eps=1e-6):
+        self.width, self.features = w_out.shape
+        if tuple(w_in.shape) != (3 * self.features, self.width) or tuple(norm.shape) != (self.width,):
+            raise ValueError(f"w_out {tuple(w_out.shape)} needs w_in ({3 * self.features}, {self.width}) and norm "
+                             f"({self.width},)")
+        self.norm, self.b_in, self.eps = norm, b_in, eps
+        self.w_in, self.w_out = _Weights(w_in), _Weights(w_out)
+
+    def set_weights(self, w_in, w_out):
+        """New weights of the same shapes (after an update of the masters)."""
+        self.w_in.set(w_in)
+        self.w_out.set(w_out)
+
+    def state(self, batch, device="cuda"):
+        """The state before the first step."""
+        return torch.zeros((batch, self.features), dtype=torch.float32, device=device)
+
+    def _split(self, p):
+        F = self.features
+        return p[..., :F], p[..., F:2 * F], p[..., 2 * F:]
+
+    def forward(self, x, res, state=None, lengths=None, keep=None):
+        """x: (B, T, W), the branch of the block before (bfloat16, or float32
+        for the first); res: (B, T, W) float32 or None, updated in place unless
+        `keep` is given.  Returns the block's branch (bfloat16) and the residual.
+        state: (B, F) float32, updated in place; one step with a state is a
+        serving step.  keep: a dict that receives what backward needs."""
+        B, T, W = x.shape
+        F, R, dev = self.features, B * T, x.device
+        bf = torch.bfloat16
+        x2 = x.reshape(R, W)
+        u = torch.empty((R, W), dtype=torch.float32, device=dev) if res is None else res.view(R, W)
+        res2 = None if res is None else u
+        n = empty_codes(R, W, dev)
+        p, y = torch.empty((B, T, 3 * F), dtype=bf, device=dev), torch.empty((B, T, F), dtype=bf, device=dev)
+        z, v, o = self._split(p)
+        states = None
+        if keep is None:
+            dtst_rms_norm(x2, self.norm, n[0], res=res2, sum_out=u, scale=n[1], eps=self.eps)
+        else:
+            rstd, nt = torch.empty(R, dtype=torch.float32, device=dev), empty_codes(W, R, dev)
+            plain = torch.empty((R, W), dtype=x.dtype, device=dev)
+            u = u if res is None else torch.empty_like(u)  # (the caller's stays: backward needs this one)
+            dtst_rms_norm(x2, self.norm, plain, res=res2, sum_out=u, rstd=rstd, eps=self.eps)
+            dtst_quantise(plain, *n, qt=nt[0], scale_t=nt[1])
+            states = torch.empty(recurrence_states_shape(B, T, F), dtype=torch.float32, device=dev)
+            keep.update(shape=(B, T), u=u, rstd=rstd, nt=nt, p=p, states=states, lengths=lengths, x_dtype=x.dtype)
+        dtst_product(*n, *self.w_in.rows, p.view(R, 3 * F), bias=self.b_in, short_sums=True)
+        dtst_recurrence(z, v, y, o=o, h0=state, h_out=state, lengths=lengths, states=states)
+        yq = empty_codes(R, F, dev)
+        if keep is None:
+            dtst_quantise(y.view(R, F), *yq)
+        else:
+            keep["yt"] = empty_codes(F, R, dev)
+            dtst_quantise(y.view(R, F), *yq, qt=keep["yt"][0], scale_t=keep["yt"][1])
+        out = torch.empty((B, T, W), dtype=bf, device=dev)
+        dtst_product(*yq, *self.w_out.rows, out.view(R, W), short_sums=True)
+        return out, u.view(B, T, W)
+
+    def backward(self, kept, g_out, g_res, g_state=None):
+        """Gradients from those of the branch (B, T, W) bfloat16, of the
+        residual (B, T, W) float32 and of the last state (B, F), or None.
+        Returns a dict: x (in x's type), res (float32), state, norm, w_in, b_in,
+        w_out (float32)."""
+        B, T = kept["shape"]
+        W, F, R, dev = self.width, self.features, B * T, g_out.device
+        f32, bf = torch.float32, torch.bfloat16
+
+        def both(t):
+            r, c = t.shape
+            q, qt = empty_codes(r, c, dev), empty_codes(c, r, dev)
+            dtst_quantise(t, *q, qt=qt[0], scale_t=qt[1])
+            return q, qt
+
+        q, qt = both(g_out.reshape(R, W))
+        g_y, g_w_out = torch.empty((B, T, F), dtype=bf, device=dev), torch.empty((W, F), dtype=f32, device=dev)
+        dtst_product(*q, *self.w_out.cols, g_y.view(R, F), short_sums=True)
+        dtst_product(*qt, *kept["yt"], g_w_out)
+        g_p = torch.empty((B, T, 3 * F), dtype=bf, device=dev)
+        g_h = torch.empty((B, F), dtype=f32, device=dev)
+        z, v, o = self._split(kept["p"])
+        g_z, g_v, g_o = self._split(g_p)
+        dtst_recurrence_adj(z, v, g_y, kept["states"], g_z, g_v, o=o, g_o=g_o, g_h=g_state, g_hzero=g_h,
+                            lengths=kept["lengths"])
+        q, qt = both(g_p.view(R, 3 * F))
+        g_n = torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
+        g_w_in = torch.empty((3 * F, W), dtype=f32, device=dev)
+        dtst_product(*q, *self.w_in.cols, g_n, short_sums=g_n.dtype != f32)
+        dtst_product(*qt, *kept["nt"], g_w_in)
+        g_u, g_norm = torch.empty((R, W), dtype=f32, device=dev), torch.empty_like(self.norm)
+        g_x = g_u if kept["x_dtype"] == f32 else torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
+        dtst_rms_norm_adj(g_n, kept["u"], self.norm, kept["rstd"], g_u, g_norm,
+                          g_sum=None if g_res is None else g_res.reshape(R, W), g_x=None if g_x is g_u else g_x)
+        return dict(x=g_x.view(B, T, W), res=g_u.view(B, T, W), state=g_h, norm=g_norm, w_in=g_w_in,
+                    b_in=g_p.float().sum(dim=(0, 1)), w_out=g_w_out)
+
+
+class Rollout:
+    """Fields of `channels` channels on one shard, batch sequences at a time.
+    grid: a descriptor's n_global, n_local, offset and kmax in x, y, z (3 each);
+    blocks: LatentBlocks of width 2 channels M, M the retained modes."""
+
+    def __init__(self, grid, channels, batch, blocks, device="cuda"):
+        self.grid, self.channels, self.batch, self.blocks, self.device = grid, channels, batch, list(blocks), device
+        self.plans = {}
+        self.plan(1)  # one step: serving
+        for b in self.blocks:
+            if b.width != self.width:
+                raise ValueError(f"a block's width must be 2 * channels * modes = {self.width}")
+        self.states = None
+
+    def plan(self, steps):
+        """The plan of `steps` frames of every sequence at once."""
+        if steps not in self.plans:
+            g = self.grid
+            self.plans[steps] = Plan(dict(
+                n_global=tuple(g["n_global"]) + (1,), n_local=tuple(g["n_local"]) + (1,),
+                offset=tuple(g["offset"]) + (0,), kmax=tuple(g["kmax"]), kt=1, batch=self.batch * steps,
+                c_in=self.channels, c_out=self.channels), self.device)
+        return self.plans[steps]
+
+    @property
+    def width(self):
+        return 2 * self.channels * self.plan(1).n_modes
+
+    def encode(self, frames):
+        """(B, T, channels, x, y, z) float32 to tokens (B, T, width) float32."""
+        B, T = frames.shape[:2]
+        plan = self.plan(T)
+        xhat = torch.empty(plan.spectral_shape(self.channels), dtype=torch.complex64, device=self.device)
+        plan.forward(frames.contiguous().view(plan.spatial_shape(self.channels)), xhat)
+        return torch.view_as_real(xhat).view(B, T, self.width)
+
+    def decode(self, tokens):
+        B, T = tokens.shape[:2]
+        plan = self.plan(T)
+        yhat = torch.view_as_complex(tokens.contiguous().view(plan.spectral_shape(self.channels) + (2,)))
+        y = torch.empty(plan.spatial_shape(self.channels), dtype=torch.float32, device=self.device)
+        plan.inverse(yhat, y)
+        return y.view(B, T, self.channels, *plan.n_local[:3])
+
+    def reset(self):
+        """Forget the sequences so far."""
+        self.states = [b.state(self.batch, self.device) for b in self.blocks]
+
+    def advance(self, frames, lengths=None):
+        """The prediction after each of the frames (B, T, channels, x, y, z) of
+        the sequences, which go on from the frames of earlier calls."""
+        if self.states is None:
+            self.reset()
+        x, res = self.encode(frames), None
+        for block, state in zip(self.blocks, self.states):
+            x, res = block.forward(x, res, state, lengths)
+        return self.decode(res + x if res is not None else x)
+
+    def march(self, frame, steps):
+        """`steps` predictions, each from the one before, after (B, channels, x,
+        y, z) and what the sequences have seen."""
+        out = torch.empty((frame.shape[0], steps) + tuple(frame.shape[1:]), dtype=torch.float32, device=self.device)
+        for t in range(steps):
+            frame = self.advance(frame[:, None])[:, 0]
+            out[:, t] = frame
+        return out
+
+    def close(self):
+        for p in self.plans.values():
+            p.close()
+        self.plans = {}
