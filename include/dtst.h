@@ -382,9 +382,10 @@ dtst_status dtst_quantise(const dtst_quantise_desc* d, const void* x, void* q, v
  * are exact to 32 bits (the codes go to the matrix cores as bf16, which holds
  * them and their scales without loss; what a scale brings below 2^-126 loses
  * low bits).  short_sums = 1 lets the library take the 8-bit matrix
- * instruction, up to twice as fast: its sum of eight neighbouring products
- * keeps 13 bits below the largest of them (1e-5 to 2e-5 of the result on
- * normally distributed values), the sum of those sums 32 bits.  k and the
+ * instruction, which it does for large products (2 m n k >= 2^38), at nearly
+ * twice the rate: its sum of eight neighbouring products keeps 13 bits below
+ * the largest of them (1e-5 to 2e-5 of the result on normally distributed
+ * values), the sum of those sums 32 bits.  k and the
  * strides up to 2^23 (DTST_ERR_UNSUPPORTED above).  workspace: dtst_product_workspace bytes; it
  * is 0 for most sizes, and then workspace may be NULL. */
 typedef struct {

@@ -346,28 +346,23 @@ int launch_tile(const Operands& p, void* c, hipStream_t s) {
 
 // The tile.  A card of 256 CUs is short of workgroups long before it is short of
 // products, so small results take the smallest tile that still leaves one
-// workgroup a CU, its waves dividing the summed axis.  Measured with 16-bit
-// results, in us:
+// workgroup a CU, its waves dividing the summed axis.  Measured, in us:
 //                        16 x 32   64 x 32   64 x 64   128 x 64
-//   4 x 4608 x 2048          3.9       5.4       6.5
-//   48 x 8192 x 8192                  13.0      16.6
-//   256 x 4096 x 4096                 13.9       9.7       17.7
-//   2048 x 2048 x 2048                          14.4       13.0
+//   4 x 4608 x 2048          4.7       6.9       9.0
+//   48 x 8192 x 8192        24.4      17.7      24.5
+//   256 x 4096 x 4096                 19.4      14.9       28.6
+//   2048 x 2048 x 2048                                     23.6
 // Larger ones take the tile whose rounds of workgroups over the card cost least,
 // at the rates that full rounds reach (at_once: workgroups that the card holds;
-// where a CU holds two, the last round of a few overlaps the one before):
-//                       128 x 64  128 x 128  128 x 192  192 x 192  192 x 256  256 x 256
-//   2048 x 2048 x 2048      15.0       16.5
-//   4096 x 1536 x 2048      22.2       18.5       18.0       20.7
-//   4096 x 2048 x 4608                 39.5                  41.2       43.6
-//   3000 x 3000 x 2944                                       29.4       30.4       36.8
-//   4608 x 2048 x 4096                 54.8                             40.3       48.3
-//   8192 x 8192 x 8192                  554                              511        437
-// and with exact sums, which widen each operand once per wave that reads it, what
-// large tiles do least (128 x 256 in place of 128 x 64):
-//   4096 x 2048 x 4608      68.4       77.8                  74.3       87.6
-//   4608 x 2048 x 4096                 96.3       93.8                  79.5       96.5
-//   8192 x 8192 x 8192       918       1039                              927        812
+// where a CU holds two, the last round of a few overlaps the one before).  Every
+// wave widens the rows that it reads, which large tiles do least:
+//                       128 x 128  128 x 192  128 x 256  192 x 192  192 x 256  256 x 256
+//   2048 x 2048 x 2048       26.3                  31.0
+//   4096 x 1536 x 2048       35.1       30.0       32.7       35.9
+//   4096 x 2048 x 4608       77.8                  68.4       74.3       87.6
+//   3000 x 3000 x 2944                                        51.9       60.3
+//   4608 x 2048 x 4096       96.3       93.8                             79.5       96.5
+//   8192 x 8192 x 8192       1039                   918                   927        812
 struct Tile {
   int64_t bm, bn, at_once;
   double rate;  // TFLOP/s of full rounds
@@ -380,35 +375,35 @@ double cost(const Operands& p, const Tile& t) {
   return rounds * double(t.at_once * t.bm * t.bn) / t.rate;
 }
 
-template <bool SHORT, class TC>
-int launch(const Operands& p, void* c, hipStream_t s) {
+template <class TC>
+int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
-  if (tiles(16, 32) <= 256) return launch_tile<SHORT, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
-  if (tiles(64, 32) <= 256) return launch_tile<SHORT, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
-  if (tiles(64, 64) <= 256) return launch_tile<SHORT, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
-  const Tile forms[] = {{128, 64, 512, SHORT ? 1250 : 740},   {128, 128, 512, SHORT ? 1850 : 1000},
-                        {128, 192, 256, SHORT ? 1650 : 950},  {192, 192, 256, SHORT ? 1950 : 1100},
-                        {192, 256, 256, SHORT ? 2420 : 1300}, {256, 256, 256, SHORT ? 2500 : 1340},
-                        {128, 256, 256, 1140}};
+  // Short sums, where they are allowed, from 2^38 operations on: they save 375 of
+  // 812 us at 8192^3.  Below it they would save tens, and layers of that size
+  // feed others: 0.4% of the bf16 results round to the other neighbour, and the
+  // 32-bit states of a recurrence on them move by 3e-3.
+  if (short_sums && 2.0 * double(p.m) * double(p.n) * double(p.k) >= double(int64_t(1) << 38) && tiles(256, 256) >= 128) {
+    const Tile one{192, 256, 256, 2420}, two{256, 256, 256, 2500};
+    if (cost(p, one) < cost(p, two)) return launch_tile<true, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
+    return launch_tile<true, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
+  }
+  if (tiles(16, 32) <= 256) return launch_tile<false, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
+  if (tiles(64, 32) <= 256) return launch_tile<false, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
+  if (tiles(64, 64) <= 256) return launch_tile<false, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
+  const Tile forms[] = {{128, 64, 512, 740},   {128, 128, 512, 1000},  {128, 192, 256, 950}, {128, 256, 256, 1140},
+                        {192, 192, 256, 1100}, {192, 256, 256, 1300}, {256, 256, 256, 1340}};
   int best = 0;
-  for (int i = 1; i < (SHORT ? 6 : 7); ++i)
+  for (int i = 1; i < 7; ++i)
     if (cost(p, forms[i]) < cost(p, forms[best])) best = i;
   switch (best) {
-    case 0: return launch_tile<SHORT, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
-    case 1: return launch_tile<SHORT, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
-    case 2: return launch_tile<SHORT, 2, 4, 4, 3, 2, 1, TC>(p, c, s);
-    case 3: return launch_tile<SHORT, 2, 4, 6, 3, 2, 1, TC>(p, c, s);
-    case 4: return launch_tile<SHORT, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
-    case 5: return launch_tile<SHORT, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
-    default:
-      if constexpr (!SHORT) return launch_tile<SHORT, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
-      return hipErrorInvalidValue;
+    case 0: return launch_tile<false, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
+    case 1: return launch_tile<false, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
+    case 2: return launch_tile<false, 2, 4, 4, 3, 2, 1, TC>(p, c, s);
+    case 3: return launch_tile<false, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
+    case 4: return launch_tile<false, 2, 4, 6, 3, 2, 1, TC>(p, c, s);
+    case 5: return launch_tile<false, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
+    default: return launch_tile<false, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
   }
-}
-
-template <class TC>
-int launch_sums(const Operands& p, int short_sums, void* c, hipStream_t s) {
-  return short_sums ? launch<true, TC>(p, c, s) : launch<false, TC>(p, c, s);
 }
 
 }  // namespace
@@ -421,9 +416,9 @@ int launch_product(const dtst_product_desc& d, const void* a, const void* a_scal
   const Operands p{static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(b),
                    static_cast<const uint8_t*>(a_scale), static_cast<const uint8_t*>(b_scale),
                    d.m, d.n, d.k, d.ld_a, d.ld_a_scale, d.ld_b, d.ld_b_scale, d.ld_c, bias, d.accumulate};
-  if (d.c_type == DTST_F32) return launch_sums<float>(p, d.short_sums, c, s);
-  if (d.c_type == DTST_BF16) return launch_sums<bf16_t>(p, d.short_sums, c, s);
-  return launch_sums<f16_t>(p, d.short_sums, c, s);
+  if (d.c_type == DTST_F32) return launch<float>(p, d.short_sums, c, s);
+  if (d.c_type == DTST_BF16) return launch<bf16_t>(p, d.short_sums, c, s);
+  return launch<f16_t>(p, d.short_sums, c, s);
 }
 
 }  // namespace dtst

@@ -97,6 +97,42 @@ def test_short_sums(m, n, k):
         assert worst <= 1
 
 
+# Large enough for the 8-bit instruction (2^38 operations): each tile, and rows
+# and columns that end inside one.
+@pytest.mark.parametrize("m,n,k", [(4096, 4100, 8200), (6003, 5000, 5000), (2500, 7777, 8192)])
+def test_short_sums_of_large_products(m, n, k):
+    torch, D = lib()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m)
+    x, w = (torch.randn((r, k), generator=g, device="cuda") * torch.exp2(2 * torch.randn((r, 1), generator=g, device="cuda"))
+            for r in (m, n))
+    a, b = D.empty_codes(m, k), D.empty_codes(n, k)
+    D.dtst_quantise(x, *a)
+    D.dtst_quantise(w, *b)
+    c, e = (torch.full((m, n), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    D.dtst_product(*a, *b, c, short_sums=True)
+    D.dtst_product(*a, *b, e)
+    assert not torch.isnan(c).any() and not torch.isnan(e).any()
+    rng = np.random.RandomState(k)
+    rows, cols = rng.permutation(m)[:120], rng.permutation(n)[:120]
+    rows[:2], cols[:2] = (m - 1, 0), (n - 1, 0)
+
+    def values(q, i):
+        return S.values(q[0][i].float().cpu().numpy(), q[1].view(torch.uint8)[i].cpu().numpy()[:, :(k + 127) // 128].astype(int) - 127)
+
+    ra, rb = values(a, rows), values(b, cols)
+    ref = S.product(ra, rb)
+    size = np.sqrt((ra ** 2).sum(axis=1)[:, None] * (rb ** 2).sum(axis=1)[None, :])
+    lost = np.zeros_like(ref)
+    for i in range(0, ra.shape[1], 8):
+        lost += 2.0 ** -10 * (np.abs(ra[:, None, i:i + 8]) * np.abs(rb[None, :, i:i + 8])).max(axis=2)
+    for got, name, more in ((f64(c)[np.ix_(rows, cols)], "short", lost), (f64(e)[np.ix_(rows, cols)], "exact", 0.0)):
+        tol = HALF_STEP["bf16"] * np.abs(ref) * (1 + 1e-5) + 1e-5 * (np.abs(ref) + size) + more
+        worst = (np.abs(got - ref) / tol).max()
+        say(f"  {name}: up to {worst:.2f} of the bar")
+        assert worst <= 1, name
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 70, 300), (70, 90, 700), (300, 520, 256)])
 def test_strides(m, n, k):
     torch, D = lib()
