@@ -78,7 +78,7 @@ rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __res
 #pragma unroll
     for (int j = 0; j < VEC; ++j) ss += u[i][j] * u[i][j];
   ss = row_sum<RW>(ss, part);
-  const float r = 1.f / sqrtf(ss / float(cols) + d.eps);
+  const float r = rsqrtf(ss * (1.f / float(cols)) + d.eps);
   if (rstd != nullptr && first == 0) rstd[row] = r;
   if (sum_out != nullptr) {
 #pragma unroll
@@ -93,7 +93,7 @@ rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __res
     float wv[VEC];
     load_n<VEC>(w + c, cols - c, wv);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u[i][j] *= r * wv[j];
+    for (int j = 0; j < VEC; ++j) u[i][j] = u[i][j] * r * wv[j];
     if constexpr (Q8) {
       if (c + VEC > cols) {  // (not by the product: 1 / rms may be no number)
 #pragma unroll
