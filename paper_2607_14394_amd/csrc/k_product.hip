@@ -225,30 +225,72 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
         if (PARTS > 1 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
       }
     } else {
-      float sa[TM], sb[TN];
+      // A lane's 32 codes of a row are two halves of 16.  Products of a row tile go
+      // with the widening of the next one, and in the first half with that of b's
+      // second: a product takes the issue of four instructions, so that between two
+      // of them others are free.  Codes are read a tile before they are widened.
+      constexpr int Q = 2 * TM;  // (half, row tile) in turn
+      v8b fa[2][2], fb[2][TN][2];
+      v4i xa[2], xb;
+      int ba[2], bb[TN];  // scale bytes of the codes read
+      const auto read_a = [&](int q) {
+        xa[q & 1] = *reinterpret_cast<const v4i*>(at_a + q % TM * 16 * ROW + (place ^ (q / TM * 64)));
+        ba[q & 1] = at_sa[q % TM * 64];
+      };
+      const auto widen_a = [&](int q) {
+        const float s = scale_value(ba[q & 1]);
+        fa[q & 1][0] = widen(xa[q & 1][0], xa[q & 1][1], s), fa[q & 1][1] = widen(xa[q & 1][2], xa[q & 1][3], s);
+      };
+      const auto widen_b = [&](int h, int j, const v4i& x) {
+        const float s = scale_value(bb[j]);
+        fb[h][j][0] = widen(x[0], x[1], s), fb[h][j][1] = widen(x[2], x[3], s);
+      };
+      const auto read_b = [&](int h, int j) {
+        return *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + (place ^ (h * 64)));
+      };
+      {
+        v4i x[TN];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] = scale_value(at_sb[j * 64]);
+        for (int j = 0; j < TN; ++j) x[j] = read_b(0, j), bb[j] = at_sb[j * 64];
+        read_a(0);
+        read_a(1);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = scale_value(at_sa[i * 64]);
+        for (int j = 0; j < TN; ++j) widen_b(0, j, x[j]);
+        widen_a(0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // b's second half: tile j is read at step first_b[j] and widened at the next
+      constexpr int STEP_B = TM >= TN + 1 ? 1 : 0;  // a tile a step, or all of them in the last step of the first half
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {  // half of the quarter at a time: fewer registers
-        v8b fb[TN][2];
+      for (int q = 0; q < Q; ++q) {
+        const int h = q / TM, i = q % TM;
+        v4i late[TN];
+        if (STEP_B == 1 && h == 0 && i >= 1 && i <= TN) widen_b(1, i - 1, xb);
+        if (STEP_B == 1 && h == 0 && i < TN) xb = read_b(1, i);
+        if (STEP_B == 0 && q == TM - 1) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const v4i x = *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + (place ^ (h * 64)));
-          fb[j][0] = widen(x[0], x[1], sb[j]), fb[j][1] = widen(x[2], x[3], sb[j]);
+          for (int j = 0; j < TN; ++j) late[j] = read_b(1, j);
         }
+        if (q + 1 < Q) widen_a(q + 1);
+        if (q + 2 < Q) read_a(q + 2);  // (over the codes of tile q)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const v4i x = *reinterpret_cast<const v4i*>(at_a + i * 16 * ROW + (place ^ (h * 64)));
-          const v8b fa[2] = {widen(x[0], x[1], sa[i]), widen(x[2], x[3], sa[i])};
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
+          for (int j = 0; j < TN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[h][j][e], fa[q & 1][e], acc[i][j], 0, 0, 0);
+        if (STEP_B == 0 && q == TM - 1) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j][e], fa[e], acc[i][j], 0, 0, 0);
-          if (PARTS > 1 && h == 0 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
+          for (int j = 0; j < TN; ++j) widen_b(1, j, late[j]);
         }
+        // one product, then up to three of the others
+#pragma unroll
+        for (int e = 0; e < 2 * TN; ++e) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (PARTS > 1 && h == 0 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
       }
     }
   }
