@@ -37,9 +37,11 @@ __device__ __forceinline__ v8b widen(uint32_t lo, uint32_t hi, float scale) {
   return v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// 2^(s - 127); s = 255 is no number.
-__device__ __forceinline__ float scale_value(uint32_t s) {
-  return __uint_as_float(s == 0 ? 0x00400000u : s == 255 ? 0x7fc00000u : s << 23);
+// 2^(s - 127), s = 1 .. 254, of a byte read a tile ago.  (The empty statement
+// keeps the shift here: next to the read it would wait for it.)
+__device__ __forceinline__ float scale_value(int s) {
+  asm volatile("" : "+v"(s));
+  return __int_as_float(s << 23);
 }
 
 struct Operands {
@@ -82,6 +84,74 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
 }
 
+// Tile row and column of a workgroup.  Workgroups go to the 8 dies in turn: a die
+// gets neighbouring tiles, in bands of 8 tile rows, so that its cache holds their
+// operands.  (readfirstlane: the addresses that follow belong in scalar registers)
+__device__ __forceinline__ void tile_of(int m_tiles, int n_tiles, int& tm, int& tn) {
+  int id = blockIdx.x;
+  const int all = m_tiles * n_tiles;
+  if (all >= 64) {
+    const int die = id % 8, per = all / 8, extra = all % 8;
+    id = die * per + min(die, extra) + id / 8;
+  }
+  const int band = id / (8 * n_tiles), band_rows = min(8, m_tiles - band * 8), in_band = id - band * 8 * n_tiles;
+  tm = __builtin_amdgcn_readfirstlane(band * 8 + in_band % band_rows);
+  tn = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+}
+
+// A wave's TM x TN tiles of sums to c from (row0, col0) on: 16 rows at a time
+// through the wave's own strip of LDS, so that a lane stores eight neighbouring
+// columns and a row's lanes whole lines.
+constexpr int strip_pitch(int tn) { return tn * 16 + 4; }  // (8 rows' accesses of 16 bytes meet all banks)
+constexpr int strip_floats(int tn) { return 16 * strip_pitch(tn); }
+
+template <int TM, int TN, class TC>
+__device__ __forceinline__ void put_tiles(const Operands& p, TC* c, const v4f (&acc)[TM][TN], int64_t row0, int64_t col0,
+                                          int lane, float* strip) {
+  constexpr int PITCH = strip_pitch(TN);
+  const int r = lane & 15, g = lane >> 4;
+  constexpr int PARTS_C = (TN + 1) / 2;  // eights of a strip's columns that a lane takes
+  float bias[PARTS_C][8];                // (read once: inside the loop each read would hold up a store)
+#pragma unroll
+  for (int e = 0; e < PARTS_C; ++e) {
+    const int64_t col = col0 + (e * 64 + lane) % (TN * 2) * 8;
+    if (p.bias != nullptr) {
+      load_n<8>(p.bias + col, p.n - col, bias[e]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 8; ++h) bias[e][h] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
+#pragma unroll
+    for (int e = 0; e < PARTS_C; ++e) {
+      const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
+      if (TN % 2 != 0 && at >= 16) continue;
+      float v[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const v4f x = *reinterpret_cast<const v4f*>(strip + at * PITCH + c8 + h * 4);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) v[4 * h + l] = x[l] + bias[e][4 * h + l];
+      }
+      const int64_t row = row0 + i * 16 + at, col = col0 + c8;
+      if (row < p.m && col < p.n) {
+        TC* to = c + row * p.ld_c + col;
+        if (p.accumulate) {
+          float old[8];
+          load_n<8>(to, p.n - col, old);
+#pragma unroll
+          for (int h = 0; h < 8; ++h) v[h] += old[h];
+        }
+        store_n<8>(to, p.n - col, v);
+      }
+    }
+  }
+}
+
 template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
 __global__ void __launch_bounds__(64 * WM * WN * KS)
 product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
@@ -98,18 +168,9 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
   uint8_t* lds = lds_all + group * GROUP;
   const int r = lane & 15, g = lane >> 4;
 
-  // Workgroups go to the 8 dies in turn: a die gets neighbouring tiles, in bands
-  // of 8 tile rows, so that its cache holds their operands.
-  int id = blockIdx.x;
-  const int all = m_tiles * n_tiles;
-  if (all >= 64) {
-    const int die = id % 8, per = all / 8, extra = all % 8;
-    id = die * per + min(die, extra) + id / 8;
-  }
-  const int band = id / (8 * n_tiles), band_rows = min(8, m_tiles - band * 8), in_band = id - band * 8 * n_tiles;
-  // (readfirstlane: the addresses that follow from them belong in scalar registers)
-  const int64_t m0 = int64_t(__builtin_amdgcn_readfirstlane(band * 8 + in_band % band_rows)) * BM;
-  const int64_t n0 = int64_t(__builtin_amdgcn_readfirstlane(in_band / band_rows)) * BN;
+  int tile_m, tile_n;
+  tile_of(m_tiles, n_tiles, tile_m, tile_n);
+  const int64_t m0 = int64_t(tile_m) * BM, n0 = int64_t(tile_n) * BN;
 
   // Where this lane's loads start: row wave * L + .. of each operand.  Rows past
   // the end read the last one; their results are not stored.
@@ -312,51 +373,9 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] += sums[((k * TM + i) * TN + j) * WAVES * 64];
   }
-  // 16 rows at a time through the wave's own strip of LDS, so that a lane stores
-  // eight neighbouring columns and a row's lanes whole lines.
-  constexpr int PITCH = TN * 16 + 4;  // (8 rows' accesses of 16 bytes meet all banks)
-  static_assert((KS - 1) * BM * BN * 4 + WAVES * 16 * PITCH * 4 <= KS * GROUP, "the strips fit beside the sums");
-  float* strip = reinterpret_cast<float*>(lds_all + (KS - 1) * BM * BN * 4) + wave * 16 * PITCH;
-  constexpr int PARTS_C = (TN + 1) / 2;  // eights of a strip's columns that a lane takes
-  float bias[PARTS_C][8];                // (read once: inside the loop each read would hold up a store)
-#pragma unroll
-  for (int e = 0; e < PARTS_C; ++e) {
-    const int64_t col = n0 + wn * TN * 16 + (e * 64 + lane) % (TN * 2) * 8;
-    if (p.bias != nullptr) {
-      load_n<8>(p.bias + col, p.n - col, bias[e]);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 8; ++h) bias[e][h] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-#pragma unroll
-    for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
-#pragma unroll
-    for (int e = 0; e < PARTS_C; ++e) {
-      const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
-      if (TN % 2 != 0 && at >= 16) continue;
-      float v[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const v4f x = *reinterpret_cast<const v4f*>(strip + at * PITCH + c8 + h * 4);
-#pragma unroll
-        for (int l = 0; l < 4; ++l) v[4 * h + l] = x[l] + bias[e][4 * h + l];
-      }
-      const int64_t row = m0 + (wm * TM + i) * 16 + at, col = n0 + wn * TN * 16 + c8;
-      if (row < p.m && col < p.n) {
-        TC* to = c + row * p.ld_c + col;
-        if (p.accumulate) {
-          float old[8];
-          load_n<8>(to, p.n - col, old);
-#pragma unroll
-          for (int h = 0; h < 8; ++h) v[h] += old[h];
-        }
-        store_n<8>(to, p.n - col, v);
-      }
-    }
-  }
+  static_assert((KS - 1) * BM * BN * 4 + WAVES * strip_floats(TN) * 4 <= KS * GROUP, "the strips fit beside the sums");
+  put_tiles<TM, TN>(p, c, acc, m0 + wm * TM * 16, n0 + wn * TN * 16, lane,
+                    reinterpret_cast<float*>(lds_all + (KS - 1) * BM * BN * 4) + wave * strip_floats(TN));
 }
 
 // Raises a kernel's limit of dynamic LDS on the current device, once (the call
@@ -398,13 +417,12 @@ int launch_tile(const Operands& p, void* c, hipStream_t s) {
 // at the rates that full rounds reach (at_once: workgroups that the card holds;
 // where a CU holds two, the last round of a few overlaps the one before).  Every
 // wave widens the rows that it reads, which large tiles do least:
-//                       128 x 128  128 x 192  128 x 256  192 x 192  192 x 256  256 x 256
-//   2048 x 2048 x 2048       26.3                  31.0
-//   4096 x 1536 x 2048       35.1       30.0       32.7       35.9
-//   4096 x 2048 x 4608       77.8                  68.4       74.3       87.6
-//   3000 x 3000 x 2944                                        51.9       60.3
-//   4608 x 2048 x 4096       96.3       93.8                             79.5       96.5
-//   8192 x 8192 x 8192       1039                   918                   927        812
+//                        128 x 64  128 x 128  128 x 192  128 x 256  192 x 192  192 x 256  256 x 256
+//   2048 x 2048 x 2048       23.6       26.3                  31.0
+//   4096 x 1536 x 2048       36.6       35.6       29.0       34.1       35.8
+//   4096 x 2048 x 4608       88.5       72.9                  65.4       69.0       78.4
+//   4608 x 2048 x 4096       95.9       93.2       86.2                             71.2       88.6
+//   8192 x 8192 x 8192                   956                   893        907        847        759
 struct Tile {
   int64_t bm, bn, at_once;
   double rate;  // TFLOP/s of full rounds
@@ -420,8 +438,8 @@ double cost(const Operands& p, const Tile& t) {
 template <class TC>
 int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
-  // Short sums, where they are allowed, from 2^38 operations on: they save 375 of
-  // 812 us at 8192^3.  Below it they would save tens, and layers of that size
+  // Short sums, where they are allowed, from 2^38 operations on: they save 320 of
+  // 760 us at 8192^3.  Below it they would save tens, and layers of that size
   // feed others: 0.4% of the bf16 results round to the other neighbour, and the
   // 32-bit states of a recurrence on them move by 3e-3.
   if (short_sums && 2.0 * double(p.m) * double(p.n) * double(p.k) >= double(int64_t(1) << 38) && tiles(256, 256) >= 128) {
@@ -432,8 +450,8 @@ int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
   if (tiles(16, 32) <= 256) return launch_tile<false, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
   if (tiles(64, 32) <= 256) return launch_tile<false, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
   if (tiles(64, 64) <= 256) return launch_tile<false, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
-  const Tile forms[] = {{128, 64, 512, 740},   {128, 128, 512, 1000},  {128, 192, 256, 950}, {128, 256, 256, 1140},
-                        {192, 192, 256, 1100}, {192, 256, 256, 1300}, {256, 256, 256, 1340}};
+  const Tile forms[] = {{128, 64, 512, 800},   {128, 128, 512, 1080}, {128, 192, 256, 1050}, {128, 256, 256, 1200},
+                        {192, 192, 256, 1180}, {192, 256, 256, 1340}, {256, 256, 256, 1450}};
   int best = 0;
   for (int i = 1; i < 7; ++i)
     if (cost(p, forms[i]) < cost(p, forms[best])) best = i;
