@@ -17,8 +17,10 @@ from __future__ import annotations
 
 import torch
 
-from . import (Plan, dtst_product, dtst_quantise, dtst_recurrence, dtst_recurrence_adj, dtst_rms_norm,
+from . import (DtstError, Plan, dtst_desc_validate, dtst_product, dtst_quantise, dtst_recurrence, dtst_recurrence_adj, dtst_rms_norm,
                dtst_rms_norm_adj, empty_codes, recurrence_states_shape)
+
+_UNSUPPORTED = 2  # DTST_ERR_UNSUPPORTED
 
 
 class _Weights:
@@ -140,44 +142,64 @@ class Rollout:
     grid: a descriptor's n_global, n_local, offset and kmax in x, y, z (3 each);
     blocks: LatentBlocks of width 2 channels M, M the retained modes."""
 
+    GROUP = 256  # frames of one plan at most; halved until the library takes such a plan
+
     def __init__(self, grid, channels, batch, blocks, device="cuda"):
         self.grid, self.channels, self.batch, self.blocks, self.device = grid, channels, batch, list(blocks), device
         self.plans = {}
-        self.plan(1)  # one step: serving
+        self.group = self.GROUP
+        while self.group > 1 and not self._supported(self.group):
+            self.group //= 2
+        self.width = 2 * channels * self.plan(1).n_modes
         for b in self.blocks:
             if b.width != self.width:
                 raise ValueError(f"a block's width must be 2 * channels * modes = {self.width}")
         self.states = None
 
-    def plan(self, steps):
-        """The plan of `steps` frames of every sequence at once."""
-        if steps not in self.plans:
-            g = self.grid
-            self.plans[steps] = Plan(dict(
-                n_global=tuple(g["n_global"]) + (1,), n_local=tuple(g["n_local"]) + (1,),
-                offset=tuple(g["offset"]) + (0,), kmax=tuple(g["kmax"]), kt=1, batch=self.batch * steps,
-                c_in=self.channels, c_out=self.channels), self.device)
-        return self.plans[steps]
+    def _desc(self, frames):
+        g = self.grid
+        return dict(n_global=tuple(g["n_global"]) + (1,), n_local=tuple(g["n_local"]) + (1,),
+                    offset=tuple(g["offset"]) + (0,), kmax=tuple(g["kmax"]), kt=1, batch=frames,
+                    c_in=self.channels, c_out=self.channels)
 
-    @property
-    def width(self):
-        return 2 * self.channels * self.plan(1).n_modes
+    def _supported(self, frames):
+        try:
+            dtst_desc_validate(self._desc(frames))
+        except DtstError as e:
+            if e.status != _UNSUPPORTED:
+                raise
+            return False
+        return True
+
+    def plan(self, frames):
+        """The plan of `frames` frames at once."""
+        if frames not in self.plans:
+            self.plans[frames] = Plan(self._desc(frames), self.device)
+        return self.plans[frames]
+
+    def _groups(self, frames):
+        for i in range(0, frames, self.group):
+            n = min(self.group, frames - i)
+            yield self.plan(n), slice(i, i + n)
 
     def encode(self, frames):
         """(B, T, channels, x, y, z) float32 to tokens (B, T, width) float32."""
         B, T = frames.shape[:2]
-        plan = self.plan(T)
-        xhat = torch.empty(plan.spectral_shape(self.channels), dtype=torch.complex64, device=self.device)
-        plan.forward(frames.contiguous().view(plan.spatial_shape(self.channels)), xhat)
+        xhat = torch.empty(B * T, self.width // 2, dtype=torch.complex64, device=self.device)
+        flat = frames.contiguous().view(B * T, -1)
+        for plan, s in self._groups(B * T):
+            plan.forward(flat[s].view(plan.spatial_shape(self.channels)),
+                         xhat[s].view(plan.spectral_shape(self.channels)))
         return torch.view_as_real(xhat).view(B, T, self.width)
 
     def decode(self, tokens):
         B, T = tokens.shape[:2]
-        plan = self.plan(T)
-        yhat = torch.view_as_complex(tokens.contiguous().view(plan.spectral_shape(self.channels) + (2,)))
-        y = torch.empty(plan.spatial_shape(self.channels), dtype=torch.float32, device=self.device)
-        plan.inverse(yhat, y)
-        return y.view(B, T, self.channels, *plan.n_local[:3])
+        yhat = torch.view_as_complex(tokens.contiguous().view(B * T, self.width // 2, 2))
+        n = self.plan(1).n_local[:3]
+        y = torch.empty(B * T, self.channels * n[0] * n[1] * n[2], dtype=torch.float32, device=self.device)
+        for plan, s in self._groups(B * T):
+            plan.inverse(yhat[s].view(plan.spectral_shape(self.channels)), y[s].view(plan.spatial_shape(self.channels)))
+        return y.view(B, T, self.channels, *n)
 
     def reset(self):
         """Forget the sequences so far."""

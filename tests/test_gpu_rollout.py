@@ -198,6 +198,24 @@ def test_fields_are_marched():
     ro.close()
 
 
+@pytest.mark.parametrize("B,T,C", [(1, 1, 3), (2, 131, 1), (1, 257, 2), (3, 67, 16)])
+def test_more_frames_than_one_plan_takes(B, T, C):
+    """Frames are encoded and decoded in groups: each frame as by itself."""
+    torch = torch_gpu()
+    from paper_2607_14394_amd.rollout import Rollout
+    grid = dict(n_global=(8, 6, 8), n_local=(8, 6, 8), offset=(0, 0, 0), kmax=(1, 1, 2))
+    ro = Rollout(grid, C, B, [])
+    g = O.Geometry((8, 6, 8, 1), (8, 6, 8, 1), (0, 0, 0, 0), (1, 1, 2), 1, B * T, C, C)
+    f, fv = rounded(torch, np.random.RandomState(T).randn(B, T, C, 8, 6, 8), "f32")
+    tok = ro.encode(f)
+    assert tok.shape == (B, T, 2 * C * 2 * 2 * 4)
+    ref = O.forward(fv.reshape(B * T, C, 8, 6, 8, 1), g)
+    got = f64(tok).reshape(-1, 2)
+    assert rel(got[:, 0] + 1j * got[:, 1], ref.ravel()) <= 1e-5
+    assert rel(f64(ro.decode(tok)).reshape(B * T, C, 8, 6, 8, 1), O.inverse(ref, g)) <= 1e-5
+    ro.close()
+
+
 def test_blocks_refuse_other_shapes():
     torch = torch_gpu()
     from paper_2607_14394_amd.rollout import LatentBlock, Rollout
