@@ -313,14 +313,14 @@ enum {
 /* 8-bit arrays with scales.  An (R, K) array is R rows of codes (E4M3) of
  * round_up(K, 128) bytes, the columns past K zero, at a row stride that is a
  * multiple of 16 bytes on a 16-byte aligned pointer, and R rows of scales, one
- * byte s = 1 .. 254 for each 128 columns standing for 2^(s - 127), at a row stride
- * that is a multiple of 4 bytes on a 4-byte aligned pointer.  A value is its code times
- * its scale.  Powers of two lose no bits, and the matrix cores apply them
- * inside the product.  The library writes the smallest scale >= 2^-126 that
- * brings the block's largest magnitude to at most 448 (1 for a block of
- * zeros), rounds to nearest even, and fills the last four bytes of a row of
- * scales with 127; the values that are infinite or no number become the code
- * of no number and do not count for the scale. */
+ * byte s = 1 .. 254 for each 128 columns standing for 2^(s - 127), at a row
+ * stride that is a multiple of 4 bytes on a 4-byte aligned pointer.  A value
+ * is its code times its scale.  Powers of two lose no bits, and the matrix
+ * cores apply them inside the product.  The library writes the smallest scale
+ * >= 2^-126 that brings the block's largest magnitude to at most 448 (1 for a
+ * block of zeros), rounds to nearest even, and fills the last four bytes of a
+ * row of scales with 127; the values that are infinite or no number become the
+ * code of no number and do not count for the scale. */
 
 /* RMS norm with the residual's addition, row by row:
  *   u = x + res,  rounded to the residual's type and stored in sum_out;

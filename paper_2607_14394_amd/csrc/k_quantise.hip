@@ -7,7 +7,9 @@
 // transposed form a workgroup takes 128 x 128 values, a lane 8 x 8 of them: the
 // columns' scales are maxima over a lane's rows, lanes and waves, and a lane's
 // codes of 8 rows of a column go to LDS as one word, from which each column's 128
-// codes are written as one line.
+// codes are written as one line.  4096 x 2048 bf16 by rows 6.3 us (4.0 TB/s); 4096
+// x 4608 bf16 both ways from one reading 22 us (3.4 TB/s), where its vector
+// instructions, some 20 a value, take half.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
