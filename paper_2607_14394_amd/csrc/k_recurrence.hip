@@ -291,7 +291,6 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
     if (FULL || rows > 0) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        if (!FULL && i >= rows) break;
         float r[CPL];
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
@@ -302,8 +301,10 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
             r[c] *= x * logistic(x);
           }
         }
-        put<T, CPL>(row, q.c, r);
-        row += p.y.t;
+        if (FULL || i < rows) {  // (past them h stands still; leaving the loop instead keeps it from being unrolled)
+          put<T, CPL>(row, q.c, r);
+          row += p.y.t;
+        }
       }
     }
     if (!FULL) put_zeros<T, CPL>(y, p.y, q.b, t0 + rows, end, q.c);
@@ -511,9 +512,19 @@ Args args_of(const dtst_recurrence_desc& d, const int32_t* lengths, int cpl) {
   return p;
 }
 
-// Features of a lane: two, one where there is only one, and in the backward one
-// of 32 bits (two would hold more registers than there are).
-int lane_features(int type, int64_t features, bool adj) { return features >= 2 && !(adj && type == DTST_F32) ? 2 : 1; }
+// Features of a lane: two, but one in the backward of 32 bits (two would hold
+// more registers than there are) and where two leave half of the CUs idle (2 x
+// 128 x 1000 bf16: backward 11 against 9 us; 2 x 1024 x 2048, 256 workgroups: 22
+// against 23).
+// The last lanes of a tile of 128 step back over features of the same tile.  A
+// single feature left over would be computed with its neighbour, which another
+// workgroup has too and may have updated in place already: such a number of
+// features is taken one a lane.
+int lane_features(const dtst_recurrence_desc& d, bool adj) {
+  const int64_t spans = (d.steps + SPAN - 1) / SPAN;
+  const bool fills = d.batch * ((d.features + 127) / 128) * spans > 128;
+  return fills && d.features % 128 != 1 && !(adj && d.type == DTST_F32) ? 2 : 1;
+}
 
 template <class F>
 int by_type(int type, F&& f) {
@@ -557,18 +568,17 @@ int by_form(const dtst_recurrence_desc& d, const int32_t* lengths, bool with_o, 
     };
     const auto with_gate = [&](auto cpl) { return with_o ? rest(cpl, true_type()) : rest(cpl, false_type()); };
     if constexpr (!(ADJ && std::is_same_v<decltype(t), float>))
-      if (lane_features(d.type, d.features, ADJ) == 2) return with_gate(integral_constant<int, 2>());
+      if (lane_features(d, ADJ) == 2) return with_gate(integral_constant<int, 2>());
     return with_gate(integral_constant<int, 1>());
   });
 }
 
 }  // namespace
 
-size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type) {
+size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int) {
   if (steps <= SPAN) return 0;
-  // (the forward's, which is no smaller than the backward's)
-  const int64_t w = 64 * lane_features(type, features, false);
-  return 64 + size_t(batch * ((features + w - 1) / w)) * ((steps + SPAN - 1) / SPAN) * w * 8;
+  // (tiles of 128 features; those of 64 have no more words)
+  return 64 + size_t(batch * ((features + 127) / 128)) * ((steps + SPAN - 1) / SPAN) * 128 * 8;
 }
 
 int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o, const float* h_zero,

@@ -235,3 +235,39 @@ def test_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (y, h, *g))), i
+
+
+@pytest.mark.parametrize("B,T,F", [(4096, 1, 129), (512, 1, 1025), (96, 300, 257), (40, 128, 641)])
+def test_states_in_place_where_a_feature_is_left_over(B, T, F):
+    """A last tile of a single feature shares none with the one before."""
+    torch, D = lib()
+    c = Case(torch, B, T, F, "bf16", F)
+    y, h, st = torch.empty_like(c.g), c.h0.clone(), torch.empty(D.recurrence_states_shape(B, T, F), device="cuda")
+    y2, h2 = torch.empty_like(c.g), torch.empty_like(c.h0)
+    D.dtst_recurrence(c.z, c.v, y, o=c.o, h0=h, h_out=h, states=st)
+    D.dtst_recurrence(c.z, c.v, y2, o=c.o, h0=c.h0, h_out=h2)
+    assert torch.equal(h, h2) and torch.equal(y, y2)
+    g = [torch.empty_like(c.g) for _ in range(3)]
+    gh, gh2 = c.gh.clone(), torch.empty_like(c.gh)
+    D.dtst_recurrence_adj(c.z, c.v, c.g, st, g[0], g[1], o=c.o, g_o=g[2], g_h=gh, g_hzero=gh)
+    D.dtst_recurrence_adj(c.z, c.v, c.g, st, g[0], g[1], o=c.o, g_o=g[2], g_h=c.gh, g_hzero=gh2)
+    assert torch.equal(gh, gh2)
+    near(f64(h2), S.recurrence(c.zv, c.vv, c.ov, c.h0v)[1][:, -1], "f32", "h",
+         rms=max(1.0, float(np.abs(c.h0v).max())))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,T,F", [(130, 1, 2), (130, 17, 3), (150, 16, 127), (70, 40, 130), (70, 128, 254),
+                                   (66, 129, 200), (45, 300, 127), (6, 3300, 2), (33, 257, 386), (129, 1, 128)])
+def test_many_workgroups(B, T, F, t):
+    """Enough of them that a lane takes two features."""
+    torch, D = lib()
+    run(torch, D, Case(torch, B, T, F, t, B + T + F))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_many_workgroups_of_unlike_lengths(t):
+    torch, D = lib()
+    B, T = 48, 390
+    lengths = [0, 1, 15, 16, 17, 127, 128, 129, 200, 255, 256, 257, 383, 384, 385, 389, 390, 400, -3] * 3
+    run(torch, D, Case(torch, B, T, 131, t, 5, lengths=lengths[:B], pad=3))
