@@ -143,15 +143,17 @@ int launch_norm_cols(const dtst_norm_desc& d, const void* x, const void* res, co
   return launch_norm<TX, TR, Q8, 16, 4>(d, x, res, w, sum_out, y, scale, rstd, s);
 }
 
-// Backward.  A workgroup takes rows blockIdx, + gridDim, ... and keeps its
+// Backward.  RW waves hold a row, ROWS rows a workgroup at once (one where
+// several waves share a row); it takes every gridDim-th of them and keeps its
 // columns' sums of g_y h in registers; they go to part (gridDim, cols), which
 // sum_parts_kernel adds up.
-template <class TX, class TR, int RW, int V>
-__global__ void __launch_bounds__(RW * 64)
+template <class TX, class TR, int RW, int V, int ROWS>
+__global__ void __launch_bounds__(RW * ROWS * 64, V == 2 ? 4 : 1)  // (4: two registers fewer hold one more wave)
 rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* __restrict__ w,
                     const float* __restrict__ rstd, const TR* g_sum, TR* g_u, TX* g_x, float* part) {
+  static_assert(ROWS == 1 || (RW == 1 && V == 1), "a wave a row, in one access");
   __shared__ float red[2][RW];
-  const int first = threadIdx.x * VEC;
+  const int first = int(threadIdx.x % (RW * 64)) * VEC, sub = threadIdx.x / (RW * 64);
   const int64_t cols = d.cols;
   float wv[V][VEC], gw[V][VEC];
 #pragma unroll
@@ -162,7 +164,7 @@ rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const floa
     for (int j = 0; j < VEC; ++j) gw[i][j] = 0.f;
   }
   int odd = 0;
-  for (int64_t row = blockIdx.x; row < d.rows; row += gridDim.x, odd ^= 1) {
+  for (int64_t row = int64_t(blockIdx.x) * ROWS + sub; row < d.rows; row += int64_t(gridDim.x) * ROWS, odd ^= 1) {
     const float r = rstd[row];
     float g[V][VEC], h[V][VEC];
     float dot = 0.f;
@@ -198,6 +200,19 @@ rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const floa
       if (g_x != nullptr) store_n<VEC>(g_x + row * d.ld_g_x + c, cols - c, e);
     }
   }
+  if constexpr (ROWS > 1) {  // (in order)
+    __shared__ float sums[ROWS][64 * VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sums[sub][first + j] = gw[0][j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += ROWS * 64) {
+      float t = 0.f;
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) t += sums[k][c];
+      part[blockIdx.x * cols + c] = t;
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int64_t c = first + i * RW * 64 * VEC;
@@ -228,15 +243,20 @@ sum_parts_kernel(const float* __restrict__ part, int parts, int64_t cols, int ac
   }
 }
 
-// Workgroups of the backward: enough for the card, eight rows or more each
-// where there are many rows (the parts are then a tenth of the traffic or less).
-int64_t norm_adj_parts(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(1024, (rows + 7) / 8)); }
+// Workgroups of the backward: two rows a wave or group of waves, until the card
+// is full (two groups of 16 waves a CU, four of 4, two of 8 single ones).  Eight
+// rows each left CUs idle (backward of 495 x 7931: 33 against 21 us).
+constexpr int SINGLE = 512, SINGLE_ROWS = 8;  // up to so many columns a wave holds a row, so many rows a workgroup
+int64_t norm_adj_parts(int64_t rows, int64_t cols) {
+  const int64_t each = cols <= SINGLE ? 2 * SINGLE_ROWS : 2, most = cols <= SINGLE || cols > 4096 ? 512 : 1024;
+  return std::max<int64_t>(1, std::min<int64_t>(most, (rows + each - 1) / each));
+}
 
-template <class TX, class TR, int RW, int V>
+template <class TX, class TR, int RW, int V, int ROWS = 1>
 int launch_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* w, const float* rstd,
                     const void* g_sum, void* g_u, void* g_x, float* part, hipStream_t s) {
-  hipLaunchKernelGGL((rms_norm_adj_kernel<TX, TR, RW, V>), dim3(unsigned(norm_adj_parts(d.rows))), dim3(RW * 64), 0, s,
-                     d, static_cast<const TX*>(g_y), static_cast<const TR*>(u), w, rstd,
+  hipLaunchKernelGGL((rms_norm_adj_kernel<TX, TR, RW, V, ROWS>), dim3(unsigned(norm_adj_parts(d.rows, d.cols))),
+                     dim3(RW * ROWS * 64), 0, s, d, static_cast<const TX*>(g_y), static_cast<const TR*>(u), w, rstd,
                      static_cast<const TR*>(g_sum), static_cast<TR*>(g_u), static_cast<TX*>(g_x), part);
   return hipGetLastError();
 }
@@ -245,7 +265,7 @@ template <class TX, class TR>
 int launch_norm_adj_cols(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* w,
                          const float* rstd, const void* g_sum, void* g_u, void* g_x, float* part, hipStream_t s) {
   const int64_t c = d.cols;
-  if (c <= 512) return launch_norm_adj<TX, TR, 1, 1>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
+  if (c <= SINGLE) return launch_norm_adj<TX, TR, 1, 1, SINGLE_ROWS>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
   if (c <= 2048) return launch_norm_adj<TX, TR, 4, 1>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
   if (c <= 4096) return launch_norm_adj<TX, TR, 4, 2>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
   if (c <= 8192) return launch_norm_adj<TX, TR, 16, 1>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
@@ -276,7 +296,7 @@ int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, con
   });
 }
 
-size_t rms_norm_adj_workspace(int64_t rows, int64_t cols) { return size_t(norm_adj_parts(rows)) * cols * 4; }
+size_t rms_norm_adj_workspace(int64_t rows, int64_t cols) { return size_t(norm_adj_parts(rows, cols)) * cols * 4; }
 
 int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
                         const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight, void* workspace,
@@ -288,7 +308,7 @@ int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void
   });
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((d.cols + 31) / 32)), dim3(1024), 0, s, part,
-                     int(norm_adj_parts(d.rows)), d.cols, d.accumulate, g_weight);
+                     int(norm_adj_parts(d.rows, d.cols)), d.cols, d.accumulate, g_weight);
   return hipGetLastError();
 }
 
