@@ -194,21 +194,22 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
     scale_rows[i] = row < BM ? p.sa + min(m0 + row, p.m - 1) * p.ld_sa : p.sb + min(n0 + row - BM, p.n - 1) * p.ld_sb;
   }
 
-  // this group's blocks of 128: nk from block k0 on (groups of scale words stay
-  // whole); every group meets at `steps` barriers
+  // this group's blocks of 128: nk from block k0 on, the first of them number
+  // k_odd of its scale word; every group meets at `steps` barriers
   const int blocks = int((p.k + 127) / 128);
-  const int steps = KS == 1 ? blocks : ((blocks + KS - 1) / KS + 3) / 4 * 4;
+  const int steps = (blocks + KS - 1) / KS;
   const int k0 = group * steps, nk = KS == 1 ? blocks : min(max(blocks - k0, 0), steps);
+  const int k_odd = KS == 1 ? 0 : k0 % 4;
   base_a += int64_t(k0) * ROW, base_b += int64_t(k0) * ROW;
 
   const uint32_t lds0 = lds_address(lds);
-  // the scale words (every fourth stage) and part i of n of a stage's loads
+  // the scale words (at a word's first stage) and part i of n of a stage's loads
   const auto fetch_scales = [&](int kb) {
-    if (kb % 4 == 0) {
+    if ((k_odd + kb) % 4 == 0 || (KS > 1 && kb == 0)) {
 #pragma unroll
       for (int i = 0; i < SPW; ++i) {
         const int part = wave + i * WAVES;
-        if (part < SL) fetch4(scale_rows[i] + k0 + kb, lds0 + STAGES * STAGE + (kb / 4 % 2) * SCALES + part * 256);
+        if (part < SL) fetch4(scale_rows[i] + (k0 + kb) / 4 * 4, lds0 + STAGES * STAGE + ((k_odd + kb) / 4 % 2) * SCALES + part * 256);
       }
     }
   };
@@ -253,8 +254,9 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
     if (KS > 1 && kb >= nk) continue;
     const uint8_t* at_a = lds + (kb % STAGES) * STAGE + wm * TM * 16 * ROW;
     const uint8_t* at_b = lds + (kb % STAGES) * STAGE + BM * ROW + wn * TN * 16 * ROW;
-    const uint8_t* at_sa = lds + STAGES * STAGE + (kb / 4 % 2) * SCALES + (wm * TM * 16 + r) * 4 + kb % 4;
-    const uint8_t* at_sb = lds + STAGES * STAGE + (kb / 4 % 2) * SCALES + (BM + wn * TN * 16 + r) * 4 + kb % 4;
+    const int word = (k_odd + kb) / 4, byte = (k_odd + kb) % 4;
+    const uint8_t* at_sa = lds + STAGES * STAGE + word % 2 * SCALES + (wm * TM * 16 + r) * 4 + byte;
+    const uint8_t* at_sb = lds + STAGES * STAGE + word % 2 * SCALES + (BM + wn * TN * 16 + r) * 4 + byte;
     if constexpr (SHORT) {
       v8i fb[TN];
       int sb[TN];
@@ -448,6 +450,7 @@ int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
     return launch_tile<true, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
   }
   if (tiles(16, 32) <= 256) return launch_tile<false, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
+  if (tiles(32, 32) <= 256) return launch_tile<false, 1, 1, 2, 2, 2, 8, TC>(p, c, s);
   if (tiles(64, 32) <= 256) return launch_tile<false, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
   if (tiles(64, 64) <= 256) return launch_tile<false, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
   const Tile forms[] = {{128, 64, 512, 800},   {128, 128, 512, 1080}, {128, 192, 256, 1050}, {128, 256, 256, 1200},

@@ -70,6 +70,13 @@ def test_product(m, n, k):
 # the largest: each of the eight loses less than 2^-13 of it, so a result's error
 # is below the sum over its eights of 8 * 2^-13 of their largest product; beside
 # the bar of the 32-bit sums.
+@pytest.mark.parametrize("k", [520, 640, 1152, 1500, 2944, 6560])
+@pytest.mark.parametrize("m,n", [(5, 70), (300, 700), (690, 700), (990, 1000)])
+def test_parts_of_the_summed_axis(m, n, k):
+    """Blocks of 128 that the waves' parts do not divide, parts that begin inside a word of scales."""
+    test_product(m, n, k)
+
+
 @pytest.mark.parametrize("m,n,k", SIZES + [(3000, 4200, 300), (4096, 3600, 1152)])
 def test_short_sums(m, n, k):
     torch, D = lib()
