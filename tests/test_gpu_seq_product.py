@@ -71,7 +71,7 @@ def test_product(m, n, k):
 # is below the sum over its eights of 8 * 2^-13 of their largest product; beside
 # the bar of the 32-bit sums.
 @pytest.mark.parametrize("k", [520, 640, 1152, 1500, 2944, 6560])
-@pytest.mark.parametrize("m,n", [(5, 70), (300, 700), (690, 700), (990, 1000)])
+@pytest.mark.parametrize("m,n", [(5, 70), (300, 700), (690, 700), (990, 1000), (1400, 1390), (1500, 1490)])
 def test_parts_of_the_summed_axis(m, n, k):
     """Blocks of 128 that the waves' parts do not divide, parts that begin inside a word of scales."""
     test_product(m, n, k)
