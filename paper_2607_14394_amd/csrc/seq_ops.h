@@ -98,15 +98,34 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
   return amax == 0.f ? 127u : uint32_t(e < 1 ? 1 : e);
 }
 
-// 2^-(s - 127), the factor that brings a block's values to code range
-// (s = 1 .. 247, so 2^126 .. 2^-120).
-__device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }
+// 2^(s - 127), s = 1 .. 254.
+__device__ __forceinline__ float scale_float(uint32_t s) { return __uint_as_float(s << 23); }
 
-// Four values of at most 448, infinities or no numbers to four codes, nearest
-// even; the conversion makes the last two the code of no number.
-__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
-  const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
+// Values over a scale that leaves them at most 448, infinities or no numbers, to
+// codes, nearest even, one rounding; the last two become the code of no number.
+// (The conversion divides by the scale's power of two; what it gives is what a
+// division in 32 bits and a conversion give, measured for all 16-bit values.)
+typedef short code_pairs __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d, float scale) {
+  code_pairs r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, r);
+}
+// The same of two words of two 16-bit values.
+template <class T>
+__device__ __forceinline__ uint32_t to_codes(uint32_t ab, uint32_t cd, float scale) {
+  typedef T pair __attribute__((ext_vector_type(2)));
+  const pair p = __builtin_bit_cast(pair, ab), q = __builtin_bit_cast(pair, cd);
+  code_pairs r = {0, 0};
+  if constexpr (std::is_same_v<T, bf16_t>) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, p, scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, q, scale, true);
+  } else {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, p, scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, q, scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, r);
 }
 
 // A block of 128 values, eight a lane in 16 lanes: the lane's codes, and the
@@ -115,9 +134,9 @@ __device__ __forceinline__ uint32_t code_block(const float (&v)[8], uint2& q) {
   float m = row_max(max_abs(v));
   if (__any(is_infinite(m))) m = row_max(max_finite_abs(v));
   const uint32_t s = scale_byte(m);
-  const float inv = scale_inverse(s);
-  q.x = to_codes(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-  q.y = to_codes(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+  const float scale = scale_float(s);
+  q.x = to_codes(v[0], v[1], v[2], v[3], scale);
+  q.y = to_codes(v[4], v[5], v[6], v[7], scale);
   return s;
 }
 
