@@ -411,15 +411,17 @@ int launch_tile(const Operands& p, void* c, hipStream_t s) {
 // products, so small results take the smallest tile that still leaves one
 // workgroup a CU, its waves dividing the summed axis (KS).  Measured, in us:
 //                        16 x 32  32 x 32  64 x 32  64 x 64  128 x 64  128 x 128    without KS
-//   4 x 4608 x 2048          4.4               6.9      9.0
-//   48 x 8192 x 8192        24.4              17.7     24.5
-//   512 x 512 x 8192        15.0     10.9     15.8
-//   4096 x 64 x 2048                  4.9      6.1
-//   1024 x 1024 x 8192                        30.5     23.1      33.3
-//   1900 x 1000 x 2048                                 16.8      13.6       18.6          18.4
-//   1400 x 1400 x 8192                                 44.2      38.3       54.7          59.1
+//   4 x 4608 x 2048          4.1      4.6      5.8      8.2
+//   48 x 4608 x 2048         7.2      8.5      6.3      7.8
+//   512 x 512 x 8192        15.0     10.9     15.8     21.4
+//   4096 x 64 x 2048         7.0      5.0      6.2      8.0
+//   1024 x 1024 x 8192                        30.7     22.6      33.3
+//   1900 x 1000 x 2048                                 16.6      13.6       18.6          18.4
+//   1400 x 1400 x 8192                                 44.0      38.5       54.7          59.1
 //   2048 x 2048 x 2048                                           25.3       21.5          23.9
 //   2048 x 2048 x 512                                                       11.3          10.4
+// (64 x 64 by two waves, each all of a's rows: four of 32 x 32, which widen more,
+// take 3% longer, one that widens least 25%, and fewer groups of more stages 2 to 8%.)
 // Larger ones take the tile whose rounds of workgroups over the card cost least,
 // at the rates that full rounds reach (at_once: workgroups that the card holds;
 // where a CU holds two, the last round of a few overlaps the one before).  Every
@@ -457,7 +459,7 @@ int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
   if (tiles(16, 32) <= 256) return launch_tile<false, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
   if (tiles(32, 32) <= 256) return launch_tile<false, 1, 1, 2, 2, 2, 8, TC>(p, c, s);
   if (tiles(64, 32) <= 256) return launch_tile<false, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
-  if (tiles(64, 64) <= 256) return launch_tile<false, 2, 2, 2, 2, 2, 4, TC>(p, c, s);
+  if (tiles(64, 64) <= 256) return launch_tile<false, 1, 2, 4, 2, 2, 4, TC>(p, c, s);
   if (tiles(128, 64) <= 256) return launch_tile<false, 2, 2, 4, 2, 2, 2, TC>(p, c, s);
   if (tiles(128, 128) <= 256 && p.k >= 1024) return launch_tile<false, 2, 2, 4, 4, 2, 2, TC>(p, c, s);
   const Tile forms[] = {{128, 64, 512, 800},   {128, 128, 512, 1080}, {128, 192, 256, 1050}, {128, 256, 256, 1200},
