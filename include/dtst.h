@@ -385,19 +385,16 @@ dtst_status dtst_quantise(const dtst_quantise_desc* d, const void* x, void* q, v
  * instruction, which it does for large products (2 m n k >= 2^38), at nearly
  * twice the rate: its sum of eight neighbouring products keeps 13 bits below
  * the largest of them (1e-5 to 2e-5 of the result on normally distributed
- * values), the sum of those sums 32 bits.  k and the
- * strides up to 2^23 (DTST_ERR_UNSUPPORTED above).  workspace: dtst_product_workspace bytes; it
- * is 0 for most sizes, and then workspace may be NULL. */
+ * values), the sum of those sums 32 bits.  k and the strides up to 2^23
+ * (DTST_ERR_UNSUPPORTED above). */
 typedef struct {
   int64_t m, n, k;
   int64_t ld_a, ld_a_scale, ld_b, ld_b_scale, ld_c;
   int32_t c_type;
   int32_t accumulate, short_sums;
 } dtst_product_desc;
-dtst_status dtst_product_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes);
 dtst_status dtst_product(const dtst_product_desc* d, const void* a, const void* a_scale, const void* b,
-                         const void* b_scale, const float* bias, void* c, void* workspace, size_t workspace_bytes,
-                         void* stream);
+                         const void* b_scale, const float* bias, void* c, void* stream);
 
 /* Gated linear recurrence along the steps, feature by feature, with the
  * logistic function s(v) = 1 / (1 + exp(-v)):

@@ -29,7 +29,7 @@ __all__ = [
     "dtst_profile_collect", "dtst_plan_block_info", "Schedule", "dtst_desc_schedule", "Plan", "LIB_PATH",
     "PLAN_SPLIT_SCHEDULE", "PLAN_UNFUSED_BLOCK", "SCRATCH_BYTES", "torch_stream",
     "RECURRENCE_SPAN", "code_columns", "scale_columns", "empty_codes", "recurrence_states_shape", "dtst_rms_norm",
-    "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product", "dtst_product_workspace",
+    "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
 ]
 
@@ -121,8 +121,7 @@ def _load():
         "dtst_rms_norm_adj_workspace": [I64, I64, ctypes.POINTER(SZ)],
         "dtst_rms_norm_adj": [VP] * 10 + [SZ, VP],
         "dtst_quantise": [VP] * 7,
-        "dtst_product_workspace": [I64, I64, I64, ctypes.POINTER(SZ)],
-        "dtst_product": [VP] * 8 + [SZ, VP],
+        "dtst_product": [VP] * 8,
         "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
         "dtst_recurrence": [VP] * 10 + [SZ, VP],
         "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
@@ -347,11 +346,8 @@ def _device():
         return -2
 
 
-def _on(stream, dev):
-    """The stream of a call on device dev."""
-    if stream is not None:
-        return int(stream)
-    return _raw_stream(dev) if _raw_stream is not None else torch_stream()
+# The current stream of a device.
+_current = _raw_stream if _raw_stream is not None else lambda dev: torch_stream()
 
 
 def _refuse(t, shape, name, dtypes):
@@ -364,6 +360,8 @@ def _rows(t, shape, name, dtypes, dev):
     """Row stride of a 2-D tensor on device dev with contiguous rows."""
     if t.shape == shape and t.dtype in dtypes and t.get_device() == dev:
         rows, cols = shape
+        if rows > 1 and t.is_contiguous():
+            return cols
         s0, s1 = t.stride()
         if s1 == 1 or cols == 1 or rows == 0:
             return s0 if rows > 1 else cols + 15 & -16  # (that of a single row is any; one that suits every type)
@@ -385,7 +383,7 @@ def _codes(q, s, rows, k, name, dev):
     ks = (kq >> 7) + 3 & -4
     if (q.shape == (rows, kq) and s.shape == (rows, ks) and q.dtype is _CODE and s.dtype is _SCALE
             and q.get_device() == dev and s.get_device() == dev):
-        if rows <= 1:
+        if q.is_contiguous() and s.is_contiguous():
             return kq, ks
         (q0, q1), (s0, s1) = q.stride(), s.stride()
         if q1 == 1 and s1 == 1:
@@ -423,10 +421,13 @@ def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, e
     _vector(weight, cols, "weight", dev)
     if rstd is not None:
         _vector(rstd, rows, "rstd", dev)
-    _check(lib.dtst_rms_norm(NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt],
-                                            _TYPES[y.dtype], eps),
-                             x.data_ptr(), _ptr(res), weight.data_ptr(), _ptr(sum_out), y.data_ptr(), _ptr(scale),
-                             _ptr(rstd), _on(stream, dev)))
+    status = lib.dtst_rms_norm(
+        NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt], _TYPES[y.dtype], eps),
+        x.data_ptr(), None if res is None else res.data_ptr(), weight.data_ptr(),
+        None if sum_out is None else sum_out.data_ptr(), y.data_ptr(), None if scale is None else scale.data_ptr(),
+        None if rstd is None else rstd.data_ptr(), _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -453,8 +454,12 @@ def dtst_rms_norm_adj(g_y, u, weight, rstd, g_u, g_weight, g_sum=None, g_x=None,
     _vector(g_weight, cols, "g_weight", dev)
     _vector(rstd, rows, "rstd", dev)
     p, n, ws = _scratch(ws, dtst_rms_norm_adj_workspace(rows, cols), g_y.device, stream)
-    _check(lib.dtst_rms_norm_adj(d, g_y.data_ptr(), u.data_ptr(), weight.data_ptr(), rstd.data_ptr(), _ptr(g_sum),
-                                 g_u.data_ptr(), _ptr(g_x), g_weight.data_ptr(), p, n, _on(stream, dev)))
+    status = lib.dtst_rms_norm_adj(d, g_y.data_ptr(), u.data_ptr(), weight.data_ptr(), rstd.data_ptr(),
+                                   None if g_sum is None else g_sum.data_ptr(), g_u.data_ptr(),
+                                   None if g_x is None else g_x.data_ptr(), g_weight.data_ptr(), p, n,
+                                   _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
 def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
@@ -469,18 +474,16 @@ def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
     ld_x = _rows(x, (rows, cols), "x", _FLOATS, dev)
     ld_q, ld_s = (0, 0) if q is None else _codes(q, scale, rows, cols, "q", dev)
     ld_qt, ld_st = (0, 0) if qt is None else _codes(qt, scale_t, cols, rows, "qt", dev)
-    _check(lib.dtst_quantise(QUANTISE_DESC.pack(rows, cols, ld_x, ld_q, ld_s, ld_qt, ld_st, _TYPES[x.dtype]),
-                             x.data_ptr(), _ptr(q), _ptr(scale), _ptr(qt), _ptr(scale_t), _on(stream, dev)))
+    status = lib.dtst_quantise(QUANTISE_DESC.pack(rows, cols, ld_x, ld_q, ld_s, ld_qt, ld_st, _TYPES[x.dtype]),
+                               x.data_ptr(), None if q is None else q.data_ptr(),
+                               None if scale is None else scale.data_ptr(), None if qt is None else qt.data_ptr(),
+                               None if scale_t is None else scale_t.data_ptr(),
+                               _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
-@functools.lru_cache(maxsize=1024)
-def dtst_product_workspace(m, n, k) -> int:
-    b = ctypes.c_size_t(0)
-    _check(lib.dtst_product_workspace(int(m), int(n), int(k), ctypes.byref(b)))
-    return b.value
-
-
-def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_sums=False, ws=None, stream=None):
+def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_sums=False, stream=None):
     """c = a b^T + bias (+ c): codes a (m, k) and b (n, k) with their scales
     into c (m, n).  short_sums: allow the 8-bit matrix instruction's sums."""
     if c.dim() != 2 or a.dim() != 2:
@@ -494,9 +497,11 @@ def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_s
                           int(accumulate), int(short_sums))
     if bias is not None:
         _vector(bias, n, "bias", dev)
-    p, nb, ws = _scratch(ws, dtst_product_workspace(m, n, k), c.device, stream)
-    _check(lib.dtst_product(d, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(), _ptr(bias),
-                            c.data_ptr(), p, nb, _on(stream, dev)))
+    status = lib.dtst_product(d, a.data_ptr(), a_scale.data_ptr(), b.data_ptr(), b_scale.data_ptr(),
+                              None if bias is None else bias.data_ptr(), c.data_ptr(),
+                              _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -541,9 +546,17 @@ def dtst_recurrence(z, v, y, o=None, h0=None, h_out=None, lengths=None, states=N
         _state(states, recurrence_states_shape(B, T, F), "states", dev)
     if lengths is not None:
         _vector(lengths, B, "lengths", dev, torch.int32)
-    p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
-    _check(lib.dtst_recurrence(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(h0), _ptr(lengths), y.data_ptr(),
-                               _ptr(h_out), _ptr(states), p, n, _on(stream, dev)))
+    if T <= RECURRENCE_SPAN and ws is None:  # (none is needed)
+        p, n = None, 0
+    else:
+        p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
+    status = lib.dtst_recurrence(d, z.data_ptr(), v.data_ptr(), None if o is None else o.data_ptr(),
+                                 None if h0 is None else h0.data_ptr(), None if lengths is None else lengths.data_ptr(),
+                                 y.data_ptr(), None if h_out is None else h_out.data_ptr(),
+                                 None if states is None else states.data_ptr(), p, n,
+                                 _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
 def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None, g_hzero=None, lengths=None, ws=None,
@@ -572,9 +585,11 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     if lengths is not None:
         _vector(lengths, B, "lengths", dev, torch.int32)
     p, n, ws = _scratch(ws, dtst_recurrence_workspace(B, T, F, e), z.device, stream)
-    _check(lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
-                                   g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o), _ptr(g_hzero),
-                                   p, n, _on(stream, dev)))
+    status = lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
+                                     g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o),
+                                     _ptr(g_hzero), p, n, _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
 
 
 def dtst_profile_enable(on=True):

@@ -233,7 +233,7 @@ dtst_status quantise(const dtst_quantise_desc* d, const void* x, void* q, void* 
 }
 
 dtst_status product(const dtst_product_desc* d, const void* a, const void* a_scale, const void* b, const void* b_scale,
-                    const float* bias, void* c, void* workspace, size_t workspace_bytes, void* stream) {
+                    const float* bias, void* c, void* stream) {
   if (d == nullptr) return bad("descriptor is null");
   if (d->m < 0 || d->n < 0 || d->k < 1) return bad("need m >= 0, n >= 0 and k >= 1");
   if (!is_float_type(d->c_type)) return bad("c_type must be DTST_F32, DTST_BF16 or DTST_F16");
@@ -253,16 +253,8 @@ dtst_status product(const dtst_product_desc* d, const void* a, const void* a_sca
   if (d->m > (int64_t(1) << 31) || d->n > (int64_t(1) << 31))
     return fail(DTST_ERR_UNSUPPORTED, "m or n above 2^31");
   DTST_TRY(check_grid(((d->m + 127) / 128) * ((d->n + 127) / 128), 512));
-  const size_t need = product_workspace(d->m, d->n, d->k);
-  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
-  const Array aws{need ? workspace : nullptr, 1, int64_t(need), int64_t(need), 1, "workspace"};
-  for (const Array* in : {&aa, &asa, &ab, &asb, &abi}) {
-    DTST_TRY(check_apart(ac, *in, false));
-    DTST_TRY(check_apart(aws, *in, false));
-  }
-  DTST_TRY(check_apart(aws, ac, false));
-  const int e = timed(K_PRODUCT, stream,
-                      [&] { return launch_product(*d, a, a_scale, b, b_scale, bias, c, workspace, stream); });
+  for (const Array* in : {&aa, &asa, &ab, &asb, &abi}) DTST_TRY(check_apart(ac, *in, false));
+  const int e = timed(K_PRODUCT, stream, [&] { return launch_product(*d, a, a_scale, b, b_scale, bias, c, stream); });
   return device_status(e, "product launch");
 }
 
@@ -435,21 +427,9 @@ dtst_status dtst_quantise(const dtst_quantise_desc* d, const void* x, void* q, v
   return guarded([&] { return quantise(d, x, q, scale, qt, scale_t, stream); });
 }
 
-dtst_status dtst_product_workspace(int64_t m, int64_t n, int64_t k, size_t* bytes) {
-  return guarded([&] {
-    if (bytes == nullptr) return bad("bytes is null");
-    if (m < 0 || n < 0 || k < 1) return bad("need m >= 0, n >= 0 and k >= 1");
-    if (m > (int64_t(1) << 31) || n > (int64_t(1) << 31) || k > (1 << 23))
-      return fail(DTST_ERR_UNSUPPORTED, "m or n above 2^31, or k above 2^23");
-    *bytes = product_workspace(m, n, k);
-    return ok();
-  });
-}
-
 dtst_status dtst_product(const dtst_product_desc* d, const void* a, const void* a_scale, const void* b,
-                         const void* b_scale, const float* bias, void* c, void* workspace, size_t workspace_bytes,
-                         void* stream) {
-  return guarded([&] { return product(d, a, a_scale, b, b_scale, bias, c, workspace, workspace_bytes, stream); });
+                         const void* b_scale, const float* bias, void* c, void* stream) {
+  return guarded([&] { return product(d, a, a_scale, b, b_scale, bias, c, stream); });
 }
 
 dtst_status dtst_recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type, size_t* bytes) {

@@ -480,10 +480,8 @@ int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
 
 }  // namespace
 
-size_t product_workspace(int64_t, int64_t, int64_t) { return 0; }
-
 int launch_product(const dtst_product_desc& d, const void* a, const void* a_scale, const void* b, const void* b_scale,
-                   const float* bias, void* c, void*, void* stream) {
+                   const float* bias, void* c, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const Operands p{static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(b),
                    static_cast<const uint8_t*>(a_scale), static_cast<const uint8_t*>(b_scale),

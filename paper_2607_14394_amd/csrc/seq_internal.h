@@ -19,9 +19,8 @@ int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void
                         void* stream);
 int launch_quantise(const dtst_quantise_desc& d, const void* x, void* q, void* scale, void* qt, void* scale_t,
                     void* stream);
-size_t product_workspace(int64_t m, int64_t n, int64_t k);
 int launch_product(const dtst_product_desc& d, const void* a, const void* a_scale, const void* b, const void* b_scale,
-                   const float* bias, void* c, void* workspace, void* stream);
+                   const float* bias, void* c, void* stream);
 size_t recurrence_workspace(int64_t batch, int64_t steps, int64_t features, int type);
 int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o, const float* h_zero,
                       const int32_t* lengths, void* y, float* h_out, float* states, void* workspace, void* stream);

@@ -164,11 +164,11 @@ def test_quantise_refusals(kw, code, word):
     assert st == code and word in msg, (st, msg)
 
 
-def product_call(a=P, sa=P * 2, b=P * 3, sb=P * 4, bias=None, c=P * 5, ws=None, nws=0, **kw):
+def product_call(a=P, sa=P * 2, b=P * 3, sb=P * 4, bias=None, c=P * 5, **kw):
     f = dict(m=70, n=80, k=200, ld_a=256, ld_a_scale=4, ld_b=256, ld_b_scale=4, ld_c=80, c_type=1, accumulate=0, short_sums=0)
     f.update(kw)
     d = D.PRODUCT_DESC.pack(*f.values())
-    return status(D.lib.dtst_product, d, a, sa, b, sb, bias, c, ws, nws, None)
+    return status(D.lib.dtst_product, d, a, sa, b, sb, bias, c, None)
 
 
 @pytest.mark.parametrize("kw,code,word", [
