@@ -11,6 +11,12 @@
 // the 128 codes (any quarter, as long as it is the same for both); with b as the
 // first operand a lane ends with four neighbouring columns 4 (l / 16) + r of row
 // l % 16 of c.
+//
+// Large products are bound by the matrix cores and what feeds them: 8192^3 438 us
+// short (2510 TFLOP/s, the cores busy 62% of the time at 1.96 GHz; 323 us if no
+// stage had to be fetched) and 759 us exact (1450; without the widening, two codes
+// an instruction in between, 12 to 15% less).  Smaller ones wait for their first
+// loads and their stores.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

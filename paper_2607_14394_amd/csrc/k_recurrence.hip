@@ -19,8 +19,9 @@
 //
 // 1 x 65536 x 1280 in bf16: 139 us and 5 us for clearing the chain's words, 4.8
 // TB/s (two launches, maps then states, would read z and v twice); 4 x 4096 x
-// 2048 60 us forward and 107 us backward (4.5 and 4.4 TB/s), where some 35 and 70
-// vector instructions a value come close to the time of the loads.
+// 2048 60 us forward and 107 us backward (4.5 and 4.4 TB/s), where 24 and 46
+// vector instructions a value, 4 and 6 of them at a quarter of the rate, come
+// close to the time of the loads.
 //
 // Waiting ends: spans are taken by ticket, spans earlier in the chain have
 // earlier tickets, so a workgroup waits only for workgroups that already run,
