@@ -140,6 +140,38 @@ def test_short_sums_of_large_products(m, n, k):
         assert worst <= 1, name
 
 
+@pytest.mark.parametrize("m,n,k", [(4097, 6200, 100), (4097, 6200, 700), (8200, 8200, 300), (5000, 5003, 130),
+                                   (12000, 4100, 513), (4600, 9000, 1100)])
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_several_rounds_of_tiles(m, n, k, t):
+    """All of the result against a 32-bit product of the values: 2^-22 k / 2 of
+    its terms' size each side, and half a unit of the result's type."""
+    torch, D = lib()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + k)
+    x, w = (torch.randn((r, k), generator=g, device="cuda") * torch.exp2(torch.randn((r, 1), generator=g, device="cuda"))
+            for r in (m, n))
+    bias = torch.randn(n, generator=g, device="cuda")
+    a, b = D.empty_codes(m, k), D.empty_codes(n, k)
+    D.dtst_quantise(x, *a)
+    D.dtst_quantise(w, *b)
+
+    def values(q, s):
+        e = torch.exp2(s.view(torch.uint8)[:, :q.shape[1] // 128].float() - 127)
+        return q.float() * e.repeat_interleave(128, dim=1)
+
+    av, bv = values(*a), values(*b)
+    c = torch.full((m, n), float("nan"), device="cuda").to(dtype(torch, t))
+    D.dtst_product(*a, *b, c, bias=bias)
+    ref = av @ bv.t().contiguous() + bias
+    size = av.norm(dim=1)[:, None] * bv.norm(dim=1)[None, :] + bias.abs()
+    bar = size * (2.0 ** -22 * max(1.0, k / 16)) + (ref.abs() * 2.0 ** -8 if t == "bf16" else 0)
+    assert bool(((c.float() - ref).abs() <= bar).all())
+    again = torch.full_like(c, float("nan"))
+    D.dtst_product(*a, *b, again, bias=bias)
+    assert torch.equal(c, again)
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 70, 300), (70, 90, 700), (300, 520, 256)])
 def test_strides(m, n, k):
     torch, D = lib()
