@@ -9,7 +9,8 @@ and the result is expanded back onto the shard.
 Orchestration only: every step is a call of the DTST library
 (``dtst_rms_norm``, ``dtst_quantise``, ``dtst_product``, ``dtst_recurrence``,
 their backward calls, and the plan's transforms), apart from the last residual's
-addition and the sum of a bias' gradient.  Weights are kept in 8 bits with their
+addition, the sum of a bias' gradient, and in training with lengths the clearing
+of what lies past them.  Weights are kept in 8 bits with their
 transposes, as the backward needs them; the masters stay with the caller.
 """
 
@@ -21,6 +22,11 @@ from . import (DtstError, Plan, dtst_desc_validate, dtst_product, dtst_quantise,
                dtst_rms_norm_adj, empty_codes, recurrence_states_shape)
 
 _UNSUPPORTED = 2  # DTST_ERR_UNSUPPORTED
+
+
+def _past(lengths, steps):
+    """(B T, 1), true where a step lies past its sequence's length."""
+    return (torch.arange(steps, device=lengths.device) >= lengths[:, None]).view(-1, 1)
 
 
 class _Weights:
@@ -66,7 +72,8 @@ class LatentBlock:
         for the first); res: (B, T, W) float32 or None, updated in place unless
         `keep` is given.  Returns the block's branch (bfloat16) and the residual.
         state: (B, F) float32, updated in place; one step with a state is a
-        serving step.  keep: a dict that receives what backward needs."""
+        serving step.  keep: a dict that receives what backward needs.
+        Past a sequence's length (B,) int32 x and res may hold anything."""
         B, T, W = x.shape
         F, R, dev = self.features, B * T, x.device
         bf = torch.bfloat16
@@ -84,9 +91,18 @@ class LatentBlock:
             plain = torch.empty((R, W), dtype=x.dtype, device=dev)
             u = u if res is None else torch.empty_like(u)  # (the caller's stays: backward needs this one)
             dtst_rms_norm(x2, self.norm, plain, res=res2, sum_out=u, rstd=rstd, eps=self.eps)
+            kept_u, past = u, None if lengths is None else _past(lengths, T)
+            if past is not None:
+                # The weights' gradients sum over the rows, and the transposed
+                # form scales 128 of them at once: what lies past a length would
+                # reach the others there, and zero times no number is none.
+                plain.masked_fill_(past, 0)
+                rstd.masked_fill_(past[:, 0], 0)
+                kept_u = u.masked_fill(past, 0)
             dtst_quantise(plain, *n, qt=nt[0], scale_t=nt[1])
             states = torch.empty(recurrence_states_shape(B, T, F), dtype=torch.float32, device=dev)
-            keep.update(shape=(B, T), u=u, rstd=rstd, nt=nt, p=p, states=states, lengths=lengths, x_dtype=x.dtype)
+            keep.update(shape=(B, T), u=kept_u, rstd=rstd, nt=nt, p=p, states=states, lengths=lengths, past=past,
+                        x_dtype=x.dtype)
         dtst_product(*n, *self.w_in.rows, p.view(R, 3 * F), bias=self.b_in, short_sums=True)
         dtst_recurrence(z, v, y, o=o, h0=state, h_out=state, lengths=lengths, states=states)
         yq = empty_codes(R, F, dev)
@@ -114,7 +130,10 @@ class LatentBlock:
             dtst_quantise(t, *q, qt=qt[0], scale_t=qt[1])
             return q, qt
 
-        q, qt = both(g_out.reshape(R, W))
+        go = g_out.reshape(R, W)
+        if kept["past"] is not None:
+            go = go.masked_fill(kept["past"], 0)  # (as in forward)
+        q, qt = both(go)
         g_y, g_w_out = torch.empty((B, T, F), dtype=bf, device=dev), torch.empty((W, F), dtype=f32, device=dev)
         dtst_product(*q, *self.w_out.cols, g_y.view(R, F), short_sums=True)
         dtst_product(*qt, *kept["yt"], g_w_out)

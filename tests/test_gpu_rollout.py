@@ -225,3 +225,28 @@ def test_blocks_refuse_other_shapes():
     b = LatentBlock(one(64), one(96, 64), one(96), one(64, 32))
     with pytest.raises(ValueError):
         Rollout(dict(n_global=(8, 8, 8), n_local=(8, 8, 8), offset=(0, 0, 0), kmax=(1, 1, 1)), 1, 1, [b])
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), 1e30])
+def test_what_lies_past_a_length_reaches_no_gradient(junk):
+    """Zeros there or anything else: the same gradients, bit for bit."""
+    torch = torch_gpu()
+    B, T, W, F, lengths = 3, 130, 200, 96, [130, 0, 71]
+    k = Block(torch, W, F, 5)
+    rng = np.random.RandomState(6)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    past = (torch.arange(T, device="cuda") >= n[:, None])[..., None]
+    x, res, g_out, g_res = (rounded(torch, rng.randn(B, T, W), t)[0] for t in ("bf16", "f32", "bf16", "f32"))
+    h0, g_h = (rounded(torch, rng.randn(B, F), "f32")[0] for _ in range(2))
+    say(f"[past lengths] {junk}")
+    runs = []
+    for fill in (0.0, junk):
+        state, keep = h0.clone(), {}
+        out, u = k.block.forward(x.masked_fill(past, fill), res.masked_fill(past, fill), state, n, keep)
+        g = k.block.backward(keep, g_out.masked_fill(past, fill), g_res.masked_fill(past, fill), g_h)
+        g.update(out=out, last=state, u=u.masked_fill(past, 0), x=g["x"].masked_fill(past, 0),
+                 res=g["res"].masked_fill(past, 0))
+        runs.append(g)
+    for name, ref in runs[0].items():
+        assert torch.isfinite(ref).all(), name
+        assert torch.equal(runs[1][name], ref), name
