@@ -400,6 +400,8 @@ def _scratch(ws, need, device, stream):
         ws = torch.empty(need, dtype=torch.uint8, device=device)
         if stream is not None and int(stream) != torch_stream():
             ws.record_stream(torch.cuda.ExternalStream(int(stream)))
+    elif ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws: need a contiguous tensor on {device}, got strides {ws.stride()} on {ws.device}")
     return ws.data_ptr(), ws.nbytes, ws
 
 

@@ -88,3 +88,26 @@ def test_recurrence():
         D.dtst_recurrence_adj(z, v, y, st, new(torch, 2, 5, 8), new(torch, 2, 5, 8), o=v)
     with pytest.raises(ValueError):
         D.dtst_recurrence_adj(z, v, y, st[:, :, :7], new(torch, 2, 5, 8), new(torch, 2, 5, 8))
+
+
+def test_workspaces():
+    """One on the host, with gaps, too small or at an odd address is refused."""
+    torch, D = lib()
+    f32, u8 = torch.float32, torch.uint8
+    z, v, y = new(torch, 1, 300, 8), new(torch, 1, 300, 8), new(torch, 1, 300, 8)
+    need = D.dtst_recurrence_workspace(1, 300, 8, z.dtype)
+    good = torch.empty(need, dtype=u8, device="cuda")
+    D.dtst_recurrence(z, v, y, ws=good)
+    g, w, g_w = new(torch, 5, 64), new(torch, 64, dtype=f32), new(torch, 64, dtype=f32)
+    rstd = new(torch, 5, dtype=f32)
+    need_n = D.dtst_rms_norm_adj_workspace(5, 64)
+    D.dtst_rms_norm_adj(g, new(torch, 5, 64), w, rstd, new(torch, 5, 64), g_w, ws=torch.empty(need_n, dtype=u8, device="cuda"))
+    for n, call in ((need, lambda ws: D.dtst_recurrence(z, v, y, ws=ws)),
+                    (need_n, lambda ws: D.dtst_rms_norm_adj(g, new(torch, 5, 64), w, rstd, new(torch, 5, 64), g_w, ws=ws))):
+        wide = torch.empty(2 * n + 16, dtype=u8, device="cuda")
+        for bad in (torch.empty(n, dtype=u8), wide[:2 * n:2]):
+            with pytest.raises(ValueError):
+                call(bad)
+        for bad in (wide[:n - 1], wide[1:n + 1]):
+            with pytest.raises(D.DtstError):
+                call(bad)
