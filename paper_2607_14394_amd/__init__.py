@@ -423,6 +423,8 @@ def dtst_rms_norm(x, weight, y, res=None, sum_out=None, scale=None, rstd=None, e
     _vector(weight, cols, "weight", dev)
     if rstd is not None:
         _vector(rstd, rows, "rstd", dev)
+    if not rows:  # (the library knows y's scales by their address, which an empty tensor has not)
+        return
     status = lib.dtst_rms_norm(
         NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt], _TYPES[y.dtype], eps),
         x.data_ptr(), None if res is None else res.data_ptr(), weight.data_ptr(),
@@ -476,6 +478,8 @@ def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
     ld_x = _rows(x, (rows, cols), "x", _FLOATS, dev)
     ld_q, ld_s = (0, 0) if q is None else _codes(q, scale, rows, cols, "q", dev)
     ld_qt, ld_st = (0, 0) if qt is None else _codes(qt, scale_t, cols, rows, "qt", dev)
+    if not rows:  # (as in dtst_rms_norm)
+        return
     status = lib.dtst_quantise(QUANTISE_DESC.pack(rows, cols, ld_x, ld_q, ld_s, ld_qt, ld_st, _TYPES[x.dtype]),
                                x.data_ptr(), None if q is None else q.data_ptr(),
                                None if scale is None else scale.data_ptr(), None if qt is None else qt.data_ptr(),

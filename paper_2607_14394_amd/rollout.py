@@ -26,7 +26,7 @@ _UNSUPPORTED = 2  # DTST_ERR_UNSUPPORTED
 
 def _past(lengths, steps):
     """(B T, 1), true where a step lies past its sequence's length."""
-    return (torch.arange(steps, device=lengths.device) >= lengths[:, None]).view(-1, 1)
+    return (torch.arange(steps, device=lengths.device) >= lengths[:, None]).view(len(lengths) * steps, 1)
 
 
 class _Weights:
@@ -130,13 +130,19 @@ class LatentBlock:
             dtst_quantise(t, *q, qt=qt[0], scale_t=qt[1])
             return q, qt
 
+        def weights(qt, xt, g):  # (a product has to have something to sum)
+            if R:
+                dtst_product(*qt, *xt, g)
+            else:
+                g.zero_()
+
         go = g_out.reshape(R, W)
         if kept["past"] is not None:
             go = go.masked_fill(kept["past"], 0)  # (as in forward)
         q, qt = both(go)
         g_y, g_w_out = torch.empty((B, T, F), dtype=bf, device=dev), torch.empty((W, F), dtype=f32, device=dev)
         dtst_product(*q, *self.w_out.cols, g_y.view(R, F), short_sums=True)
-        dtst_product(*qt, *kept["yt"], g_w_out)
+        weights(qt, kept["yt"], g_w_out)
         g_p = torch.empty((B, T, 3 * F), dtype=bf, device=dev)
         g_h = torch.empty((B, F), dtype=f32, device=dev)
         z, v, o = self._split(kept["p"])
@@ -147,7 +153,7 @@ class LatentBlock:
         g_n = torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
         g_w_in = torch.empty((3 * F, W), dtype=f32, device=dev)
         dtst_product(*q, *self.w_in.cols, g_n, short_sums=g_n.dtype != f32)
-        dtst_product(*qt, *kept["nt"], g_w_in)
+        weights(qt, kept["nt"], g_w_in)
         g_u, g_norm = torch.empty((R, W), dtype=f32, device=dev), torch.empty_like(self.norm)
         g_x = g_u if kept["x_dtype"] == f32 else torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
         dtst_rms_norm_adj(g_n, kept["u"], self.norm, kept["rstd"], g_u, g_norm,

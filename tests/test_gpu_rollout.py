@@ -250,3 +250,24 @@ def test_what_lies_past_a_length_reaches_no_gradient(junk):
     for name, ref in runs[0].items():
         assert torch.isfinite(ref).all(), name
         assert torch.equal(runs[1][name], ref), name
+
+
+@pytest.mark.parametrize("B,T", [(2, 0), (0, 3)])
+@pytest.mark.parametrize("with_lengths", [False, True])
+def test_a_block_over_no_steps(B, T, with_lengths):
+    """The state stands still, its gradient passes, the others are zero."""
+    torch = torch_gpu()
+    W, F = 200, 96
+    k = Block(torch, W, F, 7)
+    say(f"[no steps] {B} x {T}, lengths {with_lengths}")
+    n = torch.zeros(B, dtype=torch.int32, device="cuda") if with_lengths else None
+    x, res = torch.zeros(B, T, W, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, T, W, device="cuda")
+    h0, g_h = torch.randn(B, F, device="cuda"), torch.randn(B, F, device="cuda")
+    state, keep = h0.clone(), {}
+    out, u = k.block.forward(x, res, state, n, keep)
+    assert out.shape == u.shape == (B, T, W) and torch.equal(state, h0)
+    assert k.block.forward(x, res, state, n)[0].shape == (B, T, W) and torch.equal(state, h0)  # (the serving form)
+    g = k.block.backward(keep, torch.zeros_like(out), torch.zeros_like(u), g_h)
+    assert torch.equal(g["state"], g_h) and g["x"].shape == g["res"].shape == (B, T, W)
+    for name, shape in (("norm", (W,)), ("w_in", (3 * F, W)), ("b_in", (3 * F,)), ("w_out", (W, F))):
+        assert g[name].shape == shape and not g[name].any(), name
