@@ -397,9 +397,13 @@ def _scratch(ws, need, device, stream):
     if ws is None:
         if not need:
             return None, 0, None
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None and int(stream) != torch_stream():
-            ws.record_stream(torch.cuda.ExternalStream(int(stream)))
+        if stream is None or int(stream) == torch_stream():
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            # From the memory of the stream that the call runs on: a block that the
+            # current stream has freed may still be in use by what is queued there.
+            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device)):
+                ws = torch.empty(need, dtype=torch.uint8, device=device)
     elif ws.device != device or not ws.is_contiguous():
         raise ValueError(f"ws: need a contiguous tensor on {device}, got strides {ws.stride()} on {ws.device}")
     return ws.data_ptr(), ws.nbytes, ws
