@@ -303,12 +303,14 @@ int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void
                         void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   float* part = static_cast<float*>(workspace);
-  const int e = by_types(d.x_type, d.res_type, [&](auto tx, auto tr) {
-    return launch_norm_adj_cols<decltype(tx), decltype(tr)>(d, g_y, u, weight, rstd, g_sum, g_u, g_x, part, s);
-  });
-  if (e != hipSuccess) return e;
+  if (d.rows > 0) {  // (the kernel reads the weight before its rows; of none there is nothing to add up)
+    const int e = by_types(d.x_type, d.res_type, [&](auto tx, auto tr) {
+      return launch_norm_adj_cols<decltype(tx), decltype(tr)>(d, g_y, u, weight, rstd, g_sum, g_u, g_x, part, s);
+    });
+    if (e != hipSuccess) return e;
+  }
   hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((d.cols + 31) / 32)), dim3(1024), 0, s, part,
-                     int(norm_adj_parts(d.rows, d.cols)), d.cols, d.accumulate, g_weight);
+                     d.rows > 0 ? int(norm_adj_parts(d.rows, d.cols)) : 0, d.cols, d.accumulate, g_weight);
   return hipGetLastError();
 }
 
