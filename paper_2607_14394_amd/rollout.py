@@ -165,12 +165,20 @@ class LatentBlock:
 class Rollout:
     """Fields of `channels` channels on one shard, batch sequences at a time.
     grid: a descriptor's n_global, n_local, offset and kmax in x, y, z (3 each);
-    blocks: LatentBlocks of width 2 channels M, M the retained modes."""
+    blocks: LatentBlocks of width 2 channels M, M the retained modes.  A shard's
+    coefficients are its part of the domain's: where n_local is not n_global,
+    reduce(tokens) has to sum them in place over the shards, as
+    torch.distributed.all_reduce does; every shard then runs the same blocks on
+    the same tokens, and decodes its own part of the field."""
 
     GROUP = 256  # frames of one plan at most; halved until the library takes such a plan
 
-    def __init__(self, grid, channels, batch, blocks, device="cuda"):
+    def __init__(self, grid, channels, batch, blocks, device="cuda", reduce=None):
+        if reduce is None and tuple(grid["n_local"]) != tuple(grid["n_global"]):
+            raise ValueError(f"a shard {tuple(grid['n_local'])} of {tuple(grid['n_global'])} holds its part of the "
+                             "coefficients: need reduce, which sums them over the shards")
         self.grid, self.channels, self.batch, self.blocks, self.device = grid, channels, batch, list(blocks), device
+        self.reduce = reduce
         self.plans = {}
         self.group = self.GROUP
         while self.group > 1 and not self._supported(self.group):
@@ -215,7 +223,10 @@ class Rollout:
         for plan, s in self._groups(B * T):
             plan.forward(flat[s].view(plan.spatial_shape(self.channels)),
                          xhat[s].view(plan.spectral_shape(self.channels)))
-        return torch.view_as_real(xhat).view(B, T, self.width)
+        tokens = torch.view_as_real(xhat).view(B, T, self.width)
+        if self.reduce is not None:
+            self.reduce(tokens)
+        return tokens
 
     def decode(self, tokens):
         B, T = tokens.shape[:2]

@@ -32,3 +32,10 @@ def test_a_workspace_comes_from_the_memory_of_the_calls_stream(monkeypatch, stre
     monkeypatch.setattr(torch, "empty", record)
     p, n, ws = D._scratch(None, 100, torch.device("cpu"), stream)
     assert taken == [pool] and n == 100 and p == ws.data_ptr() and current == [5]
+
+
+def test_a_rollout_on_a_shard_needs_the_sum_over_the_shards():
+    from paper_2607_14394_amd.rollout import Rollout
+    for local, offset in (((4, 8, 8), (4, 0, 0)), ((8, 8, 7), (0, 0, 0))):
+        with pytest.raises(ValueError, match="reduce"):
+            Rollout(dict(n_global=(8, 8, 8), n_local=local, offset=offset, kmax=(1, 1, 1)), 1, 1, [], device="cpu")
