@@ -103,7 +103,7 @@ class LatentBlock:
             states = torch.empty(recurrence_states_shape(B, T, F), dtype=torch.float32, device=dev)
             keep.update(shape=(B, T), u=kept_u, rstd=rstd, nt=nt, p=p, states=states, lengths=lengths, past=past,
                         x_dtype=x.dtype)
-        dtst_product(*n, *self.w_in.rows, p.view(R, 3 * F), bias=self.b_in, short_sums=True)
+        dtst_product(*n, *self.w_in.rows, p.view(R, 3 * F), bias=self.b_in)
         dtst_recurrence(z, v, y, o=o, h0=state, h_out=state, lengths=lengths, states=states)
         yq = empty_codes(R, F, dev)
         if keep is None:
@@ -112,7 +112,7 @@ class LatentBlock:
             keep["yt"] = empty_codes(F, R, dev)
             dtst_quantise(y.view(R, F), *yq, qt=keep["yt"][0], scale_t=keep["yt"][1])
         out = torch.empty((B, T, W), dtype=bf, device=dev)
-        dtst_product(*yq, *self.w_out.rows, out.view(R, W), short_sums=True)
+        dtst_product(*yq, *self.w_out.rows, out.view(R, W))
         return out, u.view(B, T, W)
 
     def backward(self, kept, g_out, g_res, g_state=None):
@@ -141,7 +141,7 @@ class LatentBlock:
             go = go.masked_fill(kept["past"], 0)  # (as in forward)
         q, qt = both(go)
         g_y, g_w_out = torch.empty((B, T, F), dtype=bf, device=dev), torch.empty((W, F), dtype=f32, device=dev)
-        dtst_product(*q, *self.w_out.cols, g_y.view(R, F), short_sums=True)
+        dtst_product(*q, *self.w_out.cols, g_y.view(R, F))
         weights(qt, kept["yt"], g_w_out)
         g_p = torch.empty((B, T, 3 * F), dtype=bf, device=dev)
         g_h = torch.empty((B, F), dtype=f32, device=dev)
@@ -152,7 +152,7 @@ class LatentBlock:
         q, qt = both(g_p.view(R, 3 * F))
         g_n = torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
         g_w_in = torch.empty((3 * F, W), dtype=f32, device=dev)
-        dtst_product(*q, *self.w_in.cols, g_n, short_sums=g_n.dtype != f32)
+        dtst_product(*q, *self.w_in.cols, g_n)
         weights(qt, kept["nt"], g_w_in)
         g_u, g_norm = torch.empty((R, W), dtype=f32, device=dev), torch.empty_like(self.norm)
         g_x = g_u if kept["x_dtype"] == f32 else torch.empty((R, W), dtype=kept["x_dtype"], device=dev)
