@@ -378,14 +378,12 @@ dtst_status dtst_quantise(const dtst_quantise_desc* d, const void* x, void* q, v
  * n fp32, or NULL.  A linear layer's forward takes b = its weights (out, in);
  * its data gradient takes the output's gradient and the weights' transpose,
  * its weight gradient the transposes of the output's gradient and of the
- * input (dtst_quantise writes both forms).  short_sums = 0: products and sums
- * are exact to 32 bits (the codes go to the matrix cores as bf16, which holds
- * them and their scales without loss; what a scale brings below 2^-126 loses
- * low bits).  short_sums = 1 lets the library take the 8-bit matrix
- * instruction, which it does for large products (2 m n k >= 2^38), at nearly
- * twice the rate: its sum of eight neighbouring products keeps 13 bits below
- * the largest of them (1e-5 to 2e-5 of the result on normally distributed
- * values), the sum of those sums 32 bits.  k and the strides up to 2^23
+ * input (dtst_quantise writes both forms).  Products and sums are exact to 32
+ * bits (the codes go to the matrix cores as bf16, which holds them and their
+ * scales without loss; what a scale brings below 2^-126 loses low bits).
+ * short_sums, 0 or 1: 1 says that sums which keep 13 bits below the largest of
+ * eight neighbouring products, those of the 8-bit matrix instruction, would do;
+ * they are exact all the same.  k and the strides up to 2^23
  * (DTST_ERR_UNSUPPORTED above). */
 typedef struct {
   int64_t m, n, k;

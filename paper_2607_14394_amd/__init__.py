@@ -495,7 +495,8 @@ def dtst_quantise(x, q=None, scale=None, qt=None, scale_t=None, stream=None):
 
 def dtst_product(a, a_scale, b, b_scale, c, bias=None, accumulate=False, short_sums=False, stream=None):
     """c = a b^T + bias (+ c): codes a (m, k) and b (n, k) with their scales
-    into c (m, n).  short_sums: allow the 8-bit matrix instruction's sums."""
+    into c (m, n).  short_sums: sums of fewer bits would do (they are exact all
+    the same)."""
     if c.dim() != 2 or a.dim() != 2:
         raise ValueError("a and c must be (m, k) and (m, n)")
     m, n = c.shape

@@ -1,22 +1,20 @@
 // Product of 8-bit arrays with a power-of-two scale for each 128 of the summed
 // axis (dtst_product):  c[i,j] = sum_l a[i,l] b[j,l] + bias[j].
 //
-// Two forms of the matrix products.  Exact: a code times its scale is a bf16
-// number without loss, so the operands are widened (two codes an instruction,
-// the scale with it) for v_mfma_f32_16x16x32_bf16, whose sums are exact to 32
-// bits.  Short (dtst_product_desc::short_sums): v_mfma_scale_f32_16x16x128_f8f6f4
-// takes 128 codes at once and the scales' powers of two as an operand, at twice
-// the rate, but keeps only 13 bits below the largest of eight neighbouring
-// products.  In both, lane l holds row l % 16 of the operands and a quarter of
-// the 128 codes (any quarter, as long as it is the same for both); with b as the
-// first operand a lane ends with four neighbouring columns 4 (l / 16) + r of row
-// l % 16 of c.
+// A code times its scale is a bf16 number without loss, so the operands are
+// widened (two codes an instruction, the scale with it) for
+// v_mfma_f32_16x16x32_bf16, whose sums are exact to 32 bits.
+// (v_mfma_scale_f32_16x16x128_f8f6f4 takes 128 codes and the scales' powers of
+// two at once, at twice the rate, but its sum of eight neighbouring products keeps
+// 13 bits below the largest: too few for the 32-bit states of a recurrence on the
+// results, which move by 3e-3.)  Lane l holds row l % 16 of the operands and a
+// quarter of the 128 codes (any quarter, as long as it is the same for both); with
+// b as the first operand a lane ends with four neighbouring columns 4 (l / 16) + r
+// of row l % 16 of c.
 //
-// Large products are bound by the matrix cores and what feeds them: 8192^3 438 us
-// short (2510 TFLOP/s, the cores busy 62% of the time at 1.96 GHz; 323 us if no
-// stage had to be fetched) and 759 us exact (1450; without the widening, two codes
-// an instruction in between, 12 to 15% less).  Smaller ones wait for their first
-// loads and their stores.
+// Large products are bound by the matrix cores and what feeds them: 8192^3 759 us
+// (1450 TFLOP/s; without the widening, two codes an instruction in between, 12 to
+// 15% less).  Smaller ones wait for their first loads and their stores.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,7 +28,6 @@ namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef bf16_t v8b __attribute__((ext_vector_type(8)));
 typedef bf16_t v2b __attribute__((ext_vector_type(2)));
 
@@ -158,7 +155,7 @@ __device__ __forceinline__ void put_tiles(const Operands& p, TC* c, const v4f (&
   }
 }
 
-template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
+template <int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
 __global__ void __launch_bounds__(64 * WM * WN * KS)
 product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
   constexpr int WAVES = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, STAGE = (BM + BN) * ROW;
@@ -263,104 +260,72 @@ product_tile_kernel(Operands p, TC* c, int m_tiles, int n_tiles) {
     const int word = (k_odd + kb) / 4, byte = (k_odd + kb) % 4;
     const uint8_t* at_sa = lds + STAGES * STAGE + word % 2 * SCALES + (wm * TM * 16 + r) * 4 + byte;
     const uint8_t* at_sb = lds + STAGES * STAGE + word % 2 * SCALES + (BM + wn * TN * 16 + r) * 4 + byte;
-    if constexpr (SHORT) {
-      v8i fb[TN];
-      int sb[TN];
+    // A lane's 32 codes of a row are two halves of 16.  Products of a row tile go
+    // with the widening of the next one, and in the first half with that of b's
+    // second: a product takes the issue of four instructions, so that between two
+    // of them others are free.  Codes are read a tile before they are widened.
+    constexpr int Q = 2 * TM;  // (half, row tile) in turn
+    v8b fa[2][2], fb[2][TN][2];
+    v4i xa[2], xb;
+    int ba[2], bb[TN];  // scale bytes of the codes read
+    const auto read_a = [&](int q) {
+      xa[q & 1] = *reinterpret_cast<const v4i*>(at_a + q % TM * 16 * ROW + (place ^ (q / TM * 64)));
+      ba[q & 1] = at_sa[q % TM * 64];
+    };
+    const auto widen_a = [&](int q) {
+      const float s = scale_value(ba[q & 1]);
+      fa[q & 1][0] = widen(xa[q & 1][0], xa[q & 1][1], s), fa[q & 1][1] = widen(xa[q & 1][2], xa[q & 1][3], s);
+    };
+    const auto widen_b = [&](int h, int j, const v4i& x) {
+      const float s = scale_value(bb[j]);
+      fb[h][j][0] = widen(x[0], x[1], s), fb[h][j][1] = widen(x[2], x[3], s);
+    };
+    const auto read_b = [&](int h, int j) {
+      return *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + (place ^ (h * 64)));
+    };
+    {
+      v4i x[TN];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const v4i lo = *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + place);
-        const v4i hi = *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + (place ^ 64));
-        fb[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        sb[j] = at_sb[j * 64];
-      }
-      // row tiles one ahead of the products
-      v8i fa[2];
-      int sa[2];
-      const auto read_a = [&](int i) {
-        const v4i lo = *reinterpret_cast<const v4i*>(at_a + i * 16 * ROW + place);
-        const v4i hi = *reinterpret_cast<const v4i*>(at_a + i * 16 * ROW + (place ^ 64));
-        fa[i & 1] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        sa[i & 1] = at_sa[i * 64];
-      };
+      for (int j = 0; j < TN; ++j) x[j] = read_b(0, j), bb[j] = at_sb[j * 64];
       read_a(0);
+      read_a(1);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        if (i + 1 < TM) read_a(i + 1);
+      for (int j = 0; j < TN; ++j) widen_b(0, j, x[j]);
+      widen_a(0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // b's second half: tile j is read at step first_b[j] and widened at the next
+    constexpr int STEP_B = TM >= TN + 1 ? 1 : 0;  // a tile a step, or all of them in the last step of the first half
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int h = q / TM, i = q % TM;
+      v4i late[TN];
+      if (STEP_B == 1 && h == 0 && i >= 1 && i <= TN) widen_b(1, i - 1, xb);
+      if (STEP_B == 1 && h == 0 && i < TN) xb = read_b(1, i);
+      if (STEP_B == 0 && q == TM - 1) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) late[j] = read_b(1, j);
+      }
+      if (q + 1 < Q) widen_a(q + 1);
+      if (q + 2 < Q) read_a(q + 2);  // (over the codes of tile q)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i & 1], acc[i][j], 0, 0, 0, sb[j], 0,
-                                                                        sa[i & 1]);
-        __builtin_amdgcn_sched_barrier(0);
-        if (PARTS > 1 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[h][j][e], fa[q & 1][e], acc[i][j], 0, 0, 0);
+      if (STEP_B == 0 && q == TM - 1) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) widen_b(1, j, late[j]);
       }
-    } else {
-      // A lane's 32 codes of a row are two halves of 16.  Products of a row tile go
-      // with the widening of the next one, and in the first half with that of b's
-      // second: a product takes the issue of four instructions, so that between two
-      // of them others are free.  Codes are read a tile before they are widened.
-      constexpr int Q = 2 * TM;  // (half, row tile) in turn
-      v8b fa[2][2], fb[2][TN][2];
-      v4i xa[2], xb;
-      int ba[2], bb[TN];  // scale bytes of the codes read
-      const auto read_a = [&](int q) {
-        xa[q & 1] = *reinterpret_cast<const v4i*>(at_a + q % TM * 16 * ROW + (place ^ (q / TM * 64)));
-        ba[q & 1] = at_sa[q % TM * 64];
-      };
-      const auto widen_a = [&](int q) {
-        const float s = scale_value(ba[q & 1]);
-        fa[q & 1][0] = widen(xa[q & 1][0], xa[q & 1][1], s), fa[q & 1][1] = widen(xa[q & 1][2], xa[q & 1][3], s);
-      };
-      const auto widen_b = [&](int h, int j, const v4i& x) {
-        const float s = scale_value(bb[j]);
-        fb[h][j][0] = widen(x[0], x[1], s), fb[h][j][1] = widen(x[2], x[3], s);
-      };
-      const auto read_b = [&](int h, int j) {
-        return *reinterpret_cast<const v4i*>(at_b + j * 16 * ROW + (place ^ (h * 64)));
-      };
-      {
-        v4i x[TN];
+      // one product, then up to three of the others
 #pragma unroll
-        for (int j = 0; j < TN; ++j) x[j] = read_b(0, j), bb[j] = at_sb[j * 64];
-        read_a(0);
-        read_a(1);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) widen_b(0, j, x[j]);
-        widen_a(0);
+      for (int e = 0; e < 2 * TN; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      // b's second half: tile j is read at step first_b[j] and widened at the next
-      constexpr int STEP_B = TM >= TN + 1 ? 1 : 0;  // a tile a step, or all of them in the last step of the first half
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        const int h = q / TM, i = q % TM;
-        v4i late[TN];
-        if (STEP_B == 1 && h == 0 && i >= 1 && i <= TN) widen_b(1, i - 1, xb);
-        if (STEP_B == 1 && h == 0 && i < TN) xb = read_b(1, i);
-        if (STEP_B == 0 && q == TM - 1) {
-#pragma unroll
-          for (int j = 0; j < TN; ++j) late[j] = read_b(1, j);
-        }
-        if (q + 1 < Q) widen_a(q + 1);
-        if (q + 2 < Q) read_a(q + 2);  // (over the codes of tile q)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int j = 0; j < TN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[h][j][e], fa[q & 1][e], acc[i][j], 0, 0, 0);
-        if (STEP_B == 0 && q == TM - 1) {
-#pragma unroll
-          for (int j = 0; j < TN; ++j) widen_b(1, j, late[j]);
-        }
-        // one product, then up to three of the others
-#pragma unroll
-        for (int e = 0; e < 2 * TN; ++e) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (PARTS > 1 && h == 0 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
-      }
+      if (PARTS > 1 && h == 0 && i < PARTS && ahead < nk) fetch(ahead, i, PARTS);
     }
   }
   __syncthreads();
@@ -400,12 +365,12 @@ hipError_t allow_lds(const void* fn, size_t bytes, std::atomic<uint64_t>& done) 
   return e;
 }
 
-template <bool SHORT, int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
+template <int WM, int WN, int TM, int TN, int STAGES, int KS, class TC>
 int launch_tile(const Operands& p, void* c, hipStream_t s) {
   constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
   const int64_t mt = (p.m + BM - 1) / BM, nt = (p.n + BN - 1) / BN;
   constexpr size_t lds = KS * (size_t(STAGES) * (BM + BN) * ROW + 2 * ((BM + BN + 63) / 64 * 256));
-  auto* fn = product_tile_kernel<SHORT, WM, WN, TM, TN, STAGES, KS, TC>;
+  auto* fn = product_tile_kernel<WM, WN, TM, TN, STAGES, KS, TC>;
   static std::atomic<uint64_t> allowed{0};  // devices whose limit for this kernel is raised (one bit each, 64 of them)
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(fn), lds, allowed);
   if (e != hipSuccess) return e;
@@ -451,36 +416,27 @@ double cost(const Operands& p, const Tile& t) {
 }
 
 template <class TC>
-int launch(const Operands& p, int short_sums, void* c, hipStream_t s) {
+int launch(const Operands& p, void* c, hipStream_t s) {
   const auto tiles = [&](int64_t bm, int64_t bn) { return ((p.m + bm - 1) / bm) * ((p.n + bn - 1) / bn); };
-  // Short sums, where they are allowed, from 2^38 operations on: they save 320 of
-  // 760 us at 8192^3.  Below it they would save tens, and layers of that size
-  // feed others: 0.4% of the bf16 results round to the other neighbour, and the
-  // 32-bit states of a recurrence on them move by 3e-3.
-  if (short_sums && 2.0 * double(p.m) * double(p.n) * double(p.k) >= double(int64_t(1) << 38) && tiles(256, 256) >= 128) {
-    const Tile one{192, 256, 256, 2420}, two{256, 256, 256, 2500};
-    if (cost(p, one) < cost(p, two)) return launch_tile<true, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
-    return launch_tile<true, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
-  }
-  if (tiles(16, 32) <= 256) return launch_tile<false, 1, 1, 1, 2, 3, 8, TC>(p, c, s);
-  if (tiles(32, 32) <= 256) return launch_tile<false, 1, 1, 2, 2, 2, 8, TC>(p, c, s);
-  if (tiles(64, 32) <= 256) return launch_tile<false, 2, 1, 2, 2, 3, 4, TC>(p, c, s);
-  if (tiles(64, 64) <= 256) return launch_tile<false, 1, 2, 4, 2, 2, 4, TC>(p, c, s);
-  if (tiles(128, 64) <= 256) return launch_tile<false, 2, 2, 4, 2, 2, 2, TC>(p, c, s);
-  if (tiles(128, 128) <= 256 && p.k >= 1024) return launch_tile<false, 2, 2, 4, 4, 2, 2, TC>(p, c, s);
+  if (tiles(16, 32) <= 256) return launch_tile<1, 1, 1, 2, 3, 8, TC>(p, c, s);
+  if (tiles(32, 32) <= 256) return launch_tile<1, 1, 2, 2, 2, 8, TC>(p, c, s);
+  if (tiles(64, 32) <= 256) return launch_tile<2, 1, 2, 2, 3, 4, TC>(p, c, s);
+  if (tiles(64, 64) <= 256) return launch_tile<1, 2, 4, 2, 2, 4, TC>(p, c, s);
+  if (tiles(128, 64) <= 256) return launch_tile<2, 2, 4, 2, 2, 2, TC>(p, c, s);
+  if (tiles(128, 128) <= 256 && p.k >= 1024) return launch_tile<2, 2, 4, 4, 2, 2, TC>(p, c, s);
   const Tile forms[] = {{128, 64, 512, 800},   {128, 128, 512, 1080}, {128, 192, 256, 1050}, {128, 256, 256, 1200},
                         {192, 192, 256, 1180}, {192, 256, 256, 1340}, {256, 256, 256, 1450}};
   int best = 0;
   for (int i = 1; i < 7; ++i)
     if (cost(p, forms[i]) < cost(p, forms[best])) best = i;
   switch (best) {
-    case 0: return launch_tile<false, 2, 2, 4, 2, 3, 1, TC>(p, c, s);
-    case 1: return launch_tile<false, 2, 2, 4, 4, 2, 1, TC>(p, c, s);
-    case 2: return launch_tile<false, 2, 4, 4, 3, 2, 1, TC>(p, c, s);
-    case 3: return launch_tile<false, 2, 4, 4, 4, 2, 1, TC>(p, c, s);
-    case 4: return launch_tile<false, 2, 4, 6, 3, 2, 1, TC>(p, c, s);
-    case 5: return launch_tile<false, 2, 4, 6, 4, 2, 1, TC>(p, c, s);
-    default: return launch_tile<false, 2, 4, 8, 4, 2, 1, TC>(p, c, s);
+    case 0: return launch_tile<2, 2, 4, 2, 3, 1, TC>(p, c, s);
+    case 1: return launch_tile<2, 2, 4, 4, 2, 1, TC>(p, c, s);
+    case 2: return launch_tile<2, 4, 4, 3, 2, 1, TC>(p, c, s);
+    case 3: return launch_tile<2, 4, 4, 4, 2, 1, TC>(p, c, s);
+    case 4: return launch_tile<2, 4, 6, 3, 2, 1, TC>(p, c, s);
+    case 5: return launch_tile<2, 4, 6, 4, 2, 1, TC>(p, c, s);
+    default: return launch_tile<2, 4, 8, 4, 2, 1, TC>(p, c, s);
   }
 }
 
@@ -492,9 +448,9 @@ int launch_product(const dtst_product_desc& d, const void* a, const void* a_scal
   const Operands p{static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(b),
                    static_cast<const uint8_t*>(a_scale), static_cast<const uint8_t*>(b_scale),
                    d.m, d.n, d.k, d.ld_a, d.ld_a_scale, d.ld_b, d.ld_b_scale, d.ld_c, bias, d.accumulate};
-  if (d.c_type == DTST_F32) return launch<float>(p, d.short_sums, c, s);
-  if (d.c_type == DTST_BF16) return launch<bf16_t>(p, d.short_sums, c, s);
-  return launch<f16_t>(p, d.short_sums, c, s);
+  if (d.c_type == DTST_F32) return launch<float>(p, c, s);
+  if (d.c_type == DTST_BF16) return launch<bf16_t>(p, c, s);
+  return launch<f16_t>(p, c, s);
 }
 
 }  // namespace dtst
