@@ -70,7 +70,8 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 
 // 64 lanes' 16 bytes at base + off (4 bytes at p) to LDS at `to` + 16 (4) times
 // the lane.  (The compiler does not see the load: whoever reads the bytes waits
-// for it.)
+// for it.  m0 is no register that it keeps values in: it writes m0 itself where an
+// instruction of its own takes it.)
 __device__ __forceinline__ void fetch16(const uint8_t* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
@@ -129,6 +130,7 @@ __device__ __forceinline__ void put_tiles(const Operands& p, TC* c, const v4f (&
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(strip + r * PITCH + j * 16 + g * 4) = acc[i][j];
+    wave_sync();  // (the strip's values go from lane to lane)
 #pragma unroll
     for (int e = 0; e < PARTS_C; ++e) {
       const int at = (e * 64 + lane) / (TN * 2), c8 = (e * 64 + lane) % (TN * 2) * 8;
@@ -152,6 +154,7 @@ __device__ __forceinline__ void put_tiles(const Operands& p, TC* c, const v4f (&
         store_n<8>(to, p.n - col, v);
       }
     }
+    wave_sync();
   }
 }
 

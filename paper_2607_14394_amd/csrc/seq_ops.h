@@ -57,6 +57,14 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Orders a wave's LDS accesses before this point with those of its other lanes
+// after it (no instruction: a wave's LDS accesses stay in order).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The value of lane ^ partner within 16 lanes, rotated by R (1, 2, 4 or 8).
 template <int R>
 __device__ __forceinline__ float row_rotate(float v) {
