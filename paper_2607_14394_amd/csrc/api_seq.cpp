@@ -5,10 +5,13 @@
 // why.  No exception leaves an entry point.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
+#include <cstdlib>
 #include <new>
 #include <string>
+#include <utility>
 
 #include "api_common.h"
 #include "seq_internal.h"
@@ -295,33 +298,54 @@ dtst_status check_sequence_sizes(const dtst_recurrence_desc* d) {
   return DTST_OK;
 }
 
-// Whether two sequences share an element, where their strides tell (column
-// ranges of one array do not).
+// The rows of a sequence in bytes: `outer` groups of `inner` rows of `row` bytes,
+// each group's rows before the next group's first (check_sequence).
+struct Rows {
+  int64_t at, outer, outer_ld, inner, inner_ld, row;
+};
+Rows rows_of(const dtst_recurrence_desc* d, const Sequence& s, int size) {
+  Rows r{int64_t(reinterpret_cast<uintptr_t>(s.p)), d->batch, s.st[0] * size, d->steps, s.st[1] * size, d->features * size};
+  if (r.outer <= 1) r.outer_ld = 0;
+  if (r.inner <= 1) r.inner_ld = 0;
+  if (r.outer_ld < r.inner_ld) std::swap(r.outer, r.inner), std::swap(r.outer_ld, r.inner_ld);
+  return r;
+}
+bool is_dense(const Rows& r) {
+  return (r.inner <= 1 || r.inner_ld == r.row) && (r.outer <= 1 || r.outer_ld == r.inner * r.row);
+}
+int64_t extent(const Rows& r) { return (r.outer - 1) * r.outer_ld + (r.inner - 1) * r.inner_ld + r.row; }
+
+// Whether a row of r has a byte of [at, at + n).
+bool share(const Rows& r, int64_t at, int64_t n) {
+  const int64_t most = at + n - 1 - r.at;                           // a row that does starts here at the latest,
+  const int64_t least = std::max<int64_t>(at - r.row + 1 - r.at, 0);  // here at the earliest
+  if (n <= 0 || most < least) return false;
+  const int64_t o = r.outer_ld > 0 ? std::min(least / r.outer_ld, r.outer - 1) : 0, rest = least - o * r.outer_ld;
+  const int64_t i = r.inner_ld > 0 ? (rest + r.inner_ld - 1) / r.inner_ld : rest > 0 ? r.inner : 0;
+  if (i < r.inner) return o * r.outer_ld + i * r.inner_ld <= most;
+  return o + 1 < r.outer && (o + 1) * r.outer_ld <= most;
+}
+
+// Whether two sequences share an element.  Of unlike strides, where neither is
+// without gaps, only a common first element tells.
 bool share(const dtst_recurrence_desc* d, const Sequence& a, const Sequence& b, int size) {
   if (a.p == nullptr || b.p == nullptr || d->steps < 1) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-  const uintptr_t row = uintptr_t(d->features) * size;
-  const auto end = [&](const Sequence& s) {
-    return reinterpret_cast<uintptr_t>(s.p) +
-           uintptr_t((d->batch - 1) * s.st[0] + (d->steps - 1) * s.st[1]) * size + row;
-  };
-  if (pa >= end(b) || pb >= end(a)) return false;
-  const uintptr_t delta = pb >= pa ? pb - pa : pa - pb;
-  const auto apart = [&](int64_t stride) {  // different columns of rows `stride` apart
-    const uintptr_t l = uintptr_t(stride) * size;
-    if (l == 0) return false;
-    const uintptr_t off = delta % l;
-    return off >= row && l - off >= row;
-  };
-  const bool steps_alike = d->steps == 1 || a.st[1] == b.st[1], batch_alike = d->batch == 1 || a.st[0] == b.st[0];
-  if (steps_alike && batch_alike) {
-    // all rows are whole multiples of the smaller stride apart when it divides the larger
-    const int64_t t = d->steps == 1 ? a.st[0] : a.st[1], e = d->batch == 1 ? t : a.st[0];
-    const int64_t lo = t < e ? t : e, hi = t < e ? e : t;
-    if (d->steps == 1 && d->batch == 1) return delta < row;
-    if (lo > 0 && hi % lo == 0) return !apart(lo);
+  const Rows ra = rows_of(d, a, size), rb = rows_of(d, b, size);
+  if (ra.at >= rb.at + extent(rb) || rb.at >= ra.at + extent(ra)) return false;
+  if (is_dense(ra)) return share(rb, ra.at, extent(ra));
+  if (is_dense(rb)) return share(ra, rb.at, extent(rb));
+  if (ra.outer != rb.outer || ra.outer_ld != rb.outer_ld || ra.inner_ld != rb.inner_ld) return ra.at == rb.at;
+  // Rows of the two lie j outer and i inner strides less delta apart: the nearest
+  // of either sign.
+  const auto below = [](int64_t x, int64_t ld) { return ld > 0 ? (x >= 0 ? x / ld : -((ld - 1 - x) / ld)) : 0; };
+  const int64_t delta = rb.at - ra.at, j0 = below(delta, ra.outer_ld);
+  for (int64_t j = j0; j <= j0 + 1; ++j) {
+    if (j <= -ra.outer || j >= ra.outer) continue;
+    const int64_t rest = delta - j * ra.outer_ld, i0 = below(rest, ra.inner_ld);
+    for (int64_t i = i0; i <= i0 + 1; ++i)
+      if (i > -ra.inner && i < ra.inner && std::abs(rest - i * ra.inner_ld) < ra.row) return true;
   }
-  return pa == pb;
+  return false;
 }
 
 // (one workgroup of 64 lanes a step's features, or of 512 for each 128 steps)

@@ -1,0 +1,79 @@
+"""Views of one array as the recurrence's operands: those that share an element
+are refused, all others are taken."""
+
+import numpy as np
+import pytest
+
+from gpu_common import say, torch_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+def lib():
+    torch = torch_gpu()
+    import paper_2607_14394_amd as D
+    return torch, D
+
+
+def whole(torch, D, z, v):
+    """The same from arrays of their own."""
+    y = torch.empty(z.shape, dtype=z.dtype, device="cuda")
+    D.dtst_recurrence(z.contiguous(), v.contiguous(), y)
+    return y
+
+
+def test_steps_and_entries_of_one_array():
+    torch, D = lib()
+    B, T, F = 3, 40, 72
+    a = torch.randn(B, 3 * T, F, device="cuda")
+    b = torch.randn(B, T, 3, F, device="cuda")
+    c = torch.randn(3 * B, T, F, device="cuda")
+    d = torch.randn(T, B, 3 * F, device="cuda").transpose(0, 1)
+    for name, z, v, y in (("runs of steps", a[:, :T], a[:, T:2 * T], a[:, 2 * T:]),
+                          ("every third step", b[:, :, 0], b[:, :, 1], b[:, :, 2]),
+                          ("runs of entries", c[:B], c[B:2 * B], c[2 * B:]),
+                          ("every third entry", c[::3], c[1::3], c[2::3]),
+                          ("columns, steps first", d[..., :F], d[..., F:2 * F], d[..., 2 * F:])):
+        say(f"[views] {name}")
+        want = whole(torch, D, z, v)
+        D.dtst_recurrence(z, v, y)
+        assert torch.equal(y, want), name
+    for z, v, y in ((a[:, :T], a[:, T:2 * T], a[:, 2 * T - 1:3 * T - 1]), (c[:B], c[B:2 * B], c[B - 1:2 * B - 1]),
+                    (d[..., :F], d[..., F:2 * F], d[..., 2 * F - 1:3 * F - 1])):
+        with pytest.raises(D.DtstError, match="overlap"):
+            D.dtst_recurrence(z, v, y)
+
+
+def test_random_views():
+    torch, D = lib()
+    rng = np.random.RandomState(3)
+    a = torch.randn(4000, device="cuda")
+    ids = np.arange(4000)
+    v0 = torch.randn(5 * 6 * 9, device="cuda")
+    taken = refused = 0
+    for _ in range(500):
+        B, T, F = rng.randint(1, 5), rng.randint(1, 6), rng.randint(1, 9)
+        if rng.rand() < 0.5:
+            st = F + rng.randint(0, 3)
+            sb = T * st + rng.randint(0, 20)
+        else:
+            sb = F + rng.randint(0, 3)
+            st = B * sb + rng.randint(0, 20)
+        at = 500 + rng.randint(-200, 200)
+        views = [torch.as_strided(a, (B, T, F), (sb, st, 1), o) for o in (500, at)]
+        where = [set(np.lib.stride_tricks.as_strided(ids[o:], (B, T, F), (sb * 8, st * 8, 8)).ravel()) for o in (500, at)]
+        z, y = views
+        v = v0[:B * T * F].view(B, T, F)
+        if where[0] & where[1]:
+            refused += 1
+            before = a.clone()
+            with pytest.raises(D.DtstError, match="overlap"):
+                D.dtst_recurrence(z, v, y)
+            assert torch.equal(a, before)
+        else:
+            taken += 1
+            want = whole(torch, D, z, v)
+            D.dtst_recurrence(z, v, y)
+            assert torch.equal(y, want)
+    say(f"[views] {taken} taken, {refused} refused")
+    assert taken > 50 and refused > 50
