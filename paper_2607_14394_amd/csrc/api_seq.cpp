@@ -359,6 +359,28 @@ dtst_status check_no_share(const dtst_recurrence_desc* d, const Sequence& out, c
   return DTST_OK;
 }
 
+// An array without gaps: states, lengths, the workspace.
+struct Block {
+  const void* p;
+  int64_t bytes;
+  const char* name;
+};
+dtst_status check_no_share(const Block& out, const Block& other) {
+  if (out.p == nullptr || other.p == nullptr || out.bytes <= 0 || other.bytes <= 0) return DTST_OK;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(out.p), b = reinterpret_cast<uintptr_t>(other.p);
+  if (a < b + uintptr_t(other.bytes) && b < a + uintptr_t(out.bytes)) return bad(std::string(out.name) + " and " + other.name + " overlap");
+  return DTST_OK;
+}
+dtst_status check_no_share(const dtst_recurrence_desc* d, const Sequence& s, const Block& b, int size) {
+  if (s.p == nullptr || b.p == nullptr || d->steps < 1) return DTST_OK;
+  if (share(rows_of(d, s, size), int64_t(reinterpret_cast<uintptr_t>(b.p)), b.bytes))
+    return bad(std::string(s.name) + " and " + b.name + " overlap");
+  return DTST_OK;
+}
+Block of_features(const dtst_recurrence_desc* d, const void* p, int64_t rows, const char* name) {
+  return Block{p, d->batch * d->features * rows * 4, name};
+}
+
 dtst_status recurrence(const dtst_recurrence_desc* d, const void* z, const void* v, const void* o, const float* h_zero,
                        const int32_t* lengths, void* y, float* h_out, float* states, void* workspace,
                        size_t workspace_bytes, void* stream) {
@@ -377,9 +399,21 @@ dtst_status recurrence(const dtst_recurrence_desc* d, const void* z, const void*
   if (h_out) DTST_TRY(check_align(h_out, 4, "h_out"));
   if (states) DTST_TRY(check_align(states, 4, "states"));
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
-  DTST_TRY(check_workspace(workspace, workspace_bytes,
-                           recurrence_workspace(d->batch, d->steps, d->features, d->type)));
+  const size_t need = recurrence_workspace(d->batch, d->steps, d->features, d->type);
+  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   DTST_TRY(check_recurrence_grid(d));
+  const Block bin = of_features(d, h_zero, 1, "h_zero"), bout = of_features(d, h_out, 1, "h_out");
+  const Block bst = of_features(d, states, (d->steps + 127) / 128, "states"), bn{lengths, d->batch * 4, "lengths"};
+  const Block bws{need ? workspace : nullptr, int64_t(need), "workspace"};
+  for (const Block* b : {&bin, &bn, &bout, &bst, &bws}) DTST_TRY(check_no_share(d, sy, *b, size));
+  for (const Block* out : {&bout, &bst, &bws}) {
+    for (const Sequence* in : {&sz, &sv, &so}) DTST_TRY(check_no_share(d, *in, *out, size));
+    if (out != &bout || h_out != h_zero) DTST_TRY(check_no_share(*out, bin));
+    DTST_TRY(check_no_share(*out, bn));
+  }
+  DTST_TRY(check_no_share(bst, bout));
+  DTST_TRY(check_no_share(bws, bout));
+  DTST_TRY(check_no_share(bws, bst));
   const int e = timed(K_RECUR, stream, [&] {
     return launch_recurrence(*d, z, v, o, h_zero, lengths, y, h_out, states, workspace, stream);
   });
@@ -410,9 +444,21 @@ dtst_status recurrence_adj(const dtst_recurrence_desc* d, const void* z, const v
   if (g_h) DTST_TRY(check_align(g_h, 4, "g_h"));
   if (g_hzero) DTST_TRY(check_align(g_hzero, 4, "g_hzero"));
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
-  DTST_TRY(check_workspace(workspace, workspace_bytes,
-                           recurrence_workspace(d->batch, d->steps, d->features, d->type)));
+  const size_t need = recurrence_workspace(d->batch, d->steps, d->features, d->type);
+  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   DTST_TRY(check_recurrence_grid(d));
+  const Block bst = of_features(d, d->steps > 0 ? states : nullptr, (d->steps + 127) / 128, "states");
+  const Block bin = of_features(d, g_h, 1, "g_h"), bout = of_features(d, g_hzero, 1, "g_hzero");
+  const Block bn{lengths, d->batch * 4, "lengths"}, bws{need ? workspace : nullptr, int64_t(need), "workspace"};
+  for (const Sequence* out : {&gz, &gv, &go})
+    for (const Block* b : {&bst, &bin, &bn, &bout, &bws}) DTST_TRY(check_no_share(d, *out, *b, size));
+  for (const Block* out : {&bout, &bws}) {
+    for (const Sequence* in : {&sz, &sv, &so, &sg}) DTST_TRY(check_no_share(d, *in, *out, size));
+    DTST_TRY(check_no_share(*out, bst));
+    if (out != &bout || g_hzero != g_h) DTST_TRY(check_no_share(*out, bin));
+    DTST_TRY(check_no_share(*out, bn));
+  }
+  DTST_TRY(check_no_share(bws, bout));
   const int e = timed(K_RECUR_ADJ, stream, [&] {
     return launch_recurrence_adj(*d, z, v, o, lengths, states, g_y, g_h, g_z, g_v, g_o, g_hzero, workspace, stream);
   });

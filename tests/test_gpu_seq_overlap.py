@@ -77,3 +77,20 @@ def test_random_views():
             assert torch.equal(y, want)
     say(f"[views] {taken} taken, {refused} refused")
     assert taken > 50 and refused > 50
+
+
+def test_states_between_the_rows():
+    """A state that lies in the columns which the steps leave free is taken, in
+    place too; one that reaches into them is refused."""
+    torch, D = lib()
+    T, F = 300, 64
+    a = torch.randn(1, T, 4 * F, device="cuda")
+    z, v, y, free = (a[..., i * F:(i + 1) * F] for i in range(4))
+    want, last = torch.empty(1, T, F, device="cuda"), torch.empty(1, F, device="cuda")
+    h0 = free[:, 7].clone()
+    D.dtst_recurrence(z.contiguous(), v.contiguous(), want, h0=h0, h_out=last)
+    h = free[:, 7]
+    D.dtst_recurrence(z, v, y, h0=h, h_out=h)
+    assert torch.equal(y, want) and torch.equal(h, last)
+    with pytest.raises(D.DtstError, match="y and h_out"):
+        D.dtst_recurrence(z, v, y, h_out=a[:, 7, 3 * F - 1:4 * F - 1])

@@ -6,6 +6,8 @@ import contextlib
 import pytest
 import torch
 
+from test_seq_oracle_cpu import P, recur_call
+
 D = pytest.importorskip("paper_2607_14394_amd", reason="libdtst.so not built")
 
 
@@ -39,3 +41,34 @@ def test_a_rollout_on_a_shard_needs_the_sum_over_the_shards():
     for local, offset in (((4, 8, 8), (4, 0, 0)), ((8, 8, 7), (0, 0, 0))):
         with pytest.raises(ValueError, match="reduce"):
             Rollout(dict(n_global=(8, 8, 8), n_local=local, offset=offset, kmax=(1, 1, 1)), 1, 1, [], device="cpu")
+
+
+# batch 2, steps 300, features 16: entries 4800 elements apart, steps 16; h: 128
+# bytes, states: 384, the workspace 6208
+@pytest.mark.parametrize("kw,word", [
+    (dict(h=P), "z and h_out"), (dict(h=P * 2 + 9600 * 2 - 4), "v and h_out"), (dict(h=P * 3 - 124), "o and h_out"),
+    (dict(h=P * 4 + 4), "y and h_out"), (dict(h0=P * 4), "y and h_zero"), (dict(h0=P * 5, h=P * 5 + 64), "h_out and h_zero"),
+    (dict(n=P * 4 + 8), "y and lengths"), (dict(n=P * 5, h=P * 5 - 124), "h_out and lengths"),
+    (dict(st=P), "z and states"), (dict(st=P * 5, h0=P * 5 + 380), "states and h_zero"),
+    (dict(st=P * 5, h=P * 5 - 64), "states and h_out"), (dict(st=P * 5, n=P * 5 + 380), "states and lengths"),
+    (dict(st=P * 4), "y and states"), (dict(ws=P * 2), "v and workspace"), (dict(ws=P * 4), "y and workspace"),
+    (dict(ws=P * 8, st=P * 8 + 6204), "workspace and states"), (dict(h=P * 8), "workspace and h_out"),
+    (dict(h0=P * 8 + 128), "workspace and h_zero"), (dict(n=P * 8), "workspace and lengths"),
+])
+def test_recurrence_refuses_shared_states(kw, word):
+    st, msg = recur_call(**kw)
+    assert st == 1 and msg == word + " overlap", msg
+
+
+# (h0 stands for g_h and h for g_hzero here, y for g_y)
+@pytest.mark.parametrize("kw,word", [
+    (dict(h=P), "z and g_hzero"), (dict(h=P * 4), "g_y and g_hzero"), (dict(h=P * 6 + 19196), "g_v and g_hzero"),
+    (dict(h=P * 9), "g_hzero and states"), (dict(h0=P * 10, h=P * 10 + 64), "g_hzero and g_h"),
+    (dict(h0=P * 5), "g_z and g_h"), (dict(st=P * 7), "g_o and states"), (dict(n=P * 5), "g_z and lengths"),
+    (dict(n=P * 10, h=P * 10 - 124), "g_hzero and lengths"), (dict(ws=P), "z and workspace"),
+    (dict(ws=P * 6), "g_v and workspace"), (dict(ws=P * 9 - 6192), "workspace and states"),
+    (dict(h0=P * 8), "workspace and g_h"), (dict(h=P * 8), "workspace and g_hzero"), (dict(n=P * 8), "workspace and lengths"),
+])
+def test_recurrence_adj_refuses_shared_states(kw, word):
+    st, msg = recur_call(fn="dtst_recurrence_adj", **dict(dict(st=P * 9), **kw))
+    assert st == 1 and msg == word + " overlap", msg
