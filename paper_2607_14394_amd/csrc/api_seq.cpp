@@ -63,8 +63,34 @@ dtst_status check_array(const Array& a, uintptr_t align) {
   return check_extent(a.rows, a.ld * a.size, a.name);
 }
 
+// The rows of a strided array in bytes: `outer` groups of `inner` rows of `row`
+// bytes, each group's rows before the next group's first.
+struct Rows {
+  int64_t at, outer, outer_ld, inner, inner_ld, row;
+};
+bool is_dense(const Rows& r) {
+  return (r.inner <= 1 || r.inner_ld == r.row) && (r.outer <= 1 || r.outer_ld == r.inner * r.row);
+}
+int64_t extent(const Rows& r) { return (r.outer - 1) * r.outer_ld + (r.inner - 1) * r.inner_ld + r.row; }
+
+// Whether a row of r has a byte of [at, at + n).
+bool share(const Rows& r, int64_t at, int64_t n) {
+  const int64_t most = at + n - 1 - r.at;                           // a row that does starts here at the latest,
+  const int64_t least = std::max<int64_t>(at - r.row + 1 - r.at, 0);  // here at the earliest
+  if (n <= 0 || most < least) return false;
+  const int64_t o = r.outer_ld > 0 ? std::min(least / r.outer_ld, r.outer - 1) : 0, rest = least - o * r.outer_ld;
+  const int64_t i = r.inner_ld > 0 ? (rest + r.inner_ld - 1) / r.inner_ld : rest > 0 ? r.inner : 0;
+  if (i < r.inner) return o * r.outer_ld + i * r.inner_ld <= most;
+  return o + 1 < r.outer && (o + 1) * r.outer_ld <= most;
+}
+
+Rows rows_of(const Array& a) {
+  return Rows{int64_t(reinterpret_cast<uintptr_t>(a.p)), a.rows, a.rows > 1 ? a.ld * a.size : 0, 1, 0, a.cols * a.size};
+}
+
 // Whether two arrays share an element.  Column ranges of one array (equal row
-// strides, rows apart) do not.
+// strides, rows apart) do not; of unlike strides, where neither is without gaps,
+// those that reach into each other's range are taken to.
 bool share(const Array& a, const Array& b) {
   if (a.p == nullptr || b.p == nullptr || a.rows < 1 || b.rows < 1) return false;
   const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
@@ -72,6 +98,9 @@ bool share(const Array& a, const Array& b) {
   const uintptr_t wa = uintptr_t(a.cols) * a.size, wb = uintptr_t(b.cols) * b.size;
   const uintptr_t ea = pa + (a.rows - 1) * la + wa, eb = pb + (b.rows - 1) * lb + wb;
   if (pa >= eb || pb >= ea) return false;
+  const Rows ra = rows_of(a), rb = rows_of(b);
+  if (is_dense(ra)) return share(rb, ra.at, extent(ra));
+  if (is_dense(rb)) return share(ra, rb.at, extent(rb));
   if (la == lb && a.rows > 1 && b.rows > 1) {
     const uintptr_t off = pb >= pa ? (pb - pa) % la : (la - (pa - pb) % la) % la;  // b's column 0 in a's rows
     return off < wa || la - off < wb;
@@ -298,32 +327,13 @@ dtst_status check_sequence_sizes(const dtst_recurrence_desc* d) {
   return DTST_OK;
 }
 
-// The rows of a sequence in bytes: `outer` groups of `inner` rows of `row` bytes,
-// each group's rows before the next group's first (check_sequence).
-struct Rows {
-  int64_t at, outer, outer_ld, inner, inner_ld, row;
-};
+// (Of a sequence whose strides check_sequence takes.)
 Rows rows_of(const dtst_recurrence_desc* d, const Sequence& s, int size) {
   Rows r{int64_t(reinterpret_cast<uintptr_t>(s.p)), d->batch, s.st[0] * size, d->steps, s.st[1] * size, d->features * size};
   if (r.outer <= 1) r.outer_ld = 0;
   if (r.inner <= 1) r.inner_ld = 0;
   if (r.outer_ld < r.inner_ld) std::swap(r.outer, r.inner), std::swap(r.outer_ld, r.inner_ld);
   return r;
-}
-bool is_dense(const Rows& r) {
-  return (r.inner <= 1 || r.inner_ld == r.row) && (r.outer <= 1 || r.outer_ld == r.inner * r.row);
-}
-int64_t extent(const Rows& r) { return (r.outer - 1) * r.outer_ld + (r.inner - 1) * r.inner_ld + r.row; }
-
-// Whether a row of r has a byte of [at, at + n).
-bool share(const Rows& r, int64_t at, int64_t n) {
-  const int64_t most = at + n - 1 - r.at;                           // a row that does starts here at the latest,
-  const int64_t least = std::max<int64_t>(at - r.row + 1 - r.at, 0);  // here at the earliest
-  if (n <= 0 || most < least) return false;
-  const int64_t o = r.outer_ld > 0 ? std::min(least / r.outer_ld, r.outer - 1) : 0, rest = least - o * r.outer_ld;
-  const int64_t i = r.inner_ld > 0 ? (rest + r.inner_ld - 1) / r.inner_ld : rest > 0 ? r.inner : 0;
-  if (i < r.inner) return o * r.outer_ld + i * r.inner_ld <= most;
-  return o + 1 < r.outer && (o + 1) * r.outer_ld <= most;
 }
 
 // Whether two sequences share an element.  Of unlike strides, where neither is

@@ -1,5 +1,5 @@
-"""Views of one array as the recurrence's operands: those that share an element
-are refused, all others are taken."""
+"""Views of one array as operands: those that share an element are refused, all
+others are taken."""
 
 import numpy as np
 import pytest
@@ -94,3 +94,25 @@ def test_states_between_the_rows():
     assert torch.equal(y, want) and torch.equal(h, last)
     with pytest.raises(D.DtstError, match="y and h_out"):
         D.dtst_recurrence(z, v, y, h_out=a[:, 7, 3 * F - 1:4 * F - 1])
+
+
+def test_vectors_between_the_rows():
+    """The norm's weight, 1 / rms and single rows in the columns that other
+    operands leave free."""
+    torch, D = lib()
+    R, C = 9, 64
+    a = torch.randn(R, 4 * C, device="cuda")
+    x, y, u, free = (a[:, i * C:(i + 1) * C] for i in range(4))
+    w, rstd, want, r1 = free[2], free[3, :R], torch.empty(R, C, device="cuda"), torch.empty(R, device="cuda")
+    D.dtst_rms_norm(x.contiguous(), w.clone(), want, rstd=r1)
+    D.dtst_rms_norm(x, w, y, sum_out=u, rstd=rstd)
+    assert torch.equal(y, want) and torch.equal(rstd, r1) and torch.equal(u, x)
+    g_u, g_w, g_u1, g_w1 = (torch.empty(*s, device="cuda") for s in ((R, C), (C,), (R, C), (C,)))
+    ws = torch.empty(D.dtst_rms_norm_adj_workspace(R, C), dtype=torch.uint8, device="cuda")
+    D.dtst_rms_norm_adj(y, u, w, rstd, g_u, free[4], ws=ws)
+    D.dtst_rms_norm_adj(y.contiguous(), u.contiguous(), w.clone(), r1, g_u1, g_w1)
+    assert torch.equal(g_u, g_u1) and torch.equal(free[4], g_w1)
+    with pytest.raises(D.DtstError, match="y and weight"):
+        D.dtst_rms_norm(x, a[2, C + 1:2 * C + 1], y)
+    with pytest.raises(D.DtstError, match="rstd and x"):
+        D.dtst_rms_norm(x, w, y, rstd=a.view(-1)[2 * 4 * C - 3:2 * 4 * C - 3 + R])
