@@ -178,7 +178,8 @@ dtst_status rms_norm(const dtst_norm_desc* d, const void* x, const void* res, co
   if (sum_out) DTST_TRY(check_array(as, sr));
   if (rstd) DTST_TRY(check_align(rstd, 4, "rstd"));
   DTST_TRY(q8 ? check_codes(ay, asc) : check_array(ay, sx));
-  DTST_TRY(check_grid(d->rows, 1024));
+  const NormGrid grid = rms_norm_grid(d->rows, d->cols);
+  DTST_TRY(check_grid(grid.groups, grid.threads));
   DTST_TRY(check_apart(as, ar, true));
   DTST_TRY(check_apart(as, ax, res == nullptr));
   DTST_TRY(check_apart(ay, ax, !q8));

@@ -122,9 +122,8 @@ rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __res
 template <class TX, class TR, bool Q8, int RW, int V>
 int launch_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* w, void* sum_out, void* y,
                 void* scale, float* rstd, hipStream_t s) {
-  constexpr int ROWS = RW > 4 ? 1 : 4 / RW;
-  const unsigned blocks = unsigned((d.rows + ROWS - 1) / ROWS);
-  hipLaunchKernelGGL((rms_norm_kernel<TX, TR, Q8, RW, V>), dim3(blocks), dim3(RW > 4 ? RW * 64 : 256), 0, s, d,
+  const NormGrid g = rms_norm_grid(d.rows, d.cols);
+  hipLaunchKernelGGL((rms_norm_kernel<TX, TR, Q8, RW, V>), dim3(unsigned(g.groups)), dim3(g.threads), 0, s, d,
                      static_cast<const TX*>(x), static_cast<const TR*>(res), w, static_cast<TR*>(sum_out), y,
                      static_cast<uint8_t*>(scale), rstd);
   return hipGetLastError();
@@ -294,6 +293,12 @@ int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, con
                ? launch_norm_cols<TX, TR, true>(d, x, res, weight, sum_out, y, scale, rstd, s)
                : launch_norm_cols<TX, TR, false>(d, x, res, weight, sum_out, y, scale, rstd, s);
   });
+}
+
+// (one wave a row up to 1024 columns, four up to 8192, else sixteen)
+NormGrid rms_norm_grid(int64_t rows, int64_t cols) {
+  if (cols <= 1024) return {(rows + 3) / 4, 256};
+  return {rows, cols <= 8192 ? 256 : 1024};
 }
 
 size_t rms_norm_adj_workspace(int64_t rows, int64_t cols) { return size_t(norm_adj_parts(rows, cols)) * cols * 4; }

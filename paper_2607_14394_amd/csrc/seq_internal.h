@@ -11,6 +11,12 @@ namespace dtst {
 
 constexpr int64_t kNormMaxCols = 32768;
 
+// Workgroups of the norm, and the threads of each.
+struct NormGrid {
+  int64_t groups;
+  int threads;
+};
+NormGrid rms_norm_grid(int64_t rows, int64_t cols);
 int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, void* sum_out,
                     void* y, void* scale, float* rstd, void* stream);
 size_t rms_norm_adj_workspace(int64_t rows, int64_t cols);

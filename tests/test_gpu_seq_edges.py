@@ -1,4 +1,4 @@
-"""Edges of the latent-sequence operators' calls: nothing to work on."""
+"""Edges of the latent-sequence operators' calls: nothing to work on, many rows."""
 
 import pytest
 
@@ -28,3 +28,19 @@ def test_norm_backward_of_no_rows(cols, accumulate):
                                  D.torch_stream())
     assert st == 0, D.lib.dtst_last_error()
     assert torch.equal(g_w, want)
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 22) + 5, 8), ((1 << 22) + 1, 1030)])
+def test_norm_of_millions_of_rows(rows, cols):
+    """One of 65536 sequences of 64 steps and more: 2^22 rows are one launch."""
+    torch, D = lib()
+    x = torch.randn(rows, cols, dtype=torch.float32, device="cuda").to(torch.bfloat16)
+    w, y = torch.ones(cols, device="cuda"), torch.empty_like(x)
+    say(f"[norm] {rows} x {cols}")
+    D.dtst_rms_norm(x, w, y)
+    few = torch.empty_like(x[:1000])
+    for at in (0, 1 << 20, rows - 1000):
+        D.dtst_rms_norm(x[at:at + 1000], w, few)
+        assert torch.equal(y[at:at + 1000], few), at
+    u = x[-1000:].double()
+    assert ((y[-1000:].double() - u / torch.sqrt((u * u).mean(dim=1, keepdim=True) + 1e-6)).abs() <= 2.0 ** -8 * y[-1000:].double().abs() + 1e-5).all()
