@@ -75,11 +75,20 @@ __device__ __forceinline__ int64_t length_of(const Args& p, int64_t b) {
   return n < 0 ? 0 : n > p.steps ? p.steps : n;
 }
 
+// The product p of gates of which `least` is the smallest.  One that underflows
+// stays above zero where they all are: it would make no number of an infinite
+// state, which a run of open gates keeps.
+__device__ __forceinline__ float product_of_gates(float p, float least) {
+  return fmaxf(p, fminf(least, __uint_as_float(1)));  // (1: the smallest number above zero)
+}
+__device__ __forceinline__ float compose_gates(float a, float b) { return product_of_gates(a * b, fminf(a, b)); }
+
 // A span's map in a word of the chain: A >= 0 with its sign bit set (a word of
-// zeros: not there yet) and H.  A = 0 says that H is the leaving state itself;
-// a product that underflows is kept above zero, so that no number stays one.
+// zeros: not there yet) and H.  A = 0 says that H is the leaving state itself, so
+// a closed gate's zero goes as CLOSED, a number that no product of gates is.
+constexpr unsigned CLOSED = 0x40000000u;
 __device__ __forceinline__ unsigned long long map_word(float A, float H) {
-  const unsigned a = (A == 0.f ? 1u : __float_as_uint(A)) | 0x80000000u;
+  const unsigned a = (A == 0.f ? CLOSED : __float_as_uint(A)) | 0x80000000u;
   return (unsigned long long)(__float_as_uint(H)) << 32 | a;
 }
 __device__ __forceinline__ unsigned long long state_word(float h) {
@@ -119,9 +128,10 @@ __device__ void look_back(const unsigned long long* words, int64_t pitch, int k,
       if (there) {
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          const float H = __uint_as_float(unsigned(w[i][c] >> 32)), A = __uint_as_float(unsigned(w[i][c]) & 0x7fffffffu);
+          const unsigned bits = unsigned(w[i][c]) & 0x7fffffffu;
+          const float H = __uint_as_float(unsigned(w[i][c] >> 32));
           if (!done[c]) h[c] += a[c] * H;
-          a[c] *= A;
+          a[c] = compose_gates(a[c], bits == CLOSED ? 0.f : __uint_as_float(bits));
           done[c] = done[c] || unsigned(w[i][c]) == 0x80000000u;
           ended = ended && done[c];
         }
@@ -223,9 +233,9 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
     constexpr bool FULL = decltype(full_)::value;
     raw_t<T, CPL> zr[R], vr[R], orw[R];
     float s[R][CPL], bv[R][CPL];
-    float A[CPL], H[CPL], h[CPL];
+    float A[CPL], H[CPL], h[CPL], least[CPL];
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) A[c] = 1.f, H[c] = 0.f, h[c] = 0.f;
+    for (int c = 0; c < CPL; ++c) A[c] = least[c] = 1.f, H[c] = 0.f, h[c] = 0.f;
     if (FULL || rows > 0) {
       get_rows<FULL, T, CPL, R>(z, p.z, q.b, t0, q.c, rows, zr);
       get_rows<FULL, T, CPL, R>(v, p.v, q.b, t0, q.c, rows, vr);
@@ -244,9 +254,11 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
           logistic(float(zr[i][c]), s[i][c], gn);
           bv[i][c] = gn * float(vr[i][c]);
           if (!FULL && i >= rows) s[i][c] = 1.f, bv[i][c] = 0.f;
-          A[c] *= s[i][c];
+          A[c] *= s[i][c], least[c] = fminf(least[c], s[i][c]);
           H[c] = s[i][c] * H[c] + bv[i][c];
         }
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) A[c] = product_of_gates(A[c], least[c]);
     }
     // the state that enters this wave's rows
     if (waves > 1) {
@@ -263,7 +275,7 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
             for (int i = 1; i < WAVES; ++i) {
               const float a = mapA[i][lane * CPL + c];
               tH[c] = a * tH[c] + mapH[i][lane * CPL + c];
-              tA[c] *= a;
+              tA[c] = compose_gates(tA[c], a);
             }
           }
           const int64_t pitch = 64 * CPL;
@@ -357,7 +369,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
     constexpr bool FULL = decltype(full_)::value;
     raw_t<T, CPL> zr[R], vr[R], orw[R], gr[R];
     float s[R][CPL], sn[R][CPL], b[R][CPL];  // b: then the state before the row
-    float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL];
+    float h[CPL], e[CPL], A[CPL], H[CPL], G[CPL], least[CPL];
     if (FULL || rows > 0) {
       get_rows<FULL, T, CPL, R>(z, p.z, q.b, t0, q.c, rows, zr);
       get_rows<FULL, T, CPL, R>(v, p.v, q.b, t0, q.c, rows, vr);
@@ -368,7 +380,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
     for (int c = 0; c < CPL; ++c) {
       h[c] = states[(q.b * p.spans + span) * p.features + q.c + c];
       e[c] = place == 0 && g_h != nullptr ? g_h[q.b * p.features + q.c + c] : 0.f;
-      A[c] = 1.f, H[c] = 0.f, G[c] = 0.f;
+      A[c] = least[c] = 1.f, H[c] = 0.f, G[c] = 0.f;
     }
     if (FULL || rows > 0) {
 #pragma unroll
@@ -378,9 +390,11 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
           logistic(float(zr[i][c]), s[i][c], sn[i][c]);
           b[i][c] = sn[i][c] * float(vr[i][c]);
           if (!FULL && i >= rows) s[i][c] = 1.f, sn[i][c] = b[i][c] = 0.f;
-          A[c] *= s[i][c];
+          A[c] *= s[i][c], least[c] = fminf(least[c], s[i][c]);
           H[c] = s[i][c] * H[c] + b[i][c];
         }
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) A[c] = product_of_gates(A[c], least[c]);
 #pragma unroll
       for (int i = R - 1; i >= 0; --i) {
         if (!FULL && i >= rows) continue;
@@ -415,7 +429,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
             for (int i = WAVES - 1; i >= 0; --i) {
               const float a = mapA[i][lane * CPL + c];
               tG[c] = a * tG[c] + mapG[i][lane * CPL + c];
-              tA[c] *= a;
+              tA[c] = compose_gates(tA[c], a);
             }
           }
           const int64_t pitch = 64 * CPL;
