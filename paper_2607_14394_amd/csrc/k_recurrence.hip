@@ -41,18 +41,36 @@ constexpr int SPAN = DTST_RECURRENCE_SPAN;
 constexpr int WAVES = 8;
 constexpr int RPW = SPAN / WAVES;  // steps of a wave
 
-// exp(-x)
-__device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
+// exp(-x), of an x of type T.  exp2 takes x's product with -log2 e, which one
+// rounding moves by up to 2^-24 of itself, and so the result by |x| 2^-24 (and
+// the constant's own rounding by a quarter of that): 29 units of 2^-24 at x = 32.
+// That is what half a unit in x's last place does in 32 bits, where the rounding
+// is made good; 16-bit values of x are 2^13 times and more as far apart, and the
+// five instructions are spared.
+template <class T>
+__device__ __forceinline__ float exp_minus(float x) {
+  constexpr float hi = -1.44269502162933349609375f, lo = -1.92596299112661746e-8f, ln2 = 0.693147180559945309f;
+  const float t = x * hi;
+  float e = __builtin_amdgcn_exp2f(t);
+  if constexpr (std::is_same_v<T, float>) {
+    const float rest = fmaf(x, lo, fmaf(x, hi, -t));
+    e *= fmaf(__builtin_amdgcn_fmed3f(rest, -0.01f, 0.01f), ln2, 1.f);  // (far below 0.01 unless e is 0 or infinite)
+  }
+  return e;
+}
 
-// s(x) and s(-x), both to full relative precision (1 - s(x) would lose that of a
-// small s(-x), and 1 / (1 + exp(x)) costs two more transcendentals).  Infinities
-// give 0 and 1, no number gives no number.
+// s(x) and s(-x), each to the relative precision of exp_minus (1 - s(x) would
+// lose that of a small s(-x), and 1 / (1 + exp(x)) costs two more
+// transcendentals).  Infinities give 0 and 1, no number gives no number; below x =
+// -88 s(x) is 0.
+template <class T>
 __device__ __forceinline__ void logistic(float x, float& s, float& sn) {
-  const float e = exp_minus(x);
+  const float e = exp_minus<T>(x);
   s = __builtin_amdgcn_rcpf(1.f + e);
   sn = x < 0.f ? 1.f - s : e * s;
 }
-__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + exp_minus(x)); }
+template <class T>
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + exp_minus<T>(x)); }
 
 struct Strides {
   int64_t b, t;
@@ -251,7 +269,7 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
           float gn;
-          logistic(float(zr[i][c]), s[i][c], gn);
+          logistic<T>(float(zr[i][c]), s[i][c], gn);
           bv[i][c] = gn * float(vr[i][c]);
           if (!FULL && i >= rows) s[i][c] = 1.f, bv[i][c] = 0.f;
           A[c] *= s[i][c], least[c] = fminf(least[c], s[i][c]);
@@ -311,7 +329,7 @@ recurrence_kernel(Args p, const T* z, const T* v, const T* o, const float* h_zer
           r[c] = h[c];
           if constexpr (GATED) {
             const float x = float(orw[i][c]);
-            r[c] *= x * logistic(x);
+            r[c] *= x * logistic<T>(x);
           }
         }
         if (FULL || i < rows) {  // (past them h stands still; leaving the loop instead keeps it from being unrolled)
@@ -387,7 +405,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
       for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int c = 0; c < CPL; ++c) {
-          logistic(float(zr[i][c]), s[i][c], sn[i][c]);
+          logistic<T>(float(zr[i][c]), s[i][c], sn[i][c]);
           b[i][c] = sn[i][c] * float(vr[i][c]);
           if (!FULL && i >= rows) s[i][c] = 1.f, sn[i][c] = b[i][c] = 0.f;
           A[c] *= s[i][c], least[c] = fminf(least[c], s[i][c]);
@@ -403,7 +421,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
           float g = float(gr[i][c]);
           if constexpr (GATED) {
             const float x = float(orw[i][c]);
-            g *= x * logistic(x);
+            g *= x * logistic<T>(x);
           }
           G[c] = s[i][c] * (g + G[c]);
         }
@@ -475,7 +493,7 @@ recurrence_adj_kernel(Args p, const T* z, const T* v, const T* o, const float* s
           const float vv = float(vr[i][c]);
           float g = float(gr[i][c]);
           if constexpr (GATED) {
-            const float x = float(orw[i][c]), so = logistic(x), xs = x * so;
+            const float x = float(orw[i][c]), so = logistic<T>(x), xs = x * so;
             go[c] = g * (s[i][c] * b[i][c] + sn[i][c] * vv) * (so + xs * (1.f - so));
             g *= xs;
           }
