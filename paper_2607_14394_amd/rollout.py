@@ -211,9 +211,15 @@ class Rollout:
         return self.plans[frames]
 
     def _groups(self, frames):
-        for i in range(0, frames, self.group):
-            n = min(self.group, frames - i)
-            yield self.plan(n), slice(i, i + n)
+        """Plans and their frames: groups of GROUP frames, then of smaller powers
+        of two, so that few plans (each has a workspace) serve any number."""
+        i, n = 0, self.group
+        while i < frames:
+            if n <= frames - i:
+                yield self.plan(n), slice(i, i + n)
+                i += n
+            else:
+                n //= 2
 
     def encode(self, frames):
         """(B, T, channels, x, y, z) float32 to tokens (B, T, width) float32."""

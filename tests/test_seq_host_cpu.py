@@ -72,3 +72,24 @@ def test_recurrence_refuses_shared_states(kw, word):
 def test_recurrence_adj_refuses_shared_states(kw, word):
     st, msg = recur_call(fn="dtst_recurrence_adj", **dict(dict(st=P * 9), **kw))
     assert st == 1 and msg == word + " overlap", msg
+
+
+def test_a_rollout_keeps_few_plans(monkeypatch):
+    from paper_2607_14394_amd import rollout
+    made = []
+
+    class Counted:
+        n_modes = 8
+
+        def __init__(self, desc, device):
+            made.append(desc["batch"])
+
+    monkeypatch.setattr(rollout, "Plan", Counted)
+    ro = rollout.Rollout(dict(n_global=(8, 8, 8), n_local=(8, 8, 8), offset=(0, 0, 0), kmax=(1, 1, 1)), 1, 1, [], device="cpu")
+    for frames in range(700):
+        at = 0
+        for _, s in ro._groups(frames):
+            assert s.start == at and s.stop > at
+            at = s.stop
+        assert at == frames
+    assert len(made) == len(set(made)) <= 9 and max(made) == ro.group
