@@ -225,7 +225,7 @@ class Rollout:
         """(B, T, channels, x, y, z) float32 to tokens (B, T, width) float32."""
         B, T = frames.shape[:2]
         xhat = torch.empty(B * T, self.width // 2, dtype=torch.complex64, device=self.device)
-        flat = frames.contiguous().view(B * T, -1)
+        flat = frames.contiguous().view(B * T, frames[0, 0].numel() if B * T else 0)
         for plan, s in self._groups(B * T):
             plan.forward(flat[s].view(plan.spatial_shape(self.channels)),
                          xhat[s].view(plan.spectral_shape(self.channels)))
