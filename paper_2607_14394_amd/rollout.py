@@ -19,7 +19,7 @@ from __future__ import annotations
 import torch
 
 from . import (DtstError, Plan, dtst_desc_validate, dtst_product, dtst_quantise, dtst_recurrence, dtst_recurrence_adj, dtst_rms_norm,
-               dtst_rms_norm_adj, empty_codes, recurrence_states_shape)
+               dtst_rms_norm_adj, dtst_rms_norm_adj_workspace, empty_codes, recurrence_states_shape)
 
 _UNSUPPORTED = 2  # DTST_ERR_UNSUPPORTED
 
@@ -43,14 +43,19 @@ class _Weights:
 
 
 class LatentBlock:
-    """One residual block of width W with F recurrent features.  norm: (W,)
-    float32; w_in: (3 F, W); b_in: (3 F,) float32; w_out: (W, F)."""
+    """One residual block of width W (32768 at most, the norm's limit) with F
+    recurrent features.  norm: (W,) float32; w_in: (3 F, W); b_in: (3 F,)
+    float32; w_out: (W, F)."""
 
     def __init__(self, norm, w_in, b_in, w_out, eps=1e-6):
         self.width, self.features = w_out.shape
         if tuple(w_in.shape) != (3 * self.features, self.width) or tuple(norm.shape) != (self.width,):
             raise ValueError(f"w_out {tuple(w_out.shape)} needs w_in ({3 * self.features}, {self.width}) and norm "
                              f"({self.width},)")
+        try:
+            dtst_rms_norm_adj_workspace(1, self.width)
+        except DtstError as e:  # (here, rather than at the first forward)
+            raise ValueError(f"a block of width {self.width}: {e}") from None
         self.norm, self.b_in, self.eps = norm, b_in, eps
         self.w_in, self.w_out = _Weights(w_in), _Weights(w_out)
 
@@ -165,7 +170,8 @@ class LatentBlock:
 class Rollout:
     """Fields of `channels` channels on one shard, batch sequences at a time.
     grid: a descriptor's n_global, n_local, offset and kmax in x, y, z (3 each);
-    blocks: LatentBlocks of width 2 channels M, M the retained modes.  A shard's
+    blocks: LatentBlocks of width 2 channels M, M the retained modes of one time
+    step (so that 2 channels M is at most 32768).  A shard's
     coefficients are its part of the domain's: where n_local is not n_global,
     reduce(tokens) has to sum them in place over the shards, as
     torch.distributed.all_reduce does; every shard then runs the same blocks on

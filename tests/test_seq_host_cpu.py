@@ -93,3 +93,13 @@ def test_a_rollout_keeps_few_plans(monkeypatch):
             at = s.stop
         assert at == frames
     assert len(made) == len(set(made)) <= 9 and max(made) == ro.group
+
+
+def test_a_block_wider_than_the_norm_is_refused_when_it_is_made():
+    from paper_2607_14394_amd.rollout import LatentBlock
+    W, F = 32769, 1
+    meta = lambda *s: torch.empty(s, device="meta")  # noqa: E731
+    with pytest.raises(ValueError, match="width 32769.*32768"):
+        LatentBlock(meta(W), meta(3 * F, W), meta(3 * F), meta(W, F))
+    with pytest.raises(ValueError, match="width 0"):
+        LatentBlock(meta(0), meta(3, 0), meta(3), meta(0, 1))
