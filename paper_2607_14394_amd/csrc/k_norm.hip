@@ -42,15 +42,43 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
+// The same in 64 bits from 16 lanes' sums on: there the last additions, whose
+// roundings weigh most, cost a few instructions a row.
+template <int RW>
+__device__ __forceinline__ double row_sum64(float v, double* part) {
+#pragma unroll
+  for (int d = 1; d <= 8; d <<= 1) v += __shfl_xor(v, d, 64);
+  double s = v;
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  if constexpr (RW > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) part[wave] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < RW; ++i) s += part[i];
+  }
+  return s;
+}
+
+// 1 / sqrt(m), rounded once: the 32-bit root, off by a unit in its last place, and
+// a step of Newton's (no root of 0, infinity and no number).
+__device__ __forceinline__ float rsqrt_of(double m) {
+  const float r = rsqrtf(float(m));
+  const double x = r;
+  return r > 0.f && r <= 3.402823466e38f ? float(x * (1.5 - 0.5 * m * x * x)) : r;
+}
+
 // RW waves a row, V vectors of 8 columns a lane: up to 512 RW V columns.  A
 // workgroup holds max(RW, 4) waves, so four rows with RW = 1.
 template <class TX, class TR, bool Q8, int RW, int V>
 __global__ void __launch_bounds__(RW > 4 ? RW * 64 : 256)
-rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __restrict__ w, TR* sum_out, void* y,
-                uint8_t* scale, float* rstd) {
+rms_norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const float* __restrict__ w, TR* sum_out,
+                void* y, uint8_t* scale, float* rstd) {
   constexpr int ROWS = RW > 4 ? 1 : 4 / RW;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  __shared__ float part[RW];
+  __shared__ double part[RW];
   const int64_t row = int64_t(blockIdx.x) * ROWS + wave / RW;
   if (ROWS > 1 && row >= d.rows) return;  // (one wave a row: no barrier follows)
   const int first = ((wave % RW) * 64 + lane) * VEC;
@@ -83,8 +111,7 @@ rms_norm_kernel(dtst_norm_desc d, const TX* x, const TR* res, const float* __res
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int j = 0; j < VEC; ++j) ss += u[i][j] * u[i][j];
-  ss = row_sum<RW>(ss, part);
-  const float r = rsqrtf(ss * (1.f / float(cols)) + d.eps);
+  const float r = rsqrt_of(row_sum64<RW>(ss, part) * inv_cols + double(d.eps));
   if (rstd != nullptr && first == 0) rstd[row] = r;
   if (sum_out != nullptr) {
 #pragma unroll
@@ -124,6 +151,7 @@ int launch_norm(const dtst_norm_desc& d, const void* x, const void* res, const f
                 void* scale, float* rstd, hipStream_t s) {
   const NormGrid g = rms_norm_grid(d.rows, d.cols);
   hipLaunchKernelGGL((rms_norm_kernel<TX, TR, Q8, RW, V>), dim3(unsigned(g.groups)), dim3(g.threads), 0, s, d,
+                     1.0 / double(d.cols),
                      static_cast<const TX*>(x), static_cast<const TR*>(res), w, static_cast<TR*>(sum_out), y,
                      static_cast<uint8_t*>(scale), rstd);
   return hipGetLastError();
