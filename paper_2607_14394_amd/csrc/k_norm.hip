@@ -9,7 +9,7 @@
 // once, eight neighbouring columns (16 bytes of a 16-bit type) per access; 16
 // lanes then hold a block of 128 columns, whose 8-bit scale is a maximum within
 // a row of lanes.  Up to 1024 columns a wave holds a row (no barrier), then four,
-// then sixteen.  16384 x 4096 in bf16 with the residual, to 8 bits: 85 us, 5.5
+// then sixteen.  16384 x 4096 in bf16 with the residual, to 8 bits: 86 us, 5.5
 // TB/s, what a large copy reaches; 6001 x 1537 in 32 bits 33 us forward (4.5
 // TB/s) and 27 + 5 us backward.
 //

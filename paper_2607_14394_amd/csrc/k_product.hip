@@ -12,9 +12,10 @@
 // b as the first operand a lane ends with four neighbouring columns 4 (l / 16) + r
 // of row l % 16 of c.
 //
-// Large products are bound by the matrix cores and what feeds them: 8192^3 759 us
-// (1450 TFLOP/s; without the widening, two codes an instruction in between, 12 to
-// 15% less).  Smaller ones wait for their first loads and their stores.
+// Large products are bound by the matrix cores and what feeds them: 8192^3 716 to
+// 753 us, by the card (1530 to 1460 TFLOP/s; the cores are busy 67% of the time;
+// without the widening, two codes an instruction in between, 12 to 15% less).
+// Smaller ones wait for their first loads and their stores.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

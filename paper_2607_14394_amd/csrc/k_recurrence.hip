@@ -17,9 +17,9 @@
 // e_{t-1} = s(z_t) (g_t + e_t), g_t = g_y_t o_t s(o_t), and takes the states from
 // the one that the forward kept for each span.
 //
-// 1 x 65536 x 1280 in bf16: 139 us and 5 us for clearing the chain's words, 4.8
+// 1 x 65536 x 1280 in bf16: 141 us and 5 us for clearing the chain's words, 4.8
 // TB/s (two launches, maps then states, would read z and v twice); 4 x 4096 x
-// 2048 60 us forward and 107 us backward (4.5 and 4.4 TB/s), where 24 and 46
+// 2048 60 us forward and 107 us backward (4.5 and 4.4 TB/s), where 25 and 47
 // vector instructions a value, 4 and 6 of them at a quarter of the rate, come
 // close to the time of the loads.
 //
