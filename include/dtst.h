@@ -300,7 +300,8 @@ dtst_status dtst_forward_noalloc(dtst_plan_t p, const float* x, void* xhat, int 
  * and launch kernels only.  Operands need the alignment of their type unless
  * said otherwise.  Outputs share no element with each other or with an input,
  * except where a call says that they may be the same array.  All arithmetic,
- * sums and states are in 32 bits; results are rounded once, to nearest even. */
+ * sums and states are in 32 bits or more; results are rounded once, to nearest
+ * even. */
 
 /* Element types. */
 enum {
@@ -397,16 +398,16 @@ dtst_status dtst_product(const dtst_product_desc* d, const void* a, const void* 
 /* Gated linear recurrence along the steps, feature by feature, with the
  * logistic function s(v) = 1 / (1 + exp(-v)):
  *   h_t = s(z_t) h_{t-1} + (1 - s(z_t)) v_t,    y_t = h_t o_t s(o_t)
- * (y_t = h_t without o).  z, v, o, y: (batch, steps, features) of `type`, each
- * with a stride of batch entries and of steps, so they may be column ranges of
- * one array.  h_zero: (batch, features) fp32, the state before the first step,
- * NULL for zero; h_out: (batch, features) fp32, the state after the last, NULL
- * if not wanted; it may be h_zero itself, which is a serving step with steps =
- * 1.  lengths: batch int32 on the device, NULL for `steps` each; from
- * lengths[b] (clamped to 0 .. steps) on, the state stands still, y is zero and
- * z, v and o are not read.  states: (batch, ceil(steps / DTST_RECURRENCE_SPAN),
- * features) fp32, the states before steps 0, SPAN, 2 SPAN, ... that the
- * backward needs, NULL if not wanted.  workspace:
+ * (y_t = h_t without o; an s(v) below 2^-126 may be 0).  z, v, o, y: (batch, steps,
+ * features) of `type`, each with a stride of batch entries and of steps, so
+ * they may be column ranges of one array.  h_zero: (batch, features) fp32, the
+ * state before the first step, NULL for zero; h_out: (batch, features) fp32,
+ * the state after the last, NULL if not wanted; it may be h_zero itself, which
+ * is a serving step with steps = 1.  lengths: batch int32 on the device, NULL
+ * for `steps` each; from lengths[b] (clamped to 0 .. steps) on, the state
+ * stands still, y is zero and z, v and o are not read.  states: (batch,
+ * ceil(steps / DTST_RECURRENCE_SPAN), features) fp32, the states before steps
+ * 0, SPAN, 2 SPAN, ... that the backward needs, NULL if not wanted.  workspace:
  * dtst_recurrence_workspace bytes, any contents. */
 #define DTST_RECURRENCE_SPAN 128
 typedef struct {
