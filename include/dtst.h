@@ -361,6 +361,27 @@ dtst_status dtst_rms_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, cons
                               const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* Layer norm with the residual's addition, row by row, as dtst_rms_norm with
+ * the deviations from the row's mean in the place of u:
+ *   m = mean_c u[c],  r = 1 / sqrt(mean_c (u[c] - m)^2 + eps),  mean = m,  rstd = r;
+ *   y[c] = (u[c] - m) r weight[c] + bias[c].
+ * Descriptor and arrays as there; bias: cols fp32, or NULL for none; mean: rows
+ * fp32, or NULL. */
+dtst_status dtst_layer_norm(const dtst_norm_desc* d, const void* x, const void* res, const float* weight,
+                            const float* bias, void* sum_out, void* y, void* scale, float* mean, float* rstd,
+                            void* stream);
+
+/* Backward of dtst_layer_norm from its stored sum u, mean and rstd, with
+ * h = (u - mean) rstd and t = g_y weight:
+ *   g_u = rstd (t - mean_c t - h mean_c(t h)) + g_sum,
+ *   g_weight (+)= sum_rows g_y h,   g_bias (+)= sum_rows g_y.
+ * Descriptor and arrays as in dtst_rms_norm_adj; g_bias: cols fp32.  workspace:
+ * dtst_layer_norm_adj_workspace bytes. */
+dtst_status dtst_layer_norm_adj_workspace(int64_t rows, int64_t cols, size_t* bytes);
+dtst_status dtst_layer_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
+                                const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x,
+                                float* g_weight, float* g_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Rows of x, (rows, cols) of `type` at stride ld_x, in 8 bits: q and scale as
  * a (rows, cols) array, and (or) its transpose, qt and scale_t as a
  * (cols, rows) array with a scale for each 128 rows of x.  Either pair may be

@@ -22,6 +22,27 @@ def rms_norm_adj(g_y, u, w, eps, g_sum=None):
     return (g if g_sum is None else g + np.asarray(g_sum, np.float64)), g_w
 
 
+def layer_norm(u, w, b, eps):
+    """(y, mean, rstd) of rows u."""
+    u = np.asarray(u, np.float64)
+    mean = u.mean(axis=1)
+    rstd = 1.0 / np.sqrt(((u - mean[:, None]) ** 2).mean(axis=1) + eps)
+    y = (u - mean[:, None]) * rstd[:, None] * np.asarray(w, np.float64)
+    return y + (0.0 if b is None else np.asarray(b, np.float64)), mean, rstd
+
+
+def layer_norm_adj(g_y, u, w, eps, g_sum=None):
+    """(g_u, g_w, g_b) of layer_norm, g_sum added to g_u."""
+    g_y, u, w = (np.asarray(a, np.float64) for a in (g_y, u, w))
+    _, mean, rstd = layer_norm(u, w, None, eps)
+    n, v = u.shape[1], u - mean[:, None]
+    # d y_c / d u_k = w_c (rstd ([c = k] - 1 / n) - rstd^3 v_c v_k / n)
+    t = g_y * w
+    g = rstd[:, None] * (t - t.sum(axis=1, keepdims=True) / n) - v * ((t * v).sum(axis=1) * rstd ** 3 / n)[:, None]
+    g_w, g_b = (g_y * v * rstd[:, None]).sum(axis=0), g_y.sum(axis=0)
+    return (g if g_sum is None else g + np.asarray(g_sum, np.float64)), g_w, g_b
+
+
 def e4m3(v):
     """Values rounded to the nearest (ties to even) of 4 exponent and 3
     fraction bits, largest 448, smallest step 2^-9."""

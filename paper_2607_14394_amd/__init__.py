@@ -31,6 +31,7 @@ __all__ = [
     "RECURRENCE_SPAN", "code_columns", "scale_columns", "empty_codes", "recurrence_states_shape", "dtst_rms_norm",
     "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
+    "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdtst.so")
@@ -120,6 +121,9 @@ def _load():
         "dtst_rms_norm": [VP] * 9,
         "dtst_rms_norm_adj_workspace": [I64, I64, ctypes.POINTER(SZ)],
         "dtst_rms_norm_adj": [VP] * 10 + [SZ, VP],
+        "dtst_layer_norm": [VP] * 11,
+        "dtst_layer_norm_adj_workspace": [I64, I64, ctypes.POINTER(SZ)],
+        "dtst_layer_norm_adj": [VP] * 12 + [SZ, VP],
         "dtst_quantise": [VP] * 7,
         "dtst_product": [VP] * 8,
         "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
@@ -466,6 +470,76 @@ def dtst_rms_norm_adj(g_y, u, weight, rstd, g_u, g_weight, g_sum=None, g_x=None,
                                    None if g_sum is None else g_sum.data_ptr(), g_u.data_ptr(),
                                    None if g_x is None else g_x.data_ptr(), g_weight.data_ptr(), p, n,
                                    _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+def dtst_layer_norm(x, weight, bias, y, res=None, sum_out=None, scale=None, mean=None, rstd=None, eps=1e-5,
+                    stream=None):
+    """u = x + res into sum_out, y = (u - mean(u)) / std(u) * weight + bias (or
+    None); y in x's type, or codes with their scales.  x, res, sum_out: (rows,
+    cols); mean, rstd: what the backward needs, (rows,) float32."""
+    if x.dim() != 2:
+        raise ValueError("x must be (rows, cols)")
+    shape = rows, cols = x.shape
+    dev, tx = _device(), x.dtype
+    rt = res.dtype if res is not None else tx if sum_out is None else sum_out.dtype
+    ld_x = _rows(x, shape, "x", _FLOATS, dev)
+    ld_res = 0 if res is None else _rows(res, shape, "res", (tx, torch.float32), dev)
+    ld_sum = 0 if sum_out is None else _rows(sum_out, shape, "sum_out", (rt,), dev)
+    if scale is not None:
+        ld_y, ld_scale = _codes(y, scale, rows, cols, "y", dev)
+    else:
+        ld_y, ld_scale = _rows(y, shape, "y", (tx,), dev), 0
+    _vector(weight, cols, "weight", dev)
+    if bias is not None:
+        _vector(bias, cols, "bias", dev)
+    if mean is not None:
+        _vector(mean, rows, "mean", dev)
+    if rstd is not None:
+        _vector(rstd, rows, "rstd", dev)
+    if not rows:  # (as in dtst_rms_norm)
+        return
+    status = lib.dtst_layer_norm(
+        NORM_DESC.pack(rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_scale, _TYPES[tx], _TYPES[rt], _TYPES[y.dtype], eps),
+        x.data_ptr(), None if res is None else res.data_ptr(), weight.data_ptr(),
+        None if bias is None else bias.data_ptr(), None if sum_out is None else sum_out.data_ptr(), y.data_ptr(),
+        None if scale is None else scale.data_ptr(), None if mean is None else mean.data_ptr(),
+        None if rstd is None else rstd.data_ptr(), _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+@functools.lru_cache(maxsize=1024)
+def dtst_layer_norm_adj_workspace(rows, cols) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_layer_norm_adj_workspace(int(rows), int(cols), ctypes.byref(n)))
+    return n.value
+
+
+def dtst_layer_norm_adj(g_y, u, weight, mean, rstd, g_u, g_weight, g_bias, g_sum=None, g_x=None, accumulate=False,
+                        ws=None, stream=None):
+    """Backward of dtst_layer_norm from its stored sum u, mean and rstd: g_u (of
+    x and res alike; g_x the same in g_y's type), g_weight and g_bias."""
+    if g_y.dim() != 2:
+        raise ValueError("g_y must be (rows, cols)")
+    shape = rows, cols = g_y.shape
+    dev, tx, tr = _device(), g_y.dtype, (u.dtype,)
+    d = NORM_ADJ_DESC.pack(rows, cols, _rows(g_y, shape, "g_y", _FLOATS, dev),
+                           _rows(u, shape, "u", (tx, torch.float32), dev),
+                           0 if g_sum is None else _rows(g_sum, shape, "g_sum", tr, dev),
+                           _rows(g_u, shape, "g_u", tr, dev), 0 if g_x is None else _rows(g_x, shape, "g_x", (tx,), dev),
+                           _TYPES[tx], _TYPES[u.dtype], int(accumulate))
+    _vector(weight, cols, "weight", dev)
+    _vector(g_weight, cols, "g_weight", dev)
+    _vector(g_bias, cols, "g_bias", dev)
+    _vector(mean, rows, "mean", dev)
+    _vector(rstd, rows, "rstd", dev)
+    p, n, ws = _scratch(ws, dtst_layer_norm_adj_workspace(rows, cols), g_y.device, stream)
+    status = lib.dtst_layer_norm_adj(d, g_y.data_ptr(), u.data_ptr(), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                     None if g_sum is None else g_sum.data_ptr(), g_u.data_ptr(),
+                                     None if g_x is None else g_x.data_ptr(), g_weight.data_ptr(), g_bias.data_ptr(), p, n,
+                                     _current(dev) if stream is None else int(stream))
     if status:
         _check(status)
 

@@ -14,135 +14,12 @@
 #include <utility>
 
 #include "api_common.h"
+#include "seq_checks.h"
 #include "seq_internal.h"
 
 namespace {
 
 using namespace dtst;
-
-template <class F>
-dtst_status guarded(F&& f) {
-  try {
-    return f();
-  } catch (...) {
-    return DTST_ERR_OUT_OF_MEMORY;  // (the host allocations of messages and event records are all that throws)
-  }
-}
-
-dtst_status bad(const std::string& msg) { return fail(DTST_ERR_INVALID_ARG, msg); }
-
-int type_size(int t) { return t == DTST_F32 ? 4 : t == DTST_E4M3 ? 1 : 2; }
-bool is_float_type(int t) { return t == DTST_F32 || t == DTST_BF16 || t == DTST_F16; }
-
-dtst_status check_align(const void* p, uintptr_t align, const char* name) {
-  if (p == nullptr) return bad(std::string(name) + " is null");
-  if (reinterpret_cast<uintptr_t>(p) % align != 0)
-    return bad(std::string(name) + " is not aligned to " + std::to_string(align) + " bytes");
-  return DTST_OK;
-}
-
-// Element counts and strides whose products stay far inside 64 bits.
-constexpr int64_t kMost = int64_t(1) << 50;
-dtst_status check_extent(int64_t rows, int64_t ld, const char* name) {
-  int64_t n = 0;
-  if (__builtin_mul_overflow(rows, ld, &n) || n > kMost) return bad(std::string(name) + " is too large");
-  return DTST_OK;
-}
-
-// A strided (rows, cols) array.
-struct Array {
-  const void* p;
-  int64_t rows, cols, ld;
-  int size;
-  const char* name;
-};
-
-dtst_status check_array(const Array& a, uintptr_t align) {
-  DTST_TRY(check_align(a.p, align, a.name));
-  if (a.ld < a.cols) return bad(std::string("stride of ") + a.name + " is below its row");
-  return check_extent(a.rows, a.ld * a.size, a.name);
-}
-
-// The rows of a strided array in bytes: `outer` groups of `inner` rows of `row`
-// bytes, each group's rows before the next group's first.
-struct Rows {
-  int64_t at, outer, outer_ld, inner, inner_ld, row;
-};
-bool is_dense(const Rows& r) {
-  return (r.inner <= 1 || r.inner_ld == r.row) && (r.outer <= 1 || r.outer_ld == r.inner * r.row);
-}
-int64_t extent(const Rows& r) { return (r.outer - 1) * r.outer_ld + (r.inner - 1) * r.inner_ld + r.row; }
-
-// Whether a row of r has a byte of [at, at + n).
-bool share(const Rows& r, int64_t at, int64_t n) {
-  const int64_t most = at + n - 1 - r.at;                           // a row that does starts here at the latest,
-  const int64_t least = std::max<int64_t>(at - r.row + 1 - r.at, 0);  // here at the earliest
-  if (n <= 0 || most < least) return false;
-  const int64_t o = r.outer_ld > 0 ? std::min(least / r.outer_ld, r.outer - 1) : 0, rest = least - o * r.outer_ld;
-  const int64_t i = r.inner_ld > 0 ? (rest + r.inner_ld - 1) / r.inner_ld : rest > 0 ? r.inner : 0;
-  if (i < r.inner) return o * r.outer_ld + i * r.inner_ld <= most;
-  return o + 1 < r.outer && (o + 1) * r.outer_ld <= most;
-}
-
-Rows rows_of(const Array& a) {
-  return Rows{int64_t(reinterpret_cast<uintptr_t>(a.p)), a.rows, a.rows > 1 ? a.ld * a.size : 0, 1, 0, a.cols * a.size};
-}
-
-// Whether two arrays share an element.  Column ranges of one array (equal row
-// strides, rows apart) do not; of unlike strides, where neither is without gaps,
-// those that reach into each other's range are taken to.
-bool share(const Array& a, const Array& b) {
-  if (a.p == nullptr || b.p == nullptr || a.rows < 1 || b.rows < 1) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
-  const uintptr_t la = uintptr_t(a.ld) * a.size, lb = uintptr_t(b.ld) * b.size;
-  const uintptr_t wa = uintptr_t(a.cols) * a.size, wb = uintptr_t(b.cols) * b.size;
-  const uintptr_t ea = pa + (a.rows - 1) * la + wa, eb = pb + (b.rows - 1) * lb + wb;
-  if (pa >= eb || pb >= ea) return false;
-  const Rows ra = rows_of(a), rb = rows_of(b);
-  if (is_dense(ra)) return share(rb, ra.at, extent(ra));
-  if (is_dense(rb)) return share(ra, rb.at, extent(rb));
-  if (la == lb && a.rows > 1 && b.rows > 1) {
-    const uintptr_t off = pb >= pa ? (pb - pa) % la : (la - (pa - pb) % la) % la;  // b's column 0 in a's rows
-    return off < wa || la - off < wb;
-  }
-  return true;
-}
-
-bool same(const Array& a, const Array& b) { return a.p == b.p && (a.ld == b.ld || a.rows <= 1) && a.size == b.size; }
-
-dtst_status check_apart(const Array& out, const Array& other, bool may_be_same) {
-  if (share(out, other) && !(may_be_same && same(out, other)))
-    return bad(std::string(out.name) + " and " + other.name + " overlap");
-  return DTST_OK;
-}
-
-// Codes and scales of an 8-bit (rows, k) array.
-Array codes_of(const void* p, int64_t rows, int64_t k, int64_t ld, const char* name) {
-  return Array{p, rows, (k + 127) / 128 * 128, ld, 1, name};
-}
-Array scales_of(const void* p, int64_t rows, int64_t k, int64_t ld, const char* name) {
-  return Array{p, rows, ((k + 127) / 128 + 3) / 4 * 4, ld, 1, name};
-}
-dtst_status check_codes(const Array& q, const Array& s) {
-  DTST_TRY(check_array(q, 16));
-  DTST_TRY(check_array(s, 4));
-  if (q.ld % 16 != 0) return bad(std::string("stride of ") + q.name + " is no multiple of 16");
-  if (s.ld % 4 != 0) return bad(std::string("stride of ") + s.name + " is no multiple of 4");
-  return DTST_OK;
-}
-
-// Workgroups of a launch: a dimension holds fewer than 2^32 threads.
-dtst_status check_grid(int64_t groups, int64_t threads) {
-  if (groups > (int64_t(1) << 32) / threads - 1) return fail(DTST_ERR_UNSUPPORTED, "too many rows for one launch");
-  return DTST_OK;
-}
-
-dtst_status check_workspace(const void* ws, size_t have, size_t need) {
-  if (need == 0) return DTST_OK;
-  if (have < need)
-    return bad("workspace too small: need " + std::to_string(need) + " bytes, got " + std::to_string(have));
-  return check_ptr(ws, "workspace");
-}
 
 dtst_status check_norm_types(int x_type, int res_type) {
   if (!is_float_type(x_type)) return bad("x_type must be DTST_F32, DTST_BF16 or DTST_F16");
@@ -155,8 +32,9 @@ dtst_status check_rows_cols(int64_t rows, int64_t cols) {
   return DTST_OK;
 }
 
-dtst_status rms_norm(const dtst_norm_desc* d, const void* x, const void* res, const float* weight, void* sum_out,
-                     void* y, void* scale, float* rstd, void* stream) {
+// RMS norm, and layer norm with `layer` (bias and mean are null without).
+dtst_status norm(bool layer, const dtst_norm_desc* d, const void* x, const void* res, const float* weight,
+                 const float* bias, void* sum_out, void* y, void* scale, float* mean, float* rstd, void* stream) {
   if (d == nullptr) return bad("descriptor is null");
   DTST_TRY(check_rows_cols(d->rows, d->cols));
   DTST_TRY(check_norm_types(d->x_type, d->res_type));
@@ -172,35 +50,42 @@ dtst_status rms_norm(const dtst_norm_desc* d, const void* x, const void* res, co
   const Array ay = q8 ? codes_of(y, d->rows, d->cols, d->ld_y, "y") : Array{y, d->rows, d->cols, d->ld_y, sx, "y"};
   const Array asc = scales_of(scale, d->rows, d->cols, d->ld_scale, "scale");
   const Array aw{weight, 1, d->cols, d->cols, 4, "weight"}, art{rstd, 1, d->rows, d->rows, 4, "rstd"};
+  const Array ab{bias, 1, d->cols, d->cols, 4, "bias"}, am{mean, 1, d->rows, d->rows, 4, "mean"};
   DTST_TRY(check_array(ax, sx));
   DTST_TRY(check_align(weight, 4, "weight"));
+  if (bias) DTST_TRY(check_align(bias, 4, "bias"));
+  if (mean) DTST_TRY(check_align(mean, 4, "mean"));
   if (res) DTST_TRY(check_array(ar, sr));
   if (sum_out) DTST_TRY(check_array(as, sr));
   if (rstd) DTST_TRY(check_align(rstd, 4, "rstd"));
   DTST_TRY(q8 ? check_codes(ay, asc) : check_array(ay, sx));
-  const NormGrid grid = rms_norm_grid(d->rows, d->cols);
+  const NormGrid grid = norm_grid(d->rows, d->cols);
   DTST_TRY(check_grid(grid.groups, grid.threads));
   DTST_TRY(check_apart(as, ar, true));
   DTST_TRY(check_apart(as, ax, res == nullptr));
   DTST_TRY(check_apart(ay, ax, !q8));
-  for (const Array* out : {&as, &ay, &asc, &art}) DTST_TRY(check_apart(*out, aw, false));
-  for (const Array* in : {&ax, &ar}) {
-    DTST_TRY(check_apart(asc, *in, false));
-    DTST_TRY(check_apart(art, *in, false));
+  for (const Array* out : {&as, &ay, &asc, &art, &am}) {
+    DTST_TRY(check_apart(*out, aw, false));
+    DTST_TRY(check_apart(*out, ab, false));
   }
+  for (const Array* in : {&ax, &ar})
+    for (const Array* out : {&asc, &art, &am}) DTST_TRY(check_apart(*out, *in, false));
   DTST_TRY(check_apart(ay, ar, false));
   DTST_TRY(check_apart(ay, as, false));
   DTST_TRY(check_apart(asc, ay, false));
   DTST_TRY(check_apart(asc, as, false));
-  for (const Array* out : {&as, &ay, &asc}) DTST_TRY(check_apart(art, *out, false));
-  const int e = timed(K_NORM, stream,
-                      [&] { return launch_rms_norm(*d, x, res, weight, sum_out, y, scale, rstd, stream); });
+  for (const Array* out : {&as, &ay, &asc, &am}) DTST_TRY(check_apart(art, *out, false));
+  for (const Array* out : {&as, &ay, &asc}) DTST_TRY(check_apart(am, *out, false));
+  const int e = timed(layer ? K_LAYER_NORM : K_NORM, stream, [&] {
+    return layer ? launch_layer_norm(*d, x, res, weight, bias, sum_out, y, scale, mean, rstd, stream)
+                 : launch_rms_norm(*d, x, res, weight, sum_out, y, scale, rstd, stream);
+  });
   return device_status(e, "norm launch");
 }
 
-dtst_status rms_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
-                         const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight, void* workspace,
-                         size_t workspace_bytes, void* stream) {
+dtst_status norm_adj(bool layer, const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
+                     const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight,
+                     float* g_bias, void* workspace, size_t workspace_bytes, void* stream) {
   if (d == nullptr) return bad("descriptor is null");
   DTST_TRY(check_rows_cols(d->rows, d->cols));
   DTST_TRY(check_norm_types(d->x_type, d->res_type));
@@ -211,32 +96,45 @@ dtst_status rms_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const voi
   const Array as{g_sum, d->rows, d->cols, d->ld_g_sum, sr, "g_sum"};
   const Array agu{g_u, d->rows, d->cols, d->ld_g_u, sr, "g_u"}, agx{g_x, d->rows, d->cols, d->ld_g_x, sx, "g_x"};
   const Array aw{weight, 1, d->cols, d->cols, 4, "weight"}, art{rstd, 1, d->rows, d->rows, 4, "rstd"};
-  const Array agw{g_weight, 1, d->cols, d->cols, 4, "g_weight"};
-  const size_t need = rms_norm_adj_workspace(d->rows, d->cols);
+  const Array agw{g_weight, 1, d->cols, d->cols, 4, "g_weight"}, agb{g_bias, 1, d->cols, d->cols, 4, "g_bias"};
+  const Array am{mean, 1, d->rows, d->rows, 4, "mean"};
+  const size_t need = layer ? layer_norm_adj_workspace(d->rows, d->cols) : rms_norm_adj_workspace(d->rows, d->cols);
   const Array aws{workspace, 1, int64_t(need), int64_t(need), 1, "workspace"};
   DTST_TRY(check_align(g_weight, 4, "g_weight"));
+  if (layer) DTST_TRY(check_align(g_bias, 4, "g_bias"));
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   if (d->rows > 0) {
     DTST_TRY(check_array(ag, sx));
     DTST_TRY(check_array(au, sr));
     DTST_TRY(check_align(weight, 4, "weight"));
+    if (layer) DTST_TRY(check_align(mean, 4, "mean"));
     DTST_TRY(check_align(rstd, 4, "rstd"));
     if (g_sum) DTST_TRY(check_array(as, sr));
     DTST_TRY(check_array(agu, sr));
     if (g_x) DTST_TRY(check_array(agx, sx));
     DTST_TRY(check_apart(agu, as, true));
-    for (const Array* in : {&ag, &au, &aw, &art}) DTST_TRY(check_apart(agu, *in, false));
-    for (const Array* in : {&ag, &au, &as, &aw, &art, &agu}) DTST_TRY(check_apart(agx, *in, false));
-    for (const Array* in : {&ag, &au, &as, &aw, &art, &agu, &agx}) {
-      DTST_TRY(check_apart(agw, *in, false));
-      DTST_TRY(check_apart(aws, *in, false));
-    }
+    for (const Array* in : {&ag, &au, &aw, &am, &art}) DTST_TRY(check_apart(agu, *in, false));
+    for (const Array* in : {&ag, &au, &as, &aw, &am, &art, &agu}) DTST_TRY(check_apart(agx, *in, false));
+    for (const Array* in : {&ag, &au, &as, &aw, &am, &art, &agu, &agx})
+      for (const Array* out : {&agw, &agb, &aws}) DTST_TRY(check_apart(*out, *in, false));
   }
   DTST_TRY(check_apart(aws, agw, false));
-  const int e = timed(K_NORM_ADJ, stream, [&] {
-    return launch_rms_norm_adj(*d, g_y, u, weight, rstd, g_sum, g_u, g_x, g_weight, workspace, stream);
+  DTST_TRY(check_apart(aws, agb, false));
+  DTST_TRY(check_apart(agw, agb, false));
+  const int e = timed(layer ? K_LAYER_NORM_ADJ : K_NORM_ADJ, stream, [&] {
+    return layer ? launch_layer_norm_adj(*d, g_y, u, weight, mean, rstd, g_sum, g_u, g_x, g_weight, g_bias, workspace,
+                                         stream)
+                 : launch_rms_norm_adj(*d, g_y, u, weight, rstd, g_sum, g_u, g_x, g_weight, workspace, stream);
   });
   return device_status(e, "norm backward launch");
+}
+
+dtst_status norm_adj_workspace(bool layer, int64_t rows, int64_t cols, size_t* bytes) {
+  if (bytes == nullptr) return bad("bytes is null");
+  DTST_TRY(check_rows_cols(rows, cols));
+  if (cols > kNormMaxCols) return fail(DTST_ERR_UNSUPPORTED, "cols above " + std::to_string(kNormMaxCols));
+  *bytes = layer ? layer_norm_adj_workspace(rows, cols) : rms_norm_adj_workspace(rows, cols);
+  return ok();
 }
 
 dtst_status quantise(const dtst_quantise_desc* d, const void* x, void* q, void* scale, void* qt, void* scale_t,
@@ -291,28 +189,6 @@ dtst_status product(const dtst_product_desc* d, const void* a, const void* a_sca
   return device_status(e, "product launch");
 }
 
-// A (batch, steps, features) array with strides of batch entries and steps.
-struct Sequence {
-  const void* p;
-  const int64_t* st;
-  const char* name;
-};
-
-dtst_status check_sequence(const dtst_recurrence_desc* d, const Sequence& s, int size) {
-  DTST_TRY(check_align(s.p, size, s.name));
-  const int64_t sb = s.st[0], t = s.st[1];
-  if ((d->steps > 1 && t < d->features) || (d->batch > 1 && sb < d->features) || sb < 0 || t < 0)
-    return bad(std::string("strides of ") + s.name + " are below its rows");
-  // entries apart from each other: step rows inside an entry's stride, or entries inside a step's
-  if (d->batch > 1 && d->steps > 1) {
-    const bool by_entry = sb / t >= d->steps || (sb - (d->steps - 1) * t >= d->features && sb >= t);
-    const bool by_step = t / sb >= d->batch || (t - (d->batch - 1) * sb >= d->features && t >= sb);
-    if (!by_entry && !by_step) return bad(std::string("rows of ") + s.name + " overlap");
-  }
-  DTST_TRY(check_extent(d->batch, sb * size, s.name));
-  return check_extent(d->steps, t * size, s.name);
-}
-
 dtst_status check_sequence_sizes(const dtst_recurrence_desc* d) {
   if (d == nullptr) return bad("descriptor is null");
   if (d->batch < 0 || d->steps < 0 || d->features < 0) return bad("need batch, steps and features >= 0");
@@ -328,65 +204,14 @@ dtst_status check_sequence_sizes(const dtst_recurrence_desc* d) {
   return DTST_OK;
 }
 
-// (Of a sequence whose strides check_sequence takes.)
-Rows rows_of(const dtst_recurrence_desc* d, const Sequence& s, int size) {
-  Rows r{int64_t(reinterpret_cast<uintptr_t>(s.p)), d->batch, s.st[0] * size, d->steps, s.st[1] * size, d->features * size};
-  if (r.outer <= 1) r.outer_ld = 0;
-  if (r.inner <= 1) r.inner_ld = 0;
-  if (r.outer_ld < r.inner_ld) std::swap(r.outer, r.inner), std::swap(r.outer_ld, r.inner_ld);
-  return r;
-}
-
-// Whether two sequences share an element.  Of unlike strides, where neither is
-// without gaps, only a common first element tells.
-bool share(const dtst_recurrence_desc* d, const Sequence& a, const Sequence& b, int size) {
-  if (a.p == nullptr || b.p == nullptr || d->steps < 1) return false;
-  const Rows ra = rows_of(d, a, size), rb = rows_of(d, b, size);
-  if (ra.at >= rb.at + extent(rb) || rb.at >= ra.at + extent(ra)) return false;
-  if (is_dense(ra)) return share(rb, ra.at, extent(ra));
-  if (is_dense(rb)) return share(ra, rb.at, extent(rb));
-  if (ra.outer != rb.outer || ra.outer_ld != rb.outer_ld || ra.inner_ld != rb.inner_ld) return ra.at == rb.at;
-  // Rows of the two lie j outer and i inner strides less delta apart: the nearest
-  // of either sign.
-  const auto below = [](int64_t x, int64_t ld) { return ld > 0 ? (x >= 0 ? x / ld : -((ld - 1 - x) / ld)) : 0; };
-  const int64_t delta = rb.at - ra.at, j0 = below(delta, ra.outer_ld);
-  for (int64_t j = j0; j <= j0 + 1; ++j) {
-    if (j <= -ra.outer || j >= ra.outer) continue;
-    const int64_t rest = delta - j * ra.outer_ld, i0 = below(rest, ra.inner_ld);
-    for (int64_t i = i0; i <= i0 + 1; ++i)
-      if (i > -ra.inner && i < ra.inner && std::abs(rest - i * ra.inner_ld) < ra.row) return true;
-  }
-  return false;
-}
-
 // (one workgroup of 64 lanes a step's features, or of 512 for each 128 steps)
 dtst_status check_recurrence_grid(const dtst_recurrence_desc* d) {
   const int64_t tiles = d->batch * ((d->features + 63) / 64), spans = (d->steps + 127) / 128;
   return check_grid(tiles * (spans > 0 ? spans : 1), d->steps <= 1 ? 64 : 512);
 }
 
-dtst_status check_no_share(const dtst_recurrence_desc* d, const Sequence& out, const Sequence& other, int size) {
-  if (share(d, out, other, size)) return bad(std::string(out.name) + " and " + other.name + " overlap");
-  return DTST_OK;
-}
-
-// An array without gaps: states, lengths, the workspace.
-struct Block {
-  const void* p;
-  int64_t bytes;
-  const char* name;
-};
-dtst_status check_no_share(const Block& out, const Block& other) {
-  if (out.p == nullptr || other.p == nullptr || out.bytes <= 0 || other.bytes <= 0) return DTST_OK;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(out.p), b = reinterpret_cast<uintptr_t>(other.p);
-  if (a < b + uintptr_t(other.bytes) && b < a + uintptr_t(out.bytes)) return bad(std::string(out.name) + " and " + other.name + " overlap");
-  return DTST_OK;
-}
-dtst_status check_no_share(const dtst_recurrence_desc* d, const Sequence& s, const Block& b, int size) {
-  if (s.p == nullptr || b.p == nullptr || d->steps < 1) return DTST_OK;
-  if (share(rows_of(d, s, size), int64_t(reinterpret_cast<uintptr_t>(b.p)), b.bytes))
-    return bad(std::string(s.name) + " and " + b.name + " overlap");
-  return DTST_OK;
+Sequence sequence_of(const dtst_recurrence_desc* d, const void* p, const int64_t (&st)[2], const char* name) {
+  return Sequence{p, d->batch, d->steps, d->features, st, type_size(d->type), name};
 }
 Block of_features(const dtst_recurrence_desc* d, const void* p, int64_t rows, const char* name) {
   return Block{p, d->batch * d->features * rows * 4, name};
@@ -397,14 +222,14 @@ dtst_status recurrence(const dtst_recurrence_desc* d, const void* z, const void*
                        size_t workspace_bytes, void* stream) {
   DTST_TRY(check_sequence_sizes(d));
   if (d->batch == 0 || d->features == 0) return ok();
-  const int size = type_size(d->type);
-  const Sequence sz{z, d->z_stride, "z"}, sv{v, d->v_stride, "v"}, so{o, d->o_stride, "o"}, sy{y, d->y_stride, "y"};
+  const Sequence sz = sequence_of(d, z, d->z_stride, "z"), sv = sequence_of(d, v, d->v_stride, "v");
+  const Sequence so = sequence_of(d, o, d->o_stride, "o"), sy = sequence_of(d, y, d->y_stride, "y");
   if (d->steps > 0) {
-    DTST_TRY(check_sequence(d, sz, size));
-    DTST_TRY(check_sequence(d, sv, size));
-    if (o) DTST_TRY(check_sequence(d, so, size));
-    DTST_TRY(check_sequence(d, sy, size));
-    for (const Sequence* in : {&sz, &sv, &so}) DTST_TRY(check_no_share(d, sy, *in, size));
+    DTST_TRY(check_sequence(sz));
+    DTST_TRY(check_sequence(sv));
+    if (o) DTST_TRY(check_sequence(so));
+    DTST_TRY(check_sequence(sy));
+    for (const Sequence* in : {&sz, &sv, &so}) DTST_TRY(check_no_share(sy, *in));
   }
   if (h_zero) DTST_TRY(check_align(h_zero, 4, "h_zero"));
   if (h_out) DTST_TRY(check_align(h_out, 4, "h_out"));
@@ -416,9 +241,9 @@ dtst_status recurrence(const dtst_recurrence_desc* d, const void* z, const void*
   const Block bin = of_features(d, h_zero, 1, "h_zero"), bout = of_features(d, h_out, 1, "h_out");
   const Block bst = of_features(d, states, (d->steps + 127) / 128, "states"), bn{lengths, d->batch * 4, "lengths"};
   const Block bws{need ? workspace : nullptr, int64_t(need), "workspace"};
-  for (const Block* b : {&bin, &bn, &bout, &bst, &bws}) DTST_TRY(check_no_share(d, sy, *b, size));
+  for (const Block* b : {&bin, &bn, &bout, &bst, &bws}) DTST_TRY(check_no_share(sy, *b));
   for (const Block* out : {&bout, &bst, &bws}) {
-    for (const Sequence* in : {&sz, &sv, &so}) DTST_TRY(check_no_share(d, *in, *out, size));
+    for (const Sequence* in : {&sz, &sv, &so}) DTST_TRY(check_no_share(*in, *out));
     if (out != &bout || h_out != h_zero) DTST_TRY(check_no_share(*out, bin));
     DTST_TRY(check_no_share(*out, bn));
   }
@@ -438,19 +263,20 @@ dtst_status recurrence_adj(const dtst_recurrence_desc* d, const void* z, const v
   DTST_TRY(check_sequence_sizes(d));
   if (d->batch == 0 || d->features == 0) return ok();
   if ((o != nullptr) != (g_o != nullptr) && d->steps > 0) return bad("g_o goes with o");
-  const int size = type_size(d->type);
-  const Sequence sz{z, d->z_stride, "z"}, sv{v, d->v_stride, "v"}, so{o, d->o_stride, "o"}, sg{g_y, d->y_stride, "g_y"};
-  const Sequence gz{g_z, d->g_z_stride, "g_z"}, gv{g_v, d->g_v_stride, "g_v"}, go{g_o, d->g_o_stride, "g_o"};
+  const Sequence sz = sequence_of(d, z, d->z_stride, "z"), sv = sequence_of(d, v, d->v_stride, "v");
+  const Sequence so = sequence_of(d, o, d->o_stride, "o"), sg = sequence_of(d, g_y, d->y_stride, "g_y");
+  const Sequence gz = sequence_of(d, g_z, d->g_z_stride, "g_z"), gv = sequence_of(d, g_v, d->g_v_stride, "g_v");
+  const Sequence go = sequence_of(d, g_o, d->g_o_stride, "g_o");
   if (d->steps > 0) {
-    for (const Sequence* s : {&sz, &sv, &sg, &gz, &gv}) DTST_TRY(check_sequence(d, *s, size));
+    for (const Sequence* s : {&sz, &sv, &sg, &gz, &gv}) DTST_TRY(check_sequence(*s));
     if (o)
-      for (const Sequence* s : {&so, &go}) DTST_TRY(check_sequence(d, *s, size));
+      for (const Sequence* s : {&so, &go}) DTST_TRY(check_sequence(*s));
     DTST_TRY(check_align(states, 4, "states"));
     for (const Sequence* in : {&sz, &sv, &so, &sg})
-      for (const Sequence* out : {&gz, &gv, &go}) DTST_TRY(check_no_share(d, *out, *in, size));
-    DTST_TRY(check_no_share(d, gz, gv, size));
-    DTST_TRY(check_no_share(d, gz, go, size));
-    DTST_TRY(check_no_share(d, gv, go, size));
+      for (const Sequence* out : {&gz, &gv, &go}) DTST_TRY(check_no_share(*out, *in));
+    DTST_TRY(check_no_share(gz, gv));
+    DTST_TRY(check_no_share(gz, go));
+    DTST_TRY(check_no_share(gv, go));
   }
   if (g_h) DTST_TRY(check_align(g_h, 4, "g_h"));
   if (g_hzero) DTST_TRY(check_align(g_hzero, 4, "g_hzero"));
@@ -462,9 +288,9 @@ dtst_status recurrence_adj(const dtst_recurrence_desc* d, const void* z, const v
   const Block bin = of_features(d, g_h, 1, "g_h"), bout = of_features(d, g_hzero, 1, "g_hzero");
   const Block bn{lengths, d->batch * 4, "lengths"}, bws{need ? workspace : nullptr, int64_t(need), "workspace"};
   for (const Sequence* out : {&gz, &gv, &go})
-    for (const Block* b : {&bst, &bin, &bn, &bout, &bws}) DTST_TRY(check_no_share(d, *out, *b, size));
+    for (const Block* b : {&bst, &bin, &bn, &bout, &bws}) DTST_TRY(check_no_share(*out, *b));
   for (const Block* out : {&bout, &bws}) {
-    for (const Sequence* in : {&sz, &sv, &so, &sg}) DTST_TRY(check_no_share(d, *in, *out, size));
+    for (const Sequence* in : {&sz, &sv, &so, &sg}) DTST_TRY(check_no_share(*in, *out));
     DTST_TRY(check_no_share(*out, bst));
     if (out != &bout || g_hzero != g_h) DTST_TRY(check_no_share(*out, bin));
     DTST_TRY(check_no_share(*out, bn));
@@ -482,24 +308,38 @@ extern "C" {
 
 dtst_status dtst_rms_norm(const dtst_norm_desc* d, const void* x, const void* res, const float* weight, void* sum_out,
                           void* y, void* scale, float* rstd, void* stream) {
-  return guarded([&] { return rms_norm(d, x, res, weight, sum_out, y, scale, rstd, stream); });
+  return guarded([&] { return norm(false, d, x, res, weight, nullptr, sum_out, y, scale, nullptr, rstd, stream); });
 }
 
 dtst_status dtst_rms_norm_adj_workspace(int64_t rows, int64_t cols, size_t* bytes) {
-  return guarded([&] {
-    if (bytes == nullptr) return bad("bytes is null");
-    DTST_TRY(check_rows_cols(rows, cols));
-    if (cols > kNormMaxCols) return fail(DTST_ERR_UNSUPPORTED, "cols above " + std::to_string(kNormMaxCols));
-    *bytes = rms_norm_adj_workspace(rows, cols);
-    return ok();
-  });
+  return guarded([&] { return norm_adj_workspace(false, rows, cols, bytes); });
 }
 
 dtst_status dtst_rms_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
                               const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight,
                               void* workspace, size_t workspace_bytes, void* stream) {
   return guarded([&] {
-    return rms_norm_adj(d, g_y, u, weight, rstd, g_sum, g_u, g_x, g_weight, workspace, workspace_bytes, stream);
+    return norm_adj(false, d, g_y, u, weight, nullptr, rstd, g_sum, g_u, g_x, g_weight, nullptr, workspace,
+                    workspace_bytes, stream);
+  });
+}
+
+dtst_status dtst_layer_norm(const dtst_norm_desc* d, const void* x, const void* res, const float* weight,
+                            const float* bias, void* sum_out, void* y, void* scale, float* mean, float* rstd,
+                            void* stream) {
+  return guarded([&] { return norm(true, d, x, res, weight, bias, sum_out, y, scale, mean, rstd, stream); });
+}
+
+dtst_status dtst_layer_norm_adj_workspace(int64_t rows, int64_t cols, size_t* bytes) {
+  return guarded([&] { return norm_adj_workspace(true, rows, cols, bytes); });
+}
+
+dtst_status dtst_layer_norm_adj(const dtst_norm_adj_desc* d, const void* g_y, const void* u, const float* weight,
+                                const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x,
+                                float* g_weight, float* g_bias, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&] {
+    return norm_adj(true, d, g_y, u, weight, mean, rstd, g_sum, g_u, g_x, g_weight, g_bias, workspace, workspace_bytes,
+                    stream);
   });
 }
 

@@ -1,8 +1,10 @@
-// RMS norm with the residual's addition, and its backward (dtst_rms_norm,
-// dtst_rms_norm_adj).
+// RMS norm and layer norm with the residual's addition, and their backward
+// (dtst_rms_norm, dtst_rms_norm_adj; MEAN: dtst_layer_norm, dtst_layer_norm_adj).
 //
 //   u = x + res,  r = 1 / sqrt(mean u^2 + eps),  y = u r w
 //   g_u = r (t - h mean(t h)) + g_sum,  t = g_y w,  h = u r;   g_w = sum_rows g_y h
+// MEAN: v = u - mean u in the place of u, y = v r w + b,
+//   g_u = r (t - mean t - h mean(t h)) + g_sum,   g_b = sum_rows g_y
 //
 // A few operations per value: bound by HBM.  A row stays in the registers of
 // its RW waves between the sum and the result, so each array is read or written
@@ -44,6 +46,7 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 
 // The same in 64 bits from 16 lanes' sums on: there the last additions, whose
 // roundings weigh most, cost a few instructions a row.
+// (A second call on the same slots needs a barrier before it where RW > 1.)
 template <int RW>
 __device__ __forceinline__ double row_sum64(float v, double* part) {
 #pragma unroll
@@ -72,13 +75,14 @@ __device__ __forceinline__ float rsqrt_of(double m) {
 
 // RW waves a row, V vectors of 8 columns a lane: up to 512 RW V columns.  A
 // workgroup holds max(RW, 4) waves, so four rows with RW = 1.
-template <class TX, class TR, bool Q8, int RW, int V>
+template <class TX, class TR, bool Q8, int RW, int V, bool MEAN>
 __global__ void __launch_bounds__(RW > 4 ? RW * 64 : 256)
-rms_norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const float* __restrict__ w, TR* sum_out,
-                void* y, uint8_t* scale, float* rstd) {
+norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const float* __restrict__ w,
+            const float* __restrict__ b, TR* sum_out, void* y, uint8_t* scale, float* mean_out, float* rstd) {
   constexpr int ROWS = RW > 4 ? 1 : 4 / RW;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  __shared__ double part[RW];
+  __shared__ double part[RW], part2[RW], part3[RW];
+  double mean = 0.0;
   const int64_t row = int64_t(blockIdx.x) * ROWS + wave / RW;
   if (ROWS > 1 && row >= d.rows) return;  // (one wave a row: no barrier follows)
   const int first = ((wave % RW) * 64 + lane) * VEC;
@@ -106,27 +110,68 @@ rms_norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, c
 #pragma unroll
       for (int j = 0; j < VEC; ++j) u[i][j] = float(TR(u[i][j]));
   }
-  float ss = 0.f;
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) ss += u[i][j] * u[i][j];
-  const float r = rsqrt_of(row_sum64<RW>(ss, part) * inv_cols + double(d.eps));
-  if (rstd != nullptr && first == 0) rstd[row] = r;
-  if (sum_out != nullptr) {
+  const auto store_sum = [&] {
+    if (sum_out == nullptr) return;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = first + i * RW * 64 * VEC;
       store_n<VEC>(sum_out + row * d.ld_sum + c, cols - c, u[i]);
     }
+  };
+  float s = 0.f;
+  if constexpr (MEAN) {
+    // Deviations from a mean in 32 bits, which a mean far above them shifts all
+    // alike by the roundings of its sum: what they have in common, `low`, is taken
+    // off them below.
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s += u[i][j];
+    const float high = float(row_sum64<RW>(s, part2) * inv_cols);
+    store_sum();
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int64_t c = first + i * RW * 64 * VEC;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        u[i][j] = c + j < cols ? u[i][j] - high : 0.f;
+        s += u[i][j];
+      }
+    }
+    mean = high;
   }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) ss += u[i][j] * u[i][j];
+  double low = 0.0, square;
+  if constexpr (MEAN) {
+    low = row_sum64<RW>(s, part3) * inv_cols;
+    mean += low;
+    square = row_sum64<RW>(ss, part) * inv_cols - low * low;
+    if (square < 0.0) square = 0.0;  // (no number stays)
+  } else {
+    square = row_sum64<RW>(ss, part) * inv_cols;
+  }
+  const float r = rsqrt_of(square + double(d.eps)), shift = float(low);
+  if (MEAN && mean_out != nullptr && first == 0) mean_out[row] = float(mean);
+  if (rstd != nullptr && first == 0) rstd[row] = r;
+  if constexpr (!MEAN) store_sum();
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int64_t c = first + i * RW * 64 * VEC;
     float wv[VEC];
     load_n<VEC>(w + c, cols - c, wv);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u[i][j] = u[i][j] * r * wv[j];
+    for (int j = 0; j < VEC; ++j) u[i][j] = (MEAN ? u[i][j] - shift : u[i][j]) * r * wv[j];
+    if (MEAN && b != nullptr) {
+      float bv[VEC];
+      load_n<VEC>(b + c, cols - c, bv);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) u[i][j] += bv[j];
+    }
     if constexpr (Q8) {
       if (c + VEC > cols) {  // (not by the product: 1 / rms may be no number)
 #pragma unroll
@@ -146,55 +191,61 @@ rms_norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, c
   }
 }
 
-template <class TX, class TR, bool Q8, int RW, int V>
-int launch_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* w, void* sum_out, void* y,
-                void* scale, float* rstd, hipStream_t s) {
-  const NormGrid g = rms_norm_grid(d.rows, d.cols);
-  hipLaunchKernelGGL((rms_norm_kernel<TX, TR, Q8, RW, V>), dim3(unsigned(g.groups)), dim3(g.threads), 0, s, d,
-                     1.0 / double(d.cols),
-                     static_cast<const TX*>(x), static_cast<const TR*>(res), w, static_cast<TR*>(sum_out), y,
-                     static_cast<uint8_t*>(scale), rstd);
+struct NormArgs {
+  const void *x, *res;
+  const float *w, *b;
+  void *sum_out, *y, *scale;
+  float *mean, *rstd;
+};
+
+template <class TX, class TR, bool Q8, int RW, int V, bool MEAN>
+int launch_norm(const dtst_norm_desc& d, const NormArgs& a, hipStream_t s) {
+  const NormGrid g = norm_grid(d.rows, d.cols);
+  hipLaunchKernelGGL((norm_kernel<TX, TR, Q8, RW, V, MEAN>), dim3(unsigned(g.groups)), dim3(g.threads), 0, s, d,
+                     1.0 / double(d.cols), static_cast<const TX*>(a.x), static_cast<const TR*>(a.res), a.w, a.b,
+                     static_cast<TR*>(a.sum_out), a.y, static_cast<uint8_t*>(a.scale), a.mean, a.rstd);
   return hipGetLastError();
 }
 
-template <class TX, class TR, bool Q8>
-int launch_norm_cols(const dtst_norm_desc& d, const void* x, const void* res, const float* w, void* sum_out, void* y,
-                     void* scale, float* rstd, hipStream_t s) {
+template <class TX, class TR, bool Q8, bool MEAN>
+int launch_norm_cols(const dtst_norm_desc& d, const NormArgs& a, hipStream_t s) {
   const int64_t c = d.cols;
-  if (c <= 512) return launch_norm<TX, TR, Q8, 1, 1>(d, x, res, w, sum_out, y, scale, rstd, s);
-  if (c <= 1024) return launch_norm<TX, TR, Q8, 1, 2>(d, x, res, w, sum_out, y, scale, rstd, s);
-  if (c <= 2048) return launch_norm<TX, TR, Q8, 4, 1>(d, x, res, w, sum_out, y, scale, rstd, s);
-  if (c <= 4096) return launch_norm<TX, TR, Q8, 4, 2>(d, x, res, w, sum_out, y, scale, rstd, s);
-  if (c <= 8192) return launch_norm<TX, TR, Q8, 4, 4>(d, x, res, w, sum_out, y, scale, rstd, s);
-  if (c <= 16384) return launch_norm<TX, TR, Q8, 16, 2>(d, x, res, w, sum_out, y, scale, rstd, s);
-  return launch_norm<TX, TR, Q8, 16, 4>(d, x, res, w, sum_out, y, scale, rstd, s);
+  if (c <= 512) return launch_norm<TX, TR, Q8, 1, 1, MEAN>(d, a, s);
+  if (c <= 1024) return launch_norm<TX, TR, Q8, 1, 2, MEAN>(d, a, s);
+  if (c <= 2048) return launch_norm<TX, TR, Q8, 4, 1, MEAN>(d, a, s);
+  if (c <= 4096) return launch_norm<TX, TR, Q8, 4, 2, MEAN>(d, a, s);
+  if (c <= 8192) return launch_norm<TX, TR, Q8, 4, 4, MEAN>(d, a, s);
+  if (c <= 16384) return launch_norm<TX, TR, Q8, 16, 2, MEAN>(d, a, s);
+  return launch_norm<TX, TR, Q8, 16, 4, MEAN>(d, a, s);
 }
 
 // Backward.  RW waves hold a row, ROWS rows a workgroup at once (one where
 // several waves share a row); it takes every gridDim-th of them and keeps its
-// columns' sums of g_y h in registers; they go to part (gridDim, cols), which
-// sum_parts_kernel adds up.
-template <class TX, class TR, int RW, int V, int ROWS>
-__global__ void __launch_bounds__(RW * ROWS * 64, V == 2 ? 4 : 1)  // (4: two registers fewer hold one more wave)
-rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* __restrict__ w,
-                    const float* __restrict__ rstd, const TR* g_sum, TR* g_u, TX* g_x, float* part) {
+// columns' sums of g_y h (MEAN: and of g_y) in registers; they go to part
+// (gridDim, cols; MEAN: cols twice), which sum_parts_kernel adds up.
+template <class TX, class TR, int RW, int V, int ROWS, bool MEAN>
+__global__ void __launch_bounds__(RW * ROWS * 64, V == 2 && !MEAN ? 4 : 1)  // (4: two registers fewer hold one more wave)
+norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* __restrict__ w,
+                const float* __restrict__ mean_of, const float* __restrict__ rstd, const TR* g_sum, TR* g_u, TX* g_x,
+                float* part) {
   static_assert(ROWS == 1 || (RW == 1 && V == 1), "a wave a row, in one access");
-  __shared__ float red[2][RW];
+  __shared__ float red[2][RW], red2[2][RW];
   const int first = int(threadIdx.x % (RW * 64)) * VEC, sub = threadIdx.x / (RW * 64);
   const int64_t cols = d.cols;
-  float wv[V][VEC], gw[V][VEC];
+  float wv[V][VEC], gw[V][VEC], gb[V][VEC];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int64_t c = first + i * RW * 64 * VEC;
     load_n<VEC>(w + c, cols - c, wv[i]);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) gw[i][j] = 0.f;
+    for (int j = 0; j < VEC; ++j) gw[i][j] = gb[i][j] = 0.f;
   }
   int odd = 0;
   for (int64_t row = int64_t(blockIdx.x) * ROWS + sub; row < d.rows; row += int64_t(gridDim.x) * ROWS, odd ^= 1) {
     const float r = rstd[row];
     float g[V][VEC], h[V][VEC];
-    float dot = 0.f;
+    float dot = 0.f, sum = 0.f, m = 0.f;
+    if constexpr (MEAN) m = mean_of[row];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = first + i * RW * 64 * VEC;
@@ -205,12 +256,26 @@ rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const floa
     for (int i = 0; i < V; ++i)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        h[i][j] *= r;
+        h[i][j] = (MEAN ? h[i][j] - m : h[i][j]) * r;  // (past the row g and w are zero)
         gw[i][j] += g[i][j] * h[i][j];
+        if constexpr (MEAN) gb[i][j] += g[i][j];
         g[i][j] *= wv[i][j];
+        if constexpr (MEAN) sum += g[i][j];
         dot += g[i][j] * h[i][j];
       }
-    const float mean = row_sum<RW>(dot, red[odd]) / float(cols);  // (two sets of slots: one barrier a row)
+    // (two sets of slots: one barrier a row)
+    float mean_t = 0.f;
+    if constexpr (MEAN) mean_t = wave_sum(sum);
+    if constexpr (MEAN && RW > 1) {
+      if ((threadIdx.x & 63) == 0) red2[odd][threadIdx.x >> 6] = mean_t;
+    }
+    const float mean = row_sum<RW>(dot, red[odd]) / float(cols);
+    if constexpr (MEAN && RW > 1) {
+      mean_t = 0.f;
+#pragma unroll
+      for (int i = 0; i < RW; ++i) mean_t += red2[odd][i];
+    }
+    mean_t /= float(cols);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = first + i * RW * 64 * VEC;
@@ -222,51 +287,63 @@ rms_norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const floa
         for (int j = 0; j < VEC; ++j) e[j] = 0.f;
       }
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) e[j] += r * (g[i][j] - h[i][j] * mean);
+      for (int j = 0; j < VEC; ++j) e[j] += r * ((MEAN ? g[i][j] - mean_t : g[i][j]) - h[i][j] * mean);
       store_n<VEC>(g_u + row * d.ld_g_u + c, cols - c, e);
       if (g_x != nullptr) store_n<VEC>(g_x + row * d.ld_g_x + c, cols - c, e);
     }
   }
+  part += blockIdx.x * cols * (MEAN ? 2 : 1);
   if constexpr (ROWS > 1) {  // (in order)
     __shared__ float sums[ROWS][64 * VEC];
+    const auto add_up = [&](const float (&v)[VEC], float* out) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sums[sub][first + j] = gw[0][j];
-    __syncthreads();
-    for (int c = threadIdx.x; c < cols; c += ROWS * 64) {
-      float t = 0.f;
+      for (int j = 0; j < VEC; ++j) sums[sub][first + j] = v[j];
+      __syncthreads();
+      for (int c = threadIdx.x; c < cols; c += ROWS * 64) {
+        float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < ROWS; ++k) t += sums[k][c];
-      part[blockIdx.x * cols + c] = t;
+        for (int k = 0; k < ROWS; ++k) t += sums[k][c];
+        out[c] = t;
+      }
+    };
+    add_up(gw[0], part);
+    if constexpr (MEAN) {
+      __syncthreads();
+      add_up(gb[0], part + cols);
     }
     return;
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int64_t c = first + i * RW * 64 * VEC;
-    store_n<VEC>(part + blockIdx.x * cols + c, cols - c, gw[i]);
+    store_n<VEC>(part + c, cols - c, gw[i]);
+    if constexpr (MEAN) store_n<VEC>(part + cols + c, cols - c, gb[i]);
   }
 }
 
-// g_w[c] (+)= sum_p part[p][c]: 32 columns a workgroup, 32 lanes a column, each
-// taking every 32nd part (64 columns by 16 waves left the loads one after the
-// other: 15 us for 751 parts of 1537 columns).
+// g_w[c] (+)= sum_p part[p][c], and g_b from the columns past g_w's where there
+// is one: 32 columns a workgroup, 32 lanes a column, each taking every 32nd part
+// (64 columns by 16 waves left the loads one after the other: 15 us for 751 parts
+// of 1537 columns).
 __global__ void __launch_bounds__(1024)
-sum_parts_kernel(const float* __restrict__ part, int parts, int64_t cols, int accumulate, float* g_w) {
+sum_parts_kernel(const float* __restrict__ part, int parts, int64_t cols, int64_t width, int accumulate, float* g_w,
+                 float* g_b) {
   __shared__ float red[32][33];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int64_t c = int64_t(blockIdx.x) * 32 + lane;
   float s = 0.f;
-  if (c < cols) {
+  if (c < width) {
 #pragma unroll 8
-    for (int p = group; p < parts; p += 32) s += part[p * cols + c];
+    for (int p = group; p < parts; p += 32) s += part[p * width + c];
   }
   red[group][lane] = s;
   __syncthreads();
-  if (group == 0 && c < cols) {
-    float t = accumulate ? g_w[c] : 0.f;
+  if (group == 0 && c < width) {
+    float* out = c < cols ? g_w + c : g_b + (c - cols);
+    float t = accumulate ? *out : 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) t += red[i][lane];
-    g_w[c] = t;
+    *out = t;
   }
 }
 
@@ -279,25 +356,32 @@ int64_t norm_adj_parts(int64_t rows, int64_t cols) {
   return std::max<int64_t>(1, std::min<int64_t>(most, (rows + each - 1) / each));
 }
 
-template <class TX, class TR, int RW, int V, int ROWS = 1>
-int launch_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* w, const float* rstd,
-                    const void* g_sum, void* g_u, void* g_x, float* part, hipStream_t s) {
-  hipLaunchKernelGGL((rms_norm_adj_kernel<TX, TR, RW, V, ROWS>), dim3(unsigned(norm_adj_parts(d.rows, d.cols))),
-                     dim3(RW * ROWS * 64), 0, s, d, static_cast<const TX*>(g_y), static_cast<const TR*>(u), w, rstd,
-                     static_cast<const TR*>(g_sum), static_cast<TR*>(g_u), static_cast<TX*>(g_x), part);
+struct NormAdjArgs {
+  const void *g_y, *u;
+  const float *w, *mean, *rstd;
+  const void* g_sum;
+  void *g_u, *g_x;
+  float* part;
+};
+
+template <class TX, class TR, bool MEAN, int RW, int V, int ROWS = 1>
+int launch_norm_adj(const dtst_norm_adj_desc& d, const NormAdjArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((norm_adj_kernel<TX, TR, RW, V, ROWS, MEAN>), dim3(unsigned(norm_adj_parts(d.rows, d.cols))),
+                     dim3(RW * ROWS * 64), 0, s, d, static_cast<const TX*>(a.g_y), static_cast<const TR*>(a.u), a.w,
+                     a.mean, a.rstd, static_cast<const TR*>(a.g_sum), static_cast<TR*>(a.g_u), static_cast<TX*>(a.g_x),
+                     a.part);
   return hipGetLastError();
 }
 
-template <class TX, class TR>
-int launch_norm_adj_cols(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* w,
-                         const float* rstd, const void* g_sum, void* g_u, void* g_x, float* part, hipStream_t s) {
+template <class TX, class TR, bool MEAN>
+int launch_norm_adj_cols(const dtst_norm_adj_desc& d, const NormAdjArgs& a, hipStream_t s) {
   const int64_t c = d.cols;
-  if (c <= SINGLE) return launch_norm_adj<TX, TR, 1, 1, SINGLE_ROWS>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
-  if (c <= 2048) return launch_norm_adj<TX, TR, 4, 1>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
-  if (c <= 4096) return launch_norm_adj<TX, TR, 4, 2>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
-  if (c <= 8192) return launch_norm_adj<TX, TR, 16, 1>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
-  if (c <= 16384) return launch_norm_adj<TX, TR, 16, 2>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
-  return launch_norm_adj<TX, TR, 16, 4>(d, g_y, u, w, rstd, g_sum, g_u, g_x, part, s);
+  if (c <= SINGLE) return launch_norm_adj<TX, TR, MEAN, 1, 1, SINGLE_ROWS>(d, a, s);
+  if (c <= 2048) return launch_norm_adj<TX, TR, MEAN, 4, 1>(d, a, s);
+  if (c <= 4096) return launch_norm_adj<TX, TR, MEAN, 4, 2>(d, a, s);
+  if (c <= 8192) return launch_norm_adj<TX, TR, MEAN, 16, 1>(d, a, s);
+  if (c <= 16384) return launch_norm_adj<TX, TR, MEAN, 16, 2>(d, a, s);
+  return launch_norm_adj<TX, TR, MEAN, 16, 4>(d, a, s);
 }
 
 // Calls f with values of the types x_type and res_type stand for (checked:
@@ -309,42 +393,67 @@ int by_types(int x_type, int res_type, F&& f) {
   return res_type == DTST_F32 ? f(f16_t(), float()) : f(f16_t(), f16_t());
 }
 
-}  // namespace
-
-int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, void* sum_out,
-                    void* y, void* scale, float* rstd, void* stream) {
+template <bool MEAN>
+int norm_forward(const dtst_norm_desc& d, const NormArgs& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   return by_types(d.x_type, d.res_type, [&](auto tx, auto tr) {
     using TX = decltype(tx);
     using TR = decltype(tr);
-    return d.y_type == DTST_E4M3
-               ? launch_norm_cols<TX, TR, true>(d, x, res, weight, sum_out, y, scale, rstd, s)
-               : launch_norm_cols<TX, TR, false>(d, x, res, weight, sum_out, y, scale, rstd, s);
+    return d.y_type == DTST_E4M3 ? launch_norm_cols<TX, TR, true, MEAN>(d, a, s)
+                                 : launch_norm_cols<TX, TR, false, MEAN>(d, a, s);
   });
 }
 
+template <bool MEAN>
+int norm_backward(const dtst_norm_adj_desc& d, const NormAdjArgs& a, float* g_weight, float* g_bias, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (d.rows > 0) {  // (the kernel reads the weight before its rows; of none there is nothing to add up)
+    const int e = by_types(d.x_type, d.res_type, [&](auto tx, auto tr) {
+      return launch_norm_adj_cols<decltype(tx), decltype(tr), MEAN>(d, a, s);
+    });
+    if (e != hipSuccess) return e;
+  }
+  const int64_t width = d.cols * (MEAN ? 2 : 1);
+  hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((width + 31) / 32)), dim3(1024), 0, s, a.part,
+                     d.rows > 0 ? int(norm_adj_parts(d.rows, d.cols)) : 0, d.cols, width, d.accumulate, g_weight, g_bias);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, void* sum_out,
+                    void* y, void* scale, float* rstd, void* stream) {
+  return norm_forward<false>(d, NormArgs{x, res, weight, nullptr, sum_out, y, scale, nullptr, rstd}, stream);
+}
+
+int launch_layer_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, const float* bias,
+                      void* sum_out, void* y, void* scale, float* mean, float* rstd, void* stream) {
+  return norm_forward<true>(d, NormArgs{x, res, weight, bias, sum_out, y, scale, mean, rstd}, stream);
+}
+
 // (one wave a row up to 1024 columns, four up to 8192, else sixteen)
-NormGrid rms_norm_grid(int64_t rows, int64_t cols) {
+NormGrid norm_grid(int64_t rows, int64_t cols) {
   if (cols <= 1024) return {(rows + 3) / 4, 256};
   return {rows, cols <= 8192 ? 256 : 1024};
 }
 
 size_t rms_norm_adj_workspace(int64_t rows, int64_t cols) { return size_t(norm_adj_parts(rows, cols)) * cols * 4; }
+size_t layer_norm_adj_workspace(int64_t rows, int64_t cols) { return 2 * rms_norm_adj_workspace(rows, cols); }
 
 int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
                         const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight, void* workspace,
                         void* stream) {
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  float* part = static_cast<float*>(workspace);
-  if (d.rows > 0) {  // (the kernel reads the weight before its rows; of none there is nothing to add up)
-    const int e = by_types(d.x_type, d.res_type, [&](auto tx, auto tr) {
-      return launch_norm_adj_cols<decltype(tx), decltype(tr)>(d, g_y, u, weight, rstd, g_sum, g_u, g_x, part, s);
-    });
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((d.cols + 31) / 32)), dim3(1024), 0, s, part,
-                     d.rows > 0 ? int(norm_adj_parts(d.rows, d.cols)) : 0, d.cols, d.accumulate, g_weight);
-  return hipGetLastError();
+  return norm_backward<false>(
+      d, NormAdjArgs{g_y, u, weight, nullptr, rstd, g_sum, g_u, g_x, static_cast<float*>(workspace)}, g_weight, nullptr,
+      stream);
+}
+
+int launch_layer_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
+                          const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x,
+                          float* g_weight, float* g_bias, void* workspace, void* stream) {
+  return norm_backward<true>(
+      d, NormAdjArgs{g_y, u, weight, mean, rstd, g_sum, g_u, g_x, static_cast<float*>(workspace)}, g_weight, g_bias,
+      stream);
 }
 
 }  // namespace dtst

@@ -16,13 +16,19 @@ struct NormGrid {
   int64_t groups;
   int threads;
 };
-NormGrid rms_norm_grid(int64_t rows, int64_t cols);
+NormGrid norm_grid(int64_t rows, int64_t cols);
 int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, void* sum_out,
                     void* y, void* scale, float* rstd, void* stream);
 size_t rms_norm_adj_workspace(int64_t rows, int64_t cols);
 int launch_rms_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
                         const float* rstd, const void* g_sum, void* g_u, void* g_x, float* g_weight, void* workspace,
                         void* stream);
+int launch_layer_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, const float* bias,
+                      void* sum_out, void* y, void* scale, float* mean, float* rstd, void* stream);
+size_t layer_norm_adj_workspace(int64_t rows, int64_t cols);
+int launch_layer_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
+                          const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x,
+                          float* g_weight, float* g_bias, void* workspace, void* stream);
 int launch_quantise(const dtst_quantise_desc& d, const void* x, void* q, void* scale, void* qt, void* scale_t,
                     void* stream);
 int launch_product(const dtst_product_desc& d, const void* a, const void* a_scale, const void* b, const void* b_scale,

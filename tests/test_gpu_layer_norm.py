@@ -1,0 +1,222 @@
+"""Layer norm with the residual's addition and its backward against the fp64
+oracle: row lengths around every kernel form's limits, the types, strides and
+odd offsets, updates in place, means far above the deviations, values that are
+no numbers, more rows than workgroups."""
+
+import numpy as np
+import pytest
+
+from gpu_common import say, torch_gpu
+from oracle import seq_oracle as S
+from seq_common import f64, near, outside, rounded, strided
+from test_gpu_seq_norm import COLS, TYPES, lib
+
+pytestmark = pytest.mark.gpu
+
+
+def codes_near(torch, q, s, v, terms, name):
+    """Codes and scales of v = h weight + bias: each within half a code's step and
+    the arithmetic of 32 bits, whose roundings are relative to the terms |h
+    weight| + |bias| and not to what a sum that cancels leaves of them: 1 / std
+    one, h one, the product and the sum one each, the mean's less than one more: 5
+    of 2^-24, below 1e-6."""
+    r, k = v.shape
+    kb = -(-k // 128)
+    qv, sb = q.float().cpu().double().numpy(), s.view(torch.uint8).cpu().numpy().astype(np.int64)
+    assert not qv[:, k:].any() and (sb[:, kb:] == 127).all(), f"{name}: padding"
+    e = sb[:, :kb] - 127
+    low, high = (S.quantise(np.sign(v) * np.maximum(np.abs(v) + d * terms, 0))[1] for d in (-1e-6, 1e-6))
+    assert ((e >= low) & (e <= high)).all(), f"{name}: scales"
+    sc = np.repeat(np.exp2(e.astype(np.float64)), 128, axis=1)[:, :k]
+    with np.errstate(divide="ignore"):
+        step = np.exp2(np.maximum(np.floor(np.log2(np.abs(v) / sc)), -6) - 3) * sc
+    off = np.abs(qv[:, :k] * sc - v) - step / 2 - 1e-6 * terms
+    assert (off <= 0).all(), f"{name}: {int((off > 0).sum())} codes off, by up to {off.max():.3e}"
+
+
+def inputs(torch, rows, cols, tx, tr, seed, res=True, mean=1.0):
+    rng = np.random.RandomState(seed)
+    x, xv = rounded(torch, (rng.randn(rows, cols) + mean) * np.exp2(rng.uniform(-3, 3, (rows, 1))), tx)
+    r, rv = rounded(torch, rng.randn(rows, cols), tr) if res else (None, 0.0)
+    w, wv = rounded(torch, 1 + 0.3 * rng.randn(cols), "f32")
+    b, bv = rounded(torch, 0.3 * rng.randn(cols), "f32")
+    u = np.float32(xv) + np.float32(rv)
+    return x, r, (w, b), (wv, bv), rounded(torch, u, tr)[1]
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("tx,tr", TYPES)
+def test_forward(cols, tx, tr):
+    torch, D = lib()
+    rows = 5
+    x, r, wb, v, u = inputs(torch, rows, cols, tx, tr, cols)
+    say(f"[layer_norm] {rows} x {cols} {tx} {tr}")
+    s, y = torch.empty_like(r), torch.empty_like(x)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    D.dtst_layer_norm(x, *wb, y, res=r, sum_out=s, mean=mean, rstd=rstd, eps=1e-5)
+    yv, mv, rv = S.layer_norm(u, *v, 1e-5)
+    assert np.array_equal(f64(s), u)
+    near(f64(y), yv, tx, "y")
+    near(f64(mean), mv, "f32", "mean")
+    near(f64(rstd), rv, "f32", "rstd")
+    q, sc = D.empty_codes(rows, cols)
+    D.dtst_layer_norm(x, *wb, q, res=r, sum_out=s, scale=sc, eps=1e-5)
+    assert np.array_equal(f64(s), u)
+    codes_near(torch, q, sc, yv, np.abs(yv - v[1]) + np.abs(v[1]), "codes")
+    D.dtst_layer_norm(x, wb[0], None, y, res=r, eps=1e-5)
+    near(f64(y), S.layer_norm(u, v[0], None, 1e-5)[0], tx, "y without a bias")
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("tx,tr", TYPES)
+def test_backward(cols, tx, tr):
+    torch, D = lib()
+    rows = 11
+    rng = np.random.RandomState(cols + 1)
+    _, _, (w, b), (wv, bv), _ = inputs(torch, rows, cols, tx, tr, cols)
+    u, uv = rounded(torch, rng.randn(rows, cols) + 2, tr)
+    g, gv = rounded(torch, rng.randn(rows, cols), tx)
+    gs, gsv = rounded(torch, rng.randn(rows, cols), tr)
+    say(f"[layer_norm_adj] {rows} x {cols} {tx} {tr}")
+    _, mv, rv = S.layer_norm(uv, wv, bv, 1e-5)
+    mean, rstd = torch.from_numpy(mv).float().cuda(), torch.from_numpy(rv).float().cuda()
+    g_u, g_x, g_w, g_b = torch.empty_like(u), torch.empty_like(g), torch.full_like(w, 3.0), torch.full_like(w, 3.0)
+    D.dtst_layer_norm_adj(g, u, w, mean, rstd, g_u, g_w, g_b, g_sum=gs, g_x=g_x)
+    ru, rw, rb = S.layer_norm_adj(gv, uv, wv, 1e-5, gsv)
+    # relative to the terms t rstd of the difference, which one column cancels
+    # altogether; the weight's to those that are summed
+    terms = gv * wv * rv[:, None]
+    rms = np.sqrt((terms ** 2).mean()) + 1
+    near(f64(g_u), ru, tr, "g_u", rms=rms)
+    near(f64(g_x), ru, tx, "g_x", rms=rms)
+    near(f64(g_w), rw, "f32", "g_w", rms=np.sqrt(rows))
+    near(f64(g_b), rb, "f32", "g_b", rms=np.sqrt(rows))
+    # added to, without the other gradient, in place of it
+    D.dtst_layer_norm_adj(g, u, w, mean, rstd, gs, g_w, g_b, g_sum=gs, accumulate=True)
+    near(f64(gs), ru, tr, "g_u in place", rms=rms)
+    near(f64(g_w), 2 * rw, "f32", "g_w twice", rms=2 * np.sqrt(rows))
+    near(f64(g_b), 2 * rb, "f32", "g_b twice", rms=2 * np.sqrt(rows))
+    D.dtst_layer_norm_adj(g, u, w, mean, rstd, g_u, g_w, g_b)
+    near(f64(g_u), S.layer_norm_adj(gv, uv, wv, 1e-5)[0], tr, "g_u alone", rms=rms)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 384), (2, 384), (9, 512), (1000, 384), (8193, 384), (5000, 520), (3001, 4100)])
+def test_rows(rows, cols):
+    torch, D = lib()
+    x, r, (w, b), v, u = inputs(torch, rows, cols, "bf16", "bf16", rows)
+    y, s, mean, rstd = torch.empty_like(x), torch.empty_like(r), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    D.dtst_layer_norm(x, w, b, y, res=r, sum_out=s, mean=mean, rstd=rstd)
+    near(f64(y), S.layer_norm(u, *v, 1e-5)[0], "bf16", "y")
+    g, gv = rounded(torch, np.random.RandomState(rows).randn(rows, cols), "bf16")
+    g_u, g_w, g_b, g_w2, g_b2 = torch.empty_like(s), *(torch.empty_like(w) for _ in range(4))
+    D.dtst_layer_norm_adj(g, s, w, mean, rstd, g_u, g_w, g_b)
+    ru, rw, rb = S.layer_norm_adj(gv, u, v[0], 1e-5)
+    near(f64(g_u), ru, "bf16", "g_u")
+    near(f64(g_w), rw, "f32", "g_w")
+    near(f64(g_b), rb, "f32", "g_b")
+    D.dtst_layer_norm_adj(g, s, w, mean, rstd, g_u, g_w2, g_b2)
+    assert torch.equal(g_w, g_w2) and torch.equal(g_b, g_b2)   # a fixed order of sums
+
+
+@pytest.mark.parametrize("offset", [0, 1, 3])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_column_ranges_at_any_alignment(t, offset):
+    torch, D = lib()
+    rows, cols = 6, 333
+    x, r, wb, v, u = inputs(torch, rows, cols, t, t, 5)
+    xs, _ = strided(torch, x, 6, offset)
+    rs, _ = strided(torch, r, 2, offset)
+    yb, sb, gb = (strided(torch, x, k, offset) for k in (4, 1, 3))
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    D.dtst_layer_norm(xs, *wb, yb[0], res=rs, sum_out=sb[0], mean=mean, rstd=rstd)
+    near(f64(yb[0]), S.layer_norm(u, *v, 1e-5)[0], t, "y")
+    assert np.array_equal(f64(sb[0]), u)
+    g_w, g_b = torch.empty_like(wb[0]), torch.empty_like(wb[0])
+    D.dtst_layer_norm_adj(xs, sb[0], wb[0], mean, rstd, gb[0], g_w, g_b, g_sum=rs)
+    ru, rw, rb = S.layer_norm_adj(f64(x), u, v[0], 1e-5, f64(r))
+    # (8: rows' sizes; the sums over six rows of x up to three times that)
+    near(f64(gb[0]), ru, t, "g_u", rms=8.0)
+    near(f64(g_w), rw, "f32", "g_w", rms=24.0)
+    near(f64(g_b), rb, "f32", "g_b", rms=24.0)
+    for wide in (yb[1], sb[1], gb[1]):
+        assert outside(wide, cols, offset)
+
+
+def test_updates_in_place():
+    torch, D = lib()
+    x, r, wb, v, u = inputs(torch, 7, 640, "bf16", "f32", 8)
+    D.dtst_layer_norm(x, *wb, x, res=r, sum_out=r)
+    assert np.array_equal(f64(r), u)
+    near(f64(x), S.layer_norm(u, *v, 1e-5)[0], "bf16", "y")
+    x, _, wb, v, u = inputs(torch, 7, 640, "f16", "f16", 9, res=False)
+    D.dtst_layer_norm(x, *wb, x)
+    near(f64(x), S.layer_norm(u, *v, 1e-5)[0], "f16", "y without a residual")
+
+
+@pytest.mark.parametrize("cols", [100, 700, 1537, 20000])
+def test_mean_far_above_the_deviations(cols):
+    """The deviations are exact to 32 bits whatever the mean is (rounded to 32
+    bits, it would shift them by up to 2^-25 of itself, 3e-3 here)."""
+    torch, D = lib()
+    rng = np.random.RandomState(cols)
+    x, xv = rounded(torch, 1e5 * rng.uniform(0.5, 1, (9, 1)) + rng.randn(9, cols), "f32")
+    w, b = torch.ones(cols, device="cuda"), torch.zeros(cols, device="cuda")
+    y = torch.empty_like(x)
+    D.dtst_layer_norm(x, w, b, y, eps=1e-5)
+    near(f64(y), S.layer_norm(xv, f64(w), None, 1e-5)[0], "f32", "y")
+
+
+def test_equal_columns_and_no_numbers():
+    torch, D = lib()
+    x = torch.randn(5, 300, device="cuda")
+    x[0] = 3.7
+    x[1, 7] = float("nan")
+    x[2, 9] = float("inf")
+    w, b = torch.ones(300, device="cuda"), torch.full((300,), 0.25, device="cuda")
+    y, q = torch.empty_like(x), D.empty_codes(5, 300)
+    D.dtst_layer_norm(x, w, b, y)
+    # (their mean's last bit over sqrt(eps): 3.7 2^-48 316)
+    assert (y[0] - 0.25).abs().max() < 1e-9 and torch.isnan(y[1]).all() and torch.isnan(y[2]).all()
+    assert torch.isfinite(y[3:]).all()
+    D.dtst_layer_norm(x, w, b, q[0], scale=q[1])
+    v = q[0].float()
+    assert torch.isnan(v[1, :300]).all() and not v[:, 300:].any() and torch.isfinite(v[3:]).all()
+    D.dtst_layer_norm(torch.zeros_like(x[:1]), w, b, y[:1], eps=0.0)                   # 0 / 0
+    assert torch.isnan(y[0]).all()
+    n = torch.empty(0, 300, device="cuda")
+    D.dtst_layer_norm(n, w, b, torch.empty_like(n))
+    g_w, g_b, e = torch.full_like(w, 2.0), torch.full_like(w, 2.0), torch.empty(0, device="cuda")
+    D.dtst_layer_norm_adj(n, n, w, e, e, n, g_w, g_b, accumulate=True)
+    assert (g_w == 2).all() and (g_b == 2).all()
+    D.dtst_layer_norm_adj(n, n, w, e, e, n, g_w, g_b)
+    assert not g_w.any() and not g_b.any()
+
+
+def test_gradients_are_differences():
+    """Central differences of the 32-bit forward, whose 2^-24 over the step of
+    2^-6 leaves 4e-6 a value, with the step's own square 2e-4."""
+    torch, D = lib()
+    rows, cols, step = 2, 9, 2.0 ** -6
+    rng = np.random.RandomState(3)
+    x, w, b = (torch.from_numpy(rng.randn(*s)).float().cuda() for s in ((rows, cols), (cols,), (cols,)))
+    g = torch.from_numpy(rng.randn(rows, cols)).float().cuda()
+
+    def f(x, w, b):
+        y = torch.empty_like(x)
+        D.dtst_layer_norm(x, w, b, y, eps=1e-2)
+        return float((y.double() * g.double()).sum())
+
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    D.dtst_layer_norm(x, w, b, y, mean=mean, rstd=rstd, eps=1e-2)
+    got = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    D.dtst_layer_norm_adj(g, x, w, mean, rstd, *got)
+    args = [x, w, b]
+    for k in range(3):
+        for i in np.ndindex(*args[k].shape):
+            at = float(args[k][i])
+            args[k][i] = at + step
+            up = f(*args)
+            args[k][i] = at - step
+            down = f(*args)
+            args[k][i] = at
+            assert abs((up - down) / (2 * step) - float(got[k][i])) < 5e-3, (k, i)

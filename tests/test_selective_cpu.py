@@ -1,0 +1,80 @@
+"""The operators of a selective block without a GPU: the fp64 oracle's
+gradients against central differences, and what the library refuses."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import seq_oracle as S
+from test_seq_oracle_cpu import P, differences, status
+
+D = pytest.importorskip("paper_2607_14394_amd", reason="libdtst.so not built")
+
+
+def test_layer_norm_gradient_is_the_derivative():
+    rng = np.random.RandomState(1)
+    u, w, b, g, gs = rng.randn(3, 7) + 1, rng.randn(7), rng.randn(7), rng.randn(3, 7), rng.randn(3, 7)
+    g_u, g_w, g_b = S.layer_norm_adj(g, u, w, 1e-3, gs)
+    assert np.abs(g_u - gs - differences(lambda a: S.layer_norm(a, w, b, 1e-3)[0], u, g)).max() < 1e-7
+    assert np.abs(g_w - differences(lambda a: S.layer_norm(u, a, b, 1e-3)[0], w, g)).max() < 1e-7
+    assert np.abs(g_b - differences(lambda a: S.layer_norm(u, w, a, 1e-3)[0], b, g)).max() < 1e-7
+
+
+def test_layer_norm_is_torchs():
+    rng = np.random.RandomState(2)
+    u, w, b = rng.randn(4, 30) * 3 + 5, rng.randn(30), rng.randn(30)
+    want = torch.nn.functional.layer_norm(*(torch.from_numpy(u), (30,), torch.from_numpy(w), torch.from_numpy(b)), eps=1e-4)
+    assert np.abs(S.layer_norm(u, w, b, 1e-4)[0] - want.numpy()).max() < 1e-13
+
+
+def norm_call(x=P, res=None, w=P * 2, b=P * 9, s=None, y=P * 3, scale=None, mean=None, rstd=None, **kw):
+    f = dict(rows=4, cols=64, ld_x=64, ld_res=64, ld_sum=64, ld_y=128, ld_scale=4, x_type=1, res_type=1, y_type=1,
+             eps=1e-6)
+    f.update(kw)
+    return status(D.lib.dtst_layer_norm, D.NORM_DESC.pack(*f.values()), x, res, w, b, s, y, scale, mean, rstd, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(rows=-1), 1, "rows"), (dict(x_type=3), 1, "x_type"), (dict(eps=float("nan")), 1, "eps"),
+    (dict(cols=32769, ld_x=32769, ld_y=40000), 2, "cols"), (dict(w=None), 1, "weight"), (dict(b=P * 9 + 2), 1, "bias"),
+    (dict(mean=P * 9 + 2), 1, "mean"), (dict(mean=P * 9), 1, "mean and bias overlap"),
+    (dict(mean=P * 2 + 252), 1, "mean and weight overlap"), (dict(mean=P * 3), 1, "mean and y overlap"),
+    (dict(mean=P), 1, "mean and x overlap"), (dict(mean=P * 11, rstd=P * 11 + 12), 1, "rstd and mean overlap"),
+    (dict(y=P * 9 - 64), 1, "y and bias overlap"), (dict(s=P * 9), 1, "sum_out and bias overlap"),
+    (dict(y=P + 2), 1, "overlap"), (dict(rows=1 << 40), 2, "rows"),
+])
+def test_layer_norm_refusals(kw, code, word):
+    st, msg = norm_call(**kw)
+    assert st == code and word in msg, (st, msg)
+
+
+def test_layer_norm_of_no_rows_is_done():
+    assert norm_call(rows=0, x=None, w=None, b=None, y=None)[0] == 0
+
+
+def norm_adj_call(gy=P, u=P * 2, w=P * 3, m=P * 8, r=P * 4, gs=None, gu=P * 5, gx=None, gw=P * 6, gb=P * 9, ws=P * 7,
+                  nws=1 << 16, **kw):
+    f = dict(rows=4, cols=64, ld_g_y=64, ld_u=64, ld_g_sum=64, ld_g_u=64, ld_g_x=64, x_type=1, res_type=0, accumulate=0)
+    f.update(kw)
+    d = D.NORM_ADJ_DESC.pack(*f.values())
+    return status(D.lib.dtst_layer_norm_adj, d, gy, u, w, m, r, gs, gu, gx, gw, gb, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(cols=0), 1, "cols"), (dict(accumulate=2), 1, "accumulate"), (dict(nws=16), 1, "workspace"),
+    (dict(gw=None), 1, "g_weight"), (dict(gb=None), 1, "g_bias"), (dict(m=None), 1, "mean"), (dict(r=None), 1, "rstd"),
+    (dict(gb=P * 6 + 252), 1, "g_weight and g_bias overlap"), (dict(gb=P * 7), 1, "workspace and g_bias overlap"),
+    (dict(gb=P * 8), 1, "g_bias and mean overlap"), (dict(gu=P * 8, ld_g_u=64), 1, "g_u and mean overlap"),
+    (dict(ws=P * 8 - 496), 1, "workspace and mean overlap"), (dict(gx=P * 5), 1, "overlap"),
+])
+def test_layer_norm_adj_refusals(kw, code, word):
+    st, msg = norm_adj_call(**kw)
+    assert st == code and word in msg, (st, msg)
+
+
+def test_layer_norm_binding_refuses_tensors_off_the_device():
+    x, w = torch.zeros(4, 64), torch.ones(64)
+    with pytest.raises(ValueError):
+        D.dtst_layer_norm(x, w, w, torch.empty_like(x))
+    with pytest.raises(ValueError):
+        D.dtst_layer_norm_adj(x, x, w, w[:4], w[:4], torch.empty_like(x), w, w)
