@@ -455,6 +455,28 @@ dtst_status dtst_recurrence_adj(const dtst_recurrence_desc* d, const void* z, co
                                 void* g_z, void* g_v, void* g_o, float* g_hzero, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* The norm of n tensors together,
+ *   norm = sqrt( sum_i sum_j tensors[i][j]^2 ),
+ * in 64 bits and in a fixed order, rounded to fp32 at the end.  tensors[i]:
+ * counts[i] >= 0 values of types[i] (DTST_F32, DTST_BF16 or DTST_F16) without
+ * gaps, a device pointer (any where the count is zero); complex values are twice
+ * as many real ones.  A tensor listed twice counts twice.  The three arrays are
+ * host memory, read before the call returns.  norm: one fp32 on the device; its
+ * square summed over shards gives the square of the whole's.  workspace:
+ * dtst_global_norm_workspace bytes. */
+dtst_status dtst_global_norm_workspace(int64_t n, const int64_t* counts, size_t* bytes);
+dtst_status dtst_global_norm(int64_t n, const void* const* tensors, const int64_t* counts, const int32_t* types,
+                             float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same tensors scaled down to a largest norm:
+ *   out[i][j] = tensors[i][j] f,   f = 1 where *norm <= most, else most / *norm.
+ * norm: one fp32 on the device (dtst_global_norm's); infinite it makes zeros of
+ * all finite values, and no number no numbers.  most >= 0, may be infinite.  out:
+ * n pointers to tensors of the same counts and types, or NULL for in place (with
+ * f = 1 nothing is read or written then); out[i] may be tensors[i]. */
+dtst_status dtst_clip(int64_t n, void* const* tensors, const int64_t* counts, const int32_t* types, const float* norm,
+                      float most, void* const* out, void* stream);
+
 /* ---- instrumentation ----------------------------------------------------- */
 
 /* Per-kernel device time, for callers that time the path (benchmarks,

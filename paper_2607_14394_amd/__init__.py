@@ -10,8 +10,10 @@ loudly when it is missing -- there is no fallback implementation.
 
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
+import operator
 import os
 import struct
 
@@ -31,7 +33,7 @@ __all__ = [
     "RECURRENCE_SPAN", "code_columns", "scale_columns", "empty_codes", "recurrence_states_shape", "dtst_rms_norm",
     "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
-    "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace",
+    "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace", "dtst_global_norm", "dtst_clip",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdtst.so")
@@ -129,6 +131,9 @@ def _load():
         "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
         "dtst_recurrence": [VP] * 10 + [SZ, VP],
         "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
+        "dtst_global_norm_workspace": [I64, VP, ctypes.POINTER(SZ)],
+        "dtst_global_norm": [I64] + [VP] * 5 + [SZ, VP],
+        "dtst_clip": [I64] + [VP] * 4 + [ctypes.c_float, VP, VP],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -673,6 +678,72 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     status = lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
                                      g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o),
                                      _ptr(g_hzero), p, n, _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+# ---- the gradients of a training step ----------------------------------------
+
+_dtype_of = operator.attrgetter("dtype")
+_COUNTED = {**_TYPES, torch.complex64: 0}  # (as twice as many real values)
+del _COUNTED[torch.float8_e4m3fn]
+
+
+def _tensors(tensors, name, dev):
+    """Addresses, counts, types and dtypes of a list of tensors.  (Hundreds of
+    them: each property is read by one pass in C.)"""
+    T = torch.Tensor
+    tensors = list(tensors)
+    dtypes = list(map(_dtype_of, tensors))
+    kinds = set(dtypes)
+    if not (kinds <= _COUNTED.keys() and set(map(T.get_device, tensors)) <= {dev} and all(map(T.is_contiguous, tensors))
+            and not (torch.complex64 in kinds and any(map(T.is_conj, tensors)))):
+        raise ValueError(f"{name}: need contiguous tensors of {', '.join(str(d) for d in _COUNTED)} on the current device")
+    counts = array.array("q", map(T.numel, tensors))
+    if torch.complex64 in kinds:
+        counts = array.array("q", [n * (1 + (d is torch.complex64)) for n, d in zip(counts, dtypes)])
+    types = array.array("i", [_COUNTED[dtypes[0]]] * len(dtypes) if len(kinds) == 1 else map(_COUNTED.get, dtypes))
+    return array.array("Q", map(T.data_ptr, tensors)), counts, types, dtypes
+
+
+def _at(a):
+    return a.buffer_info()[0]
+
+
+def _one(t, name, dev):
+    if t.numel() != 1 or t.dtype != torch.float32 or t.get_device() != dev:
+        raise ValueError(f"{name}: need one torch.float32 on the current device")
+
+
+def dtst_global_norm(tensors, norm, ws=None, stream=None):
+    """The norm of all tensors (float32, bfloat16, float16, complex64) together
+    into norm, one float32 on the device.  Over shards, the root of the sum of
+    the norms' squares is the whole's."""
+    dev = _device()
+    p, counts, types, _ = _tensors(tensors, "tensors", dev)
+    _one(norm, "norm", dev)
+    need = ctypes.c_size_t(0)
+    _check(lib.dtst_global_norm_workspace(len(counts), _at(counts), ctypes.byref(need)))
+    q, n, ws = _scratch(ws, need.value, norm.device, stream)
+    status = lib.dtst_global_norm(len(counts), _at(p), _at(counts), _at(types), norm.data_ptr(), q, n,
+                                  _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+def dtst_clip(tensors, norm, most, out=None, stream=None):
+    """tensors min(1, most / norm), in place or into the tensors `out` of the same
+    shapes and types; norm: one float32 on the device."""
+    dev = _device()
+    p, counts, types, dtypes = _tensors(tensors, "tensors", dev)
+    _one(norm, "norm", dev)
+    po = None
+    if out is not None:
+        po, n_out, _, d_out = _tensors(out, "out", dev)
+        if n_out != counts or d_out != dtypes:
+            raise ValueError("out: need the tensors' sizes and types")
+    status = lib.dtst_clip(len(counts), _at(p), _at(counts), _at(types), norm.data_ptr(), float(most),
+                           None if po is None else _at(po), _current(dev) if stream is None else int(stream))
     if status:
         _check(status)
 

@@ -33,7 +33,8 @@ const char* const kRoleNames[K_COUNT] = {"stream_fwd_tz", "axis_fwd_y", "axis_fw
                                          "stream_inv_zt", "mix", "mix_h", "wgrad", "block_epilogue",
                                          "stream_fwd_tzy", "stream_inv_yzt", "pointwise", "stream_inv_zt_block",
                                          "rms_norm", "rms_norm_adj", "quantise", "product", "recurrence",
-                                         "recurrence_adj", "layer_norm", "layer_norm_adj"};
+                                         "recurrence_adj", "layer_norm", "layer_norm_adj", "global_norm", "clip", "conv",
+                                         "conv_adj", "scan", "scan_adj"};
 
 Profiler& prof() {
   static Profiler p;

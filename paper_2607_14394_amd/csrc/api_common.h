@@ -32,7 +32,8 @@ dtst_status check_ptr(const void* ptr, const char* name);
 // ---- per-kernel event timing (dtst_profile_enable / dtst_profile_collect) ----
 enum KernelRole { K_FWD_TZ, K_AXIS_FWD_Y, K_AXIS_FWD_X, K_AXIS_INV_X, K_AXIS_INV_Y, K_INV_ZT, K_MIX, K_MIX_H,
                   K_WGRAD, K_BLOCK, K_FWD_TZY, K_INV_YZT, K_POINTWISE, K_INV_ZT_BLOCK, K_NORM, K_NORM_ADJ,
-                  K_QUANTISE, K_PRODUCT, K_RECUR, K_RECUR_ADJ, K_LAYER_NORM, K_LAYER_NORM_ADJ, K_COUNT };
+                  K_QUANTISE, K_PRODUCT, K_RECUR, K_RECUR_ADJ, K_LAYER_NORM, K_LAYER_NORM_ADJ,
+                  K_GLOBAL_NORM, K_CLIP, K_CONV, K_CONV_ADJ, K_SCAN, K_SCAN_ADJ, K_COUNT };
 extern const char* const kRoleNames[K_COUNT];
 
 struct Profiler {

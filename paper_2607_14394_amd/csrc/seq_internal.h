@@ -40,4 +40,18 @@ int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const vo
                           const int32_t* lengths, const float* states, const void* g_y, const float* g_h, void* g_z,
                           void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream);
 
+// n tensors: pointers, counts of values, types.  out: where the scaled ones go,
+// null for in place.
+struct TensorList {
+  int64_t n;
+  void* const* p;
+  void* const* out;
+  const int64_t* counts;
+  const int32_t* types;
+};
+int64_t clip_chunks(int64_t count);  // a launch holds fewer than 2^31 of them
+size_t global_norm_workspace(const TensorList& l);
+int launch_global_norm(const TensorList& l, float* norm, void* workspace, void* stream);
+int launch_clip(const TensorList& l, const float* norm, float most, void* stream);
+
 }  // namespace dtst

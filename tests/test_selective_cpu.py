@@ -78,3 +78,47 @@ def test_layer_norm_binding_refuses_tensors_off_the_device():
         D.dtst_layer_norm(x, w, w, torch.empty_like(x))
     with pytest.raises(ValueError):
         D.dtst_layer_norm_adj(x, x, w, w[:4], w[:4], torch.empty_like(x), w, w)
+
+
+def listed(tensors, counts, types):
+    import array
+    return [array.array(t, v) for t, v in (("Q", tensors), ("q", counts), ("i", types))]
+
+
+def norm_of(tensors=(P, P * 2), counts=(100, 50), types=(0, 1), n=None, norm=P * 3, ws=P * 4, nws=1 << 16):
+    a = listed(tensors, counts, types)
+    return status(D.lib.dtst_global_norm, len(counts) if n is None else n, *(D._at(x) for x in a), norm, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(n=-1), 1, "n >= 0"), (dict(counts=(-1, 5)), 1, "count of tensor 0"), (dict(counts=(1, 1 << 51)), 1, "count of tensor 1"),
+    (dict(types=(0, 3)), 1, "type of tensor 1"), (dict(types=(9, 0)), 1, "type of tensor 0"),
+    (dict(tensors=(0, P)), 1, "tensor 0 is null"), (dict(tensors=(P, P * 2 + 1)), 1, "tensor 1 is not aligned"),
+    (dict(norm=None), 1, "norm is null"), (dict(norm=P * 3 + 2), 1, "norm is not aligned"), (dict(ws=None), 1, "workspace"),
+    (dict(nws=8), 1, "workspace"), (dict(norm=P + 396), 1, "overlap"), (dict(ws=P + 384), 1, "overlap"),
+    (dict(ws=P * 3 - 0, norm=P * 3 + 8), 1, "overlap"), (dict(counts=(1 << 46, 5)), 2, "too many"),
+])
+def test_global_norm_refusals(kw, code, word):
+    st, msg = norm_of(**kw)
+    assert st == code and word in msg, (st, msg)
+
+
+def clip_of(tensors=(P, P * 2), counts=(100, 50), types=(0, 1), out=None, norm=P * 3, most=1.0):
+    a, o = listed(tensors, counts, types), None if out is None else listed(out, (), ())[0]
+    return status(D.lib.dtst_clip, len(counts), *(D._at(x) for x in a), norm, most, None if o is None else D._at(o), None)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(most=-1.0), "most"), (dict(most=float("nan")), "most"), (dict(norm=None), "norm is null"),
+    (dict(norm=P + 8), "overlap"), (dict(tensors=(P, P)), "overlap"), (dict(tensors=(P, P + 398)), "overlap"),
+    (dict(out=(P * 5, 0)), "out of tensor 1 is null"), (dict(out=(P * 5 + 2, P * 6)), "out of tensor 0 is not aligned"),
+    (dict(out=(P * 2, P * 6)), "overlap"), (dict(out=(P + 4, P * 6)), "overlap"), (dict(out=(P * 5, P * 5 + 100)), "overlap"),
+    (dict(out=(P * 3 - 396, P * 6)), "overlap"),
+])
+def test_clip_refusals(kw, word):
+    st, msg = clip_of(**kw)
+    assert st == 1 and word in msg, (st, msg)
+
+
+def test_clip_of_nothing_is_done():
+    assert clip_of((), (), ())[0] == 0 and clip_of((0, 0), (0, 0))[0] == 0 and clip_of((0, 0), (0, 0), out=(0, 0))[0] == 0
