@@ -455,6 +455,40 @@ dtst_status dtst_recurrence_adj(const dtst_recurrence_desc* d, const void* z, co
                                 void* g_z, void* g_v, void* g_o, float* g_hzero, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* Selective state-space scan along the steps: each feature has N states h[n],
+ * whose decay and input depend on the step,
+ *   D_t = log(1 + exp(delta_t)),
+ *   h_t[n] = exp(D_t a[n]) h_{t-1}[n] + D_t x_t b_t[n],
+ *   y_t = ( sum_n c_t[n] h_t[n] + d x_t ) o_t s(o_t),   s as in dtst_recurrence
+ * (without o: the sum alone; without d: no d x_t; an exponential below 2^-126 may be
+ * 0).  x, delta, o, y: (batch, steps, features) of `type`, b and c, common to all
+ * features: (batch, steps, states) of `type`, each with a stride of batch entries
+ * and of steps, so they may be column ranges of one array; groups of features with
+ * b and c of their own are calls on the groups' column ranges.  a: (states,
+ * features) fp32, meant to be negative (above zero, the product of many steps'
+ * exponentials may be infinite and make no number of a state that is zero); d:
+ * features fp32, or NULL.  h_zero, h_out: (batch, states, features) fp32, the states
+ * before the first and after the last step, NULL for zero and if not wanted;
+ * h_out may be h_zero itself, which is a serving step with steps = 1.  lengths as
+ * in dtst_recurrence: from lengths[b] on the states stand still, y is zero and x,
+ * delta, b, c and o are not read.  states: (batch, ceil(steps / DTST_SCAN_SPAN),
+ * states, features) fp32, the states before steps 0, SPAN, 2 SPAN, ... that the
+ * backward needs, NULL if not wanted.  1 to 64 states (DTST_ERR_UNSUPPORTED above).
+ * workspace: dtst_scan_workspace bytes, any contents. */
+#define DTST_SCAN_SPAN 64
+typedef struct {
+  int64_t batch, steps, features, states;
+  int64_t x_stride[2], delta_stride[2], b_stride[2], c_stride[2], o_stride[2];
+  int64_t y_stride[2];                                                            /* of g_y in dtst_scan_adj */
+  int64_t g_x_stride[2], g_delta_stride[2], g_b_stride[2], g_c_stride[2], g_o_stride[2]; /* dtst_scan_adj only */
+  int32_t type;
+  int32_t accumulate; /* dtst_scan_adj only */
+} dtst_scan_desc;
+dtst_status dtst_scan_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes);
+dtst_status dtst_scan(const dtst_scan_desc* desc, const void* x, const void* delta, const float* a, const void* b,
+                      const void* c, const float* d, const void* o, const float* h_zero, const int32_t* lengths,
+                      void* y, float* h_out, float* states, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The norm of n tensors together,
  *   norm = sqrt( sum_i sum_j tensors[i][j]^2 ),
  * in 64 bits and in a fixed order, rounded to fp32 at the end.  tensors[i]:

@@ -112,6 +112,64 @@ def recurrence(z, v, o=None, h0=None, lengths=None):
     return y, h
 
 
+def scan(x, delta, a, b, c, d=None, o=None, h0=None, lengths=None):
+    """(y, every state (B, T + 1, N, F) with the first before step 0)."""
+    x, delta, a, b, c = (np.asarray(v, np.float64) for v in (x, delta, a, b, c))
+    B, T, F = x.shape
+    n = np.full(B, T) if lengths is None else np.clip(lengths, 0, T)
+    h = np.zeros((B, T + 1) + a.shape)
+    if h0 is not None:
+        h[:, 0] = h0
+    y = np.zeros((B, T, F))
+    for i in range(B):
+        for t in range(T):
+            if t >= n[i]:
+                h[i, t + 1] = h[i, t]
+                continue
+            D = np.logaddexp(0.0, delta[i, t])
+            h[i, t + 1] = np.exp(D * a) * h[i, t] + (D * x[i, t]) * b[i, t][:, None]
+            y[i, t] = (c[i, t][:, None] * h[i, t + 1]).sum(axis=0)
+            if d is not None:
+                y[i, t] += np.asarray(d, np.float64) * x[i, t]
+            if o is not None:
+                ot = np.asarray(o[i, t], np.float64)
+                y[i, t] *= ot * logistic(ot)
+    return y, h
+
+
+def scan_adj(x, delta, a, b, c, g_y, h, d=None, o=None, g_h=None, lengths=None):
+    """Gradients of x, delta, a, b, c, d, o and h0 (a dict) from the states h of scan."""
+    x, delta, a, b, c, g_y = (np.asarray(v, np.float64) for v in (x, delta, a, b, c, g_y))
+    B, T, F = x.shape
+    n = np.full(B, T) if lengths is None else np.clip(lengths, 0, T)
+    g = {k: np.zeros(v.shape) for k, v in dict(x=x, delta=x, a=a, b=b, c=c, o=x).items()}
+    g["d"] = np.zeros(F)
+    q = np.zeros((B,) + a.shape) if g_h is None else np.array(g_h, np.float64)
+    for i in range(B):
+        for t in range(int(n[i]) - 1, -1, -1):
+            D, gy = np.logaddexp(0.0, delta[i, t]), g_y[i, t]
+            before, after = h[i, t], h[i, t + 1]
+            if o is not None:
+                ot = np.asarray(o[i, t], np.float64)
+                s = (c[i, t][:, None] * after).sum(axis=0) + (0.0 if d is None else np.asarray(d, np.float64) * x[i, t])
+                g["o"][i, t] = gy * s * logistic(ot) * (1 + ot * logistic(-ot))
+                gy = gy * ot * logistic(ot)
+            if d is not None:
+                g["d"] += gy * x[i, t]
+                g["x"][i, t] += gy * np.asarray(d, np.float64)
+            g["c"][i, t] = (gy * after).sum(axis=1)
+            q[i] += gy * c[i, t][:, None]
+            g["b"][i, t] = (q[i] * D * x[i, t]).sum(axis=1)
+            E = np.exp(D * a)
+            qb = (q[i] * b[i, t][:, None]).sum(axis=0)
+            g["x"][i, t] += D * qb
+            g["delta"][i, t] = ((q[i] * E * before * a).sum(axis=0) + qb * x[i, t]) * logistic(delta[i, t])
+            g["a"] += q[i] * E * before * D
+            q[i] = E * q[i]
+    g["h0"] = q
+    return g
+
+
 def recurrence_adj(z, v, g_y, h, o=None, g_h=None, lengths=None):
     """(g_z, g_v, g_o, g_h0) from the states h of recurrence."""
     z, v, g_y = (np.asarray(a, np.float64) for a in (z, v, g_y))

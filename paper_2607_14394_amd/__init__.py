@@ -34,6 +34,7 @@ __all__ = [
     "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
     "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace", "dtst_global_norm", "dtst_clip",
+    "SCAN_SPAN", "scan_states_shape", "dtst_scan", "dtst_scan_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdtst.so")
@@ -83,10 +84,12 @@ NORM_ADJ_DESC = struct.Struct("@7q3i4x")
 QUANTISE_DESC = struct.Struct("@7qi4x")
 PRODUCT_DESC = struct.Struct("@8q3i4x")
 RECURRENCE_DESC = struct.Struct("@17qi4x")
+SCAN_DESC = struct.Struct("@26q2i")
 
 # DTST_F32 .. DTST_E4M3 of include/dtst.h
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
 RECURRENCE_SPAN = 128        # DTST_RECURRENCE_SPAN of include/dtst.h
+SCAN_SPAN = 64               # DTST_SCAN_SPAN of include/dtst.h
 
 # DTST_ROWS_* and DTST_BLOCK_* of include/dtst.h
 ROWS_T_FIRST, ROWS_T_FIRST_Y, ROWS_Z_FIRST, ROWS_Z_FIRST_Y = range(4)
@@ -131,6 +134,8 @@ def _load():
         "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
         "dtst_recurrence": [VP] * 10 + [SZ, VP],
         "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
+        "dtst_scan_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
+        "dtst_scan": [VP] * 14 + [SZ, VP],
         "dtst_global_norm_workspace": [I64, VP, ctypes.POINTER(SZ)],
         "dtst_global_norm": [I64] + [VP] * 5 + [SZ, VP],
         "dtst_clip": [I64] + [VP] * 4 + [ctypes.c_float, VP, VP],
@@ -678,6 +683,69 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     status = lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
                                      g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o),
                                      _ptr(g_hzero), p, n, _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+def scan_states_shape(batch, steps, features, states):
+    return (batch, -(-steps // SCAN_SPAN), states, features)
+
+
+@functools.lru_cache(maxsize=1024)
+def dtst_scan_workspace(batch, steps, features, states) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_scan_workspace(int(batch), int(steps), int(features), int(states), ctypes.byref(n)))
+    return n.value
+
+
+def _array(t, shape, name, dev):
+    if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: need contiguous torch.float32 of shape {tuple(shape)} on the current device")
+
+
+_NONE = (0, 0)
+_NO_GRADIENTS = (0,) * 10
+
+
+def dtst_scan(x, delta, a, b, c, y, d=None, o=None, h0=None, h_out=None, lengths=None, states=None, ws=None, stream=None):
+    """h_t = exp(D_t a) h_{t-1} + D_t x_t b_t with D = log(1 + exp(delta)),
+    y_t = (sum over the states of c_t h_t, + d x_t) o_t s(o_t).  x, delta, o, y:
+    (batch, steps, features), b, c: (batch, steps, states), a: (states, features)
+    float32, d: (features,) float32, h0, h_out: (batch, states, features) float32,
+    lengths: (batch,) int32, states: scan_states_shape float32, for the backward."""
+    if x.dim() != 3 or a.dim() != 2:
+        raise ValueError("x must be (batch, steps, features), a (states, features)")
+    shape = B, T, F = x.shape
+    N = a.shape[0]
+    e, dev = x.dtype, _device()
+    if e not in _FLOATS:
+        raise ValueError(f"x: need {' or '.join(str(t) for t in _FLOATS)}")
+    bc = (B, T, N)
+    desc = SCAN_DESC.pack(B, T, F, N, *_sequence(x, shape, "x", e, dev), *_sequence(delta, shape, "delta", e, dev),
+                          *_sequence(b, bc, "b", e, dev), *_sequence(c, bc, "c", e, dev),
+                          *(_NONE if o is None else _sequence(o, shape, "o", e, dev)), *_sequence(y, shape, "y", e, dev),
+                          *_NO_GRADIENTS, _TYPES[e], 0)
+    _array(a, (N, F), "a", dev)
+    if d is not None:
+        _vector(d, F, "d", dev)
+    if h0 is not None:
+        _array(h0, (B, N, F), "h0", dev)
+    if h_out is not None:
+        _array(h_out, (B, N, F), "h_out", dev)
+    if states is not None:
+        _array(states, scan_states_shape(B, T, F, N), "states", dev)
+    if lengths is not None:
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    if T <= SCAN_SPAN and ws is None:  # (none is needed)
+        p, n = None, 0
+    else:
+        p, n, ws = _scratch(ws, dtst_scan_workspace(B, T, F, N), x.device, stream)
+    status = lib.dtst_scan(desc, x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(),
+                           None if d is None else d.data_ptr(), None if o is None else o.data_ptr(),
+                           None if h0 is None else h0.data_ptr(), None if lengths is None else lengths.data_ptr(),
+                           y.data_ptr(), None if h_out is None else h_out.data_ptr(),
+                           None if states is None else states.data_ptr(), p, n,
+                           _current(dev) if stream is None else int(stream))
     if status:
         _check(status)
 

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
+#include <string>
 #include <vector>
 
 #include "api_common.h"
@@ -93,9 +95,124 @@ dtst_status clip(const TensorList& l, const float* norm, float most, void* strea
   return device_status(e, "clip launch");
 }
 
+// The sizes of a scan (or, with states = taps - 1, of a convolution).
+dtst_status check_sizes(int64_t batch, int64_t steps, int64_t features, int64_t states, int type) {
+  if (batch < 0 || steps < 0 || features < 0) return bad("need batch, steps and features >= 0");
+  if (!is_float_type(type)) return bad("type must be DTST_F32, DTST_BF16 or DTST_F16");
+  if (features > (int64_t(1) << 28)) return fail(DTST_ERR_UNSUPPORTED, "features above 2^28");
+  int64_t n = 0, m = 0;
+  if (__builtin_mul_overflow(batch, steps, &n) || __builtin_mul_overflow(n, features, &m) || m > kMost ||
+      __builtin_mul_overflow(n, states + 2, &m) || m > kMost || __builtin_mul_overflow(batch, features, &n) ||
+      __builtin_mul_overflow(n, states + 2, &m) || m > kMost)
+    return bad("problem size overflows the supported element counts");
+  return DTST_OK;
+}
+
+dtst_status check_strides(std::initializer_list<const int64_t*> all) {
+  for (const int64_t* s : all)
+    for (int i = 0; i < 2; ++i)
+      if (s[i] > kMost || s[i] < -kMost) return bad("a stride is too large");
+  return DTST_OK;
+}
+
+dtst_status check_states(int64_t states) {
+  if (states < 1) return bad("need states >= 1");
+  if (states > kScanMaxStates) return fail(DTST_ERR_UNSUPPORTED, "states above " + std::to_string(kScanMaxStates));
+  return DTST_OK;
+}
+
+dtst_status check_scan_desc(const dtst_scan_desc* d) {
+  if (d == nullptr) return bad("descriptor is null");
+  DTST_TRY(check_states(d->states));
+  DTST_TRY(check_sizes(d->batch, d->steps, d->features, d->states, d->type));
+  if (d->accumulate != 0 && d->accumulate != 1) return bad("accumulate must be 0 or 1");
+  return check_strides({d->x_stride, d->delta_stride, d->b_stride, d->c_stride, d->o_stride, d->y_stride, d->g_x_stride,
+                        d->g_delta_stride, d->g_b_stride, d->g_c_stride, d->g_o_stride});
+}
+
+// (workgroups of 256 threads for 256 features of a segment, and for the states)
+dtst_status check_scan_grid(const dtst_scan_desc* d) {
+  const int64_t segments = scan_segments(d->batch, d->steps, d->features);
+  DTST_TRY(check_grid((d->features + 255) / 256 * segments * d->batch, 256));
+  return check_grid((d->batch * d->states * d->features + 255) / 256, 256);
+}
+
+// Every written sequence and block apart from all others but those that it may be.
+dtst_status check_outputs(std::initializer_list<const Sequence*> out, std::initializer_list<const Block*> out_blocks,
+                          std::initializer_list<const Sequence*> in, std::initializer_list<const Block*> in_blocks,
+                          const Block* inplace_out = nullptr, const Block* inplace_in = nullptr) {
+  for (auto o = out.begin(); o != out.end(); ++o) {
+    for (const Sequence* s : in) DTST_TRY(check_no_share(**o, *s));
+    for (const Block* s : in_blocks) DTST_TRY(check_no_share(**o, *s));
+    for (const Block* s : out_blocks) DTST_TRY(check_no_share(**o, *s));
+    for (auto q = out.begin(); q != o; ++q) DTST_TRY(check_no_share(**o, **q));
+  }
+  for (auto o = out_blocks.begin(); o != out_blocks.end(); ++o) {
+    for (const Sequence* s : in) DTST_TRY(check_no_share(*s, **o));
+    for (const Block* s : in_blocks)
+      if (!(*o == inplace_out && s == inplace_in && s->p == (*o)->p)) DTST_TRY(check_no_share(**o, *s));
+    for (auto q = out_blocks.begin(); q != o; ++q) DTST_TRY(check_no_share(**o, **q));
+  }
+  return DTST_OK;
+}
+
+dtst_status scan(const dtst_scan_desc* d, const void* x, const void* delta, const float* a, const void* b,
+                 const void* c, const float* skip, const void* o, const float* h_zero, const int32_t* lengths, void* y,
+                 float* h_out, float* states, void* workspace, size_t workspace_bytes, void* stream) {
+  DTST_TRY(check_scan_desc(d));
+  if (d->batch == 0 || d->features == 0) return ok();
+  const int64_t B = d->batch, T = d->steps, F = d->features, N = d->states;
+  const int size = type_size(d->type);
+  const Sequence sx{x, B, T, F, d->x_stride, size, "x"}, sd{delta, B, T, F, d->delta_stride, size, "delta"};
+  const Sequence sb{b, B, T, N, d->b_stride, size, "b"}, sc{c, B, T, N, d->c_stride, size, "c"};
+  const Sequence so{o, B, T, F, d->o_stride, size, "o"}, sy{y, B, T, F, d->y_stride, size, "y"};
+  if (T > 0) {
+    for (const Sequence* s : {&sx, &sd, &sb, &sc, &sy}) DTST_TRY(check_sequence(*s));
+    if (o) DTST_TRY(check_sequence(so));
+    DTST_TRY(check_align(a, 4, "a"));
+  }
+  if (skip) DTST_TRY(check_align(skip, 4, "d"));
+  if (h_zero) DTST_TRY(check_align(h_zero, 4, "h_zero"));
+  if (h_out) DTST_TRY(check_align(h_out, 4, "h_out"));
+  if (states) DTST_TRY(check_align(states, 4, "states"));
+  if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
+  const size_t need = scan_carry_bytes(*d);
+  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
+  DTST_TRY(check_scan_grid(d));
+  const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
+  const Block ba{T > 0 ? a : nullptr, N * F * 4, "a"}, bd{skip, F * 4, "d"}, bn{lengths, B * 4, "lengths"};
+  const Block bin{h_zero, one, "h_zero"}, bout{h_out, one, "h_out"}, bst{states, one * spans, "states"};
+  const Block bws{need ? workspace : nullptr, int64_t(need), "workspace"};
+  DTST_TRY(check_outputs({&sy}, {&bout, &bst, &bws}, {&sx, &sd, &sb, &sc, &so}, {&ba, &bd, &bn, &bin}, &bout, &bin));
+  const int e = timed(K_SCAN, stream, [&] {
+    return launch_scan(*d, x, delta, a, b, c, skip, o, h_zero, lengths, y, h_out, states, workspace, stream);
+  });
+  return device_status(e, "scan launch");
+}
+
 }  // namespace
 
 extern "C" {
+
+dtst_status dtst_scan_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes) {
+  return guarded([&] {
+    if (bytes == nullptr) return bad("bytes is null");
+    DTST_TRY(check_states(states));
+    DTST_TRY(check_sizes(batch, steps, features, states, DTST_F32));
+    dtst_scan_desc d{};
+    d.batch = batch, d.steps = steps, d.features = features, d.states = states;
+    *bytes = scan_carry_bytes(d);
+    return ok();
+  });
+}
+
+dtst_status dtst_scan(const dtst_scan_desc* desc, const void* x, const void* delta, const float* a, const void* b,
+                      const void* c, const float* d, const void* o, const float* h_zero, const int32_t* lengths,
+                      void* y, float* h_out, float* states, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&] {
+    return scan(desc, x, delta, a, b, c, d, o, h_zero, lengths, y, h_out, states, workspace, workspace_bytes, stream);
+  });
+}
 
 dtst_status dtst_global_norm_workspace(int64_t n, const int64_t* counts, size_t* bytes) {
   return guarded([&] { return global_norm_workspace_of(n, counts, bytes); });

@@ -41,42 +41,6 @@ constexpr int SPAN = DTST_RECURRENCE_SPAN;
 constexpr int WAVES = 8;
 constexpr int RPW = SPAN / WAVES;  // steps of a wave
 
-// exp(-x), of an x of type T.  exp2 takes x's product with -log2 e, which one
-// rounding moves by up to 2^-24 of itself, and so the result by |x| 2^-24 (and
-// the constant's own rounding by a quarter of that): 29 units of 2^-24 at x = 32.
-// That is what half a unit in x's last place does in 32 bits, where the rounding
-// is made good; 16-bit values of x are 2^13 times and more as far apart, and the
-// five instructions are spared.
-template <class T>
-__device__ __forceinline__ float exp_minus(float x) {
-  constexpr float hi = -1.44269502162933349609375f, lo = -1.92596299112661746e-8f, ln2 = 0.693147180559945309f;
-  const float t = x * hi;
-  float e = __builtin_amdgcn_exp2f(t);
-  if constexpr (std::is_same_v<T, float>) {
-    const float rest = fmaf(x, lo, fmaf(x, hi, -t));
-    e *= fmaf(__builtin_amdgcn_fmed3f(rest, -0.01f, 0.01f), ln2, 1.f);  // (far below 0.01 unless e is 0 or infinite)
-  }
-  return e;
-}
-
-// s(x) and s(-x), each to the relative precision of exp_minus (1 - s(x) would
-// lose that of a small s(-x), and 1 / (1 + exp(x)) costs two more
-// transcendentals).  Infinities give 0 and 1, no number gives no number; below x =
-// -88 s(x) is 0.
-template <class T>
-__device__ __forceinline__ void logistic(float x, float& s, float& sn) {
-  const float e = exp_minus<T>(x);
-  s = __builtin_amdgcn_rcpf(1.f + e);
-  sn = x < 0.f ? 1.f - s : e * s;
-}
-template <class T>
-__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + exp_minus<T>(x)); }
-
-struct Strides {
-  int64_t b, t;
-};
-__device__ __forceinline__ int64_t at(Strides s, int64_t b, int64_t t) { return b * s.b + t * s.t; }
-
 struct Args {
   int64_t batch, steps, features;
   Strides z, v, o, y, gz, gv, go;

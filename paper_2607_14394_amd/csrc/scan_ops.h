@@ -1,0 +1,54 @@
+// What the state-space scan's two directions share: the step size of a raw value,
+// the decay of a run of steps, and the arrays' places.
+#pragma once
+
+#include "seq_internal.h"
+#include "seq_ops.h"
+
+namespace dtst {
+
+constexpr int SCAN_SPAN = DTST_SCAN_SPAN;
+constexpr float LOG2E = 1.44269502162933349609375f;
+
+// D = log(1 + exp(d)) = max(d, 0) + log(1 + e), e = exp(-|d|).  1 + e rounds e's
+// low bits off; what it lost, c, goes back in (to first order, whose error is c e /
+// (1 + e), 2^-24 of the result).
+__device__ __forceinline__ float softplus(float d) {
+  constexpr float ln2 = 0.693147180559945309f;
+  const float e = exp_minus<float>(fabsf(d));
+  const float u = 1.f + e, c = e - (u - 1.f);
+  return fmaxf(d, 0.f) + fmaf(__builtin_amdgcn_logf(u), ln2, c);
+}
+
+// exp(a D) of a run of steps whose D come to `sum`, the largest being `most`; a2 =
+// a log2(e).  One that underflows though no step's does stays above zero: it would
+// make no number of an infinite state, which the steps one by one keep.
+__device__ __forceinline__ float run_decay(float a2, float sum, float most) {
+  const float A = __builtin_amdgcn_exp2f(a2 * sum);
+  return a2 * most >= -126.f ? fmaxf(A, __uint_as_float(1)) : A;
+}
+
+struct ScanArgs {
+  int64_t batch, steps, features;
+  int states;
+  Strides x, delta, b, c, o, y, gx, gdelta, gb, gc, go;
+  const int32_t* lengths;
+  int segments;          // of a sequence
+  int64_t segment;       // steps of each but the last, a multiple of SCAN_SPAN
+  int64_t tiles, spans;  // of 64 features; of SCAN_SPAN steps
+};
+
+__device__ __forceinline__ int64_t scan_length(const ScanArgs& p, int64_t b) {
+  if (p.lengths == nullptr) return p.steps;
+  const int64_t n = p.lengths[b];
+  return n < 0 ? 0 : n > p.steps ? p.steps : n;
+}
+
+ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths);
+// Turns the ends in carry (batch, segments, states + 2, features: the state's end
+// from zero, the sum and the largest of the segment's D) into what enters.
+int launch_scan_carry(const ScanArgs& p, const float* a, const float* first, float* carry, float* final, bool reverse,
+                      void* stream);
+int launch_copy_states(const float* in, float* out, int64_t n, void* stream);
+
+}  // namespace dtst

@@ -39,6 +39,12 @@ int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* 
 int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o,
                           const int32_t* lengths, const float* states, const void* g_y, const float* g_h, void* g_z,
                           void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream);
+constexpr int64_t kScanMaxStates = 64;
+int scan_segments(int64_t batch, int64_t steps, int64_t features);
+size_t scan_carry_bytes(const dtst_scan_desc& d);
+int launch_scan(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b, const void* c,
+                const float* skip, const void* o, const float* h_zero, const int32_t* lengths, void* y, float* h_out,
+                float* states, void* workspace, void* stream);
 
 // n tensors: pointers, counts of values, types.  out: where the scaled ones go,
 // null for in place.

@@ -122,3 +122,79 @@ def test_clip_refusals(kw, word):
 
 def test_clip_of_nothing_is_done():
     assert clip_of((), (), ())[0] == 0 and clip_of((0, 0), (0, 0))[0] == 0 and clip_of((0, 0), (0, 0), out=(0, 0))[0] == 0
+
+
+@pytest.mark.parametrize("gated,skip", [(True, True), (False, False)])
+def test_scan_gradient_is_the_derivative(gated, skip):
+    rng = np.random.RandomState(3)
+    B, T, F, N = 3, 4, 2, 3
+    v = dict(x=rng.randn(B, T, F), delta=rng.randn(B, T, F), a=-np.exp(rng.randn(N, F)), b=rng.randn(B, T, N),
+             c=rng.randn(B, T, N), d=rng.randn(F) if skip else None, o=rng.randn(B, T, F) if gated else None,
+             h0=rng.randn(B, N, F))
+    n = np.array([4, 0, 2])
+    g, gh = rng.randn(B, T, F), rng.randn(B, N, F)
+    y, h = S.scan(**v, lengths=n)
+    assert np.array_equal(h[1, -1], v["h0"][1]) and not y[1].any() and not y[2, 2:].any()
+    got = S.scan_adj(*(v[k] for k in ("x", "delta", "a", "b", "c")), g, h, v["d"], v["o"], gh, n)
+
+    def run(**k):
+        y, h = S.scan(**dict(v, **k), lengths=n)
+        return np.concatenate([y.ravel(), h[:, -1].ravel()])
+
+    up = np.concatenate([g.ravel(), gh.ravel()])
+    for k in v:
+        if v[k] is not None:
+            assert np.abs(got[k] - differences(lambda w: run(**{k: w}), v[k], up)).max() < 1e-7, k
+
+
+# batch 2, steps 300, features 16, states 4: sequences 4800 elements an entry, b
+# and c 1200; a: 256 bytes, h: 512, states: 2560
+def scan_call(fn="dtst_scan", x=P, delta=P * 2, a=P * 3, b=P * 4, c=P * 5, d=None, o=None, h0=None, n=None, y=P * 6, h=None,
+              st=None, ws=P * 15, nws=1 << 30, gy=P * 6, gx=P * 7, gdelta=P * 8, ga=P * 9, gb=P * 10, gc=P * 11, gd=None, go=None,
+              **kw):
+    f = dict(batch=2, steps=300, features=16, states=4)
+    f.update({k + "_stride": (4800, 16) for k in ("x", "delta", "b", "c", "o", "y", "g_x", "g_delta", "g_b", "g_c", "g_o")})
+    f.update({k: (1200, 4) for k in ("b_stride", "c_stride", "g_b_stride", "g_c_stride")})
+    f.update(type=1, accumulate=0)
+    f.update(kw)
+    flat = []
+    for v in f.values():
+        flat += list(v) if isinstance(v, tuple) else [v]
+    desc = D.SCAN_DESC.pack(*flat)
+    if fn == "dtst_scan":
+        return status(D.lib.dtst_scan, desc, x, delta, a, b, c, d, o, h0, n, y, h, st, ws, nws, None)
+    return status(D.lib.dtst_scan_adj, desc, x, delta, a, b, c, d, o, n, st, gy, h0, gx, gdelta, ga, gb, gc, gd, go, h, ws, nws,
+                  None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(batch=-1), 1, "batch"), (dict(steps=-1), 1, "steps"), (dict(states=0), 1, "states"), (dict(states=65), 2, "states"),
+    (dict(type=3), 1, "type"), (dict(accumulate=2), 1, "accumulate"), (dict(x=None), 1, "x is null"),
+    (dict(b=None), 1, "b is null"), (dict(a=None), 1, "a is null"), (dict(a=P * 3 + 2), 1, "a is not aligned"),
+    (dict(d=P * 12 + 2), 1, "d is not aligned"), (dict(h0=P * 12 + 2), 1, "h_zero is not aligned"),
+    (dict(delta=P * 2 + 1), 1, "aligned"), (dict(x_stride=(4800, 15)), 1, "strides of x"), (dict(c_stride=(1200, 3)), 1, "strides of c"),
+    (dict(y_stride=(160, 16)), 1, "rows of y"), (dict(o_stride=(1 << 60, 16)), 1, "too large"),
+    (dict(batch=1 << 40, steps=1 << 40), 1, "overflow"), (dict(nws=64), 1, "workspace"), (dict(ws=None), 1, "workspace"),
+    (dict(y=P), 1, "y and x overlap"), (dict(y=P * 2 + 16), 1, "y and delta overlap"), (dict(y=P * 4), 1, "y and b overlap"),
+    (dict(y=P * 5 + 2400), 1, "y and c overlap"), (dict(o=P * 6), 1, "y and o overlap"), (dict(y=P * 3), 1, "y and a overlap"),
+    (dict(y=P * 12, d=P * 12 + 64), 1, "y and d overlap"), (dict(h=P * 6), 1, "y and h_out overlap"),
+    (dict(st=P * 6 + 4), 1, "y and states overlap"), (dict(ws=P * 6), 1, "y and workspace overlap"),
+    (dict(h=P * 4), 1, "b and h_out overlap"), (dict(h=P * 3 + 252), 1, "h_out and a overlap"),
+    (dict(h0=P * 12, h=P * 12 + 64), 1, "h_out and h_zero overlap"), (dict(h=P * 12, st=P * 12 + 508), 1, "states and h_out overlap"),
+    (dict(n=P * 12, h=P * 12 + 4), 1, "h_out and lengths overlap"), (dict(ws=P), 1, "x and workspace overlap"),
+    (dict(ws=P * 12, h0=P * 12 + 64), 1, "workspace and h_zero overlap"), (dict(batch=1 << 33, steps=1), 2, "too many"),
+])
+def test_scan_refusals(kw, code, word):
+    st, msg = scan_call(**kw)
+    assert st == code and word in msg, (st, msg)
+
+
+def test_scan_of_nothing_is_done():
+    assert scan_call(batch=0, x=None)[0] == 0 and scan_call(features=0, x=None)[0] == 0
+    assert D.scan_states_shape(3, 129, 5, 7) == (3, 3, 7, 5) and D.scan_states_shape(3, 0, 5, 7) == (3, 0, 7, 5)
+
+
+def test_scan_binding_refuses_tensors_off_the_device():
+    z, a = torch.zeros(1, 4, 8), torch.zeros(2, 8)
+    with pytest.raises(ValueError):
+        D.dtst_scan(z, z, a, z[..., :2], z[..., :2], torch.empty_like(z))
