@@ -489,6 +489,26 @@ dtst_status dtst_scan(const dtst_scan_desc* desc, const void* x, const void* del
                       const void* c, const float* d, const void* o, const float* h_zero, const int32_t* lengths,
                       void* y, float* h_out, float* states, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Backward of dtst_scan from its inputs and states, with E_t = exp(D_t a),
+ * g_t = g_y_t o_t s(o_t) (g_y_t without o), q_t the gradient that reaches h_t,
+ * q_t = g_t c_t + e_t, e_{t-1} = E_t q_t, and g_h (the gradient of h_out; NULL for
+ * zero) as the last e_t; sums over the features f, the states n, and the steps and
+ * entries t:
+ *   g_x_t = D_t sum_n q_t b_t + g_t d,    g_b_t = sum_f q_t D_t x_t,
+ *   g_delta_t = ( x_t sum_n q_t b_t + sum_n a e_{t-1} h_{t-1} ) s(delta_t),
+ *   g_c_t = sum_f g_t h_t,   g_a = sum_t D_t e_{t-1} h_{t-1},   g_d = sum_t g_t x_t,
+ *   g_o_t = g_y_t ( sum_n c_t h_t + d x_t ) s(o_t) (1 + o_t s(-o_t)),  g_hzero = e_{-1}.
+ * g_y, g_x, g_delta, g_b, g_c and g_o are of `type`; g_o NULL without o; g_a:
+ * (states, features) fp32 and g_d: features fp32 (NULL without d), overwritten or
+ * (accumulate = 1) added to; g_hzero: (batch, states, features) fp32 or NULL, and
+ * may be g_h itself.  Gradients are zero past a sequence's length.  The sums have a
+ * fixed order.  workspace: dtst_scan_adj_workspace bytes, any contents. */
+dtst_status dtst_scan_adj_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes);
+dtst_status dtst_scan_adj(const dtst_scan_desc* desc, const void* x, const void* delta, const float* a, const void* b,
+                          const void* c, const float* d, const void* o, const int32_t* lengths, const float* states,
+                          const void* g_y, const float* g_h, void* g_x, void* g_delta, float* g_a, void* g_b, void* g_c,
+                          float* g_d, void* g_o, float* g_hzero, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The norm of n tensors together,
  *   norm = sqrt( sum_i sum_j tensors[i][j]^2 ),
  * in 64 bits and in a fixed order, rounded to fp32 at the end.  tensors[i]:

@@ -34,7 +34,8 @@ __all__ = [
     "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
     "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace", "dtst_global_norm", "dtst_clip",
-    "SCAN_SPAN", "scan_states_shape", "dtst_scan", "dtst_scan_workspace",
+    "SCAN_SPAN", "scan_states_shape", "dtst_scan", "dtst_scan_workspace", "dtst_scan_adj",
+    "dtst_scan_adj_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdtst.so")
@@ -136,6 +137,8 @@ def _load():
         "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
         "dtst_scan_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
         "dtst_scan": [VP] * 14 + [SZ, VP],
+        "dtst_scan_adj_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
+        "dtst_scan_adj": [VP] * 21 + [SZ, VP],
         "dtst_global_norm_workspace": [I64, VP, ctypes.POINTER(SZ)],
         "dtst_global_norm": [I64] + [VP] * 5 + [SZ, VP],
         "dtst_clip": [I64] + [VP] * 4 + [ctypes.c_float, VP, VP],
@@ -746,6 +749,55 @@ def dtst_scan(x, delta, a, b, c, y, d=None, o=None, h0=None, h_out=None, lengths
                            y.data_ptr(), None if h_out is None else h_out.data_ptr(),
                            None if states is None else states.data_ptr(), p, n,
                            _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+@functools.lru_cache(maxsize=1024)
+def dtst_scan_adj_workspace(batch, steps, features, states) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_scan_adj_workspace(int(batch), int(steps), int(features), int(states), ctypes.byref(n)))
+    return n.value
+
+
+def dtst_scan_adj(x, delta, a, b, c, g_y, states, g_x, g_delta, g_a, g_b, g_c, d=None, g_d=None, o=None, g_o=None, g_h=None,
+                  g_hzero=None, lengths=None, accumulate=False, ws=None, stream=None):
+    """Backward of dtst_scan from its inputs and states: the gradients of each
+    operand in its shape and type and, from the gradient g_h of the last states,
+    g_hzero of the first.  accumulate: g_a and g_d are added to."""
+    if x.dim() != 3 or a.dim() != 2:
+        raise ValueError("x must be (batch, steps, features), a (states, features)")
+    shape = B, T, F = x.shape
+    N = a.shape[0]
+    e, dev = x.dtype, _device()
+    if e not in _FLOATS:
+        raise ValueError(f"x: need {' or '.join(str(t) for t in _FLOATS)}")
+    if (o is None) != (g_o is None):
+        raise ValueError("g_o goes with o")
+    bc = (B, T, N)
+    desc = SCAN_DESC.pack(B, T, F, N, *_sequence(x, shape, "x", e, dev), *_sequence(delta, shape, "delta", e, dev),
+                          *_sequence(b, bc, "b", e, dev), *_sequence(c, bc, "c", e, dev),
+                          *(_NONE if o is None else _sequence(o, shape, "o", e, dev)),
+                          *_sequence(g_y, shape, "g_y", e, dev), *_sequence(g_x, shape, "g_x", e, dev),
+                          *_sequence(g_delta, shape, "g_delta", e, dev), *_sequence(g_b, bc, "g_b", e, dev),
+                          *_sequence(g_c, bc, "g_c", e, dev),
+                          *(_NONE if g_o is None else _sequence(g_o, shape, "g_o", e, dev)), _TYPES[e], int(accumulate))
+    _array(a, (N, F), "a", dev)
+    _array(g_a, (N, F), "g_a", dev)
+    _array(states, scan_states_shape(B, T, F, N), "states", dev)
+    for t, name in ((d, "d"), (g_d, "g_d")):
+        if t is not None:
+            _vector(t, F, name, dev)
+    for t, name in ((g_h, "g_h"), (g_hzero, "g_hzero")):
+        if t is not None:
+            _array(t, (B, N, F), name, dev)
+    if lengths is not None:
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    p, n, ws = _scratch(ws, dtst_scan_adj_workspace(B, T, F, N), x.device, stream)
+    status = lib.dtst_scan_adj(desc, x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(), _ptr(d),
+                               _ptr(o), _ptr(lengths), states.data_ptr(), g_y.data_ptr(), _ptr(g_h), g_x.data_ptr(),
+                               g_delta.data_ptr(), g_a.data_ptr(), g_b.data_ptr(), g_c.data_ptr(), _ptr(g_d), _ptr(g_o),
+                               _ptr(g_hzero), p, n, _current(dev) if stream is None else int(stream))
     if status:
         _check(status)
 

@@ -137,6 +137,16 @@ dtst_status check_scan_grid(const dtst_scan_desc* d) {
   return check_grid((d->batch * d->states * d->features + 255) / 256, 256);
 }
 
+dtst_status scan_workspace_of(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj, size_t* bytes) {
+  if (bytes == nullptr) return bad("bytes is null");
+  DTST_TRY(check_states(states));
+  DTST_TRY(check_sizes(batch, steps, features, states, DTST_F32));
+  dtst_scan_desc d{};
+  d.batch = batch, d.steps = steps, d.features = features, d.states = states;
+  *bytes = adj ? scan_adj_workspace(d) : scan_carry_bytes(d);
+  return ok();
+}
+
 // Every written sequence and block apart from all others but those that it may be.
 dtst_status check_outputs(std::initializer_list<const Sequence*> out, std::initializer_list<const Block*> out_blocks,
                           std::initializer_list<const Sequence*> in, std::initializer_list<const Block*> in_blocks,
@@ -190,20 +200,77 @@ dtst_status scan(const dtst_scan_desc* d, const void* x, const void* delta, cons
   return device_status(e, "scan launch");
 }
 
+dtst_status scan_adj(const dtst_scan_desc* d, const void* x, const void* delta, const float* a, const void* b,
+                     const void* c, const float* skip, const void* o, const int32_t* lengths, const float* states,
+                     const void* g_y, const float* g_h, void* g_x, void* g_delta, float* g_a, void* g_b, void* g_c,
+                     float* g_skip, void* g_o, float* g_hzero, void* workspace, size_t workspace_bytes, void* stream) {
+  DTST_TRY(check_scan_desc(d));
+  const int64_t B = d->batch, T = d->steps, F = d->features, N = d->states;
+  if (F == 0) return ok();
+  const bool steps = B > 0 && T > 0;
+  if (steps && (o != nullptr) != (g_o != nullptr)) return bad("g_o goes with o");
+  if (g_skip != nullptr && skip == nullptr) return bad("g_d goes with d");
+  const int size = type_size(d->type);
+  const Sequence sx{x, B, T, F, d->x_stride, size, "x"}, sd{delta, B, T, F, d->delta_stride, size, "delta"};
+  const Sequence sb{b, B, T, N, d->b_stride, size, "b"}, sc{c, B, T, N, d->c_stride, size, "c"};
+  const Sequence so{o, B, T, F, d->o_stride, size, "o"}, sg{g_y, B, T, F, d->y_stride, size, "g_y"};
+  const Sequence gx{g_x, B, T, F, d->g_x_stride, size, "g_x"}, gd{g_delta, B, T, F, d->g_delta_stride, size, "g_delta"};
+  const Sequence gb{g_b, B, T, N, d->g_b_stride, size, "g_b"}, gc{g_c, B, T, N, d->g_c_stride, size, "g_c"};
+  const Sequence go{g_o, B, T, F, d->g_o_stride, size, "g_o"};
+  DTST_TRY(check_align(g_a, 4, "g_a"));
+  if (steps) {
+    for (const Sequence* s : {&sx, &sd, &sb, &sc, &sg, &gx, &gd, &gb, &gc}) DTST_TRY(check_sequence(*s));
+    if (o)
+      for (const Sequence* s : {&so, &go}) DTST_TRY(check_sequence(*s));
+    DTST_TRY(check_align(a, 4, "a"));
+    DTST_TRY(check_align(states, 4, "states"));
+  }
+  if (skip) DTST_TRY(check_align(skip, 4, "d"));
+  if (g_skip) DTST_TRY(check_align(g_skip, 4, "g_d"));
+  if (g_h) DTST_TRY(check_align(g_h, 4, "g_h"));
+  if (g_hzero) DTST_TRY(check_align(g_hzero, 4, "g_hzero"));
+  if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
+  const size_t need = scan_adj_workspace(*d);
+  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
+  DTST_TRY(check_scan_grid(d));
+  // (a workgroup for 64 features of a segment; four waves for 64 steps of g_b and g_c)
+  DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F) * B, 256));
+  const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
+  DTST_TRY(check_grid((B * spans * 2 * N + 3) / 4, 256));
+  DTST_TRY(check_grid(((N + 1) * F + 31) / 32, 1024));
+  const Block ba{steps ? a : nullptr, N * F * 4, "a"}, bd{skip, F * 4, "d"}, bn{lengths, B * 4, "lengths"};
+  const Block bst{steps ? states : nullptr, one * spans, "states"}, bin{g_h, one, "g_h"}, bout{g_hzero, one, "g_hzero"};
+  const Block bga{g_a, N * F * 4, "g_a"}, bgd{g_skip, F * 4, "g_d"};
+  const Block bws{need ? workspace : nullptr, int64_t(need), "workspace"};
+  DTST_TRY(check_outputs({&gx, &gd, &gb, &gc, &go}, {&bga, &bgd, &bout, &bws}, {&sx, &sd, &sb, &sc, &so, &sg},
+                         {&ba, &bd, &bn, &bst, &bin}, &bout, &bin));
+  const int e = timed(K_SCAN_ADJ, stream, [&] {
+    return launch_scan_adj(*d, x, delta, a, b, c, skip, o, lengths, states, g_y, g_h, g_x, g_delta, g_a, g_b, g_c, g_skip,
+                           g_o, g_hzero, workspace, stream);
+  });
+  return device_status(e, "scan backward launch");
+}
+
 }  // namespace
 
 extern "C" {
 
-dtst_status dtst_scan_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes) {
+dtst_status dtst_scan_adj_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes) {
+  return guarded([&] { return scan_workspace_of(batch, steps, features, states, true, bytes); });
+}
+
+dtst_status dtst_scan_adj(const dtst_scan_desc* desc, const void* x, const void* delta, const float* a, const void* b,
+                          const void* c, const float* d, const void* o, const int32_t* lengths, const float* states,
+                          const void* g_y, const float* g_h, void* g_x, void* g_delta, float* g_a, void* g_b, void* g_c,
+                          float* g_d, void* g_o, float* g_hzero, void* workspace, size_t workspace_bytes, void* stream) {
   return guarded([&] {
-    if (bytes == nullptr) return bad("bytes is null");
-    DTST_TRY(check_states(states));
-    DTST_TRY(check_sizes(batch, steps, features, states, DTST_F32));
-    dtst_scan_desc d{};
-    d.batch = batch, d.steps = steps, d.features = features, d.states = states;
-    *bytes = scan_carry_bytes(d);
-    return ok();
+    return scan_adj(desc, x, delta, a, b, c, d, o, lengths, states, g_y, g_h, g_x, g_delta, g_a, g_b, g_c, g_d, g_o,
+                    g_hzero, workspace, workspace_bytes, stream);
   });
+}
+
+dtst_status dtst_scan_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes) {
+  return guarded([&] { return scan_workspace_of(batch, steps, features, states, false, bytes); });
 }
 
 dtst_status dtst_scan(const dtst_scan_desc* desc, const void* x, const void* delta, const float* a, const void* b,

@@ -321,20 +321,20 @@ norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* _
   }
 }
 
-// g_w[c] (+)= sum_p part[p][c], and g_b from the columns past g_w's where there
-// is one: 32 columns a workgroup, 32 lanes a column, each taking every 32nd part
+// g_w[c] (+)= sum_p part[p][c] of rows `pitch` apart, and g_b from the columns
+// past g_w's, up to `width`: 32 columns a workgroup, 32 lanes a column, each taking every 32nd part
 // (64 columns by 16 waves left the loads one after the other: 15 us for 751 parts
 // of 1537 columns).
 __global__ void __launch_bounds__(1024)
-sum_parts_kernel(const float* __restrict__ part, int parts, int64_t cols, int64_t width, int accumulate, float* g_w,
-                 float* g_b) {
+sum_parts_kernel(const float* __restrict__ part, int64_t parts, int64_t pitch, int64_t cols, int64_t width,
+                 int accumulate, float* g_w, float* g_b) {
   __shared__ float red[32][33];
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int64_t c = int64_t(blockIdx.x) * 32 + lane;
   float s = 0.f;
   if (c < width) {
 #pragma unroll 8
-    for (int p = group; p < parts; p += 32) s += part[p * width + c];
+    for (int64_t p = group; p < parts; p += 32) s += part[p * pitch + c];
   }
   red[group][lane] = s;
   __syncthreads();
@@ -414,12 +414,18 @@ int norm_backward(const dtst_norm_adj_desc& d, const NormAdjArgs& a, float* g_we
     if (e != hipSuccess) return e;
   }
   const int64_t width = d.cols * (MEAN ? 2 : 1);
-  hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((width + 31) / 32)), dim3(1024), 0, s, a.part,
-                     d.rows > 0 ? int(norm_adj_parts(d.rows, d.cols)) : 0, d.cols, width, d.accumulate, g_weight, g_bias);
-  return hipGetLastError();
+  return launch_sum_parts(a.part, d.rows > 0 ? norm_adj_parts(d.rows, d.cols) : 0, width, d.cols, width, d.accumulate,
+                          g_weight, g_bias, stream);
 }
 
 }  // namespace
+
+int launch_sum_parts(const float* part, int64_t parts, int64_t pitch, int64_t cols, int64_t width, int accumulate,
+                     float* first, float* second, void* stream) {
+  hipLaunchKernelGGL(sum_parts_kernel, dim3(unsigned((width + 31) / 32)), dim3(1024), 0,
+                     static_cast<hipStream_t>(stream), part, parts, pitch, cols, width, accumulate, first, second);
+  return hipGetLastError();
+}
 
 int launch_rms_norm(const dtst_norm_desc& d, const void* x, const void* res, const float* weight, void* sum_out,
                     void* y, void* scale, float* rstd, void* stream) {

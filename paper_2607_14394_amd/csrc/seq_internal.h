@@ -29,6 +29,10 @@ size_t layer_norm_adj_workspace(int64_t rows, int64_t cols);
 int launch_layer_norm_adj(const dtst_norm_adj_desc& d, const void* g_y, const void* u, const float* weight,
                           const float* mean, const float* rstd, const void* g_sum, void* g_u, void* g_x,
                           float* g_weight, float* g_bias, void* workspace, void* stream);
+// first (cols) and second (the columns from there to width) as the sum, or (accumulate)
+// with the sum, of `parts` rows of part.  In a fixed order.
+int launch_sum_parts(const float* part, int64_t parts, int64_t pitch, int64_t cols, int64_t width, int accumulate,
+                     float* first, float* second, void* stream);
 int launch_quantise(const dtst_quantise_desc& d, const void* x, void* q, void* scale, void* qt, void* scale_t,
                     void* stream);
 int launch_product(const dtst_product_desc& d, const void* a, const void* a_scale, const void* b, const void* b_scale,
@@ -45,6 +49,11 @@ size_t scan_carry_bytes(const dtst_scan_desc& d);
 int launch_scan(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b, const void* c,
                 const float* skip, const void* o, const float* h_zero, const int32_t* lengths, void* y, float* h_out,
                 float* states, void* workspace, void* stream);
+size_t scan_adj_workspace(const dtst_scan_desc& d);
+int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b,
+                    const void* c, const float* skip, const void* o, const int32_t* lengths, const float* states,
+                    const void* g_y, const float* g_h, void* g_x, void* g_delta, float* g_a, void* g_b, void* g_c,
+                    float* g_skip, void* g_o, float* g_hzero, void* workspace, void* stream);
 
 // n tensors: pointers, counts of values, types.  out: where the scaled ones go,
 // null for in place.

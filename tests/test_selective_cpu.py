@@ -198,3 +198,29 @@ def test_scan_binding_refuses_tensors_off_the_device():
     z, a = torch.zeros(1, 4, 8), torch.zeros(2, 8)
     with pytest.raises(ValueError):
         D.dtst_scan(z, z, a, z[..., :2], z[..., :2], torch.empty_like(z))
+
+
+# as scan_call, with states at P * 13; g_h in h0's place, g_hzero in h's
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(states=65), 2, "states"), (dict(accumulate=2), 1, "accumulate"), (dict(st=None), 1, "states is null"),
+    (dict(ga=None), 1, "g_a is null"), (dict(ga=P * 9 + 2), 1, "g_a is not aligned"), (dict(gx=None), 1, "g_x is null"),
+    (dict(gc=None), 1, "g_c is null"), (dict(gb=P * 10 + 1), 1, "g_b is not aligned"), (dict(o=P * 12), 1, "g_o goes with o"),
+    (dict(go=P * 12), 1, "g_o goes with o"), (dict(gd=P * 12), 1, "g_d goes with d"), (dict(ws=None), 1, "workspace"),
+    (dict(nws=64), 1, "workspace"), (dict(g_x_stride=(4800, 15)), 1, "strides of g_x"), (dict(g_c_stride=(1200, 3)), 1, "strides of g_c"),
+    (dict(gx=P), 1, "g_x and x overlap"), (dict(gdelta=P * 6 + 32), 1, "g_delta and g_y overlap"),
+    (dict(gb=P * 7), 1, "g_b and g_x overlap"), (dict(gc=P * 10 + 1200), 1, "g_c and g_b overlap"),
+    (dict(gx=P * 13), 1, "g_x and states overlap"), (dict(ga=P * 3), 1, "g_a and a overlap"),
+    (dict(ga=P * 8 + 64), 1, "g_delta and g_a overlap"), (dict(ga=P * 13 - 252), 1, "g_a and states overlap"),
+    (dict(d=P * 12, gd=P * 12), 1, "g_d and d overlap"), (dict(d=P * 12, gd=P * 9 + 252), 1, "g_d and g_a overlap"),
+    (dict(h=P * 13), 1, "g_hzero and states overlap"), (dict(h=P * 14, h0=P * 14 + 256), 1, "g_hzero and g_h overlap"),
+    (dict(h=P * 9 + 4), 1, "g_hzero and g_a overlap"), (dict(ws=P * 13), 1, "workspace and states overlap"),
+    (dict(ws=P * 9 - 64), 1, "workspace and g_a overlap"), (dict(n=P * 7), 1, "g_x and lengths overlap"),
+    (dict(batch=1 << 33, steps=1, nws=1 << 62), 2, "too many"),
+])
+def test_scan_adj_refusals(kw, code, word):
+    st, msg = scan_call("dtst_scan_adj", **dict(dict(st=P * 13), **kw))
+    assert st == code and word in msg, (st, msg)
+
+
+def test_scan_adj_of_no_features_is_done():
+    assert scan_call("dtst_scan_adj", features=0, x=None, ga=None)[0] == 0
