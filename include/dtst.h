@@ -455,6 +455,41 @@ dtst_status dtst_recurrence_adj(const dtst_recurrence_desc* d, const void* z, co
                                 void* g_z, void* g_v, void* g_o, float* g_hzero, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* Short causal convolution along the steps, feature by feature, with K = taps:
+ *   v_t = bias + sum_{k < K} weight[k] x_{t-K+1+k},   y_t = v_t s(v_t) with silu = 1, else v_t,
+ * s as in dtst_recurrence.  x, y: (batch, steps, features) of `type`, each with a
+ * stride of batch entries and of steps; weight: (K, features) fp32, the last for the
+ * step itself; bias: features fp32, or NULL.  state: (batch, K - 1, features) of
+ * `type`, the inputs before the first step, oldest first, NULL for zeros; state_out:
+ * the same after the last step, NULL if not wanted; it may be state itself, which is
+ * a serving step with steps = 1.  lengths as in dtst_recurrence: from lengths[b] on y
+ * is zero and x is not read, and state_out is of what lies before.  1 to 8 taps
+ * (DTST_ERR_UNSUPPORTED above). */
+typedef struct {
+  int64_t batch, steps, features, taps;
+  int64_t x_stride[2], y_stride[2]; /* y_stride: of g_y in dtst_conv_adj */
+  int64_t g_x_stride[2];            /* dtst_conv_adj only */
+  int32_t type, silu;
+  int32_t accumulate; /* dtst_conv_adj only */
+} dtst_conv_desc;
+dtst_status dtst_conv(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias, const void* state,
+                      const int32_t* lengths, void* y, void* state_out, void* stream);
+
+/* Backward of dtst_conv from its inputs, with p_t = g_y_t s(v_t) (1 + v_t s(-v_t))
+ * (g_y_t without silu; zero past a sequence's length):
+ *   g_x_t = sum_k weight[k] p_{t+K-1-k},  and the state's rows alike,
+ *   g_weight[k] = sum p_t x_{t-K+1+k},   g_bias = sum p_t,
+ * and g_state_out (the gradient of state_out; NULL for zero) added to the rows that
+ * state_out holds.  g_y, g_x, g_state_out and g_state are of `type`; g_weight: (K,
+ * features) fp32 and g_bias: features fp32 (NULL if not wanted), overwritten or
+ * (accumulate = 1) added to, in a fixed order; g_state NULL if not wanted.  Past a
+ * sequence's length g_x is zero.  workspace: dtst_conv_adj_workspace bytes. */
+dtst_status dtst_conv_adj_workspace(int64_t batch, int64_t steps, int64_t features, int64_t taps, size_t* bytes);
+dtst_status dtst_conv_adj(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias,
+                          const void* state, const int32_t* lengths, const void* g_y, const void* g_state_out, void* g_x,
+                          float* g_weight, float* g_bias, void* g_state, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
 /* Selective state-space scan along the steps: each feature has N states h[n],
  * whose decay and input depend on the step,
  *   D_t = log(1 + exp(delta_t)),

@@ -112,6 +112,47 @@ def recurrence(z, v, o=None, h0=None, lengths=None):
     return y, h
 
 
+def conv(x, w, bias=None, state=None, lengths=None, silu=True):
+    """(y, the state after the last step)."""
+    x, w = np.asarray(x, np.float64), np.asarray(w, np.float64)
+    (B, T, F), K = x.shape, len(w)
+    n = np.full(B, T) if lengths is None else np.clip(lengths, 0, T)
+    y, last = np.zeros((B, T, F)), np.zeros((B, K - 1, F))
+    for i in range(B):
+        z = np.zeros((K - 1 + n[i], F))
+        if state is not None:
+            z[:K - 1] = state[i]
+        z[K - 1:] = x[i, :n[i]]
+        for t in range(n[i]):
+            v = (w * z[t:t + K]).sum(axis=0) + (0.0 if bias is None else np.asarray(bias, np.float64))
+            y[i, t] = v * logistic(v) if silu else v
+        last[i] = z[n[i]:]
+    return y, last
+
+
+def conv_adj(x, w, g_y, bias=None, state=None, g_last=None, lengths=None, silu=True):
+    """(g_x, g_w, g_bias, g_state) of conv."""
+    x, w, g_y = (np.asarray(a, np.float64) for a in (x, w, g_y))
+    (B, T, F), K = x.shape, len(w)
+    n = np.full(B, T) if lengths is None else np.clip(lengths, 0, T)
+    g_x, g_w, g_b, g_s = np.zeros((B, T, F)), np.zeros((K, F)), np.zeros(F), np.zeros((B, K - 1, F))
+    for i in range(B):
+        z, gz = np.zeros((K - 1 + n[i], F)), np.zeros((K - 1 + n[i], F))
+        if state is not None:
+            z[:K - 1] = state[i]
+        z[K - 1:] = x[i, :n[i]]
+        if g_last is not None:
+            gz[n[i]:] = g_last[i]
+        for t in range(n[i]):
+            v = (w * z[t:t + K]).sum(axis=0) + (0.0 if bias is None else np.asarray(bias, np.float64))
+            p = g_y[i, t] * (logistic(v) * (1 + v * logistic(-v)) if silu else 1.0)
+            gz[t:t + K] += w * p
+            g_w += p * z[t:t + K]
+            g_b += p
+        g_s[i], g_x[i, :n[i]] = gz[:K - 1], gz[K - 1:]
+    return g_x, g_w, g_b, g_s
+
+
 def scan(x, delta, a, b, c, d=None, o=None, h0=None, lengths=None):
     """(y, every state (B, T + 1, N, F) with the first before step 0)."""
     x, delta, a, b, c = (np.asarray(v, np.float64) for v in (x, delta, a, b, c))

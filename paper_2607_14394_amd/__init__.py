@@ -34,7 +34,7 @@ __all__ = [
     "dtst_rms_norm_adj", "dtst_rms_norm_adj_workspace", "dtst_quantise", "dtst_product",
     "dtst_recurrence", "dtst_recurrence_adj", "dtst_recurrence_workspace",
     "dtst_layer_norm", "dtst_layer_norm_adj", "dtst_layer_norm_adj_workspace", "dtst_global_norm", "dtst_clip",
-    "SCAN_SPAN", "scan_states_shape", "dtst_scan", "dtst_scan_workspace", "dtst_scan_adj",
+    "dtst_conv", "dtst_conv_adj", "dtst_conv_adj_workspace", "SCAN_SPAN", "scan_states_shape", "dtst_scan", "dtst_scan_workspace", "dtst_scan_adj",
     "dtst_scan_adj_workspace",
 ]
 
@@ -85,6 +85,7 @@ NORM_ADJ_DESC = struct.Struct("@7q3i4x")
 QUANTISE_DESC = struct.Struct("@7qi4x")
 PRODUCT_DESC = struct.Struct("@8q3i4x")
 RECURRENCE_DESC = struct.Struct("@17qi4x")
+CONV_DESC = struct.Struct("@10q3i4x")
 SCAN_DESC = struct.Struct("@26q2i")
 
 # DTST_F32 .. DTST_E4M3 of include/dtst.h
@@ -135,6 +136,9 @@ def _load():
         "dtst_recurrence_workspace": [I64, I64, I64, I, ctypes.POINTER(SZ)],
         "dtst_recurrence": [VP] * 10 + [SZ, VP],
         "dtst_recurrence_adj": [VP] * 13 + [SZ, VP],
+        "dtst_conv": [VP] * 9,
+        "dtst_conv_adj_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
+        "dtst_conv_adj": [VP] * 13 + [SZ, VP],
         "dtst_scan_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
         "dtst_scan": [VP] * 14 + [SZ, VP],
         "dtst_scan_adj_workspace": [I64, I64, I64, I64, ctypes.POINTER(SZ)],
@@ -686,6 +690,82 @@ def dtst_recurrence_adj(z, v, g_y, states, g_z, g_v, o=None, g_o=None, g_h=None,
     status = lib.dtst_recurrence_adj(d, z.data_ptr(), v.data_ptr(), _ptr(o), _ptr(lengths), states.data_ptr(),
                                      g_y.data_ptr(), _ptr(g_h), g_z.data_ptr(), g_v.data_ptr(), _ptr(g_o),
                                      _ptr(g_hzero), p, n, _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+def _typed_state(t, shape, name, dtype, dev):
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: need contiguous {dtype} of shape {tuple(shape)} on the current device")
+
+
+def dtst_conv(x, weight, y, bias=None, state=None, state_out=None, lengths=None, silu=True, stream=None):
+    """y_t = act(bias + sum_k weight_k x_{t-K+1+k}) along the steps of (batch, steps,
+    features), act(v) = v s(v) (silu) or v.  weight: (taps, features) float32, bias:
+    (features,) float32, state, state_out: the taps - 1 inputs before the first and
+    after the last step, (batch, taps - 1, features) of x's type, lengths: (batch,)
+    int32."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be (batch, steps, features), weight (taps, features)")
+    shape = B, T, F = x.shape
+    K = weight.shape[0]
+    e, dev = x.dtype, _device()
+    if e not in _FLOATS:
+        raise ValueError(f"x: need {' or '.join(str(t) for t in _FLOATS)}")
+    d = CONV_DESC.pack(B, T, F, K, *_sequence(x, shape, "x", e, dev), *_sequence(y, shape, "y", e, dev), 0, 0, _TYPES[e],
+                       int(silu), 0)
+    _array(weight, (K, F), "weight", dev)
+    if bias is not None:
+        _vector(bias, F, "bias", dev)
+    if state is not None:
+        _typed_state(state, (B, K - 1, F), "state", e, dev)
+    if state_out is not None:
+        _typed_state(state_out, (B, K - 1, F), "state_out", e, dev)
+    if lengths is not None:
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    status = lib.dtst_conv(d, x.data_ptr(), weight.data_ptr(), None if bias is None else bias.data_ptr(),
+                           None if state is None else state.data_ptr(), None if lengths is None else lengths.data_ptr(),
+                           y.data_ptr(), None if state_out is None else state_out.data_ptr(),
+                           _current(dev) if stream is None else int(stream))
+    if status:
+        _check(status)
+
+
+@functools.lru_cache(maxsize=1024)
+def dtst_conv_adj_workspace(batch, steps, features, taps) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.dtst_conv_adj_workspace(int(batch), int(steps), int(features), int(taps), ctypes.byref(n)))
+    return n.value
+
+
+def dtst_conv_adj(x, weight, g_y, g_x, g_weight, bias=None, g_bias=None, state=None, g_state_out=None, g_state=None,
+                  lengths=None, silu=True, accumulate=False, ws=None, stream=None):
+    """Backward of dtst_conv from its inputs: g_x, g_weight, g_bias and, with the
+    gradient g_state_out of the inputs after the last step, g_state of those before
+    the first.  accumulate: g_weight and g_bias are added to."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be (batch, steps, features), weight (taps, features)")
+    shape = B, T, F = x.shape
+    K = weight.shape[0]
+    e, dev = x.dtype, _device()
+    if e not in _FLOATS:
+        raise ValueError(f"x: need {' or '.join(str(t) for t in _FLOATS)}")
+    d = CONV_DESC.pack(B, T, F, K, *_sequence(x, shape, "x", e, dev), *_sequence(g_y, shape, "g_y", e, dev),
+                       *_sequence(g_x, shape, "g_x", e, dev), _TYPES[e], int(silu), int(accumulate))
+    _array(weight, (K, F), "weight", dev)
+    _array(g_weight, (K, F), "g_weight", dev)
+    for t, name in ((bias, "bias"), (g_bias, "g_bias")):
+        if t is not None:
+            _vector(t, F, name, dev)
+    for t, name in ((state, "state"), (g_state_out, "g_state_out"), (g_state, "g_state")):
+        if t is not None:
+            _typed_state(t, (B, K - 1, F), name, e, dev)
+    if lengths is not None:
+        _vector(lengths, B, "lengths", dev, torch.int32)
+    p, n, ws = _scratch(ws, dtst_conv_adj_workspace(B, T, F, K), x.device, stream)
+    status = lib.dtst_conv_adj(d, x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), _ptr(lengths), g_y.data_ptr(),
+                               _ptr(g_state_out), g_x.data_ptr(), g_weight.data_ptr(), _ptr(g_bias), _ptr(g_state), p, n,
+                               _current(dev) if stream is None else int(stream))
     if status:
         _check(status)
 

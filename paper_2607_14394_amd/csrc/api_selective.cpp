@@ -115,6 +115,21 @@ dtst_status check_strides(std::initializer_list<const int64_t*> all) {
   return DTST_OK;
 }
 
+dtst_status check_taps(int64_t taps) {
+  if (taps < 1) return bad("need taps >= 1");
+  if (taps > kConvMaxTaps) return fail(DTST_ERR_UNSUPPORTED, "taps above " + std::to_string(kConvMaxTaps));
+  return DTST_OK;
+}
+
+dtst_status check_conv_desc(const dtst_conv_desc* d) {
+  if (d == nullptr) return bad("descriptor is null");
+  DTST_TRY(check_taps(d->taps));
+  DTST_TRY(check_sizes(d->batch, d->steps, d->features, d->taps - 1, d->type));
+  if (d->silu != 0 && d->silu != 1) return bad("silu must be 0 or 1");
+  if (d->accumulate != 0 && d->accumulate != 1) return bad("accumulate must be 0 or 1");
+  return check_strides({d->x_stride, d->y_stride, d->g_x_stride});
+}
+
 dtst_status check_states(int64_t states) {
   if (states < 1) return bad("need states >= 1");
   if (states > kScanMaxStates) return fail(DTST_ERR_UNSUPPORTED, "states above " + std::to_string(kScanMaxStates));
@@ -164,6 +179,70 @@ dtst_status check_outputs(std::initializer_list<const Sequence*> out, std::initi
     for (auto q = out_blocks.begin(); q != o; ++q) DTST_TRY(check_no_share(**o, **q));
   }
   return DTST_OK;
+}
+
+dtst_status conv(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias, const void* state,
+                 const int32_t* lengths, void* y, void* state_out, void* stream) {
+  DTST_TRY(check_conv_desc(d));
+  const int64_t B = d->batch, T = d->steps, F = d->features, rows = B * (d->taps - 1);
+  if (B == 0 || F == 0) return ok();
+  const int size = type_size(d->type);
+  const Sequence sx{x, B, T, F, d->x_stride, size, "x"}, sy{y, B, T, F, d->y_stride, size, "y"};
+  if (T > 0) {
+    DTST_TRY(check_sequence(sx));
+    DTST_TRY(check_sequence(sy));
+    DTST_TRY(check_align(weight, 4, "weight"));
+  }
+  if (bias) DTST_TRY(check_align(bias, 4, "bias"));
+  if (state) DTST_TRY(check_align(state, size, "state"));
+  if (state_out) DTST_TRY(check_align(state_out, size, "state_out"));
+  if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
+  DTST_TRY(check_grid(conv_groups(*d, false), 256));
+  DTST_TRY(check_grid((rows * F + 255) / 256, 256));
+  const Block bw{T > 0 ? weight : nullptr, d->taps * F * 4, "weight"}, bb{bias, F * 4, "bias"}, bn{lengths, B * 4, "lengths"};
+  const Block bin{state, rows * F * size, "state"}, bout{state_out, rows * F * size, "state_out"};
+  DTST_TRY(check_outputs({&sy}, {&bout}, {&sx}, {&bw, &bb, &bn, &bin}, &bout, &bin));
+  const int e = timed(K_CONV, stream,
+                      [&] { return launch_conv(*d, x, weight, bias, state, lengths, y, state_out, stream); });
+  return device_status(e, "convolution launch");
+}
+
+dtst_status conv_adj(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias, const void* state,
+                     const int32_t* lengths, const void* g_y, const void* g_state_out, void* g_x, float* g_weight,
+                     float* g_bias, void* g_state, void* workspace, size_t workspace_bytes, void* stream) {
+  DTST_TRY(check_conv_desc(d));
+  const int64_t B = d->batch, T = d->steps, F = d->features, rows = B * (d->taps - 1);
+  if (F == 0) return ok();
+  const bool steps = B > 0 && T > 0;
+  const int size = type_size(d->type);
+  const Sequence sx{x, B, T, F, d->x_stride, size, "x"}, sg{g_y, B, T, F, d->y_stride, size, "g_y"};
+  const Sequence gx{g_x, B, T, F, d->g_x_stride, size, "g_x"};
+  DTST_TRY(check_align(g_weight, 4, "g_weight"));
+  if (steps) {
+    for (const Sequence* s : {&sx, &sg, &gx}) DTST_TRY(check_sequence(*s));
+    DTST_TRY(check_align(weight, 4, "weight"));
+  }
+  if (bias) DTST_TRY(check_align(bias, 4, "bias"));
+  if (g_bias) DTST_TRY(check_align(g_bias, 4, "g_bias"));
+  if (state) DTST_TRY(check_align(state, size, "state"));
+  if (g_state_out) DTST_TRY(check_align(g_state_out, size, "g_state_out"));
+  if (g_state) DTST_TRY(check_align(g_state, size, "g_state"));
+  if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
+  const size_t need = conv_adj_workspace(*d);
+  DTST_TRY(check_workspace(workspace, workspace_bytes, need));
+  DTST_TRY(check_grid(conv_groups(*d, true), 256));
+  DTST_TRY(check_grid((rows * F + 255) / 256, 256));
+  DTST_TRY(check_grid(((d->taps + 1) * F + 31) / 32, 1024));
+  const Block bw{steps ? weight : nullptr, d->taps * F * 4, "weight"}, bb{bias, F * 4, "bias"}, bn{lengths, B * 4, "lengths"};
+  const Block bin{state, rows * F * size, "state"}, bgo{g_state_out, rows * F * size, "g_state_out"};
+  const Block bgs{g_state, rows * F * size, "g_state"}, bgw{g_weight, d->taps * F * 4, "g_weight"};
+  const Block bgb{g_bias, F * 4, "g_bias"}, bws{need ? workspace : nullptr, int64_t(need), "workspace"};
+  DTST_TRY(check_outputs({&gx}, {&bgw, &bgb, &bgs, &bws}, {&sx, &sg}, {&bw, &bb, &bn, &bin, &bgo}));
+  const int e = timed(K_CONV_ADJ, stream, [&] {
+    return launch_conv_adj(*d, x, weight, bias, state, lengths, g_y, g_state_out, g_x, g_weight, g_bias, g_state,
+                           workspace, stream);
+  });
+  return device_status(e, "convolution backward launch");
 }
 
 dtst_status scan(const dtst_scan_desc* d, const void* x, const void* delta, const float* a, const void* b,
@@ -254,6 +333,33 @@ dtst_status scan_adj(const dtst_scan_desc* d, const void* x, const void* delta, 
 }  // namespace
 
 extern "C" {
+
+dtst_status dtst_conv(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias, const void* state,
+                      const int32_t* lengths, void* y, void* state_out, void* stream) {
+  return guarded([&] { return conv(d, x, weight, bias, state, lengths, y, state_out, stream); });
+}
+
+dtst_status dtst_conv_adj_workspace(int64_t batch, int64_t steps, int64_t features, int64_t taps, size_t* bytes) {
+  return guarded([&] {
+    if (bytes == nullptr) return bad("bytes is null");
+    DTST_TRY(check_taps(taps));
+    DTST_TRY(check_sizes(batch, steps, features, taps - 1, DTST_F32));
+    dtst_conv_desc d{};
+    d.batch = batch, d.steps = steps, d.features = features, d.taps = taps;
+    *bytes = conv_adj_workspace(d);
+    return ok();
+  });
+}
+
+dtst_status dtst_conv_adj(const dtst_conv_desc* d, const void* x, const float* weight, const float* bias,
+                          const void* state, const int32_t* lengths, const void* g_y, const void* g_state_out, void* g_x,
+                          float* g_weight, float* g_bias, void* g_state, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  return guarded([&] {
+    return conv_adj(d, x, weight, bias, state, lengths, g_y, g_state_out, g_x, g_weight, g_bias, g_state, workspace,
+                    workspace_bytes, stream);
+  });
+}
 
 dtst_status dtst_scan_adj_workspace(int64_t batch, int64_t steps, int64_t features, int64_t states, size_t* bytes) {
   return guarded([&] { return scan_workspace_of(batch, steps, features, states, true, bytes); });

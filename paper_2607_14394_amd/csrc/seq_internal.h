@@ -43,6 +43,15 @@ int launch_recurrence(const dtst_recurrence_desc& d, const void* z, const void* 
 int launch_recurrence_adj(const dtst_recurrence_desc& d, const void* z, const void* v, const void* o,
                           const int32_t* lengths, const float* states, const void* g_y, const float* g_h, void* g_z,
                           void* g_v, void* g_o, float* g_hzero, void* workspace, void* stream);
+constexpr int64_t kConvMaxTaps = 8;
+int64_t conv_groups(const dtst_conv_desc& d, bool adj);  // workgroups of 256
+int launch_conv(const dtst_conv_desc& d, const void* x, const float* w, const float* bias, const void* state,
+                const int32_t* lengths, void* y, void* state_out, void* stream);
+size_t conv_adj_workspace(const dtst_conv_desc& d);
+int launch_conv_adj(const dtst_conv_desc& d, const void* x, const float* w, const float* bias, const void* state,
+                    const int32_t* lengths, const void* g_y, const void* g_state_out, void* g_x, float* g_weight,
+                    float* g_bias, void* g_state, void* workspace, void* stream);
+
 constexpr int64_t kScanMaxStates = 64;
 int scan_segments(int64_t batch, int64_t steps, int64_t features);
 size_t scan_carry_bytes(const dtst_scan_desc& d);

@@ -224,3 +224,86 @@ def test_scan_adj_refusals(kw, code, word):
 
 def test_scan_adj_of_no_features_is_done():
     assert scan_call("dtst_scan_adj", features=0, x=None, ga=None)[0] == 0
+
+
+@pytest.mark.parametrize("silu", [True, False])
+@pytest.mark.parametrize("K", [1, 2, 4])
+def test_conv_gradient_is_the_derivative(silu, K):
+    rng = np.random.RandomState(4)
+    B, T, F = 4, 5, 2
+    v = dict(x=rng.randn(B, T, F), w=rng.randn(K, F), bias=rng.randn(F), state=rng.randn(B, K - 1, F))
+    n = np.array([5, 0, 1, 3])
+    g, gl = rng.randn(B, T, F), rng.randn(B, K - 1, F)
+    got = dict(zip(("x", "w", "bias", "state"), S.conv_adj(v["x"], v["w"], g, v["bias"], v["state"], gl, n, silu)))
+
+    def run(**k):
+        y, last = S.conv(**dict(v, **k), lengths=n, silu=silu)
+        return np.concatenate([y.ravel(), last.ravel()])
+
+    up = np.concatenate([g.ravel(), gl.ravel()])
+    for k in v:
+        assert np.abs(got[k] - differences(lambda w: run(**{k: w}), v[k], up)).max(initial=0) < 1e-7, k
+
+
+def test_conv_is_torchs():
+    rng = np.random.RandomState(5)
+    x, w, b = rng.randn(2, 9, 3), rng.randn(4, 3), rng.randn(3)
+    t = torch.nn.functional.conv1d(torch.from_numpy(x).transpose(1, 2), torch.from_numpy(w.T.copy())[:, None], torch.from_numpy(b),
+                                   padding=3, groups=3)[..., :9].transpose(1, 2)
+    assert np.abs(S.conv(x, w, b, silu=False)[0] - t.numpy()).max() < 1e-13
+    assert np.abs(S.conv(x, w, b)[0] - torch.nn.functional.silu(t).numpy()).max() < 1e-13
+
+
+# batch 2, steps 300, features 16, taps 4: weight 256 bytes, state 192 (bf16)
+def conv_call(fn="dtst_conv", x=P, w=P * 2, b=None, s=None, n=None, y=P * 3, so=None, gx=P * 4, gw=P * 5, gb=None, gs=None,
+              ws=P * 15, nws=1 << 30, **kw):
+    f = dict(batch=2, steps=300, features=16, taps=4, x_stride=(4800, 16), y_stride=(4800, 16), g_x_stride=(4800, 16), type=1,
+             silu=1, accumulate=0)
+    f.update(kw)
+    flat = []
+    for v in f.values():
+        flat += list(v) if isinstance(v, tuple) else [v]
+    desc = D.CONV_DESC.pack(*flat)
+    if fn == "dtst_conv":
+        return status(D.lib.dtst_conv, desc, x, w, b, s, n, y, so, None)
+    return status(D.lib.dtst_conv_adj, desc, x, w, b, s, n, y, so, gx, gw, gb, gs, ws, nws, None)
+
+
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(batch=-1), 1, "batch"), (dict(taps=0), 1, "taps"), (dict(taps=9), 2, "taps"), (dict(type=3), 1, "type"),
+    (dict(silu=2), 1, "silu"), (dict(x=None), 1, "x is null"), (dict(w=None), 1, "weight is null"), (dict(y=P * 3 + 1), 1, "aligned"),
+    (dict(b=P * 6 + 2), 1, "bias is not aligned"), (dict(s=P * 6 + 1), 1, "state is not aligned"), (dict(x_stride=(4800, 15)), 1, "strides of x"),
+    (dict(y_stride=(1 << 60, 16)), 1, "too large"), (dict(y=P + 32), 1, "y and x overlap"), (dict(y=P * 2), 1, "y and weight overlap"),
+    (dict(s=P * 3), 1, "y and state overlap"), (dict(so=P * 3), 1, "y and state_out overlap"), (dict(so=P), 1, "x and state_out overlap"),
+    (dict(s=P * 6, so=P * 6 + 96), 1, "state_out and state overlap"), (dict(so=P * 2 + 252), 1, "state_out and weight overlap"),
+    (dict(n=P * 6, so=P * 6), 1, "state_out and lengths overlap"), (dict(batch=1 << 40, steps=1 << 40), 1, "overflow"),
+    (dict(batch=1 << 36, steps=1, x_stride=(16, 16), y_stride=(16, 16)), 2, "too many"),
+])
+def test_conv_refusals(kw, code, word):
+    st, msg = conv_call(**kw)
+    assert st == code and word in msg, (st, msg)
+
+
+# (y is g_y, so g_state_out)
+@pytest.mark.parametrize("kw,code,word", [
+    (dict(taps=9), 2, "taps"), (dict(accumulate=2), 1, "accumulate"), (dict(gw=None), 1, "g_weight is null"), (dict(gx=None), 1, "g_x is null"),
+    (dict(ws=None), 1, "workspace"), (dict(nws=64), 1, "workspace"), (dict(gx=P * 3), 1, "g_x and g_y overlap"),
+    (dict(gx=P), 1, "g_x and x overlap"), (dict(gw=P * 2), 1, "g_weight and weight overlap"), (dict(gb=P * 5 + 252), 1, "g_bias and g_weight overlap"),
+    (dict(s=P * 6, gs=P * 6), 1, "g_state and state overlap"), (dict(so=P * 6, gs=P * 6 + 188), 1, "g_state and g_state_out overlap"),
+    (dict(gs=P * 4), 1, "g_x and g_state overlap"), (dict(ws=P * 5), 1, "workspace and g_weight overlap"),
+    (dict(so=P * 15), 1, "workspace and g_state_out overlap"), (dict(ws=P), 1, "x and workspace overlap"),
+])
+def test_conv_adj_refusals(kw, code, word):
+    st, msg = conv_call("dtst_conv_adj", **kw)
+    assert st == code and word in msg, (st, msg)
+
+
+def test_conv_of_nothing_is_done():
+    assert conv_call(batch=0, x=None)[0] == 0 and conv_call(features=0, x=None)[0] == 0
+    assert conv_call("dtst_conv_adj", features=0, x=None, gw=None)[0] == 0
+
+
+def test_conv_binding_refuses_tensors_off_the_device():
+    z, w = torch.zeros(1, 4, 8), torch.zeros(2, 8)
+    with pytest.raises(ValueError):
+        D.dtst_conv(z, w, torch.empty_like(z))
