@@ -1,0 +1,321 @@
+"""The selective block: its operators one after the other against 64 bits on the
+values that each was given, forward and backward; sequences against serving steps,
+in a graph too; what lies past a length; blocks of both kinds in a rollout; the
+clipping of their gradients."""
+
+import math
+
+import numpy as np
+import pytest
+
+from gpu_common import say, torch_gpu
+from oracle import seq_oracle as S
+from seq_common import f64, near, rounded
+
+pytestmark = pytest.mark.gpu
+
+# Sequences against steps: a norm's code or a bf16 result at a rounding's edge
+# falls to either side, and a whole bf16 step bounds what that moves.
+BAR = 2.0 ** -7
+
+
+def rel(a, b):
+    return float(np.linalg.norm(a - b) / np.linalg.norm(b))
+
+
+def build(torch, W, F, N, K, seed):
+    from paper_2607_14394_amd.rollout import SelectiveBlock
+    rng = np.random.RandomState(seed)
+    f = lambda a: rounded(torch, a, "f32")[0]  # noqa: E731
+    return SelectiveBlock(f(1 + 0.2 * rng.randn(W)), f(0.2 * rng.randn(W)), f(rng.randn(2 * F, W) / W ** 0.5),
+                          f(0.3 * rng.randn(2 * F)), f(rng.randn(K, F) / K ** 0.5), f(0.2 * rng.randn(F)),
+                          f(rng.randn(F + 2 * N, F) / F ** 0.5), f(np.concatenate([rng.randn(F) - 2, 0.3 * rng.randn(2 * N)])),
+                          f(-np.exp(rng.uniform(-1, 2, (N, F)))), f(rng.randn(F)), f(rng.randn(W, F) / F ** 0.5))
+
+
+def some_state(torch, block, B, seed):
+    rng = np.random.RandomState(seed)
+    return tuple(rounded(torch, rng.randn(*t.shape), k)[0] for t, k in zip(block.state(B), ("bf16", "f32")))
+
+
+def values(q):
+    """What codes stand for."""
+    import torch
+    e = q[1].view(torch.uint8).cpu().numpy()[:, :q[0].shape[1] // 128].astype(int) - 127
+    return S.values(q[0].float().cpu().numpy(), e)
+
+
+def product_near(got, a, b, bias, name, before=None):
+    """bf16 products: one rounding, and 32-bit sums of terms of size |a| |b|."""
+    ref = S.product(a, b, bias)
+    size = np.sqrt((a ** 2).sum(axis=1)[:, None] * (b ** 2).sum(axis=1)[None, :]) + (0 if bias is None else np.abs(bias))
+    if before is not None:
+        ref, size = ref + before, size + np.abs(before)
+    off = np.abs(got - ref) - (2.0 ** -8 * np.abs(ref) + 2.0 ** -20 * size)
+    assert (off <= 0).all(), f"{name}: off by up to {off.max():.2e}"
+
+
+CASES = [(2, 150, 384, 256, 16, 4, None), (3, 140, 200, 130, 5, 3, [140, 0, 77]), (4, 1, 640, 320, 8, 4, None)]
+
+
+@pytest.mark.parametrize("B,T,W,F,N,K,lengths", CASES)
+def test_operator_by_operator(B, T, W, F, N, K, lengths):
+    torch = torch_gpu()
+    block = build(torch, W, F, N, K, T)
+    rng = np.random.RandomState(W)
+    R = B * T
+    say(f"[selective] {B} x {T} x {W}, {F} features, {N} states, {K} taps, lengths {lengths}")
+    x, xv = rounded(torch, rng.randn(B, T, W), "bf16")
+    res, rv = rounded(torch, 2 * rng.randn(B, T, W), "f32")
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    first = some_state(torch, block, B, 1)
+    state, keep = tuple(s.clone() for s in first), {}
+    out, u = block.forward(x, res, state, n, keep)
+    live = np.ones((B, T), bool) if lengths is None else np.arange(T) < np.array(lengths)[:, None]
+    past = ~live.reshape(R)
+
+    # forward: the norm, the products, the convolution and the scan, each on what it was given
+    assert np.array_equal(f64(u), np.float32(xv) + np.float32(rv))
+    uv = f64(keep["u"]).reshape(R, W)
+    y64, mean, rstd = S.layer_norm(uv, f64(block.norm), f64(block.norm_bias), 1e-5)
+    near(f64(keep["mean"])[~past], mean[~past], "f32", "mean")
+    near(f64(keep["rstd"])[~past], rstd[~past], "f32", "rstd")
+    plain = values(keep["nt"])[:, :R].T
+    e = np.exp2(np.ceil(np.log2(np.maximum(np.abs(y64).max(axis=0), 1e-30) / 448)))   # (a code's step is 2^-4 of its value, 2^-9 of the scale at least)
+    assert (np.abs(plain - y64)[~past] <= (2.0 ** -4 * 1.01 * np.abs(y64) + 2.0 ** -9 * e + 2.0 ** -7 * np.abs(y64))[~past]).all()
+    sv, vv, pv = (f64(keep[k]) for k in ("s", "v", "p"))
+    v64, last = S.conv(sv[..., :F], f64(block.conv), f64(block.conv_bias), f64(first[0]), lengths)
+    near(vv, v64, "bf16", "v")
+    assert np.array_equal(f64(state[0]), last)
+    vq = S.values(*S.quantise(vv.reshape(R, F)))
+    product_near(pv.reshape(R, -1), vq, values(block.w_x.rows), f64(block.b_x), "p")
+    args = dict(x=vv, delta=pv[..., :F], a=f64(block.a), b=pv[..., F:F + N], c=pv[..., F + N:], d=f64(block.d), o=sv[..., F:],
+                h0=f64(first[1]), lengths=None if lengths is None else np.array(lengths))
+    yv, hv = S.scan(**args)
+    near(f64(state[1]), hv[:, -1], "f32", "h")
+    yt = values(keep["yt"])[:, :R].T
+    assert rel(yt, yv.reshape(R, F)) <= 2.0 ** -4 + 2.0 ** -8
+    near(f64(keep["states"]), hv[:, :-1:64], "f32", "states")
+
+    # backward: the same
+    g_out, gov = rounded(torch, rng.randn(B, T, W), "bf16")
+    g_res, grv = rounded(torch, rng.randn(B, T, W), "f32")
+    g_end = some_state(torch, block, B, 2)
+    got = block.backward(keep, g_out, g_res, g_end)
+    go = np.where(past[:, None], 0, gov.reshape(R, W))
+    gq, gqt = S.values(*S.quantise(go)), S.values(*S.quantise(go.T))[:, :R]
+    g_y = S.product(gq, values(block.w_out.cols)).reshape(B, T, F)
+    g_y = torch.from_numpy(g_y).to(torch.bfloat16).double().numpy()
+    # (a gradient of the scan's output at a rounding's edge may be its neighbour: 2^-8 of a value, in the norm)
+    want = S.scan_adj(*(args[k] for k in ("x", "delta", "a", "b", "c")), g_y, hv, args["d"], args["o"], f64(g_end[1]), args["lengths"])
+    for k in ("a", "d"):
+        assert rel(f64(got[k]), want[k]) <= 2.0 ** -8, k
+    assert rel(f64(got["state"][1]), want["h0"]) <= 2.0 ** -8
+    assert np.linalg.norm(f64(got["w_out"]) - gqt @ yt) <= 2.0 ** -20 * np.linalg.norm(gqt) * np.linalg.norm(yt)
+    g_p = torch.from_numpy(np.concatenate([want["delta"], want["b"], want["c"]], axis=2)).to(torch.bfloat16).double().numpy().reshape(R, -1)
+    assert rel(f64(got["b_x"]), g_p.sum(axis=0)) <= BAR
+    g_v = S.product(S.values(*S.quantise(g_p)), values(block.w_x.cols)).reshape(B, T, F) + want["x"]
+    gx, gw, gb, gs = S.conv_adj(sv[..., :F], f64(block.conv), g_v, f64(block.conv_bias), f64(first[0]), f64(g_end[0]), lengths)
+    # (three roundings to 8 bits in a row: gradients at an edge fall to either side; two roundings of g_v to bf16)
+    for k, ref in (("conv", gw), ("conv_bias", gb)):
+        assert rel(f64(got[k]), ref) <= 2 * BAR, k
+    assert rel(f64(got["state"][0]), gs) <= 2 * BAR
+    g_s = torch.from_numpy(np.concatenate([gx, want["o"]], axis=2)).to(torch.bfloat16).double().numpy().reshape(R, -1)
+    assert rel(f64(got["b_in"]), g_s.sum(axis=0)) <= 2 * BAR
+    g_n = S.product(S.values(*S.quantise(g_s)), values(block.w_in.cols))
+    gu, gnw, gnb = S.layer_norm_adj(g_n[~past], uv[~past], f64(block.norm), 1e-5, grv.reshape(R, W)[~past])
+    assert rel(f64(got["res"]).reshape(R, W)[~past], gu) <= 2 * BAR and rel(f64(got["x"]).reshape(R, W)[~past], gu) <= 2 * BAR
+    assert rel(f64(got["norm"]), gnw) <= 2 * BAR and rel(f64(got["norm_bias"]), gnb) <= 2 * BAR
+
+
+def test_gradients_are_those_of_the_layer_without_8_bits():
+    """Against autograd in 64 bits on unquantised weights: e4m3 keeps a value within
+    2^-4 of itself (2.6% rms); up to five products in a row and their mutual
+    effects within 30%."""
+    torch = torch_gpu()
+    B, T, W, F, N, K = 2, 40, 256, 128, 8, 4
+    block = build(torch, W, F, N, K, 3)
+    rng = np.random.RandomState(4)
+    g32 = np.random.RandomState(3)
+    # the weights as build made them
+    norm, nb = np.float32(1 + 0.2 * g32.randn(W)).astype(float), np.float32(0.2 * g32.randn(W)).astype(float)
+    w_in = np.float32(g32.randn(2 * F, W) / W ** 0.5).astype(float)
+    g32.randn(2 * F)
+    g32.randn(K, F)
+    g32.randn(F)
+    w_x = np.float32(g32.randn(F + 2 * N, F) / F ** 0.5).astype(float)
+    g32.randn(F)
+    g32.randn(2 * N)
+    g32.uniform(-1, 2, (N, F))
+    g32.randn(F)
+    w_out = np.float32(g32.randn(W, F) / F ** 0.5).astype(float)
+    assert np.array_equal(norm, f64(block.norm)) and np.array_equal(nb, f64(block.norm_bias))
+    x, xv = rounded(torch, rng.randn(B, T, W), "bf16")
+    res, rv = rounded(torch, rng.randn(B, T, W), "f32")
+    g, gv = rounded(torch, rng.randn(B, T, W), "bf16")
+    t = {k: torch.tensor(v, requires_grad=True) for k, v in dict(
+        x=xv, norm=norm, norm_bias=nb, w_in=w_in, b_in=f64(block.b_in), conv=f64(block.conv), conv_bias=f64(block.conv_bias),
+        w_x=w_x, b_x=f64(block.b_x), a=f64(block.a), d=f64(block.d), w_out=w_out).items()}
+    u = t["x"] + torch.tensor(rv)
+    n = torch.nn.functional.layer_norm(u, (W,), t["norm"], t["norm_bias"], 1e-5)
+    s, o = (n @ t["w_in"].T + t["b_in"]).split(F, dim=2)
+    z = torch.cat([torch.zeros(B, K - 1, F, dtype=torch.float64), s], dim=1)
+    v = torch.nn.functional.silu(t["conv_bias"] + sum(z[:, k:k + T] * t["conv"][k] for k in range(K)))
+    delta, b, c = (v @ t["w_x"].T + t["b_x"]).split([F, N, N], dim=2)
+    D = torch.nn.functional.softplus(delta, threshold=50)
+    h, ys = torch.zeros(B, N, F, dtype=torch.float64), []
+    for i in range(T):
+        h = torch.exp(D[:, i, None] * t["a"]) * h + (D * v)[:, i, None] * b[:, i, :, None]
+        ys.append(((c[:, i, :, None] * h).sum(dim=1) + t["d"] * v[:, i]) * torch.nn.functional.silu(o[:, i]))
+    out = torch.stack(ys, dim=1) @ t["w_out"].T
+    out.backward(torch.tensor(gv))
+    keep = {}
+    got_out, _ = block.forward(x, res, keep=keep)
+    got = block.backward(keep, g, None)
+    assert rel(f64(got_out), out.detach().numpy()) <= 0.3
+    for name, p in t.items():
+        e = rel(f64(got[name]), p.grad.numpy())
+        say(f"  g_{name}: rel {e:.2e}")
+        assert e <= 0.3, name
+
+
+def test_steps_follow_the_sequence_and_replay():
+    torch = torch_gpu()
+    B, T, W = 4, 12, 512
+    block = build(torch, W, 320, 16, 4, 7)
+    rng = np.random.RandomState(8)
+    x, _ = rounded(torch, rng.randn(B, T, W), "bf16")
+    res, _ = rounded(torch, rng.randn(B, T, W), "f32")
+    first = some_state(torch, block, B, 9)
+    fresh = lambda: tuple(s.clone() for s in first)  # noqa: E731
+    state, step_state, outs = fresh(), fresh(), []
+    out, u = block.forward(x, res.clone(), state)
+    for t in range(T):
+        c, r = block.forward(x[:, t:t + 1].contiguous(), res[:, t:t + 1].contiguous(), step_state)
+        outs.append(c)
+        assert torch.equal(r[:, 0], u[:, t])
+    assert rel(f64(torch.cat(outs, dim=1)), f64(out)) <= BAR
+    assert all(rel(f64(a), f64(b)) <= BAR for a, b in zip(step_state, state))
+    xs, rs, live = x[:, :1].contiguous(), res[:, :1].contiguous(), fresh()
+    block.forward(xs, rs.clone(), fresh())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c, _ = block.forward(xs, rs, live)
+    for a, b in zip(live, first):
+        a.copy_(b)
+    for t in range(T):
+        xs.copy_(x[:, t:t + 1])
+        rs.copy_(res[:, t:t + 1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c, outs[t]), t
+    assert all(torch.equal(a, b) for a, b in zip(live, step_state))
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), 1e30])
+def test_what_lies_past_a_length_reaches_no_gradient(junk):
+    torch = torch_gpu()
+    B, T, W, lengths = 3, 130, 200, [130, 0, 71]
+    block = build(torch, W, 96, 6, 4, 5)
+    rng = np.random.RandomState(6)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    past = (torch.arange(T, device="cuda") >= n[:, None])[..., None]
+    x, res, g_out, g_res = (rounded(torch, rng.randn(B, T, W), t)[0] for t in ("bf16", "f32", "bf16", "f32"))
+    first, g_end = some_state(torch, block, B, 1), some_state(torch, block, B, 2)
+    say(f"[past lengths] {junk}")
+    runs = []
+    for fill in (0.0, junk):
+        state, keep = tuple(s.clone() for s in first), {}
+        out, u = block.forward(x.masked_fill(past, fill), res.masked_fill(past, fill), state, n, keep)
+        g = block.backward(keep, g_out.masked_fill(past, fill), g_res.masked_fill(past, fill), g_end)
+        g.update(out=out, u=u.masked_fill(past, 0), x=g["x"].masked_fill(past, 0), res=g["res"].masked_fill(past, 0),
+                 **{f"state{i}": s for i, s in enumerate(state + g.pop("state"))})
+        runs.append(g)
+    for name, ref in runs[0].items():
+        assert torch.isfinite(ref).all(), name
+        assert torch.equal(runs[1][name], ref), name
+
+
+@pytest.mark.parametrize("B,T", [(2, 0), (0, 3)])
+@pytest.mark.parametrize("with_lengths", [False, True])
+def test_a_block_over_no_steps(B, T, with_lengths):
+    torch = torch_gpu()
+    W, F, N, K = 200, 96, 6, 4
+    block = build(torch, W, F, N, K, 7)
+    n = torch.zeros(B, dtype=torch.int32, device="cuda") if with_lengths else None
+    x, res = torch.zeros(B, T, W, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, T, W, device="cuda")
+    first, g_end = some_state(torch, block, B, 1), some_state(torch, block, B, 2)
+    state, keep = tuple(s.clone() for s in first), {}
+    same = lambda: all(torch.equal(a, b) for a, b in zip(state, first))  # noqa: E731
+    out, u = block.forward(x, res, state, n, keep)
+    assert out.shape == u.shape == (B, T, W) and same()
+    assert block.forward(x, res, state, n)[0].shape == (B, T, W) and same()
+    g = block.backward(keep, torch.zeros_like(out), torch.zeros_like(u), g_end)
+    assert all(torch.equal(a, b) for a, b in zip(g["state"], g_end)) and g["x"].shape == g["res"].shape == (B, T, W)
+    for name in ("norm", "norm_bias", "w_in", "b_in", "conv", "conv_bias", "w_x", "b_x", "a", "d", "w_out"):
+        assert not g[name].any(), name
+
+
+def test_fields_are_marched_by_blocks_of_both_kinds():
+    torch = torch_gpu()
+    from paper_2607_14394_amd.rollout import Rollout
+    from test_gpu_rollout import Block
+    grid = dict(n_global=(16, 12, 20), n_local=(16, 12, 20), offset=(0, 0, 0), kmax=(2, 3, 2))
+    B, T, C = 2, 6, 3
+    W = 2 * C * 4 * 6 * 4
+    ro = Rollout(grid, C, B, [build(torch, W, 192, 16, 4, 1), Block(torch, W, 192, 2).block, build(torch, W, 130, 4, 2, 3)])
+    f, _ = rounded(torch, np.random.RandomState(5).randn(B, T, C, 16, 12, 20), "f32")
+    whole = ro.advance(f)
+    ro.reset()
+    steps = torch.cat([ro.advance(f[:, t:t + 1]) for t in range(T)], dim=1)
+    say(f"  steps against the sequence: rel {rel(f64(steps), f64(whole)):.2e}")
+    # (three blocks, in each of which roundings fall to either side)
+    assert rel(f64(steps), f64(whole)) <= 3 * BAR
+    far = ro.march(f[:, -1], 3)
+    assert far.shape == (B, 3, C, 16, 12, 20) and bool(torch.isfinite(far).all())
+    ro.close()
+
+
+def test_gradients_of_blocks_are_clipped_together():
+    torch = torch_gpu()
+    from paper_2607_14394_amd.rollout import clip_gradients
+    B, T, W = 2, 30, 128
+    blocks = [build(torch, W, 64, 4, 4, s) for s in (1, 2)]
+    rng = np.random.RandomState(3)
+    x, res, g = (rounded(torch, rng.randn(B, T, W), t)[0] for t in ("bf16", "f32", "bf16"))
+    grads = []
+    for b in blocks:
+        keep = {}
+        b.forward(x, res, keep=keep)
+        grads.append(b.backward(keep, g, None))
+    before = [{k: f64(v) for k, v in d.items() if k != "state"} for d in grads]
+    weights = [k for k in before[0] if k not in ("x", "res")]
+    want = math.sqrt(sum((d[k] ** 2).sum() for d in before for k in weights))
+    norm = clip_gradients(grads, 2 * want)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    assert all(np.array_equal(f64(d[k]), b[k]) for d, b in zip(grads, before) for k in b)
+    norm = clip_gradients(grads, 0.5 * want, reduce=lambda square: square.mul_(4))   # (as of four ranks alike)
+    assert abs(float(norm) - 2 * want) <= 2.0 ** -21 * want
+    for d, b in zip(grads, before):
+        for k in b:
+            scale = 0.25 if k in weights else 1.0
+            assert np.abs(f64(d[k]) - scale * b[k]).max() <= 2.0 ** -21 * np.abs(b[k]).max(), k
+    assert float(clip_gradients([], 1.0)) == 0
+
+
+def test_blocks_refuse_other_shapes():
+    torch = torch_gpu()
+    from paper_2607_14394_amd.rollout import SelectiveBlock
+    one = lambda *s: torch.ones(s, device="cuda")  # noqa: E731
+    W, F, N, K = 64, 32, 4, 3
+    good = dict(norm=one(W), norm_bias=one(W), w_in=one(2 * F, W), b_in=one(2 * F), conv=one(K, F), conv_bias=one(F),
+                w_x=one(F + 2 * N, F), b_x=one(F + 2 * N), a=one(N, F), d=one(F), w_out=one(W, F))
+    SelectiveBlock(**good)
+    for k, v in good.items():
+        if k not in ("conv", "a"):
+            with pytest.raises(ValueError):
+                SelectiveBlock(**dict(good, **{k: v[:-1]}))
+    for bad in (dict(conv=one(9, F)), dict(a=one(65, F), w_x=one(F + 130, F), b_x=one(F + 130)), dict(conv=one(K, F + 1))):
+        with pytest.raises(ValueError):
+            SelectiveBlock(**dict(good, **bad))
