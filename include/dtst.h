@@ -510,7 +510,7 @@ dtst_status dtst_conv_adj(const dtst_conv_desc* d, const void* x, const float* w
  * states, features) fp32, the states before steps 0, SPAN, 2 SPAN, ... that the
  * backward needs, NULL if not wanted.  1 to 64 states (DTST_ERR_UNSUPPORTED above).
  * workspace: dtst_scan_workspace bytes, any contents. */
-#define DTST_SCAN_SPAN 64
+#define DTST_SCAN_SPAN 16
 typedef struct {
   int64_t batch, steps, features, states;
   int64_t x_stride[2], delta_stride[2], b_stride[2], c_stride[2], o_stride[2];

@@ -91,7 +91,7 @@ SCAN_DESC = struct.Struct("@26q2i")
 # DTST_F32 .. DTST_E4M3 of include/dtst.h
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
 RECURRENCE_SPAN = 128        # DTST_RECURRENCE_SPAN of include/dtst.h
-SCAN_SPAN = 64               # DTST_SCAN_SPAN of include/dtst.h
+SCAN_SPAN = 16               # DTST_SCAN_SPAN of include/dtst.h
 
 # DTST_ROWS_* and DTST_BLOCK_* of include/dtst.h
 ROWS_T_FIRST, ROWS_T_FIRST_Y, ROWS_Z_FIRST, ROWS_Z_FIRST_Y = range(4)
@@ -819,7 +819,7 @@ def dtst_scan(x, delta, a, b, c, y, d=None, o=None, h0=None, h_out=None, lengths
         _array(states, scan_states_shape(B, T, F, N), "states", dev)
     if lengths is not None:
         _vector(lengths, B, "lengths", dev, torch.int32)
-    if T <= SCAN_SPAN and ws is None:  # (none is needed)
+    if T == 1 and ws is None:  # (none is needed)
         p, n = None, 0
     else:
         p, n, ws = _scratch(ws, dtst_scan_workspace(B, T, F, N), x.device, stream)

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "scan_ops.h"
 
@@ -37,7 +38,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   const int64_t length = scan_length(p, e), t0 = seg * p.segment, end = min(t0 + p.segment, p.steps);
   const int64_t live = min(end, length);
   // (lanes past the end take the last feature too: the same results to the same places)
-  const uint32_t f = uint32_t(min<int64_t>((active ? tile : 0) * 64 + lane, F - 1));
+  const uint32_t f = uint32_t(min<int64_t>((active ? tile : 0) * 64 + lane, F - 1)), ft = f * sizeof(T), f4 = f * 4;
   float* mine = carry + (e * p.segments + seg) * (N + 2) * F;
 
   float h[NS], a2[NS];
@@ -45,12 +46,12 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   for (int n = 0; n < NS; ++n) {
     h[n] = a2[n] = 0.f;
     if (EXACT || n < N) {
-      a2[n] = a[n * F + f] * LOG2E;
+      a2[n] = get(a + n * F, f4) * LOG2E;
       if constexpr (!ENDS) {
         if (p.segments > 1)
-          h[n] = mine[n * F + f];
+          h[n] = get(mine + n * F, f4);
         else if (h_zero != nullptr)
-          h[n] = h_zero[(e * N + n) * F + f];
+          h[n] = get(h_zero + (e * N + n) * F, f4);
       }
     }
   }
@@ -78,21 +79,25 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
     }
   };
 
-  // rows of the sequences, from t on; past the last live one that again
+  // ROWS rows of the sequences, from t on
   T rx[ROWS], rd[ROWS], ro[ROWS];
   const auto rows = [&](int64_t t) {
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int64_t at = min(t + i, live - 1);
-      rx[i] = (x + dtst::at(p.x, e, at))[f];
-      rd[i] = (delta + dtst::at(p.delta, e, at))[f];
-      if (!ENDS && o != nullptr) ro[i] = (o + dtst::at(p.o, e, at))[f];
-    }
+    const auto all = [&](auto full_) {
+      constexpr bool FULL = decltype(full_)::value;
+      const int there = int(min<int64_t>(live - t, ROWS));
+      get_rows<FULL>(x, p.x, e, t, there, ft, rx);
+      get_rows<FULL>(delta, p.delta, e, t, there, ft, rd);
+      if (!ENDS && o != nullptr) get_rows<FULL>(o, p.o, e, t, there, ft, ro);
+    };
+    if (t + ROWS <= live)
+      all(std::true_type());
+    else
+      all(std::false_type());
   };
   const auto keep = [&](int64_t span) {
 #pragma unroll
     for (int n = 0; n < NS; ++n)
-      if (EXACT || n < N) states[((e * p.spans + span) * N + n) * F + f] = h[n];
+      if (EXACT || n < N) put(states + ((e * p.spans + span) * N + n) * F, f4, h[n]);
   };
 
   if (t0 < live) {
@@ -118,23 +123,31 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
         }
         if (t + r0 + ROWS < live) rows(t + r0 + ROWS);
         if (!ENDS && states != nullptr && (t + r0) % SCAN_SPAN == 0) keep((t + r0) / SCAN_SPAN);
+        const auto steps = [&](auto full_) {  // full: all rows are live
+          constexpr bool FULL = decltype(full_)::value;
+          T* to = ENDS ? nullptr : y + dtst::at(p.y, e, t + r0);
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-          if (r0 + i >= last) break;
-          if constexpr (ENDS) sum += D[i], most = fmaxf(most, D[i]);
-          float v = dv * xv[i];
-          if (!ENDS && skip == nullptr) v = 0.f;
+          for (int i = 0; i < ROWS; ++i) {
+            if (!FULL && r0 + i >= last) continue;
+            if constexpr (ENDS) sum += D[i], most = fmaxf(most, D[i]);
+            float v = skip != nullptr ? dv * xv[i] : 0.f;
 #pragma unroll
-          for (int n = 0; n < NS; ++n)
-            if (EXACT || n < N) {
-              h[n] = __builtin_amdgcn_exp2f(D[i] * a2[n]) * h[n] + Dx[i] * bc[buffer][0][r0 + i][n];
-              if constexpr (!ENDS) v = fmaf(h[n], bc[buffer][KINDS - 1][r0 + i][n], v);
+            for (int n = 0; n < NS; ++n)
+              if (EXACT || n < N) {
+                h[n] = __builtin_amdgcn_exp2f(D[i] * a2[n]) * h[n] + Dx[i] * bc[buffer][0][r0 + i][n];
+                if constexpr (!ENDS) v = fmaf(h[n], bc[buffer][KINDS - 1][r0 + i][n], v);
+              }
+            if constexpr (!ENDS) {
+              if (o != nullptr) v *= ov[i] * logistic<T>(ov[i]);
+              put(to, ft, v);
+              to += p.y.t;
             }
-          if constexpr (!ENDS) {
-            if (o != nullptr) v *= ov[i] * logistic<float>(ov[i]);
-            (y + dtst::at(p.y, e, t + r0 + i))[f] = T(v);
           }
-        }
+        };
+        if (r0 + ROWS <= last)
+          steps(std::true_type());
+        else
+          steps(std::false_type());
       }
     }
     if (more) put_staged(buffer ^ 1);
@@ -143,17 +156,17 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   if constexpr (ENDS) {
 #pragma unroll
     for (int n = 0; n < NS; ++n)
-      if (EXACT || n < N) mine[n * F + f] = h[n];
-    mine[N * F + f] = sum;
-    mine[(N + 1) * F + f] = most;
+      if (EXACT || n < N) put(mine + n * F, f4, h[n]);
+    put(mine + N * F, f4, sum);
+    put(mine + (N + 1) * F, f4, most);
   } else {
-    for (int64_t t = max(t0, live); t < end; ++t) (y + dtst::at(p.y, e, t))[f] = T(0.f);
+    for (int64_t t = max(t0, live); t < end; ++t) put(y + dtst::at(p.y, e, t), ft, 0.f);
     if (states != nullptr)  // (past the end the state stands still)
       for (int64_t t = max(t0, (live + SCAN_SPAN - 1) / SCAN_SPAN * SCAN_SPAN); t < end; t += SCAN_SPAN) keep(t / SCAN_SPAN);
     if (h_out != nullptr && (length > t0 ? length <= end : length == 0 && seg == 0)) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
-        if (EXACT || n < N) h_out[(e * N + n) * F + f] = h[n];
+        if (EXACT || n < N) put(h_out + (e * N + n) * F, f4, h[n]);
     }
   }
 }
@@ -166,14 +179,25 @@ scan_carry_kernel(const ScanArgs p, const float* __restrict__ a, const float* fi
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, F = p.features, N = p.states;
   if (i >= p.batch * N * F) return;
   const int64_t e = i / (N * F), f = i % F, n = i / F % N;
+  constexpr int AHEAD = 8;  // segments whose loads are in flight together
   const float a2 = a[n * F + f] * LOG2E;
   float h = first != nullptr ? first[i] : 0.f;
-  float* at = carry + (e * p.segments + (reverse ? p.segments - 1 : 0)) * (N + 2) * F;
+  float* at = carry + (e * p.segments + (reverse ? p.segments - 1 : 0)) * (N + 2) * F + f;
   const int64_t step = (reverse ? -1 : 1) * (N + 2) * F;
-  for (int s = 0; s < p.segments; ++s, at += step) {
-    const float H = at[n * F + f], A = run_decay(a2, at[N * F + f], at[(N + 1) * F + f]);
-    at[n * F + f] = h;
-    h = A * h + H;
+  for (int s = 0; s < p.segments; s += AHEAD, at += AHEAD * step) {
+    const int left = p.segments - s;
+    float H[AHEAD], sum[AHEAD], most[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float* from = at + (k < left ? k : 0) * step;
+      H[k] = from[n * F], sum[k] = from[N * F], most[k] = from[(N + 1) * F];
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (k < left) {
+        at[k * step + n * F] = h;
+        h = run_decay(a2, sum[k], most[k]) * h + H[k];
+      }
   }
   if (final != nullptr) final[i] = h;
 }

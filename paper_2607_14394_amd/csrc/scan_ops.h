@@ -44,6 +44,27 @@ __device__ __forceinline__ int64_t scan_length(const ScanArgs& p, int64_t b) {
   return n < 0 ? 0 : n > p.steps ? p.steps : n;
 }
 
+// The lane's value of a row.  (Scalar row address, 32-bit lane offset in bytes.)
+template <class T>
+__device__ __forceinline__ T get(const T* row, uint32_t offset) {
+  return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + offset);
+}
+template <class T>
+__device__ __forceinline__ void put(T* row, uint32_t offset, float v) {
+  *reinterpret_cast<T*>(reinterpret_cast<char*>(row) + offset) = T(v);
+}
+// Of R rows from row t on; FULL: all there, else past `rows` the last of them again.
+template <bool FULL, int R, class T>
+__device__ __forceinline__ void get_rows(const T* p, Strides s, int64_t e, int64_t t, int rows, uint32_t offset,
+                                         T (&out)[R]) {
+  const T* row = p + at(s, e, t);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    out[i] = get(row, offset);
+    if (FULL || i + 1 < rows) row += s.t;
+  }
+}
+
 ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths);
 // Turns the ends in carry (batch, segments, states + 2, features: the state's end
 // from zero, the sum and the largest of the segment's D) into what enters.

@@ -191,7 +191,7 @@ def test_scan_refusals(kw, code, word):
 
 def test_scan_of_nothing_is_done():
     assert scan_call(batch=0, x=None)[0] == 0 and scan_call(features=0, x=None)[0] == 0
-    assert D.scan_states_shape(3, 129, 5, 7) == (3, 3, 7, 5) and D.scan_states_shape(3, 0, 5, 7) == (3, 0, 7, 5)
+    assert D.scan_states_shape(3, 129, 5, 7) == (3, 9, 7, 5) and D.scan_states_shape(3, 0, 5, 7) == (3, 0, 7, 5)
 
 
 def test_scan_binding_refuses_tensors_off_the_device():
