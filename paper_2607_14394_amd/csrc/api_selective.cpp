@@ -149,7 +149,7 @@ dtst_status check_scan_desc(const dtst_scan_desc* d) {
 dtst_status check_scan_grid(const dtst_scan_desc* d) {
   const int64_t segments = scan_segments(d->batch, d->steps, d->features);
   DTST_TRY(check_grid((d->features + 255) / 256 * segments * d->batch, 256));
-  return check_grid((d->batch * d->states * d->features + 255) / 256, 256);
+  return check_grid((d->batch * d->states * d->features + 63) / 64, 512);
 }
 
 dtst_status scan_workspace_of(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj, size_t* bytes) {

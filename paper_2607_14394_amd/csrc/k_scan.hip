@@ -12,7 +12,7 @@
 namespace dtst {
 namespace {
 
-constexpr int ROWS = 8;     // steps whose loads are in flight together
+constexpr int ROWS = 4;     // steps whose loads are in flight together
 constexpr int CHUNK = 32;   // steps whose b and c are in LDS together
 constexpr int WAVES = 4;    // of a workgroup, 64 features each
 
@@ -21,7 +21,7 @@ constexpr int WAVES = 4;    // of a workgroup, 64 features each
 // outputs, from the state that enters each segment: carry's, or h_zero's where
 // there is one segment.  EXACT: N = NS.
 template <class T, int NS, bool EXACT, bool ENDS>
-__global__ void __launch_bounds__(64 * WAVES)
+__global__ void __launch_bounds__(64 * WAVES, NS <= 16 ? 3 : 1)
 scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restrict__ a, const T* b, const T* c,
             const float* __restrict__ skip, const T* o, const float* h_zero, T* y, float* h_out, float* states,
             float* carry) {
@@ -32,13 +32,15 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   const int N = EXACT ? NS : p.states;
   const int64_t groups = (p.tiles + WAVES - 1) / WAVES;
   const int64_t tile = blockIdx.x % groups * WAVES + wave, place = blockIdx.x / groups;
-  const int seg = int(place % p.segments);
-  const int64_t e = place / p.segments, F = p.features;
+  const int segments = ENDS ? p.segments - 1 : p.segments;  // (nothing comes after the last's end)
+  const int seg = int(place % segments);
+  const int64_t e = place / segments, F = p.features;
   const bool active = tile < p.tiles;
   const int64_t length = scan_length(p, e), t0 = seg * p.segment, end = min(t0 + p.segment, p.steps);
   const int64_t live = min(end, length);
   // (lanes past the end take the last feature too: the same results to the same places)
-  const uint32_t f = uint32_t(min<int64_t>((active ? tile : 0) * 64 + lane, F - 1)), ft = f * sizeof(T), f4 = f * 4;
+  const uint32_t f = uint32_t(min<int64_t>((active ? tile : 0) * 64 + lane, F - 1)), ft = lane_offset(f * sizeof(T));
+  const uint32_t f4 = lane_offset(f * 4);
   float* mine = carry + (e * p.segments + seg) * (N + 2) * F;
 
   float h[NS], a2[NS];
@@ -80,7 +82,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   };
 
   // ROWS rows of the sequences, from t on
-  T rx[ROWS], rd[ROWS], ro[ROWS];
+  T rx[ROWS], rd[ROWS], ro[ROWS] = {};
   const auto rows = [&](int64_t t) {
     const auto all = [&](auto full_) {
       constexpr bool FULL = decltype(full_)::value;
@@ -113,13 +115,16 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
     if (active) {
       const int last = int(min<int64_t>(CHUNK, live - t));
       for (int r0 = 0; r0 < last; r0 += ROWS) {
-        float D[ROWS], Dx[ROWS], xv[ROWS], ov[ROWS];
+        float D[ROWS], Dx[ROWS], direct[ROWS], gate[ROWS];
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
-          D[i] = softplus(float(rd[i]));
-          xv[i] = float(rx[i]);
-          Dx[i] = D[i] * xv[i];
-          if (!ENDS) ov[i] = float(ro[i]);
+          D[i] = softplus<T>(float(rd[i]));
+          Dx[i] = D[i] * float(rx[i]);
+          if constexpr (!ENDS) {  // (selected, as branches would divide the steps)
+            const float v = float(ro[i]);
+            direct[i] = skip != nullptr ? dv * float(rx[i]) : 0.f;
+            gate[i] = o != nullptr ? v * logistic<T>(v) : 1.f;
+          }
         }
         if (t + r0 + ROWS < live) rows(t + r0 + ROWS);
         if (!ENDS && states != nullptr && (t + r0) % SCAN_SPAN == 0) keep((t + r0) / SCAN_SPAN);
@@ -130,7 +135,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
           for (int i = 0; i < ROWS; ++i) {
             if (!FULL && r0 + i >= last) continue;
             if constexpr (ENDS) sum += D[i], most = fmaxf(most, D[i]);
-            float v = skip != nullptr ? dv * xv[i] : 0.f;
+            float v = ENDS ? 0.f : direct[i];
 #pragma unroll
             for (int n = 0; n < NS; ++n)
               if (EXACT || n < N) {
@@ -138,8 +143,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
                 if constexpr (!ENDS) v = fmaf(h[n], bc[buffer][KINDS - 1][r0 + i][n], v);
               }
             if constexpr (!ENDS) {
-              if (o != nullptr) v *= ov[i] * logistic<T>(ov[i]);
-              put(to, ft, v);
+              put(to, ft, v * gate[i]);
               to += p.y.t;
             }
           }
@@ -171,35 +175,49 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   }
 }
 
-// The state that enters each segment, in the place of the one at its end; the
-// segments from the last to the first, with a gradient's, where `reverse`.
-__global__ void __launch_bounds__(256)
-scan_carry_kernel(const ScanArgs p, const float* __restrict__ a, const float* first, float* carry, float* final,
-                  int reverse) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, F = p.features, N = p.states;
-  if (i >= p.batch * N * F) return;
-  const int64_t e = i / (N * F), f = i % F, n = i / F % N;
+// What enters each segment, in the place of the end in `carry`; in their order, or
+// (a gradient's) from the last to the first.  Segments are many where features are
+// few: eight waves compose a run of them each, meet in LDS, and go over their runs.
+constexpr int RUNS = 8;
+__global__ void __launch_bounds__(64 * RUNS)
+scan_carry_kernel(const ScanArgs p, const float* __restrict__ a, const float* first, float* carry, int reverse) {
   constexpr int AHEAD = 8;  // segments whose loads are in flight together
+  __shared__ float mapA[RUNS][64], mapH[RUNS][64];
+  const int run = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t F = p.features, N = p.states, all = p.batch * N * F;
+  const int64_t i = min<int64_t>(int64_t(blockIdx.x) * 64 + lane, all - 1);  // (lanes past the end: the last again)
+  const int64_t e = i / (N * F), f = i % F, n = i / F % N;
   const float a2 = a[n * F + f] * LOG2E;
-  float h = first != nullptr ? first[i] : 0.f;
-  float* at = carry + (e * p.segments + (reverse ? p.segments - 1 : 0)) * (N + 2) * F + f;
+  const int each = (p.segments + RUNS - 1) / RUNS, s0 = min(run * each, p.segments), s1 = min(s0 + each, p.segments);
   const int64_t step = (reverse ? -1 : 1) * (N + 2) * F;
-  for (int s = 0; s < p.segments; s += AHEAD, at += AHEAD * step) {
-    const int left = p.segments - s;
-    float H[AHEAD], sum[AHEAD], most[AHEAD];
+  float* const at = carry + (e * p.segments + (reverse ? p.segments - 1 : 0)) * (N + 2) * F + f;
+  // f(segment, its end, its sum of D, its largest D); the last segment has none
+  const auto segments = [&](auto&& f) {
+    for (int s = s0; s < s1; s += AHEAD) {
+      float H[AHEAD], sum[AHEAD], most[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const float* from = at + (k < left ? k : 0) * step;
-      H[k] = from[n * F], sum[k] = from[N * F], most[k] = from[(N + 1) * F];
-    }
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (k < left) {
-        at[k * step + n * F] = h;
-        h = run_decay(a2, sum[k], most[k]) * h + H[k];
+      for (int k = 0; k < AHEAD; ++k) {
+        const float* from = at + min(s + k, p.segments - 2) * step;
+        H[k] = from[n * F], sum[k] = from[N * F], most[k] = from[(N + 1) * F];
       }
-  }
-  if (final != nullptr) final[i] = h;
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (s + k < s1) f(s + k, H[k], sum[k], most[k]);
+    }
+  };
+  float H = 0.f, total = 0.f, top = 0.f;
+  segments([&](int, float end, float sum, float most) {
+    H = run_decay(a2, sum, most) * H + end;
+    total += sum, top = fmaxf(top, most);
+  });
+  mapA[run][lane] = run_decay(a2, total, top), mapH[run][lane] = H;
+  float h = first != nullptr ? first[i] : 0.f;
+  __syncthreads();  // (all ends are read; what follows writes only a wave's own)
+  for (int k = 0; k < run; ++k) h = mapA[k][lane] * h + mapH[k][lane];
+  segments([&](int s, float end, float sum, float most) {
+    at[s * step + n * F] = h;
+    h = run_decay(a2, sum, most) * h + end;
+  });
 }
 
 // h_out = h_zero (g_hzero = g_h) where there are no steps.
@@ -212,29 +230,28 @@ template <class T, int NS, bool EXACT>
 int launch_forms(const ScanArgs& p, const void* x, const void* delta, const float* a, const void* b, const void* c,
                  const float* skip, const void* o, const float* h_zero, void* y, float* h_out, float* states,
                  float* carry, hipStream_t s) {
-  const unsigned groups = unsigned((p.tiles + WAVES - 1) / WAVES * p.segments * p.batch);
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * WAVES), 0, s, p, static_cast<const T*>(x),
+  const int64_t groups = (p.tiles + WAVES - 1) / WAVES * p.batch;
+  const auto go = [&](auto kernel, int segments) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(groups * segments)), dim3(64 * WAVES), 0, s, p, static_cast<const T*>(x),
                        static_cast<const T*>(delta), a, static_cast<const T*>(b), static_cast<const T*>(c), skip,
                        static_cast<const T*>(o), h_zero, static_cast<T*>(y), h_out, states, carry);
     return int(hipGetLastError());
   };
   if (p.segments > 1) {
-    int e = go(scan_kernel<T, NS, EXACT, true>);
+    int e = go(scan_kernel<T, NS, EXACT, true>, p.segments - 1);
     if (e != hipSuccess) return e;
-    e = launch_scan_carry(p, a, h_zero, carry, nullptr, false, s);
+    e = launch_scan_carry(p, a, h_zero, carry, false, s);
     if (e != hipSuccess) return e;
   }
-  return go(scan_kernel<T, NS, EXACT, false>);
+  return go(scan_kernel<T, NS, EXACT, false>, p.segments);
 }
 
 }  // namespace
 
-int launch_scan_carry(const ScanArgs& p, const float* a, const float* first, float* carry, float* final, bool reverse,
-                      void* stream) {
+int launch_scan_carry(const ScanArgs& p, const float* a, const float* first, float* carry, bool reverse, void* stream) {
   const int64_t n = p.batch * p.states * p.features;
-  hipLaunchKernelGGL(scan_carry_kernel, dim3(unsigned((n + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream),
-                     p, a, first, carry, final, int(reverse));
+  hipLaunchKernelGGL(scan_carry_kernel, dim3(unsigned((n + 63) / 64)), dim3(64 * RUNS), 0,
+                     static_cast<hipStream_t>(stream), p, a, first, carry, int(reverse));
   return hipGetLastError();
 }
 
@@ -245,11 +262,11 @@ int launch_copy_states(const float* in, float* out, int64_t n, void* stream) {
   return hipGetLastError();
 }
 
-// Segments of a sequence: as many as give the card 4096 waves.
+// Segments of a sequence: as many as give the card 4096 waves, not one more.
 int scan_segments(int64_t batch, int64_t steps, int64_t features) {
   const int64_t waves = batch * ((features + 63) / 64), spans = (steps + SCAN_SPAN - 1) / SCAN_SPAN;
   if (waves <= 0 || spans <= 1 || waves >= 2048) return 1;
-  const int64_t each = std::max<int64_t>(1, spans * waves / 4096);  // spans
+  const int64_t most = 4096 / waves, each = (spans + most - 1) / most;  // (spans)
   return int((spans + each - 1) / each);
 }
 

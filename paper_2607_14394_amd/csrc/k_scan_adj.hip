@@ -17,40 +17,55 @@ namespace dtst {
 namespace {
 
 constexpr int R = SCAN_SPAN;    // steps of a span, all in a lane's registers
+constexpr int PART = 8;  // of a span: rows whose loads are in flight together
 constexpr int PITCH = 64 + 4;  // of a row of lanes' values in LDS: four banks on, so that a read by rows meets none twice
 static_assert(R == 16, "lane_sums");
 
 // The sums over 64 lanes of 16 values; that of value i in lanes 4 i .. 4 i + 3.
 // Through LDS: a lane writes its values and reads a quarter of one's lanes (17
 // additions; by exchanges between lanes, each halving the values, it would take 44
-// cycles' worth of instructions more).
-__device__ __forceinline__ float lane_sums(const float (&v)[R], float* buffer, int lane) {
-  wave_sync();
-#pragma unroll
-  for (int i = 0; i < R; ++i) buffer[i * PITCH + lane] = v[i];
+// cycles' worth of instructions more).  Apart, so that other work hides the reading.
+__device__ __forceinline__ void read_row(const float* buffer, int lane, float4 (&r)[4]) {
   wave_sync();
   const float4* row = reinterpret_cast<const float4*>(buffer + (lane >> 2) * PITCH + (lane & 3) * 16);
-  float4 s = row[0];
 #pragma unroll
-  for (int i = 1; i < 4; ++i) {
-    const float4 q = row[i];
-    s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
-  }
+  for (int i = 0; i < 4; ++i) r[i] = row[i];
+  wave_sync();
+}
+__device__ __forceinline__ float row_sum(const float4 (&r)[4]) {
+  float4 s = r[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) s.x += r[i].x, s.y += r[i].y, s.z += r[i].z, s.w += r[i].w;
   float t = (s.x + s.y) + (s.z + s.w);
   t += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(t), 0xb1, 0xf, 0xf, false));  // (its neighbour's)
   return t + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(t), 0x4e, 0xf, 0xf, false));
 }
-
 struct AdjArrays {
   float* carry;  // (batch, segments, N + 2, features): the ends, then what enters
   float* parts;  // (batch, segments, N + 1, features): g_a and g_d of a segment
   float* sums;   // (tiles, batch, N, 2, spans SCAN_SPAN): g_b and g_c of a tile of features
+  float* bc;     // (batch, N, 2, spans SCAN_SPAN): b and c
 };
 
-// Floats of LDS: e[N][64] | gA[N][64] | b and c[N][2][R] | the sums' buffer.
-__host__ __device__ constexpr int adj_lds(int N, bool ends) {
-  return N * 64 + N * 2 * R + (ends ? 0 : N * 64 + R * PITCH);
+// b and c in 32 bits, steps next to each other, zeros past a length: so a wave takes
+// 16 steps' of a state by a scalar load.  (From LDS, where every lane would read the
+// same, they took as long as the arithmetic.)
+template <class T>
+__global__ void __launch_bounds__(256) scan_adj_lift_kernel(const ScanArgs p, const T* b, const T* c, float* bc) {
+  const int64_t N = p.states, pitch = p.spans * R, t = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t e = t / pitch, step = t % pitch;
+  if (e >= p.batch) return;
+  const bool live = step < scan_length(p, e);
+  const T *from_b = b + at(p.b, e, live ? step : 0), *from_c = c + at(p.c, e, live ? step : 0);
+  float* to = bc + e * N * 2 * pitch + step;
+  for (int n = 0; n < N; ++n, to += 2 * pitch) {
+    to[0] = live ? float(from_b[n]) : 0.f;
+    to[pitch] = live ? float(from_c[n]) : 0.f;
+  }
 }
+
+// Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer.
+__host__ __device__ constexpr int adj_lds(int N, bool ends) { return N * 64 + (ends ? 0 : N * 64 + R * PITCH); }
 
 // One wave: 64 features of a segment, a lane a feature, its spans from the last to
 // the first.  A span's steps are in registers; state by state, h goes forward over
@@ -58,19 +73,20 @@ __host__ __device__ constexpr int adj_lds(int N, bool ends) {
 // the segment's first step, from zero after its last.
 template <class T, bool GATED, bool ENDS>
 __global__ void __launch_bounds__(64, ENDS ? 4 : 2)
-scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta, const float* __restrict__ a, const T* b,
-                const T* c, const float* __restrict__ skip, const T* o, const float* __restrict__ states, const T* g_y,
+scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta, const float* __restrict__ a,
+                const float* __restrict__ bc, const float* __restrict__ skip, const T* o, const float* __restrict__ states, const T* g_y,
                 const float* g_h, T* g_x, T* g_delta, T* g_o, float* g_hzero) {
   extern __shared__ __align__(16) float lds[];
   const int lane = threadIdx.x, N = p.states;
   float* const ecarry = lds;
-  float* const bc = ecarry + N * 64;
-  float* const gA = bc + 2 * N * R;
+  float* const gA = ecarry + N * 64;
   float* const buffer = gA + N * 64;
   const int64_t F = p.features, tile = blockIdx.x % p.tiles, place = blockIdx.x / p.tiles;
-  const int64_t seg = place % p.segments, e = place / p.segments;
+  const int segments = ENDS ? p.segments - 1 : p.segments;  // (nothing comes before the first's end)
+  const int64_t seg = place % segments + (ENDS ? 1 : 0), e = place / segments;
   const bool own = tile * 64 + lane < F;  // (lanes past the end have no gradient and store nothing)
-  const uint32_t f = uint32_t(min<int64_t>(tile * 64 + lane, F - 1)), ft = f * sizeof(T), f4 = f * 4;
+  const uint32_t f = uint32_t(min<int64_t>(tile * 64 + lane, F - 1)), ft = lane_offset(f * sizeof(T));
+  const uint32_t f4 = lane_offset(f * 4);
   const int64_t length = scan_length(p, e), s0 = seg * p.segment, end = min(s0 + p.segment, p.steps);
   const int64_t live_end = min(end, length);
   float* const mine = w.carry + (e * p.segments + seg) * (N + 2) * F;
@@ -88,7 +104,8 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
   }
   const float dv = skip != nullptr ? skip[f] : 0.f;
   float gd = 0.f, total = 0.f, most = 0.f;
-  // (of a pair of neighbouring lanes one stores g_b's sum, one g_c's)
+  // Of neighbouring lanes one stores g_b's sum, one g_c's; two lanes each store the
+  // same, as a branch in the loop below would cost more.
   const int64_t pitch = p.spans * R;
   float* const sums = w.sums + ((tile * p.batch + e) * N * 2 + (lane & 1)) * pitch + (lane >> 2);
 
@@ -105,35 +122,33 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
       }
       continue;
     }
-    // the span's b and c, states first
-    wave_sync();
-    for (int i = lane; i < R * N; i += 64) {
-      const int t = i / N, n = i % N;
-      const bool there = t < rows;
-      if constexpr (!ENDS) bc[(2 * n) * R + t] = there ? float((b + at(p.b, e, t0 + t))[n]) : 0.f;
-      bc[(2 * n + 1) * R + t] = there ? float((c + at(p.c, e, t0 + t))[n]) : 0.f;
-    }
     float D[R], Dx[R], g[R];
     const auto load = [&](auto full_) {  // full: all rows are live
       constexpr bool FULL = decltype(full_)::value;
-      T rx[R], rd[R], rg[R], ro[R];
-      if constexpr (!ENDS) get_rows<FULL>(x, p.x, e, t0, rows, ft, rx);
-      get_rows<FULL>(delta, p.delta, e, t0, rows, ft, rd);
-      get_rows<FULL>(g_y, p.y, e, t0, rows, ft, rg);
-      if constexpr (GATED) get_rows<FULL>(o, p.o, e, t0, rows, ft, ro);
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        D[i] = softplus(float(rd[i]));
-        g[i] = float(rg[i]);
+      for (int i0 = 0; i0 < R; i0 += PART) {
+      T rx[PART], rd[PART], rg[PART], ro[PART];
+      const int there = max(rows - i0, 1);
+      const int64_t from = t0 + min(i0, rows - 1);
+      if constexpr (!ENDS) get_rows<FULL>(x, p.x, e, from, there, ft, rx);
+      get_rows<FULL>(delta, p.delta, e, from, there, ft, rd);
+      get_rows<FULL>(g_y, p.y, e, from, there, ft, rg);
+      if constexpr (GATED) get_rows<FULL>(o, p.o, e, from, there, ft, ro);
+#pragma unroll
+      for (int i = i0; i < i0 + PART; ++i) {
+        D[i] = softplus<T>(float(rd[i - i0]));
+        g[i] = float(rg[i - i0]);
         if constexpr (GATED) {
-          const float v = float(ro[i]);
-          g[i] *= v * logistic<float>(v);
+          const float v = float(ro[i - i0]);
+          g[i] *= v * logistic<T>(v);
         }
-        if constexpr (!ENDS) Dx[i] = D[i] * float(rx[i]);
+        if constexpr (!ENDS) Dx[i] = D[i] * float(rx[i - i0]);
         // (past the end the states and their gradients stand still)
         if (!FULL && i >= rows) D[i] = g[i] = Dx[i] = 0.f;
         if (!own) g[i] = Dx[i] = 0.f;
         if constexpr (ENDS) total += D[i], most = fmaxf(most, D[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
       }
     };
     if (rows == R)
@@ -143,27 +158,32 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     float wb[R], gD[R], yv[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) wb[i] = gD[i] = yv[i] = 0.f;
-    wave_sync();
 
     const float* kept = ENDS ? nullptr : states + (e * p.spans + t0 / R) * N * F;
+    // b and c of a state, and of the next
+    const float* from = bc + e * N * 2 * pitch + t0;
+    float bn[R], cn[R], b_next[R], c_next[R];
+    const auto fetch = [&] {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if constexpr (!ENDS) b_next[i] = from[i];
+        c_next[i] = from[pitch + i];
+      }
+    };
+    fetch();
     float a_next = get(a, f4), h_next = ENDS ? 0.f : get(kept, f4);
+    float4 last[4];  // g_b's terms of the state before, and its sum of g_c
+    float last_c = 0.f;
     for (int n = 0; n < N; ++n) {
       const float an = a_next, a2 = an * LOG2E;
       float h = own ? h_next : 0.f;
+#pragma unroll
+      for (int i = 0; i < R; ++i) bn[i] = b_next[i], cn[i] = c_next[i];
       if (n + 1 < N) {
+        from += 2 * pitch;
+        fetch();
         a_next = get(a + (n + 1) * F, f4);
         if constexpr (!ENDS) h_next = get(kept + (n + 1) * F, f4);
-      }
-      const float4* b4 = reinterpret_cast<const float4*>(bc + 2 * n * R);
-      float bn[R], cn[R];
-#pragma unroll
-      for (int i = 0; i < R / 4; ++i) {
-        if constexpr (!ENDS) {
-          const float4 v = b4[i];
-          bn[4 * i] = v.x, bn[4 * i + 1] = v.y, bn[4 * i + 2] = v.z, bn[4 * i + 3] = v.w;
-        }
-        const float4 v = b4[R / 4 + i];
-        cn[4 * i] = v.x, cn[4 * i + 1] = v.y, cn[4 * i + 2] = v.z, cn[4 * i + 3] = v.w;
       }
       float E[R], q = ecarry[n * 64 + lane];
 #pragma unroll
@@ -172,31 +192,39 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
 #pragma unroll
         for (int i = R - 1; i >= 0; --i) q = E[i] * fmaf(g[i], cn[i], q);
       } else {
-        float hp[R], v[R];  // hp: the states before the steps
+        float hp[R], ga = gA[n * 64 + lane];  // hp: the states before the steps
+        if (n > 0) {
+          const float gb = row_sum(last);
+          sums[2 * (n - 1) * pitch + t0] = lane & 1 ? last_c : gb;
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           hp[i] = h;
           h = E[i] * h + Dx[i] * bn[i];
           if constexpr (GATED) yv[i] = fmaf(cn[i], h, yv[i]);
-          v[i] = g[i] * h;
+          buffer[i * PITCH + lane] = g[i] * h;
         }
-        const float gc = lane_sums(v, buffer, lane);
-        float ga = gA[n * 64 + lane];
+        float4 terms[4];
+        read_row(buffer, lane, terms);
 #pragma unroll
         for (int i = R - 1; i >= 0; --i) {
           q = fmaf(g[i], cn[i], q);
           wb[i] = fmaf(q, bn[i], wb[i]);
-          v[i] = q * Dx[i];
+          buffer[i * PITCH + lane] = q * Dx[i];
           q *= E[i];
           const float s = q * hp[i];
           gD[i] = fmaf(an, s, gD[i]);
           ga = fmaf(D[i], s, ga);
+          if (i == R / 2) last_c = row_sum(terms);
         }
         gA[n * 64 + lane] = ga;
-        const float gb = lane_sums(v, buffer, lane);
-        if ((lane & 2) == 0) sums[2 * n * pitch + t0] = lane & 1 ? gc : gb;
+        read_row(buffer, lane, last);
       }
       ecarry[n * 64 + lane] = q;
+    }
+    if constexpr (!ENDS) {
+      const float gb = row_sum(last);
+      sums[2 * (N - 1) * pitch + t0] = lane & 1 ? last_c : gb;
     }
     const auto store = [&](auto full_) {
       constexpr bool FULL = decltype(full_)::value;
@@ -204,24 +232,28 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
       // that there are not.
       uint32_t again = ft;
       asm volatile("" : "+v"(again)::"memory");
-      T rx[R], rd[R], rg[R], ro[R];
-      get_rows<FULL>(x, p.x, e, t0, rows, again, rx);
-      get_rows<FULL>(delta, p.delta, e, t0, rows, again, rd);
-      if constexpr (GATED) get_rows<FULL>(g_y, p.y, e, t0, rows, again, rg);
-      if constexpr (GATED) get_rows<FULL>(o, p.o, e, t0, rows, again, ro);
       T *to_x = g_x + at(p.gx, e, t0), *to_delta = g_delta + at(p.gdelta, e, t0);
       T* to_o = GATED ? g_o + at(p.go, e, t0) : nullptr;
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
+      for (int i0 = 0; i0 < R; i0 += PART) {
+      T rx[PART], rd[PART], rg[PART], ro[PART];
+      const int left = max(rows - i0, 1);
+      const int64_t from = t0 + min(i0, rows - 1);
+      get_rows<FULL>(x, p.x, e, from, left, again, rx);
+      get_rows<FULL>(delta, p.delta, e, from, left, again, rd);
+      if constexpr (GATED) get_rows<FULL>(g_y, p.y, e, from, left, again, rg);
+      if constexpr (GATED) get_rows<FULL>(o, p.o, e, from, left, again, ro);
+#pragma unroll
+      for (int i = i0; i < i0 + PART; ++i) {
         const bool there = FULL || i < rows;
-        const float xv = float(rx[i]);
+        const float xv = float(rx[i - i0]);
         const float gx = there ? D[i] * wb[i] + g[i] * dv : 0.f;
-        const float gs = there ? (gD[i] + xv * wb[i]) * logistic<float>(float(rd[i])) : 0.f;
+        const float gs = there ? (gD[i] + xv * wb[i]) * logistic<T>(float(rd[i - i0])) : 0.f;
         gd += there ? g[i] * xv : 0.f;
         float go = 0.f;
         if constexpr (GATED) {
-          const float v = float(ro[i]), u = logistic<float>(v);
-          go = there ? float(rg[i]) * (yv[i] + dv * xv) * (u + v * u * (1.f - u)) : 0.f;
+          const float v = float(ro[i - i0]), u = logistic<T>(v);
+          go = there ? float(rg[i - i0]) * (yv[i] + dv * xv) * (u + v * u * (1.f - u)) : 0.f;
         }
         if ((FULL || i < rows_all) && own) {  // (no `break`: the loop stays unrolled)
           put(to_x, again, gx);
@@ -230,6 +262,8 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
         }
         to_x += p.gx.t, to_delta += p.gdelta.t;
         if constexpr (GATED) to_o += p.go.t;
+      }
+      __builtin_amdgcn_sched_barrier(0);
       }
     };
     if constexpr (!ENDS) {
@@ -248,7 +282,7 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     float* part = w.parts + (e * p.segments + seg) * (N + 1) * F;
     for (int n = 0; n < N; ++n) {
       put(part + n * F, f4, gA[n * 64 + lane]);
-      if (p.segments == 1 && g_hzero != nullptr) put(g_hzero + (e * N + n) * F, f4, ecarry[n * 64 + lane]);
+      if (seg == 0 && g_hzero != nullptr) put(g_hzero + (e * N + n) * F, f4, ecarry[n * 64 + lane]);
     }
     put(part + N * F, f4, gd);
   }
@@ -276,7 +310,7 @@ __global__ void __launch_bounds__(256) scan_adj_sums_kernel(const ScanArgs p, co
     (g_b + at(p.gb, e, t))[n] = T(s);
 }
 
-size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+size_t round64(size_t n) { return (n + 63) / 64 * 64; }
 
 }  // namespace
 
@@ -285,7 +319,7 @@ size_t scan_adj_workspace(const dtst_scan_desc& d) {
   if (d.batch == 0 || d.features == 0) return 0;
   const size_t parts = size_t(p.batch) * p.segments * (p.states + 1) * p.features * 4;
   const size_t sums = size_t(p.tiles) * p.batch * p.states * 2 * p.spans * SCAN_SPAN * 4;
-  return round16(scan_carry_bytes(d)) + round16(parts) + sums;
+  return round64(scan_carry_bytes(d)) + round64(parts) + round64(sums) + sums / p.tiles;
 }
 
 int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b,
@@ -298,22 +332,27 @@ int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, c
   char* ws = static_cast<char*>(workspace);
   AdjArrays w;
   w.carry = reinterpret_cast<float*>(ws);
-  w.parts = reinterpret_cast<float*>(ws + round16(scan_carry_bytes(d)));
-  w.sums = w.parts + round16(size_t(p.batch) * p.segments * (N + 1) * p.features * 4) / 4;
+  w.parts = reinterpret_cast<float*>(ws + round64(scan_carry_bytes(d)));
+  w.sums = w.parts + round64(size_t(p.batch) * p.segments * (N + 1) * p.features * 4) / 4;
+  const int64_t steps = p.batch * p.spans * R;  // (of all entries, whole spans)
+  w.bc = w.sums + round64(size_t(p.tiles) * steps * N * 2 * 4) / 4;
   const auto typed = [&](auto t) {
     using T = decltype(t);
     const auto go = [&](auto kernel, bool ends) {
+      const int64_t segments = ends ? p.segments - 1 : p.segments;
       const size_t lds = size_t(adj_lds(N, ends)) * 4;
-      hipLaunchKernelGGL(kernel, dim3(unsigned(p.tiles * p.segments * p.batch)), dim3(64), lds, s, p, w,
-                         static_cast<const T*>(x), static_cast<const T*>(delta), a, static_cast<const T*>(b),
-                         static_cast<const T*>(c), skip, static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h,
+      hipLaunchKernelGGL(kernel, dim3(unsigned(p.tiles * segments * p.batch)), dim3(64), lds, s, p, w,
+                         static_cast<const T*>(x), static_cast<const T*>(delta), a, w.bc, skip, static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h,
                          static_cast<T*>(g_x), static_cast<T*>(g_delta), static_cast<T*>(g_o), g_hzero);
       return int(hipGetLastError());
     };
-    int r = hipSuccess;
+    hipLaunchKernelGGL((scan_adj_lift_kernel<T>), dim3(unsigned((steps + 255) / 256)), dim3(256), 0, s, p,
+                       static_cast<const T*>(b), static_cast<const T*>(c), w.bc);
+    int r = hipGetLastError();
+    if (r != hipSuccess) return r;
     if (p.segments > 1) {
       r = o != nullptr ? go(scan_adj_kernel<T, true, true>, true) : go(scan_adj_kernel<T, false, true>, true);
-      if (r == hipSuccess) r = launch_scan_carry(p, a, g_h, w.carry, g_hzero, true, s);
+      if (r == hipSuccess) r = launch_scan_carry(p, a, g_h, w.carry, true, s);
       if (r != hipSuccess) return r;
     }
     r = o != nullptr ? go(scan_adj_kernel<T, true, false>, false) : go(scan_adj_kernel<T, false, false>, false);

@@ -10,12 +10,13 @@ namespace dtst {
 constexpr int SCAN_SPAN = DTST_SCAN_SPAN;
 constexpr float LOG2E = 1.44269502162933349609375f;
 
-// D = log(1 + exp(d)) = max(d, 0) + log(1 + e), e = exp(-|d|).  1 + e rounds e's
-// low bits off; what it lost, c, goes back in (to first order, whose error is c e /
-// (1 + e), 2^-24 of the result).
+// D = log(1 + exp(d)) = max(d, 0) + log(1 + e), e = exp(-|d|), of a d of type T.
+// 1 + e rounds e's low bits off; what it lost, c, goes back in (to first order, whose
+// error is c e / (1 + e), 2^-24 of the result).
+template <class T>
 __device__ __forceinline__ float softplus(float d) {
   constexpr float ln2 = 0.693147180559945309f;
-  const float e = exp_minus<float>(fabsf(d));
+  const float e = exp_minus<T>(fabsf(d));
   const float u = 1.f + e, c = e - (u - 1.f);
   return fmaxf(d, 0.f) + fmaf(__builtin_amdgcn_logf(u), ln2, c);
 }
@@ -44,7 +45,14 @@ __device__ __forceinline__ int64_t scan_length(const ScanArgs& p, int64_t b) {
   return n < 0 ? 0 : n > p.steps ? p.steps : n;
 }
 
-// The lane's value of a row.  (Scalar row address, 32-bit lane offset in bytes.)
+// A lane's offset in bytes, which the compiler cannot tell from any other: it would
+// fold it into each row's address, two registers and an instruction a row.
+__device__ __forceinline__ uint32_t lane_offset(uint32_t bytes) {
+  asm volatile("" : "+v"(bytes));
+  return bytes;
+}
+
+// The lane's value of a row.  (Scalar row address, 32-bit lane offset.)
 template <class T>
 __device__ __forceinline__ T get(const T* row, uint32_t offset) {
   return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + offset);
@@ -67,9 +75,9 @@ __device__ __forceinline__ void get_rows(const T* p, Strides s, int64_t e, int64
 
 ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths);
 // Turns the ends in carry (batch, segments, states + 2, features: the state's end
-// from zero, the sum and the largest of the segment's D) into what enters.
-int launch_scan_carry(const ScanArgs& p, const float* a, const float* first, float* carry, float* final, bool reverse,
-                      void* stream);
+// from zero, the sum and the largest of the segment's D; none of the last segment's,
+// in reverse of the first's) into what enters.
+int launch_scan_carry(const ScanArgs& p, const float* a, const float* first, float* carry, bool reverse, void* stream);
 int launch_copy_states(const float* in, float* out, int64_t n, void* stream);
 
 }  // namespace dtst
