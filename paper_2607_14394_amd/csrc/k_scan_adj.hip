@@ -17,7 +17,7 @@ namespace dtst {
 namespace {
 
 constexpr int R = SCAN_SPAN;    // steps of a span, all in a lane's registers
-constexpr int PART = 8;  // of a span: rows whose loads are in flight together
+constexpr int WAVES = 4;  // of a workgroup at most
 constexpr int PITCH = 64 + 4;  // of a row of lanes' values in LDS: four banks on, so that a read by rows meets none twice
 static_assert(R == 16, "lane_sums");
 
@@ -43,7 +43,7 @@ __device__ __forceinline__ float row_sum(const float4 (&r)[4]) {
 struct AdjArrays {
   float* carry;  // (batch, segments, N + 2, features): the ends, then what enters
   float* parts;  // (batch, segments, N + 1, features): g_a and g_d of a segment
-  float* sums;   // (tiles, batch, N, 2, spans SCAN_SPAN): g_b and g_c of a tile of features
+  float* sums;   // (tiles, batch, spans, N, 2, SCAN_SPAN): g_b and g_c of a tile of features
   float* bc;     // (batch, N, 2, spans SCAN_SPAN): b and c
 };
 
@@ -64,24 +64,30 @@ __global__ void __launch_bounds__(256) scan_adj_lift_kernel(const ScanArgs p, co
   }
 }
 
-// Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer.
-__host__ __device__ constexpr int adj_lds(int N, bool ends) { return N * 64 + (ends ? 0 : N * 64 + R * PITCH); }
+// Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer | a span's sums [N][2][R].
+__host__ __device__ constexpr int adj_lds(int N, bool ends) {
+  return N * 64 + (ends ? 0 : N * 64 + R * PITCH + N * 2 * R);
+}
 
-// One wave: 64 features of a segment, a lane a feature, its spans from the last to
+// A wave: 64 features of a segment, a lane a feature, its spans from the last to
 // the first.  A span's steps are in registers; state by state, h goes forward over
 // them from the state that the forward kept, then e backward.  ENDS: only e before
 // the segment's first step, from zero after its last.
 template <class T, bool GATED, bool ENDS>
-__global__ void __launch_bounds__(64, ENDS ? 4 : 2)
+__global__ void __launch_bounds__(64 * WAVES, ENDS ? 4 : 2)
 scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta, const float* __restrict__ a,
                 const float* __restrict__ bc, const float* __restrict__ skip, const T* o, const float* __restrict__ states, const T* g_y,
                 const float* g_h, T* g_x, T* g_delta, T* g_o, float* g_hzero) {
   extern __shared__ __align__(16) float lds[];
-  const int lane = threadIdx.x, N = p.states;
-  float* const ecarry = lds;
+  const int lane = threadIdx.x & 63, N = p.states, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6;
+  float* const ecarry = lds + wave * adj_lds(N, ENDS);
   float* const gA = ecarry + N * 64;
   float* const buffer = gA + N * 64;
-  const int64_t F = p.features, tile = blockIdx.x % p.tiles, place = blockIdx.x / p.tiles;
+  float* const bc_sums = buffer + R * PITCH;
+  const int64_t groups = (p.tiles + waves - 1) / waves, F = p.features;
+  const int64_t tile = blockIdx.x % groups * waves + wave, place = blockIdx.x / groups;
+  if (tile >= p.tiles) return;  // (the waves do not meet)
   const int segments = ENDS ? p.segments - 1 : p.segments;  // (nothing comes before the first's end)
   const int64_t seg = place % segments + (ENDS ? 1 : 0), e = place / segments;
   const bool own = tile * 64 + lane < F;  // (lanes past the end have no gradient and store nothing)
@@ -104,10 +110,11 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
   }
   const float dv = skip != nullptr ? skip[f] : 0.f;
   float gd = 0.f, total = 0.f, most = 0.f;
-  // Of neighbouring lanes one stores g_b's sum, one g_c's; two lanes each store the
-  // same, as a branch in the loop below would cost more.
   const int64_t pitch = p.spans * R;
-  float* const sums = w.sums + ((tile * p.batch + e) * N * 2 + (lane & 1)) * pitch + (lane >> 2);
+  // Of neighbouring lanes one has g_b's sum, one g_c's; two lanes each write the same,
+  // as a branch in the loop below would cost more.  (To memory they go together: a
+  // store in the loop would be waited for with the next state's loads.)
+  float* const sums = bc_sums + (lane & 1) * R + (lane >> 2);
 
   for (int64_t t0 = (end - 1) / R * R; t0 >= s0; t0 -= R) {
     const int rows_all = int(min<int64_t>(end - t0, R));
@@ -125,30 +132,24 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     float D[R], Dx[R], g[R];
     const auto load = [&](auto full_) {  // full: all rows are live
       constexpr bool FULL = decltype(full_)::value;
+      T rx[R], rd[R], rg[R], ro[R];
+      if constexpr (!ENDS) get_rows<FULL>(x, p.x, e, t0, rows, ft, rx);
+      get_rows<FULL>(delta, p.delta, e, t0, rows, ft, rd);
+      get_rows<FULL>(g_y, p.y, e, t0, rows, ft, rg);
+      if constexpr (GATED) get_rows<FULL>(o, p.o, e, t0, rows, ft, ro);
 #pragma unroll
-      for (int i0 = 0; i0 < R; i0 += PART) {
-      T rx[PART], rd[PART], rg[PART], ro[PART];
-      const int there = max(rows - i0, 1);
-      const int64_t from = t0 + min(i0, rows - 1);
-      if constexpr (!ENDS) get_rows<FULL>(x, p.x, e, from, there, ft, rx);
-      get_rows<FULL>(delta, p.delta, e, from, there, ft, rd);
-      get_rows<FULL>(g_y, p.y, e, from, there, ft, rg);
-      if constexpr (GATED) get_rows<FULL>(o, p.o, e, from, there, ft, ro);
-#pragma unroll
-      for (int i = i0; i < i0 + PART; ++i) {
-        D[i] = softplus<T>(float(rd[i - i0]));
-        g[i] = float(rg[i - i0]);
+      for (int i = 0; i < R; ++i) {
+        D[i] = softplus<T>(float(rd[i]));
+        g[i] = float(rg[i]);
         if constexpr (GATED) {
-          const float v = float(ro[i - i0]);
+          const float v = float(ro[i]);
           g[i] *= v * logistic<T>(v);
         }
-        if constexpr (!ENDS) Dx[i] = D[i] * float(rx[i - i0]);
+        if constexpr (!ENDS) Dx[i] = D[i] * float(rx[i]);
         // (past the end the states and their gradients stand still)
         if (!FULL && i >= rows) D[i] = g[i] = Dx[i] = 0.f;
         if (!own) g[i] = Dx[i] = 0.f;
         if constexpr (ENDS) total += D[i], most = fmaxf(most, D[i]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
       }
     };
     if (rows == R)
@@ -181,7 +182,7 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
       for (int i = 0; i < R; ++i) bn[i] = b_next[i], cn[i] = c_next[i];
       if (n + 1 < N) {
         from += 2 * pitch;
-        fetch();
+        if constexpr (ENDS) fetch();
         a_next = get(a + (n + 1) * F, f4);
         if constexpr (!ENDS) h_next = get(kept + (n + 1) * F, f4);
       }
@@ -195,7 +196,7 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
         float hp[R], ga = gA[n * 64 + lane];  // hp: the states before the steps
         if (n > 0) {
           const float gb = row_sum(last);
-          sums[2 * (n - 1) * pitch + t0] = lane & 1 ? last_c : gb;
+          sums[2 * (n - 1) * R] = lane & 1 ? last_c : gb;
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -215,7 +216,14 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
           const float s = q * hp[i];
           gD[i] = fmaf(an, s, gD[i]);
           ga = fmaf(D[i], s, ga);
-          if (i == R / 2) last_c = row_sum(terms);
+          if (i == R / 2) {
+            // The next state's b and c from here on: scalar loads in flight would be
+            // waited for with the terms.
+            last_c = row_sum(terms);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch();
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
         gA[n * 64 + lane] = ga;
         read_row(buffer, lane, last);
@@ -224,7 +232,11 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     }
     if constexpr (!ENDS) {
       const float gb = row_sum(last);
-      sums[2 * (N - 1) * pitch + t0] = lane & 1 ? last_c : gb;
+      sums[2 * (N - 1) * R] = lane & 1 ? last_c : gb;
+      wave_sync();
+      float4* to = reinterpret_cast<float4*>(w.sums + ((tile * p.batch + e) * p.spans + t0 / R) * N * 2 * R);
+      for (int i = lane; i < N * 2 * R / 4; i += 64) to[i] = reinterpret_cast<const float4*>(bc_sums)[i];
+      wave_sync();
     }
     const auto store = [&](auto full_) {
       constexpr bool FULL = decltype(full_)::value;
@@ -234,26 +246,22 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
       asm volatile("" : "+v"(again)::"memory");
       T *to_x = g_x + at(p.gx, e, t0), *to_delta = g_delta + at(p.gdelta, e, t0);
       T* to_o = GATED ? g_o + at(p.go, e, t0) : nullptr;
+      T rx[R], rd[R], rg[R], ro[R];
+      get_rows<FULL>(x, p.x, e, t0, rows, again, rx);
+      get_rows<FULL>(delta, p.delta, e, t0, rows, again, rd);
+      if constexpr (GATED) get_rows<FULL>(g_y, p.y, e, t0, rows, again, rg);
+      if constexpr (GATED) get_rows<FULL>(o, p.o, e, t0, rows, again, ro);
 #pragma unroll
-      for (int i0 = 0; i0 < R; i0 += PART) {
-      T rx[PART], rd[PART], rg[PART], ro[PART];
-      const int left = max(rows - i0, 1);
-      const int64_t from = t0 + min(i0, rows - 1);
-      get_rows<FULL>(x, p.x, e, from, left, again, rx);
-      get_rows<FULL>(delta, p.delta, e, from, left, again, rd);
-      if constexpr (GATED) get_rows<FULL>(g_y, p.y, e, from, left, again, rg);
-      if constexpr (GATED) get_rows<FULL>(o, p.o, e, from, left, again, ro);
-#pragma unroll
-      for (int i = i0; i < i0 + PART; ++i) {
+      for (int i = 0; i < R; ++i) {
         const bool there = FULL || i < rows;
-        const float xv = float(rx[i - i0]);
+        const float xv = float(rx[i]);
         const float gx = there ? D[i] * wb[i] + g[i] * dv : 0.f;
-        const float gs = there ? (gD[i] + xv * wb[i]) * logistic<T>(float(rd[i - i0])) : 0.f;
+        const float gs = there ? (gD[i] + xv * wb[i]) * logistic<T>(float(rd[i])) : 0.f;
         gd += there ? g[i] * xv : 0.f;
         float go = 0.f;
         if constexpr (GATED) {
-          const float v = float(ro[i - i0]), u = logistic<T>(v);
-          go = there ? float(rg[i - i0]) * (yv[i] + dv * xv) * (u + v * u * (1.f - u)) : 0.f;
+          const float v = float(ro[i]), u = logistic<T>(v);
+          go = there ? float(rg[i]) * (yv[i] + dv * xv) * (u + v * u * (1.f - u)) : 0.f;
         }
         if ((FULL || i < rows_all) && own) {  // (no `break`: the loop stays unrolled)
           put(to_x, again, gx);
@@ -262,8 +270,6 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
         }
         to_x += p.gx.t, to_delta += p.gdelta.t;
         if constexpr (GATED) to_o += p.go.t;
-      }
-      __builtin_amdgcn_sched_barrier(0);
       }
     };
     if constexpr (!ENDS) {
@@ -298,8 +304,8 @@ __global__ void __launch_bounds__(256) scan_adj_sums_kernel(const ScanArgs p, co
   if (e >= p.batch || t >= p.steps) return;
   float s = 0.f;
   if (t < scan_length(p, e)) {
-    const int64_t pitch = p.batch * N2 * p.spans * SCAN_SPAN;
-    const float* from = sums + (e * N2 + which) * p.spans * SCAN_SPAN + t;
+    const int64_t pitch = p.batch * N2 * p.spans * R;
+    const float* from = sums + ((e * p.spans + t / R) * N2 + which) * R + t % R;
 #pragma unroll 8
     for (int64_t i = 0; i < p.tiles; ++i) s += from[i * pitch];
   }
@@ -340,8 +346,18 @@ int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, c
     using T = decltype(t);
     const auto go = [&](auto kernel, bool ends) {
       const int64_t segments = ends ? p.segments - 1 : p.segments;
-      const size_t lds = size_t(adj_lds(N, ends)) * 4;
-      hipLaunchKernelGGL(kernel, dim3(unsigned(p.tiles * segments * p.batch)), dim3(64), lds, s, p, w,
+      // Several waves a workgroup meet in the scalar cache, whose b and c are the same
+      // for all; eight a CU have to fit its LDS.
+      int waves = WAVES;
+      while (waves > 1 && (waves * adj_lds(N, ends) * 4 > 80 * 1024 || waves / 2 >= p.tiles)) waves /= 2;
+      const size_t lds = size_t(waves) * adj_lds(N, ends) * 4;
+      if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+        if (e != hipSuccess) return int(e);
+      }
+      hipLaunchKernelGGL(kernel, dim3(unsigned((p.tiles + waves - 1) / waves * segments * p.batch)),
+                         dim3(64 * waves), lds, s, p, w,
                          static_cast<const T*>(x), static_cast<const T*>(delta), a, w.bc, skip, static_cast<const T*>(o), states, static_cast<const T*>(g_y), g_h,
                          static_cast<T*>(g_x), static_cast<T*>(g_delta), static_cast<T*>(g_o), g_hzero);
       return int(hipGetLastError());

@@ -73,6 +73,15 @@ __device__ __forceinline__ void get_rows(const T* p, Strides s, int64_t e, int64
   }
 }
 
+struct ScanPointers {
+  const void *x, *delta, *b, *c, *o;
+  const float *a, *skip, *h_zero;
+  void* y;
+  float *h_out, *states, *carry;
+};
+template <class T>
+int launch_scan_type(const ScanArgs& p, const ScanPointers& q, hipStream_t s);
+
 ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths);
 // Turns the ends in carry (batch, segments, states + 2, features: the state's end
 // from zero, the sum and the largest of the segment's D; none of the last segment's,
