@@ -7,8 +7,8 @@
 // tensors from a few values to many millions, so a launch takes up to so many
 // tensors as its arguments hold (4 KB), cut into chunks of 8192 values; each of
 // at most 2048 workgroups finds its first chunk's tensor once and goes on from
-// there.  Squares are summed in 64 bits, where no value of 32 bits overflows or
-// is lost; each workgroup leaves its sum, and one adds them up in a fixed order.
+// there.  The sums of eight squares are added up in 64 bits; each workgroup leaves
+// its sum, and one adds those up in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -80,6 +80,20 @@ __device__ __forceinline__ double group_sum(double s) {
   return s;
 }
 
+// The sum of eight squares: in 32 bits where that neither passes them nor loses what
+// matters (a square below 2^-126 beside a sum of 2^-66), as conversions to 64 bits
+// take 20 times as long (470 MB in bf16: 147 us).
+__device__ __forceinline__ double squares(const float (&v)[VEC]) {
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) s = fmaf(v[j], v[j], s);
+  if (s >= 1e-20f && s <= 1e30f) return s;
+  double d = 0.0;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) d = fma(double(v[j]), double(v[j]), d);
+  return d;
+}
+
 __global__ void __launch_bounds__(THREADS) square_sums_kernel(const NormTable t, double* sums) {
   double sum[4] = {};  // (of each load's, so that the additions do not wait for one another)
   each_chunk(t, [&](int i, int64_t at, int64_t n) {
@@ -93,9 +107,7 @@ __global__ void __launch_bounds__(THREADS) square_sums_kernel(const NormTable t,
         load_n<VEC>(p + c, n - c, v[k]);
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) sum[k] = fma(double(v[k][j]), double(v[k][j]), sum[k]);
+      for (int k = 0; k < 4; ++k) sum[k] += squares(v[k]);
     });
   });
   const double s = group_sum<THREADS / 64>((sum[0] + sum[1]) + (sum[2] + sum[3]));

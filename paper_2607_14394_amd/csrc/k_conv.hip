@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "seq_internal.h"
 #include "seq_ops.h"
@@ -27,7 +28,7 @@ struct ConvArgs {
   Strides x, y, gx;
   const int32_t* lengths;
   int64_t vectors, runs, run;  // of a row; of a sequence; steps of a run
-  int silu, lanes;             // lanes: of a workgroup's threads along the features (backward)
+  int lanes;                   // of a workgroup's threads along the features (backward)
 };
 
 __device__ __forceinline__ int64_t conv_length(const ConvArgs& p, int64_t b) {
@@ -51,7 +52,7 @@ __device__ __forceinline__ void input_row(const ConvArgs& p, const T* x, const T
   }
 }
 
-template <class T, int K, int V>
+template <class T, int K, int V, bool SILU>
 __global__ void __launch_bounds__(THREADS)
 conv_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const float* __restrict__ bias, const T* state, T* y,
             T* state_out) {
@@ -80,10 +81,17 @@ conv_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const flo
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) input_row<V, K>(p, x, state, b, t0 + k - K + 1, f, z[k]);
   }
-  for (int64_t t = t0; t < live; t += BATCH) {
+  // BATCH steps; full: all of them live, and the lane's features all there
+  const T* xr = x + at(p.x, b, t0) + f;
+  T* yr = y + at(p.y, b, t0) + f;
+  const auto steps = [&](auto full_, int64_t rows) {
+    constexpr bool FULL = decltype(full_)::value;
+    const int64_t left = FULL ? V : F - f;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i)  // (past the end the last row again)
-      load_n<V>(x + at(p.x, b, min(t + i, live - 1)) + f, F - f, z[K - 1 + i]);
+    for (int i = 0; i < BATCH; ++i) {  // (past the end the last row again)
+      load_n<V>(xr, left, z[K - 1 + i]);
+      if (FULL || i + 1 < rows) xr += p.x.t;
+    }
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
       float v[V];
@@ -92,21 +100,28 @@ conv_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const flo
         v[j] = bv[j];
 #pragma unroll
         for (int k = 0; k < K; ++k) v[j] = fmaf(z[i + k][j], wv[k][j], v[j]);
-        if (p.silu) v[j] *= logistic<T>(v[j]);
+        if constexpr (SILU) v[j] *= logistic<T>(v[j]);
       }
-      if (t + i < live) store_n<V>(y + at(p.y, b, t + i) + f, F - f, v);
+      if (FULL || i < rows) store_n<V>(yr, left, v);
+      yr += p.y.t;
     }
 #pragma unroll
     for (int k = 0; k < K - 1; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) z[k][j] = z[k + BATCH][j];
+  };
+  for (int64_t t = t0; t < live; t += BATCH) {
+    if (__all(t + BATCH <= live && f + V <= F))  // (of the whole wave, which else would take both ways)
+      steps(std::true_type(), BATCH);
+    else
+      steps(std::false_type(), live - t);
   }
   const float zero[V] = {};
   for (int64_t t = max(t0, live); t < end; ++t) store_n<V>(y + at(p.y, b, t) + f, F - f, zero);
 }
 
 // part: (workgroups along the runs, K + 1, features), each workgroup's g_w and g_bias.
-template <class T, int K, int V>
+template <class T, int K, int V, bool SILU>
 __global__ void __launch_bounds__(THREADS)
 conv_adj_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const float* __restrict__ bias, const T* state,
                 const T* g_y, const T* g_state_out, T* g_x, T* g_state, float* part) {
@@ -141,18 +156,25 @@ conv_adj_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const
     }
     // The rows of this run, the state's too in the first: written K - 1 steps behind p.
     const int64_t first = run == 0 ? 1 - K : t0;
-    for (int64_t t = t0; t < end + K - 1; t += STEP) {
+    const T *xr = x + at(p.x, b, t0) + f, *gr = g_y + at(p.y, b, t0) + f;
+    T* to = g_x + (at(p.gx, b, t0) - (K - 1) * p.gx.t) + f;  // (row t - K + 1's place)
+    // STEP steps; full: all live, of this run, as are the rows that they finish, and
+    // the lane's features all there
+    const auto steps = [&](auto full_, int64_t t) {
+      constexpr bool FULL = decltype(full_)::value;
+      const int64_t left = FULL ? V : F - f;
       float g[STEP][V];
 #pragma unroll
       for (int i = 0; i < STEP; ++i) {
-        if (t + i < n) {
-          load_n<V>(x + at(p.x, b, t + i) + f, F - f, z[K - 1 + i]);
-          load_n<V>(g_y + at(p.y, b, t + i) + f, F - f, g[i]);
+        if (FULL || t + i < n) {
+          load_n<V>(xr + i * p.x.t, left, z[K - 1 + i]);
+          load_n<V>(gr + i * p.y.t, left, g[i]);
         } else {
 #pragma unroll
           for (int j = 0; j < V; ++j) z[K - 1 + i][j] = g[i][j] = 0.f;
         }
       }
+      xr += STEP * p.x.t, gr += STEP * p.y.t;
 #pragma unroll
       for (int i = 0; i < STEP; ++i) {
 #pragma unroll
@@ -160,43 +182,51 @@ conv_adj_kernel(const ConvArgs p, const T* x, const float* __restrict__ w, const
           float v = bv[j], d = g[i][j];
 #pragma unroll
           for (int k = 0; k < K; ++k) v = fmaf(z[i + k][j], wv[k][j], v);
-          if (p.silu) {
+          if constexpr (SILU) {
             float s, sn;
             logistic<T>(v, s, sn);
             d *= s * fmaf(v, sn, 1.f);
           }
-          if (t + i >= n) d = 0.f;  // (v may be no number there)
+          if (!FULL && t + i >= n) d = 0.f;  // (v may be no number there)
           q[K - 1 + i][j] = d;
-          if (t + i < live) {
+          if (FULL || t + i < live) {
             gb[j] += d;
 #pragma unroll
             for (int k = 0; k < K; ++k) gw[k][j] = fmaf(d, z[i + k][j], gw[k][j]);
           }
         }
         const int64_t row = t + i - K + 1;
-        if (row < first || row >= end) continue;
-        float r[V] = {};
-        if (row < n) {
+        if (FULL || (row >= first && row < end)) {
+          float r[V] = {};
+          if (FULL || row < n) {
 #pragma unroll
-          for (int k = 0; k < K; ++k)  // (the row's p_{row + K - 1 - k})
+            for (int k = 0; k < K; ++k)  // (the row's p_{row + K - 1 - k})
 #pragma unroll
-            for (int j = 0; j < V; ++j) r[j] = fmaf(q[i + K - 1 - k][j], wv[k][j], r[j]);
-          if (g_state_out != nullptr && row > n - K) {
-            float s[V];
-            load_n<V>(g_state_out + (b * (K - 1) + row - (n - K + 1)) * F + f, F - f, s);
+              for (int j = 0; j < V; ++j) r[j] = fmaf(q[i + K - 1 - k][j], wv[k][j], r[j]);
+            if (g_state_out != nullptr && row > n - K) {
+              float s[V];
+              load_n<V>(g_state_out + (b * (K - 1) + row - (n - K + 1)) * F + f, F - f, s);
 #pragma unroll
-            for (int j = 0; j < V; ++j) r[j] += s[j];
+              for (int j = 0; j < V; ++j) r[j] += s[j];
+            }
           }
+          if (FULL || row >= 0)
+            store_n<V>(to + i * p.gx.t, left, r);
+          else if (g_state != nullptr)
+            store_n<V>(g_state + (b * (K - 1) + row + K - 1) * F + f, F - f, r);
         }
-        if (row >= 0)
-          store_n<V>(g_x + at(p.gx, b, row) + f, F - f, r);
-        else if (g_state != nullptr)
-          store_n<V>(g_state + (b * (K - 1) + row + K - 1) * F + f, F - f, r);
       }
+      to += STEP * p.gx.t;
 #pragma unroll
       for (int k = 0; k < K - 1; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) z[k][j] = z[k + STEP][j], q[k][j] = q[k + STEP][j];
+    };
+    for (int64_t t = t0; t < end + K - 1; t += STEP) {
+      if (__all(t + STEP <= live && t - K + 1 >= max<int64_t>(first, 0) && f + V <= F))
+        steps(std::true_type(), t);
+      else
+        steps(std::false_type(), t);
     }
   }
 #pragma unroll
@@ -241,7 +271,7 @@ constexpr int BACKWARD_LANE = 4;
 // Runs of as many steps as leave 2^17 lanes (two waves a SIMD), of at least BATCH.
 ConvArgs conv_args(const dtst_conv_desc& d, const int32_t* lengths, int lane) {
   ConvArgs p{d.batch, d.steps, d.features, {d.x_stride[0], d.x_stride[1]}, {d.y_stride[0], d.y_stride[1]},
-             {d.g_x_stride[0], d.g_x_stride[1]}, lengths, 0, 0, 0, d.silu, 64};
+             {d.g_x_stride[0], d.g_x_stride[1]}, lengths, 0, 0, 0, 64};
   p.vectors = (d.features + lane - 1) / lane;
   const int64_t rows = std::max<int64_t>(1, (int64_t(1) << 17) / std::max<int64_t>(1, p.vectors));  // runs of all entries
   p.run = std::max<int64_t>(1, d.batch * d.steps / rows);
@@ -257,17 +287,18 @@ int64_t adj_parts(const ConvArgs& p) {
 }
 
 template <class F>
-int by_taps(int64_t taps, F&& f) {
+int by_taps(int64_t taps, int silu, F&& f) {
   using std::integral_constant;
+  const auto go = [&](auto k) { return silu ? f(k, std::true_type()) : f(k, std::false_type()); };
   switch (taps) {
-    case 1: return f(integral_constant<int, 1>());
-    case 2: return f(integral_constant<int, 2>());
-    case 3: return f(integral_constant<int, 3>());
-    case 4: return f(integral_constant<int, 4>());
-    case 5: return f(integral_constant<int, 5>());
-    case 6: return f(integral_constant<int, 6>());
-    case 7: return f(integral_constant<int, 7>());
-    default: return f(integral_constant<int, 8>());
+    case 1: return go(integral_constant<int, 1>());
+    case 2: return go(integral_constant<int, 2>());
+    case 3: return go(integral_constant<int, 3>());
+    case 4: return go(integral_constant<int, 4>());
+    case 5: return go(integral_constant<int, 5>());
+    case 6: return go(integral_constant<int, 6>());
+    case 7: return go(integral_constant<int, 7>());
+    default: return go(integral_constant<int, 8>());
   }
 }
 
@@ -298,8 +329,8 @@ int launch_conv(const dtst_conv_desc& d, const void* x, const float* w, const fl
     if (d.steps == 0) return copy_rows<T>(state, state_out, d.batch * (d.taps - 1) * d.features, s);
     constexpr int V = forward_lane<T>();
     const ConvArgs p = conv_args(d, lengths, V);
-    return by_taps(d.taps, [&](auto k) {
-      hipLaunchKernelGGL((conv_kernel<T, decltype(k)::value, V>), dim3(unsigned(conv_groups(d, false))), dim3(THREADS), 0, s,
+    return by_taps(d.taps, d.silu, [&](auto k, auto silu) {
+      hipLaunchKernelGGL((conv_kernel<T, decltype(k)::value, V, decltype(silu)::value>), dim3(unsigned(conv_groups(d, false))), dim3(THREADS), 0, s,
                          p, static_cast<const T*>(x), w, bias, static_cast<const T*>(state), static_cast<T*>(y),
                          static_cast<T*>(state_out));
       return int(hipGetLastError());
@@ -322,8 +353,9 @@ int launch_conv_adj(const dtst_conv_desc& d, const void* x, const float* w, cons
   const int e = by_type(d.type, [&](auto t) {
     using T = decltype(t);
     if (!steps) return copy_rows<T>(g_state_out, g_state, d.batch * (d.taps - 1) * d.features, s);
-    return by_taps(d.taps, [&](auto k) {
-      hipLaunchKernelGGL((conv_adj_kernel<T, decltype(k)::value, BACKWARD_LANE>), dim3(unsigned(conv_groups(d, true))),
+    return by_taps(d.taps, d.silu, [&](auto k, auto silu) {
+      hipLaunchKernelGGL((conv_adj_kernel<T, decltype(k)::value, BACKWARD_LANE, decltype(silu)::value>),
+                         dim3(unsigned(conv_groups(d, true))),
                          dim3(THREADS), 0, s, p, static_cast<const T*>(x), w, bias, static_cast<const T*>(state),
                          static_cast<const T*>(g_y), static_cast<const T*>(g_state_out), static_cast<T*>(g_x),
                          static_cast<T*>(g_state), part);
