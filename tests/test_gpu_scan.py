@@ -52,6 +52,18 @@ def test_numbers_of_states(N, t):
     compare(torch, D, *inputs(torch, 2, 150, 70, N, t, N), t)
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_random_shapes(seed):
+    torch, D = lib()
+    rng = np.random.RandomState(100 + seed)
+    B, T, F, N = rng.randint(1, 5), rng.randint(1, 400), rng.randint(1, 330), rng.randint(1, 65)
+    t = ("f32", "bf16", "f16")[seed % 3]
+    lengths = rng.randint(0, T + 1, B) if seed % 2 else None
+    say(f"[scan] {B} x {T} x {F}, {N} states, {t}, lengths {lengths}")
+    dev, val = inputs(torch, B, T, F, N, t, seed, lengths, gated=seed % 4 < 2, skip=seed % 3 > 0, h0=seed % 5 > 0)
+    compare(torch, D, dev, val, t)
+
+
 @pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 31, 32, 33, 63, 64, 65, 128, 129, 500, 1100])
 @pytest.mark.parametrize("t", ["f32", "bf16"])
 def test_steps(T, t):

@@ -71,6 +71,29 @@ def test_numbers_of_states(N, t):
     compare(torch, D, *inputs(torch, 2, 100, 70, N, t, N), t, N)
 
 
+@pytest.mark.parametrize("N,F", [(16, 260), (20, 300), (24, 260), (25, 260), (48, 130)])
+def test_states_of_several_waves(N, F):
+    """Workgroups of four, two and one waves: what their states take of the LDS."""
+    torch, D = lib()
+    say(f"[scan_adj] {N} states, {F} features")
+    compare(torch, D, *inputs(torch, 2, 70, F, N, "bf16", N), "bf16", N)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_shapes(seed):
+    torch, D = lib()
+    rng = np.random.RandomState(seed)
+    B, T, F, N = rng.randint(1, 5), rng.randint(1, 260), rng.randint(1, 330), rng.randint(1, 40)
+    t = ("f32", "bf16", "f16")[seed % 3]
+    lengths = rng.randint(0, T + 1, B) if seed % 2 else None
+    say(f"[scan_adj] {B} x {T} x {F}, {N} states, {t}, lengths {lengths}")
+    dev, val = inputs(torch, B, T, F, N, t, seed, lengths, gated=seed % 4 < 2, skip=seed % 3 > 0, h0=seed % 5 > 0)
+    for v in val.values():
+        if v is not None and np.issubdtype(np.asarray(v).dtype, np.floating):
+            np.nan_to_num(v, copy=False)
+    compare(torch, D, dev, val, t, seed)
+
+
 @pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 63, 64, 65, 128, 129, 300, 700])
 @pytest.mark.parametrize("t", ["f32", "bf16"])
 def test_steps(T, t):
