@@ -23,9 +23,11 @@ __device__ __forceinline__ float softplus(float d) {
 
 // exp(a D) of a run of steps whose D come to `sum`, the largest being `most`; a2 =
 // a log2(e).  One that underflows though no step's does stays above zero: it would
-// make no number of an infinite state, which the steps one by one keep.
+// make no number of an infinite state, which the steps one by one keep.  A sum past
+// 32 bits is their largest, of which a = 0 makes 1 as of every step.  (A D that is no
+// number shows in the run's end.)
 __device__ __forceinline__ float run_decay(float a2, float sum, float most) {
-  const float A = __builtin_amdgcn_exp2f(a2 * sum);
+  const float A = __builtin_amdgcn_exp2f(a2 * fminf(sum, 3.402823466e38f));
   return a2 * most >= -126.f ? fmaxf(A, __uint_as_float(1)) : A;
 }
 

@@ -228,6 +228,26 @@ def test_infinite_states_and_no_numbers():
     assert not torch.isinf(h[0, 0, 3])
 
 
+@pytest.mark.parametrize("T", [48, 4000])
+def test_step_sizes_whose_sums_pass_32_bits(T):
+    """A state without decay stands still, and so does its gradient, however large the
+    steps are: exact, as exp(0) is 1 and the others' 0."""
+    torch, D = lib()
+    F, N = 70, 2
+    x, b = torch.zeros(1, T, F, device="cuda"), torch.zeros(1, T, N, device="cuda")
+    c, delta = torch.ones(1, T, N, device="cuda"), torch.full((1, T, F), 3e38, device="cuda")
+    a = torch.tensor([[0.0], [-1.0]], device="cuda").repeat(1, F)
+    h, y = torch.ones(1, N, F, device="cuda"), torch.empty(1, T, F, device="cuda")
+    st = torch.empty(D.scan_states_shape(1, T, F, N), device="cuda")
+    D.dtst_scan(x, delta, a, b, c, y, h0=h, h_out=h, states=st)
+    assert (y == 1).all() and (h[0, 0] == 1).all() and not h[0, 1].any()
+    g_h, (g_b, g_c) = torch.ones_like(h), (torch.empty_like(b) for _ in range(2))
+    g_x, g_delta = torch.empty_like(x), torch.empty_like(x)
+    D.dtst_scan_adj(x, delta, a, b, c, torch.zeros_like(x), st, g_x, g_delta, torch.empty_like(a), g_b, g_c, g_h=g_h,
+                    g_hzero=g_h)
+    assert (g_h[0, 0] == 1).all() and not g_h[0, 1].any() and not g_x.any() and not g_delta.any() and not g_b.any()
+
+
 def test_no_steps_and_no_sequences():
     torch, D = lib()
     dev, _ = inputs(torch, 2, 4, 10, 3, "f32", 12)
