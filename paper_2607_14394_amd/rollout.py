@@ -321,14 +321,14 @@ def clip_gradients(gradients, most, reduce=None):
     list of dicts; x, res and state are left alone) in place so that their norm
     together is at most `most`.  Returns the norm before, one float32 on the device.
     Where other ranks hold other weights' gradients, reduce(square) has to sum one
-    float32 in place over them."""
+    float64 in place over them (32 bits do not hold the square of a large norm)."""
     weights = [g for d in gradients for k, g in d.items() if k not in ("x", "res", "state")]
     norm = torch.empty(1, dtype=torch.float32, device=weights[0].device if weights else "cuda")
     dtst_global_norm(weights, norm)
     if reduce is not None:
-        norm.square_()
-        reduce(norm)
-        norm.sqrt_()
+        square = norm.double().square_()
+        reduce(square)
+        norm.copy_(square.sqrt_())
     dtst_clip(weights, norm, most)
     return norm
 

@@ -304,6 +304,16 @@ def test_gradients_of_blocks_are_clipped_together():
     assert float(clip_gradients([], 1.0)) == 0
 
 
+def test_norms_whose_squares_pass_32_bits_are_reduced():
+    """1e25 in each of four ranks: 2e25 together, and 0.5 of it left."""
+    torch = torch_gpu()
+    from paper_2607_14394_amd.rollout import clip_gradients
+    g = torch.tensor([1e25, 0.0], device="cuda")
+    norm = clip_gradients([dict(a=g)], 1e25, reduce=lambda square: square.mul_(4))
+    # (each product, root and quotient rounds once)
+    assert abs(float(norm) - 2e25) <= 2.0 ** -22 * 2e25 and abs(float(g[0]) - 0.5e25) <= 2.0 ** -22 * 0.5e25 and g[1] == 0
+
+
 def test_blocks_refuse_other_shapes():
     torch = torch_gpu()
     from paper_2607_14394_amd.rollout import SelectiveBlock
