@@ -220,3 +220,43 @@ def test_gradients_are_differences():
             down = f(*args)
             args[k][i] = at
             assert abs((up - down) / (2 * step) - float(got[k][i])) < 5e-3, (k, i)
+
+
+@pytest.mark.parametrize("cols", [300, 5000])
+def test_streams_and_replays(cols):
+    """Both directions on a stream of their own, captured, and replayed on new values
+    with eager work between: the same results every time."""
+    torch, D = lib()
+    x, r, (w, b), _, _ = inputs(torch, 33, cols, "bf16", "f32", 20)
+    y, u, g_u, g_x = torch.empty_like(x), torch.empty_like(r), torch.empty_like(r), torch.empty_like(x)
+    mean, rstd = torch.empty(33, device="cuda"), torch.empty(33, device="cuda")
+    g_w, g_b = torch.empty_like(w), torch.empty_like(b)
+    ws = torch.empty(D.dtst_layer_norm_adj_workspace(33, cols), dtype=torch.uint8, device="cuda")
+    out = (y, u, mean, rstd, g_u, g_x, g_w, g_b)
+
+    def both():
+        D.dtst_layer_norm(x, w, b, y, res=r, sum_out=u, mean=mean, rstd=rstd)
+        D.dtst_layer_norm_adj(y, u, w, mean, rstd, g_u, g_w, g_b, g_sum=u, g_x=g_x, ws=ws)
+
+    both()
+    want = [[t.clone() for t in out]]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both()
+    s.synchronize()
+    assert all(torch.equal(t, v) for t, v in zip(out, want[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    first = x.clone()
+    x.mul_(-1.5)
+    both()
+    want.append([t.clone() for t in out])
+    for i in (0, 1, 0):
+        x.copy_(first if i == 0 else first * -1.5)
+        for t in out:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, v) for t, v in zip(out, want[i]))
