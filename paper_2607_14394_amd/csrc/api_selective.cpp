@@ -146,8 +146,8 @@ dtst_status check_scan_desc(const dtst_scan_desc* d) {
 }
 
 // (workgroups of 256 threads for 256 features of a segment, and for the states)
-dtst_status check_scan_grid(const dtst_scan_desc* d) {
-  const int64_t segments = scan_segments(d->batch, d->steps, d->features);
+dtst_status check_scan_grid(const dtst_scan_desc* d, bool adj) {
+  const int64_t segments = scan_segments(d->batch, d->steps, d->features, adj);
   DTST_TRY(check_grid((d->features + 255) / 256 * segments * d->batch, 256));
   return check_grid((d->batch * d->states * d->features + 63) / 64, 512);
 }
@@ -158,7 +158,7 @@ dtst_status scan_workspace_of(int64_t batch, int64_t steps, int64_t features, in
   DTST_TRY(check_sizes(batch, steps, features, states, DTST_F32));
   dtst_scan_desc d{};
   d.batch = batch, d.steps = steps, d.features = features, d.states = states;
-  *bytes = adj ? scan_adj_workspace(d) : scan_carry_bytes(d);
+  *bytes = adj ? scan_adj_workspace(d) : scan_carry_bytes(d, false);
   return ok();
 }
 
@@ -265,9 +265,9 @@ dtst_status scan(const dtst_scan_desc* d, const void* x, const void* delta, cons
   if (h_out) DTST_TRY(check_align(h_out, 4, "h_out"));
   if (states) DTST_TRY(check_align(states, 4, "states"));
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
-  const size_t need = scan_carry_bytes(*d);
+  const size_t need = scan_carry_bytes(*d, false);
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
-  DTST_TRY(check_scan_grid(d));
+  DTST_TRY(check_scan_grid(d, false));
   const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
   const Block ba{T > 0 ? a : nullptr, N * F * 4, "a"}, bd{skip, F * 4, "d"}, bn{lengths, B * 4, "lengths"};
   const Block bin{h_zero, one, "h_zero"}, bout{h_out, one, "h_out"}, bst{states, one * spans, "states"};
@@ -311,9 +311,9 @@ dtst_status scan_adj(const dtst_scan_desc* d, const void* x, const void* delta, 
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
   const size_t need = scan_adj_workspace(*d);
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
-  DTST_TRY(check_scan_grid(d));
+  DTST_TRY(check_scan_grid(d, true));
   // (a wave for 64 features of a segment; four waves for 64 steps of g_b and g_c)
-  DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F) * B, 64));
+  DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F, true) * B, 64));
   const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
   DTST_TRY(check_grid((B * ((T + 63) / 64) * 2 * N + 3) / 4, 256));
   DTST_TRY(check_grid(((N + 1) * F + 31) / 32, 1024));

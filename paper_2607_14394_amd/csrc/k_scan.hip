@@ -89,28 +89,34 @@ int launch_copy_states(const float* in, float* out, int64_t n, void* stream) {
   return hipGetLastError();
 }
 
-// Segments of a sequence: as many as give the card 4096 waves, not one more.
-int scan_segments(int64_t batch, int64_t steps, int64_t features) {
+// Segments of a sequence: as many as give the card so many waves, not one more: three
+// a SIMD, the forward's, in one go (65536 steps of 1280 features: 589 us, and 607 with
+// 4096; 24 ragged sequences of 1001 features: 128 and 130 us), two a SIMD twice over,
+// the backward's (4 sequences of 4096 steps and 2048 features, both directions: 891 us;
+// 1315, 912, 937 and 901 with 1024, 2048, 6144 and 8192).  Whole sequences from 1024
+// waves on: the second pass over the steps costs more than waves side by side save (32
+// sequences of 1024 steps and 4096 features: 571 us whole, 908 in two segments).
+int scan_segments(int64_t batch, int64_t steps, int64_t features, bool adj) {
   const int64_t waves = batch * ((features + 63) / 64), spans = (steps + SCAN_SPAN - 1) / SCAN_SPAN;
   if (waves <= 0 || spans <= 1 || waves >= 1024) return 1;
-  const int64_t most = 4096 / waves, each = (spans + most - 1) / most;  // (spans)
+  const int64_t most = (adj ? 4096 : 3072) / waves, each = (spans + most - 1) / most;  // (spans)
   return int((spans + each - 1) / each);
 }
 
-ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths) {
+ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths, bool adj) {
   auto st = [](const int64_t (&s)[2]) { return Strides{s[0], s[1]}; };
   ScanArgs p{d.batch, d.steps, d.features, int(d.states), st(d.x_stride), st(d.delta_stride), st(d.b_stride),
              st(d.c_stride), st(d.o_stride), st(d.y_stride), st(d.g_x_stride), st(d.g_delta_stride), st(d.g_b_stride),
              st(d.g_c_stride), st(d.g_o_stride), lengths, 0, 0, 0, 0};
   p.spans = (d.steps + SCAN_SPAN - 1) / SCAN_SPAN;
   p.tiles = (d.features + 63) / 64;
-  p.segments = scan_segments(d.batch, d.steps, d.features);
+  p.segments = scan_segments(d.batch, d.steps, d.features, adj);
   p.segment = (p.spans + p.segments - 1) / p.segments * SCAN_SPAN;
   return p;
 }
 
-size_t scan_carry_bytes(const dtst_scan_desc& d) {
-  const int s = scan_segments(d.batch, d.steps, d.features);
+size_t scan_carry_bytes(const dtst_scan_desc& d, bool adj) {
+  const int s = scan_segments(d.batch, d.steps, d.features, adj);
   return s > 1 ? size_t(d.batch) * s * (d.states + 2) * d.features * 4 : 0;
 }
 
@@ -119,7 +125,7 @@ int launch_scan(const dtst_scan_desc& d, const void* x, const void* delta, const
                 float* states, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (d.steps == 0) return launch_copy_states(h_zero, h_out, d.batch * d.states * d.features, s);
-  const ScanArgs p = scan_args(d, lengths);
+  const ScanArgs p = scan_args(d, lengths, false);
   const ScanPointers q{x, delta, b, c, o, a, skip, h_zero, y, h_out, states, static_cast<float*>(workspace)};
   if (d.type == DTST_F32) return launch_scan_type<float>(p, q, s);
   if (d.type == DTST_BF16) return launch_scan_type<bf16_t>(p, q, s);

@@ -324,11 +324,11 @@ size_t round64(size_t n) { return (n + 63) / 64 * 64; }
 }  // namespace
 
 size_t scan_adj_workspace(const dtst_scan_desc& d) {
-  const ScanArgs p = scan_args(d, nullptr);
+  const ScanArgs p = scan_args(d, nullptr, true);
   if (d.batch == 0 || d.features == 0) return 0;
   const size_t parts = size_t(p.batch) * p.segments * (p.states + 1) * p.features * 4;
   const size_t sums = size_t(p.tiles) * p.batch * p.states * 2 * p.spans * SCAN_SPAN * 4;
-  return round64(scan_carry_bytes(d)) + round64(parts) + round64(sums) + sums / p.tiles;
+  return round64(scan_carry_bytes(d, true)) + round64(parts) + round64(sums) + sums / p.tiles;
 }
 
 int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b,
@@ -336,12 +336,12 @@ int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, c
                     const void* g_y, const float* g_h, void* g_x, void* g_delta, float* g_a, void* g_b, void* g_c,
                     float* g_skip, void* g_o, float* g_hzero, void* workspace, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const ScanArgs p = scan_args(d, lengths);
+  const ScanArgs p = scan_args(d, lengths, true);
   const int N = p.states;
   char* ws = static_cast<char*>(workspace);
   AdjArrays w;
   w.carry = reinterpret_cast<float*>(ws);
-  w.parts = reinterpret_cast<float*>(ws + round64(scan_carry_bytes(d)));
+  w.parts = reinterpret_cast<float*>(ws + round64(scan_carry_bytes(d, true)));
   w.sums = w.parts + round64(size_t(p.batch) * p.segments * (N + 1) * p.features * 4) / 4;
   const int64_t steps = p.batch * p.spans * R;  // (of all entries, whole spans)
   w.bc = w.sums + round64(size_t(p.tiles) * steps * N * 2 * 4) / 4;

@@ -84,7 +84,7 @@ struct ScanPointers {
 template <class T>
 int launch_scan_type(const ScanArgs& p, const ScanPointers& q, hipStream_t s);
 
-ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths);
+ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths, bool adj);
 // Turns the ends in carry (batch, segments, states + 2, features: the state's end
 // from zero, the sum and the largest of the segment's D; none of the last segment's,
 // in reverse of the first's) into what enters.

@@ -61,6 +61,7 @@ CASES = [(2, 150, 384, 256, 16, 4, None), (3, 140, 200, 130, 5, 3, [140, 0, 77])
 @pytest.mark.parametrize("B,T,W,F,N,K,lengths", CASES)
 def test_operator_by_operator(B, T, W, F, N, K, lengths):
     torch = torch_gpu()
+    from paper_2607_14394_amd import SCAN_SPAN
     block = build(torch, W, F, N, K, T)
     rng = np.random.RandomState(W)
     R = B * T
@@ -95,7 +96,7 @@ def test_operator_by_operator(B, T, W, F, N, K, lengths):
     near(f64(state[1]), hv[:, -1], "f32", "h")
     yt = values(keep["yt"])[:, :R].T
     assert rel(yt, yv.reshape(R, F)) <= 2.0 ** -4 + 2.0 ** -8
-    near(f64(keep["states"]), hv[:, :-1:16], "f32", "states")
+    near(f64(keep["states"]), hv[:, :-1:SCAN_SPAN], "f32", "states")
 
     # backward: the same
     g_out, gov = rounded(torch, rng.randn(B, T, W), "bf16")
