@@ -243,6 +243,7 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     }
     const auto store = [&](auto full_) {
       constexpr bool FULL = decltype(full_)::value;
+      if (!own) return;
       // The rows are read again: kept, they or their addresses would take registers
       // that there are not.
       uint32_t again = ft;
@@ -266,7 +267,7 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
           const float v = float(ro[i]), u = logistic<T>(v);
           go = there ? float(rg[i]) * (yv[i] + dv * xv) * (u + v * u * (1.f - u)) : 0.f;
         }
-        if ((FULL || i < rows_all) && own) {  // (no `break`: the loop stays unrolled)
+        if (FULL || i < rows_all) {  // (no `break`: the loop stays unrolled)
           put(to_x, again, gx);
           put(to_delta, again, gs);
           if constexpr (GATED) put(to_o, again, go);
