@@ -312,10 +312,10 @@ dtst_status scan_adj(const dtst_scan_desc* d, const void* x, const void* delta, 
   const size_t need = scan_adj_workspace(*d);
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   DTST_TRY(check_scan_grid(d, true));
-  // (a wave for 64 features of a segment; four waves for 64 steps of g_b and g_c)
+  // (a wave for 64 features of a segment; four waves for four times 64 of a span's g_b and g_c)
   DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F, true) * B, 64));
   const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
-  DTST_TRY(check_grid((B * ((T + 63) / 64) * 2 * N + 3) / 4, 256));
+  DTST_TRY(check_grid((B * spans * ((2 * N * DTST_SCAN_SPAN + 63) / 64) + 3) / 4, 256));
   DTST_TRY(check_grid(((N + 1) * F + 31) / 32, 1024));
   const Block ba{steps ? a : nullptr, N * F * 4, "a"}, bd{skip, F * 4, "d"}, bn{lengths, B * 4, "lengths"};
   const Block bst{steps ? states : nullptr, one * spans, "states"}, bin{g_h, one, "g_h"}, bout{g_hzero, one, "g_hzero"};
