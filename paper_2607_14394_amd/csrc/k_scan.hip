@@ -2,6 +2,14 @@
 //   D_t = log(1 + exp(delta_t)),  h_t[n] = exp(D_t a[n]) h_{t-1}[n] + D_t x_t b_t[n],
 //   y_t = (sum_n c_t[n] h_t[n] + d x_t) o_t s(o_t),
 // feature by feature, with N states h[n] each and b_t, c_t common to all features.
+//
+// N values of work a value of the sequences, five to seven instructions each (the
+// exponential's two slots among them): bound by the vector unit, not by HBM.  A lane takes
+// a feature with all its states in registers, and goes through the steps; where features
+// and entries are too few to fill the card, the steps are cut into segments: each one's
+// end from a zero state first, what enters each by composing these, then the outputs,
+// where each state's exponentials are computed a second time.  (The tables that a first
+// pass would have to keep for it are N times the sequences.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -6,6 +6,14 @@
 //   g_x_t = D_t w_t + g_t d,   g_a = sum_t D_t e_{t-1} h_{t-1},   g_d = sum_t g_t x_t
 //   g_delta_t = (x_t w_t + sum_n a e_{t-1} h_{t-1}) s(delta_t)
 //   g_o_t = g_y_t (sum_n c_t h_t + d x_t) s(o_t) (1 + o_t s(-o_t)).
+//
+// Bound by the vector unit: 16 instructions a state and step, 13 of them the formulas', two
+// the sums over the features, and 4 more of the step itself among 16 states.  The forward's
+// states at every 16th step are read; h goes on from there, and all that a state's way back
+// needs is in registers (222, two waves a SIMD).  4 x 4096 x 2048 of 16 states in bf16: 450
+// us, the vector unit busy 74% of the time, after 130 us for the segments' ends (81%), and 19
+// for g_b's and g_c's sums.  Spans of 8 steps, three waves a SIMD, took 454 with twice
+// the states kept; b and c from LDS 500; the lanes' sums by exchanges between lanes 525.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

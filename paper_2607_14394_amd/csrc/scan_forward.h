@@ -1,5 +1,11 @@
 // The forward state-space scan's kernel, by type (k_scan_f32.hip, k_scan_bf16.hip,
 // k_scan_f16.hip).
+//
+// Of 16 states, 7.3 vector instructions a state and step for the outputs, 5.7 for the
+// segments' ends, with the step size, the gate and the loads shared among the states; the
+// exponential takes two slots.  4 x 4096 x 2048 in bf16: 105 us the ends, 145 the outputs
+// with the states that the backward needs, the vector unit busy 91% and 89% of the time;
+// 65536 x 1280: 249 and 325 us (93%).  b and c come from LDS, the same word for all lanes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -12,7 +18,9 @@
 namespace dtst {
 namespace {
 
-constexpr int ROWS = 4;     // steps whose loads are in flight together
+// Steps whose loads are in flight together.  (With three waves a SIMD 248 us for 4 x 4096
+// x 2048, ends and outputs; eight steps and two waves 252, four waves 300: they spill.)
+constexpr int ROWS = 4;
 constexpr int CHUNK = 32;   // steps whose b and c are in LDS together
 constexpr int WAVES = 4;    // of a workgroup, 64 features each
 
@@ -199,6 +207,9 @@ int launch_forms(const ScanArgs& p, const ScanPointers& q, hipStream_t s) {
 }
 
 // Calls f for the number of states that holds N, and the least of its branch-free ones.
+// (24 ragged sequences of 731 steps, 1001 features and 12 states: 118 us by twelve, 164 by
+// sixteen of which four are branched around.  A form of its own for every N would be 64
+// kernels a type.)
 template <class F>
 int by_states(int N, F&& f) {
   using std::integral_constant;
