@@ -147,7 +147,7 @@ dtst_status check_scan_desc(const dtst_scan_desc* d) {
 
 // (workgroups of 256 threads for 256 features of a segment, and for the states)
 dtst_status check_scan_grid(const dtst_scan_desc* d, bool adj) {
-  const int64_t segments = scan_segments(d->batch, d->steps, d->features, adj);
+  const int64_t segments = scan_segments(d->batch, d->steps, d->features, d->states, adj);
   DTST_TRY(check_grid((d->features + 255) / 256 * segments * d->batch, 256));
   return check_grid((d->batch * d->states * d->features + 63) / 64, 512);
 }
@@ -313,7 +313,7 @@ dtst_status scan_adj(const dtst_scan_desc* d, const void* x, const void* delta, 
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   DTST_TRY(check_scan_grid(d, true));
   // (a wave for 64 features of a segment; four waves for four times 64 of a span's g_b and g_c)
-  DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F, true) * B, 64));
+  DTST_TRY(check_grid((F + 63) / 64 * scan_segments(B, T, F, N, true) * B, 64));
   const int64_t one = B * N * F * 4, spans = (T + DTST_SCAN_SPAN - 1) / DTST_SCAN_SPAN;
   DTST_TRY(check_grid((B * spans * ((2 * N * DTST_SCAN_SPAN + 63) / 64) + 3) / 4, 256));
   DTST_TRY(check_grid(((N + 1) * F + 31) / 32, 1024));

@@ -97,17 +97,17 @@ int launch_copy_states(const float* in, float* out, int64_t n, void* stream) {
   return hipGetLastError();
 }
 
-// Segments of a sequence: as many as give the card so many waves, not one more: three
-// a SIMD, the forward's, in one go (65536 steps of 1280 features: 589 us, and 607 with
-// 4096; 24 ragged sequences of 1001 features: 128 and 130 us), two a SIMD twice over,
-// the backward's (4 sequences of 4096 steps and 2048 features, both directions: 891 us;
-// 1315, 912, 937 and 901 with 1024, 2048, 6144 and 8192).  Whole sequences from 1024
-// waves on: the second pass over the steps costs more than waves side by side save (32
-// sequences of 1024 steps and 4096 features: 571 us whole, 908 in two segments).
-int scan_segments(int64_t batch, int64_t steps, int64_t features, bool adj) {
+// Segments of a sequence: as many as give the card so many waves, not one more: those that
+// the forward's kernel has registers for in one go (4 x 4096 x 1024 of 4 or 8 states: 75 and
+// 93 us with 4096, 82 and 104 with 3072; 65536 x 1280 of 16: 589 us with 3072, 607 with 4096;
+// 8 x 2048 x 1024 of 40: 375 with 2048, 460 with 3072), two a SIMD twice over, the backward's
+// (4 x 4096 x 2048 of 16, both directions: 891 us; 1315, 912, 937 and 901 with 1024, 2048,
+// 6144 and 8192).  Whole sequences from 1024 waves on: the second pass over the steps costs
+// more than waves side by side save (32 x 1024 x 4096 of 16: 571 us whole, 908 in two).
+int scan_segments(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj) {
   const int64_t waves = batch * ((features + 63) / 64), spans = (steps + SCAN_SPAN - 1) / SCAN_SPAN;
   if (waves <= 0 || spans <= 1 || waves >= 1024) return 1;
-  const int64_t most = (adj ? 4096 : 3072) / waves, each = (spans + most - 1) / most;  // (spans)
+  const int64_t most = (adj ? 4096 : 1024 * scan_waves(int(states))) / waves, each = (spans + most - 1) / most;  // (spans)
   return int((spans + each - 1) / each);
 }
 
@@ -118,13 +118,13 @@ ScanArgs scan_args(const dtst_scan_desc& d, const int32_t* lengths, bool adj) {
              st(d.g_c_stride), st(d.g_o_stride), lengths, 0, 0, 0, 0};
   p.spans = (d.steps + SCAN_SPAN - 1) / SCAN_SPAN;
   p.tiles = (d.features + 63) / 64;
-  p.segments = scan_segments(d.batch, d.steps, d.features, adj);
+  p.segments = scan_segments(d.batch, d.steps, d.features, d.states, adj);
   p.segment = (p.spans + p.segments - 1) / p.segments * SCAN_SPAN;
   return p;
 }
 
 size_t scan_carry_bytes(const dtst_scan_desc& d, bool adj) {
-  const int s = scan_segments(d.batch, d.steps, d.features, adj);
+  const int s = scan_segments(d.batch, d.steps, d.features, d.states, adj);
   return s > 1 ? size_t(d.batch) * s * (d.states + 2) * d.features * 4 : 0;
 }
 

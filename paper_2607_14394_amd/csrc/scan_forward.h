@@ -18,23 +18,27 @@
 namespace dtst {
 namespace {
 
-// Steps whose loads are in flight together.  (With three waves a SIMD 248 us for 4 x 4096
-// x 2048, ends and outputs; eight steps and two waves 252, four waves 300: they spill.)
-constexpr int ROWS = 4;
-constexpr int CHUNK = 32;   // steps whose b and c are in LDS together
-constexpr int WAVES = 4;    // of a workgroup, 64 features each
+// Steps whose loads are in flight together.  (16 states, three waves a SIMD, 4 x 4096 x
+// 2048, ends and outputs: 248 us with four; eight and two waves 252, one or two and four
+// waves 277 to 292.  With more states, four steps' b and c leave registers for one wave a
+// SIMD: 544 against 261 us for 32 sequences of 1333 steps, 168 features and 55 states, 384
+// against 240 for 4 x 4096 x 512 of 64.)
+constexpr int rows_of_states(int NS) { return NS <= 16 ? 4 : 1; }
+constexpr int EACH = 8;  // steps, for each wave of a workgroup, whose b and c are in LDS together
 
 // ENDS: the state at each segment's end from a zero state, with the sum and the
 // largest of its D, into `carry` (batch, segments, N + 2, features).  Else the
 // outputs, from the state that enters each segment: carry's, or h_zero's where
 // there is one segment.  N is NS or (N >= LEAST) below; the states past N are left
 // out by branches, as zeros in their place would meet infinities.
-template <class T, int NS, int LEAST, bool ENDS>
-__global__ void __launch_bounds__(64 * WAVES, NS <= 16 ? 3 : 1)
+template <class T, int NS, int LEAST, int WAVES, bool ENDS>
+__global__ void __launch_bounds__(64 * WAVES, scan_waves(NS))
 scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restrict__ a, const T* b, const T* c,
             const float* __restrict__ skip, const T* o, const float* h_zero, T* y, float* h_out, float* states,
             float* carry) {
   constexpr int KINDS = ENDS ? 1 : 2;
+  constexpr int ROWS = rows_of_states(NS);
+  constexpr int CHUNK = EACH * WAVES;
   __shared__ float bc[2][KINDS][CHUNK][NS];
   constexpr int LOADS = (KINDS * CHUNK * NS + 64 * WAVES - 1) / (64 * WAVES);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -69,7 +73,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   const float dv = !ENDS && skip != nullptr ? skip[f] : 0.f;
   float sum = 0.f, most = 0.f;
 
-  // b and c of CHUNK steps from t on
+  // b and c of a chunk of steps from t on
   float staged[LOADS];
   const auto fetch = [&](int64_t t) {
 #pragma unroll
@@ -150,11 +154,12 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
 #pragma unroll
             for (int n = LEAST; n < NS; ++n) bv[n] = bt[n], cv[n] = ct[n];
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+            for (int n = 0; n < NS; ++n) {
               if (n < LEAST || n < N) {
                 h[n] = __builtin_amdgcn_exp2f(D[i] * a2[n]) * h[n] + Dx[i] * (n < LEAST ? bt[n] : bv[n]);
                 if constexpr (!ENDS) v = fmaf(h[n], n < LEAST ? ct[n] : cv[n], v);
               }
+            }
             if constexpr (!ENDS) {
               put(to, ft, v * gate[i]);
               to += p.y.t;
@@ -188,7 +193,7 @@ scan_kernel(const ScanArgs p, const T* x, const T* delta, const float* __restric
   }
 }
 
-template <class T, int NS, int LEAST>
+template <class T, int NS, int LEAST, int WAVES>
 int launch_forms(const ScanArgs& p, const ScanPointers& q, hipStream_t s) {
   const int64_t groups = (p.tiles + WAVES - 1) / WAVES * p.batch;
   const auto go = [&](auto kernel, int segments) {
@@ -198,12 +203,12 @@ int launch_forms(const ScanArgs& p, const ScanPointers& q, hipStream_t s) {
     return int(hipGetLastError());
   };
   if (p.segments > 1) {
-    int e = go(scan_kernel<T, NS, LEAST, true>, p.segments - 1);
+    int e = go(scan_kernel<T, NS, LEAST, WAVES, true>, p.segments - 1);
     if (e != hipSuccess) return e;
     e = launch_scan_carry(p, q.a, q.h_zero, q.carry, false, s);
     if (e != hipSuccess) return e;
   }
-  return go(scan_kernel<T, NS, LEAST, false>, p.segments);
+  return go(scan_kernel<T, NS, LEAST, WAVES, false>, p.segments);
 }
 
 // Calls f for the number of states that holds N, and the least of its branch-free ones.
@@ -222,16 +227,23 @@ int by_states(int N, F&& f) {
   if (N <= 16) return sized(integral_constant<int, 16>(), integral_constant<int, 12>());
   if (N <= 24) return sized(integral_constant<int, 24>(), integral_constant<int, 16>());
   if (N <= 32) return sized(integral_constant<int, 32>(), integral_constant<int, 24>());
-  if (N <= 48) return sized(integral_constant<int, 48>(), integral_constant<int, 32>());
-  return sized(integral_constant<int, 64>(), integral_constant<int, 48>());
+  if (N <= 40) return sized(integral_constant<int, 40>(), integral_constant<int, 32>());
+  if (N <= 48) return sized(integral_constant<int, 48>(), integral_constant<int, 40>());
+  if (N <= 56) return sized(integral_constant<int, 56>(), integral_constant<int, 48>());
+  return sized(integral_constant<int, 64>(), integral_constant<int, 56>());
 }
 
 }  // namespace
 
 template <class T>
 int launch_scan_type(const ScanArgs& p, const ScanPointers& q, hipStream_t s) {
+  // Four waves share b and c (32 x 1024 x 4096: 568 us, and 727 with one), but those past the
+  // features' end only take others' places (8 x 4000 x 320, five of eight: 240 us, and 200
+  // with one).
+  const bool four = (p.tiles + 3) / 4 * 4 * 100 <= p.tiles * 115;
   return by_states(p.states, [&](auto ns, auto least) {
-    return launch_forms<T, decltype(ns)::value, decltype(least)::value>(p, q, s);
+    constexpr int NS = decltype(ns)::value, LEAST = decltype(least)::value;
+    return four ? launch_forms<T, NS, LEAST, 4>(p, q, s) : launch_forms<T, NS, LEAST, 1>(p, q, s);
   });
 }
 

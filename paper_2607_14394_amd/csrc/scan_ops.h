@@ -75,6 +75,10 @@ __device__ __forceinline__ void get_rows(const T* p, Strides s, int64_t e, int64
   }
 }
 
+// Waves a SIMD that the forward's kernel of so many states is built for: as its registers
+// allow.
+constexpr int scan_waves(int states) { return states <= 8 ? 4 : states <= 32 ? 3 : 2; }
+
 struct ScanPointers {
   const void *x, *delta, *b, *c, *o;
   const float *a, *skip, *h_zero;

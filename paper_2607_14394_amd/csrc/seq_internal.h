@@ -53,7 +53,7 @@ int launch_conv_adj(const dtst_conv_desc& d, const void* x, const float* w, cons
                     float* g_bias, void* g_state, void* workspace, void* stream);
 
 constexpr int64_t kScanMaxStates = 64;
-int scan_segments(int64_t batch, int64_t steps, int64_t features, bool adj);
+int scan_segments(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj);
 size_t scan_carry_bytes(const dtst_scan_desc& d, bool adj);
 int launch_scan(const dtst_scan_desc& d, const void* x, const void* delta, const float* a, const void* b, const void* c,
                 const float* skip, const void* o, const float* h_zero, const int32_t* lengths, void* y, float* h_out,
