@@ -75,9 +75,11 @@ __global__ void __launch_bounds__(256) scan_adj_lift_kernel(const ScanArgs p, co
   }
 }
 
-// Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer | a span's sums [N][2][R].
+// Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer | a span's sums of some states.
+// (Of all 64 states, they leave room for three waves a CU instead of four.)
+constexpr int TOGETHER = 16;
 __host__ __device__ constexpr int adj_lds(int N, bool ends) {
-  return N * 64 + (ends ? 0 : N * 64 + R * PITCH + N * 2 * R);
+  return N * 64 + (ends ? 0 : N * 64 + R * PITCH + (N < TOGETHER ? N : TOGETHER) * 2 * R);
 }
 
 // A wave: 64 features of a segment, a lane a feature, its spans from the last to
@@ -186,68 +188,71 @@ scan_adj_kernel(const ScanArgs p, const AdjArrays w, const T* x, const T* delta,
     float a_next = get(a, f4), h_next = ENDS ? 0.f : get(kept, f4);
     float4 last[4];  // g_b's terms of the state before, and its sum of g_c
     float last_c = 0.f;
-    for (int n = 0; n < N; ++n) {
-      const float an = a_next, a2 = an * LOG2E;
-      float h = own ? h_next : 0.f;
+    for (int first = 0; first < N; first += ENDS ? N : TOGETHER) {
+      const int past = ENDS ? N : min(first + TOGETHER, N);
+      for (int n = first; n < past; ++n) {
+        const float an = a_next, a2 = an * LOG2E;
+        float h = own ? h_next : 0.f;
 #pragma unroll
-      for (int i = 0; i < R; ++i) bn[i] = b_next[i], cn[i] = c_next[i];
-      if (n + 1 < N) {
-        from += 2 * pitch;
-        if constexpr (ENDS) fetch();
-        a_next = get(a + (n + 1) * F, f4);
-        if constexpr (!ENDS) h_next = get(kept + (n + 1) * F, f4);
-      }
-      float E[R], q = ecarry[n * 64 + lane];
-#pragma unroll
-      for (int i = 0; i < R; ++i) E[i] = __builtin_amdgcn_exp2f(a2 * D[i]);
-      if constexpr (ENDS) {
-#pragma unroll
-        for (int i = R - 1; i >= 0; --i) q = E[i] * fmaf(g[i], cn[i], q);
-      } else {
-        float hp[R], ga = gA[n * 64 + lane];  // hp: the states before the steps
-        if (n > 0) {
-          const float gb = row_sum(last);
-          sums[2 * (n - 1) * R] = lane & 1 ? last_c : gb;
+        for (int i = 0; i < R; ++i) bn[i] = b_next[i], cn[i] = c_next[i];
+        if (n + 1 < N) {
+          from += 2 * pitch;
+          if constexpr (ENDS) fetch();
+          a_next = get(a + (n + 1) * F, f4);
+          if constexpr (!ENDS) h_next = get(kept + (n + 1) * F, f4);
         }
+        float E[R], q = ecarry[n * 64 + lane];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          hp[i] = h;
-          h = E[i] * h + Dx[i] * bn[i];
-          if constexpr (GATED) yv[i] = fmaf(cn[i], h, yv[i]);
-          buffer[i * PITCH + lane] = g[i] * h;
-        }
-        float4 terms[4];
-        read_row(buffer, lane, terms);
+        for (int i = 0; i < R; ++i) E[i] = __builtin_amdgcn_exp2f(a2 * D[i]);
+        if constexpr (ENDS) {
 #pragma unroll
-        for (int i = R - 1; i >= 0; --i) {
-          q = fmaf(g[i], cn[i], q);
-          wb[i] = fmaf(q, bn[i], wb[i]);
-          buffer[i * PITCH + lane] = q * Dx[i];
-          q *= E[i];
-          const float s = q * hp[i];
-          gD[i] = fmaf(an, s, gD[i]);
-          ga = fmaf(D[i], s, ga);
-          if (i == R / 2) {
-            // The next state's b and c from here on: scalar loads in flight would be
-            // waited for with the terms.
-            last_c = row_sum(terms);
-            __builtin_amdgcn_sched_barrier(0);
-            fetch();
-            __builtin_amdgcn_sched_barrier(0);
+          for (int i = R - 1; i >= 0; --i) q = E[i] * fmaf(g[i], cn[i], q);
+        } else {
+          float hp[R], ga = gA[n * 64 + lane];  // hp: the states before the steps
+          if (n > first) {
+            const float gb = row_sum(last);
+            sums[2 * (n - 1 - first) * R] = lane & 1 ? last_c : gb;
           }
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            hp[i] = h;
+            h = E[i] * h + Dx[i] * bn[i];
+            if constexpr (GATED) yv[i] = fmaf(cn[i], h, yv[i]);
+            buffer[i * PITCH + lane] = g[i] * h;
+          }
+          float4 terms[4];
+          read_row(buffer, lane, terms);
+#pragma unroll
+          for (int i = R - 1; i >= 0; --i) {
+            q = fmaf(g[i], cn[i], q);
+            wb[i] = fmaf(q, bn[i], wb[i]);
+            buffer[i * PITCH + lane] = q * Dx[i];
+            q *= E[i];
+            const float s = q * hp[i];
+            gD[i] = fmaf(an, s, gD[i]);
+            ga = fmaf(D[i], s, ga);
+            if (i == R / 2) {
+              // The next state's b and c from here on: scalar loads in flight would be
+              // waited for with the terms.
+              last_c = row_sum(terms);
+              __builtin_amdgcn_sched_barrier(0);
+              fetch();
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+          gA[n * 64 + lane] = ga;
+          read_row(buffer, lane, last);
         }
-        gA[n * 64 + lane] = ga;
-        read_row(buffer, lane, last);
+        ecarry[n * 64 + lane] = q;
       }
-      ecarry[n * 64 + lane] = q;
-    }
-    if constexpr (!ENDS) {
-      const float gb = row_sum(last);
-      sums[2 * (N - 1) * R] = lane & 1 ? last_c : gb;
-      wave_sync();
-      float4* to = reinterpret_cast<float4*>(w.sums + ((tile * p.batch + e) * p.spans + t0 / R) * N * 2 * R);
-      for (int i = lane; i < N * 2 * R / 4; i += 64) to[i] = reinterpret_cast<const float4*>(bc_sums)[i];
-      wave_sync();
+      if constexpr (!ENDS) {
+        const float gb = row_sum(last);
+        sums[2 * (past - 1 - first) * R] = lane & 1 ? last_c : gb;
+        wave_sync();
+        float4* to = reinterpret_cast<float4*>(w.sums + (((tile * p.batch + e) * p.spans + t0 / R) * N + first) * 2 * R);
+        for (int i = lane; i < (past - first) * 2 * R / 4; i += 64) to[i] = reinterpret_cast<const float4*>(bc_sums)[i];
+        wave_sync();
+      }
     }
     const auto store = [&](auto full_) {
       constexpr bool FULL = decltype(full_)::value;
@@ -360,9 +365,11 @@ int launch_scan_adj(const dtst_scan_desc& d, const void* x, const void* delta, c
     const auto go = [&](auto kernel, bool ends) {
       const int64_t segments = ends ? p.segments - 1 : p.segments;
       // Several waves a workgroup meet in the scalar cache, whose b and c are the same
-      // for all; eight a CU have to fit its LDS.
+      // for all, but as many a CU as its LDS holds (eight, by their registers) come first.
+      const auto held = [&](int w) { return std::min(8, 160 * 1024 / (w * adj_lds(N, ends) * 4) * w); };
       int waves = WAVES;
-      while (waves > 1 && (waves * adj_lds(N, ends) * 4 > 80 * 1024 || waves / 2 >= p.tiles)) waves /= 2;
+      for (int w = WAVES / 2; w >= 1; w /= 2)
+        if (held(w) > held(waves) || w >= p.tiles) waves = w;
       const size_t lds = size_t(waves) * adj_lds(N, ends) * 4;
       if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
