@@ -252,20 +252,21 @@ def test_no_steps_and_no_sequences():
         assert not ga.any() and not gd.any()
 
 
-def test_replayed():
+@pytest.mark.parametrize("B,T,F,N", [(2, 700, 130, 5), (1, 90, 300, 64)])
+def test_replayed(B, T, F, N):
     """A backward captured and replayed, with eager work between, and two streams in turns."""
     torch, D = lib()
-    dev, val = inputs(torch, 2, 700, 130, 5, "bf16", 13)
+    dev, val = inputs(torch, B, T, F, N, "bf16", 13)
     g, _, h, _ = gradient(torch, dev, "bf16", 13)
     want = run(torch, D, dev, "bf16", g, h)
-    st = torch.empty(D.scan_states_shape(2, 700, 130, 5), device="cuda")
+    st = torch.empty(D.scan_states_shape(B, T, F, N), device="cuda")
     args = [dev[k] for k in OPERANDS]
     D.dtst_scan(*args, torch.empty_like(dev["x"]), d=dev["d"], o=dev["o"], h0=dev["h0"], states=st)
 
     def call(ws=None, stream=None):
         r = dict(x=torch.empty_like(dev["x"]), delta=torch.empty_like(dev["x"]), a=torch.empty_like(dev["a"]),
-                 b=torch.empty(2, 700, 5, dtype=torch.bfloat16, device="cuda"),
-                 c=torch.empty(2, 700, 5, dtype=torch.bfloat16, device="cuda"), d=torch.empty_like(dev["d"]),
+                 b=torch.empty(B, T, N, dtype=torch.bfloat16, device="cuda"),
+                 c=torch.empty(B, T, N, dtype=torch.bfloat16, device="cuda"), d=torch.empty_like(dev["d"]),
                  o=torch.empty_like(dev["x"]), h0=torch.empty_like(h))
         D.dtst_scan_adj(*args, g, st, *(r[k] for k in OPERANDS), d=dev["d"], g_d=r["d"], o=dev["o"], g_o=r["o"], g_h=h,
                         g_hzero=r["h0"], ws=ws, stream=stream)
@@ -278,7 +279,7 @@ def test_replayed():
     torch.cuda.synchronize()
     for r in rs:
         assert all(torch.equal(r[k], want[k]) for k in r)
-    ws = torch.empty(D.dtst_scan_adj_workspace(2, 700, 130, 5), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(D.dtst_scan_adj_workspace(B, T, F, N), dtype=torch.uint8, device="cuda")
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):
         r = call(ws)
