@@ -99,11 +99,12 @@ int launch_copy_states(const float* in, float* out, int64_t n, void* stream) {
 
 // Segments of a sequence: as many as give the card so many waves, not one more: those that
 // the forward's kernel has registers for in one go (4 x 4096 x 1024 of 4 or 8 states: 75 and
-// 93 us with 4096, 82 and 104 with 3072; 65536 x 1280 of 16: 589 us with 3072, 607 with 4096;
-// 8 x 2048 x 1024 of 40: 375 with 2048, 460 with 3072), two a SIMD twice over, the backward's
-// (4 x 4096 x 2048 of 16, both directions: 891 us; 1315, 912, 937 and 901 with 1024, 2048,
-// 6144 and 8192).  Whole sequences from 1024 waves on: the second pass over the steps costs
-// more than waves side by side save (32 x 1024 x 4096 of 16: 571 us whole, 908 in two).
+// 93 us with four a SIMD, 82 and 104 with three; 65536 x 1280 of 16: 589 us with three, 607
+// with four; 8 x 2048 x 1024 of 40: 375 with two, 460 with three), two a SIMD twice over, the
+// backward's (4 x 4096 x 2048 of 16, both directions: 891 us with 4096 waves; 1315, 912, 937
+// and 901 with 1024, 2048, 6144 and 8192).  Whole sequences from 1024 waves on: the second
+// pass over the steps costs more than waves side by side save (32 x 1024 x 4096 of 16: 571 us
+// whole, 908 in two).
 int scan_segments(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj) {
   const int64_t waves = batch * ((features + 63) / 64), spans = (steps + SCAN_SPAN - 1) / SCAN_SPAN;
   if (waves <= 0 || spans <= 1 || waves >= 1024) return 1;
