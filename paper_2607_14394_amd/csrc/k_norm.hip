@@ -50,9 +50,7 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
 // (A second call on the same slots needs a barrier before it where RW > 1.)
 template <int RW>
 __device__ __forceinline__ double row_sum64(float v, double* part) {
-#pragma unroll
-  for (int d = 1; d <= 8; d <<= 1) v += __shfl_xor(v, d, 64);
-  double s = v;
+  double s = row16_sum(v);
   s += __shfl_xor(s, 16, 64);
   s += __shfl_xor(s, 32, 64);
   if constexpr (RW > 1) {
@@ -134,11 +132,15 @@ norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = first + i * RW * 64 * VEC;
+      if (c + VEC <= cols) {  // (a select for each value would cost as much as its sums)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        u[i][j] = c + j < cols ? u[i][j] - high : 0.f;
-        s += u[i][j];
+        for (int j = 0; j < VEC; ++j) u[i][j] -= high;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) u[i][j] = c + j < cols ? u[i][j] - high : 0.f;
       }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) s += u[i][j];
     }
     mean = high;
   }

@@ -72,6 +72,15 @@ __device__ __forceinline__ float row_rotate(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + R, 0xf, 0xf, false));
 }
 
+// Sum over the 16 lanes of a row of lanes, in all of them: of neighbours, then of
+// pairs, quads and eights (mirrored, which have equal sums in all of their lanes).
+__device__ __forceinline__ float row16_sum(float v) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, false));
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, false));
+}
+
 // Largest of the 16 lanes of a row of lanes.
 __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, row_rotate<1>(v));
