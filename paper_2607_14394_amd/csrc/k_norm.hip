@@ -13,8 +13,8 @@
 // a row of lanes.  Up to 1024 columns a wave holds a row (no barrier), then four,
 // then sixteen.  16384 x 4096 in bf16 with the residual, to 8 bits: 86 us, 5.5
 // TB/s, what a large copy reaches; 6001 x 1537 in 32 bits 33 us forward (4.5
-// TB/s) and 27 + 5 us backward.  MEAN, with two rounds of sums a row: 98
-// us, and 29 and 28 + 5.
+// TB/s) and 27 + 5 us backward.  MEAN, with two rounds of sums a row: 95
+// us, and 29 and 27 + 5.
 //
 // The sum is rounded to the residual's type first and the norm is of what was
 // stored, so that the backward differentiates what the forward computed.
@@ -73,9 +73,10 @@ __device__ __forceinline__ float rsqrt_of(double m) {
 }
 
 // RW waves a row, V vectors of 8 columns a lane: up to 512 RW V columns.  A
-// workgroup holds max(RW, 4) waves, so four rows with RW = 1.
+// workgroup holds max(RW, 4) waves, so four rows with RW = 1.  (8: four registers fewer,
+// where they do not spill, hold one more wave a SIMD: 96.1 -> 94.8 us for the case above.)
 template <class TX, class TR, bool Q8, int RW, int V, bool MEAN>
-__global__ void __launch_bounds__(RW > 4 ? RW * 64 : 256)
+__global__ void __launch_bounds__(RW > 4 ? RW * 64 : 256, MEAN && Q8 && RW == 4 && V == 2 && sizeof(TR) == 2 ? 8 : 1)
 norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const float* __restrict__ w,
             const float* __restrict__ b, TR* sum_out, void* y, uint8_t* scale, float* mean_out, float* rstd) {
   constexpr int ROWS = RW > 4 ? 1 : 4 / RW;
