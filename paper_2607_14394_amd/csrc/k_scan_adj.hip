@@ -8,12 +8,12 @@
 //   g_o_t = g_y_t (sum_n c_t h_t + d x_t) s(o_t) (1 + o_t s(-o_t)).
 //
 // Bound by the vector unit: 16 instructions a state and step, 13 of them the formulas', two
-// the sums over the features, and 4 more of the step itself among 16 states.  The forward's
+// the sums over the features, and 5 more of the step itself among 16 states.  The forward's
 // states at every 16th step are read; h goes on from there, and all that a state's way back
-// needs is in registers (218, two waves a SIMD).  4 x 4096 x 2048 of 16 states in bf16: 450
-// us, the vector unit busy 74% of the time, after 130 us for the segments' ends (81%), and 19
-// for g_b's and g_c's sums.  Spans of 8 steps, three waves a SIMD, took 454 with twice
-// the states kept; b and c from LDS 500; the lanes' sums by exchanges between lanes 525.
+// needs is in registers (two waves a SIMD).  4 x 4096 x 2048 of 16 states in bf16: 420 us,
+// the vector unit busy 79% of the time, after 130 us for the segments' ends (81%), and 19
+// for g_b's and g_c's sums.  At 455 us, spans of 8 steps and three waves a SIMD took 454 with
+// twice the states kept, b and c from LDS 500, the lanes' sums by exchanges between them 525.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
