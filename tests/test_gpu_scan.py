@@ -52,6 +52,17 @@ def test_numbers_of_states(N, t):
     compare(torch, D, *inputs(torch, 2, 150, 70, N, t, N), t)
 
 
+@pytest.mark.parametrize("F", [70, 230])
+@pytest.mark.parametrize("N", [3, 4, 7, 12, 13, 16, 20, 24, 32, 36, 40, 41, 48, 52, 56, 57, 64])
+def test_every_form(N, F):
+    """Each number of states that a kernel is built for, and one with states left out,
+    by workgroups of one wave and of four, which share b and c; two segments."""
+    torch, D = lib()
+    say(f"[scan] {N} states, {F} features")
+    for t, lengths in (("f32", None), ("bf16", [77, 0, 5]), ("f16", [1, 20, 80])):
+        compare(torch, D, *inputs(torch, 3, 80, F, N, t, N, lengths), t)
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_random_shapes(seed):
     torch, D = lib()

@@ -71,7 +71,7 @@ def test_numbers_of_states(N, t):
     compare(torch, D, *inputs(torch, 2, 100, 70, N, t, N), t, N)
 
 
-@pytest.mark.parametrize("N,F", [(16, 260), (20, 300), (24, 260), (25, 260), (48, 130)])
+@pytest.mark.parametrize("N,F", [(16, 260), (20, 300), (24, 260), (25, 260), (32, 260), (33, 300), (40, 200), (48, 130), (64, 300)])
 def test_states_of_several_waves(N, F):
     """Workgroups of four, two and one waves: what their states take of the LDS."""
     torch, D = lib()
