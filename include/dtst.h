@@ -372,7 +372,8 @@ dtst_status dtst_layer_norm(const dtst_norm_desc* d, const void* x, const void* 
                             void* stream);
 
 /* Backward of dtst_layer_norm from its stored sum u, mean and rstd, with
- * h = (u - mean) rstd and t = g_y weight:
+ * h = (u - m) rstd and t = g_y weight, m the mean of u (in `mean`, whose rounding to
+ * 32 bits is made good: it would shift all h of a row alike):
  *   g_u = rstd (t - mean_c t - h mean_c(t h)) + g_sum,
  *   g_weight (+)= sum_rows g_y h,   g_bias (+)= sum_rows g_y.
  * Descriptor and arrays as in dtst_rms_norm_adj; g_bias: cols fp32.  workspace:

@@ -64,6 +64,23 @@ __device__ __forceinline__ double row_sum64(float v, double* part) {
   return s;
 }
 
+// Sum over a wave, in all lanes: 16 lanes without LDS, then their four rows.
+__device__ __forceinline__ float wave_sum16(float v) {
+  v = row16_sum(v);
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// Sum of the RW waves' slots, in all lanes, each of which reads one.
+template <int RW>
+__device__ __forceinline__ float slots_sum(const float* slots) {
+  static_assert(RW == 4 || RW == 16, "quads or rows of lanes");
+  float v = slots[threadIdx.x & (RW - 1)];
+  if constexpr (RW == 16) return row16_sum(v);
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xb1, 0xf, 0xf, false));
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4e, 0xf, 0xf, false));
+}
+
 // 1 / sqrt(m), rounded once: the 32-bit root, off by a unit in its last place, and
 // a step of Newton's (no root of 0, infinity and no number).
 __device__ __forceinline__ float rsqrt_of(double m) {
@@ -227,13 +244,19 @@ int launch_norm_cols(const dtst_norm_desc& d, const NormArgs& a, hipStream_t s) 
 // several waves share a row); it takes every gridDim-th of them and keeps its
 // columns' sums of g_y h (MEAN: and of g_y) in registers; they go to part
 // (gridDim, cols; MEAN: cols twice), which sum_parts_kernel adds up.
+//
+// MEAN: three sums a row.  Of h from the mean in 32 bits as it is, two would do, and g_u
+// would be off by 4e-3 of itself where the mean is 1e5 deviations; 2^25 values a call in 32
+// bits, 1537 columns 87 us either way, 8000: 95 and 93, 16000: 149 and 109; with g_y in bf16
+// 1537: 74 and 74, 8000: 83 and 86.  (With the single sums' shuffles and every lane adding up
+// all slots it took registers that there are not: 16000 columns 232.)
 template <class TX, class TR, int RW, int V, int ROWS, bool MEAN>
 __global__ void __launch_bounds__(RW * ROWS * 64, V == 2 && !MEAN ? 4 : 1)  // (4: two registers fewer hold one more wave)
 norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* __restrict__ w,
                 const float* __restrict__ mean_of, const float* __restrict__ rstd, const TR* g_sum, TR* g_u, TX* g_x,
                 float* part) {
   static_assert(ROWS == 1 || (RW == 1 && V == 1), "a wave a row, in one access");
-  __shared__ float red[2][RW], red2[2][RW];
+  __shared__ float red[2][RW], red2[2][RW], red3[2][RW];
   const int first = int(threadIdx.x % (RW * 64)) * VEC, sub = threadIdx.x / (RW * 64);
   const int64_t cols = d.cols;
   float wv[V][VEC], gw[V][VEC], gb[V][VEC];
@@ -248,7 +271,7 @@ norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* _
   for (int64_t row = int64_t(blockIdx.x) * ROWS + sub; row < d.rows; row += int64_t(gridDim.x) * ROWS, odd ^= 1) {
     const float r = rstd[row];
     float g[V][VEC], h[V][VEC];
-    float dot = 0.f, sum = 0.f, m = 0.f;
+    float dot = 0.f, sum = 0.f, shift = 0.f, m = 0.f;
     if constexpr (MEAN) m = mean_of[row];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -256,30 +279,64 @@ norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* _
       load_n<VEC>(g_y + row * d.ld_g_y + c, cols - c, g[i]);
       load_n<VEC>(u + row * d.ld_u + c, cols - c, h[i]);
     }
+    if constexpr (MEAN) {
+      // Deviations from the mean in 32 bits, whose rounding they have in common: `low`,
+      // their own mean, is taken off as in the forward, in the sums' one round,
+      //   mean(t h) = r (mean(t v) - low mean t),  h = r (v - low).
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+      for (int i = 0; i < V; ++i) {
+        const int64_t c = first + i * RW * 64 * VEC;
+        if (c + VEC <= cols) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        h[i][j] = (MEAN ? h[i][j] - m : h[i][j]) * r;  // (past the row g and w are zero)
-        gw[i][j] += g[i][j] * h[i][j];
-        if constexpr (MEAN) gb[i][j] += g[i][j];
-        g[i][j] *= wv[i][j];
-        if constexpr (MEAN) sum += g[i][j];
-        dot += g[i][j] * h[i][j];
+          for (int j = 0; j < VEC; ++j) h[i][j] -= m;
+        } else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) h[i][j] = c + j < cols ? h[i][j] - m : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float t = g[i][j] * wv[i][j];
+          gb[i][j] += g[i][j];
+          shift += h[i][j];
+          sum += t;
+          dot += t * h[i][j];
+        }
       }
-    // (two sets of slots: one barrier a row)
-    float mean_t = 0.f;
-    if constexpr (MEAN) mean_t = wave_sum(sum);
-    if constexpr (MEAN && RW > 1) {
-      if ((threadIdx.x & 63) == 0) red2[odd][threadIdx.x >> 6] = mean_t;
-    }
-    const float mean = row_sum<RW>(dot, red[odd]) / float(cols);
-    if constexpr (MEAN && RW > 1) {
-      mean_t = 0.f;
+    } else {
 #pragma unroll
-      for (int i = 0; i < RW; ++i) mean_t += red2[odd][i];
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          h[i][j] *= r;  // (past the row g and w are zero)
+          gw[i][j] += g[i][j] * h[i][j];
+          g[i][j] *= wv[i][j];
+          dot += g[i][j] * h[i][j];
+        }
     }
-    mean_t /= float(cols);
+    // (two sets of slots: one barrier a row)
+    float mean, mean_t = 0.f;
+    if constexpr (!MEAN) {
+      mean = row_sum<RW>(dot, red[odd]) / float(cols);
+    } else {
+      dot = wave_sum16(dot), sum = wave_sum16(sum), shift = wave_sum16(shift);
+      if constexpr (RW > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) red[odd][wave] = dot, red2[odd][wave] = sum, red3[odd][wave] = shift;
+        __syncthreads();
+        dot = slots_sum<RW>(red[odd]), sum = slots_sum<RW>(red2[odd]), shift = slots_sum<RW>(red3[odd]);
+      }
+      mean_t = sum / float(cols);
+      const float low = shift / float(cols);
+      mean = r * (dot / float(cols) - low * mean_t);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          h[i][j] = (h[i][j] - low) * r;
+          gw[i][j] += g[i][j] * h[i][j];
+          g[i][j] *= wv[i][j];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = first + i * RW * 64 * VEC;

@@ -166,6 +166,30 @@ def test_mean_far_above_the_deviations(cols):
     near(f64(y), S.layer_norm(xv, f64(w), None, 1e-5)[0], "f32", "y")
 
 
+@pytest.mark.parametrize("cols", [100, 700, 1537, 4000, 8000, 16000, 20000])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_backward_of_a_mean_far_above_the_deviations(cols, t):
+    """As the forward: h sums to zero over a row whatever its mean is, though the mean
+    is given in 32 bits (off by up to 2^-25 of itself, 3e-3 deviations here).  u - mean
+    is exact, what its values have in common and h are off by a few 2^-24 each; so
+    are g_u's three terms and, relative to the root of the rows, g_weight's sums:
+    below 1e-6 of a bar of 1e-5."""
+    torch, D = lib()
+    rng = np.random.RandomState(cols)
+    rows = 9
+    u, uv = rounded(torch, 1e5 * rng.uniform(0.5, 1, (rows, 1)) + rng.randn(rows, cols), "f32")
+    g, gv = rounded(torch, rng.randn(rows, cols) + 0.5, t)
+    w, wv = rounded(torch, 1 + 0.3 * rng.randn(cols), "f32")
+    _, mv, rv = S.layer_norm(uv, wv, None, 1e-5)
+    mean, rstd = torch.from_numpy(mv).float().cuda(), torch.from_numpy(rv).float().cuda()
+    g_u, g_w, g_b = torch.empty_like(u), torch.empty_like(w), torch.empty_like(w)
+    D.dtst_layer_norm_adj(g, u, w, mean, rstd, g_u, g_w, g_b)
+    ru, rw, rb = S.layer_norm_adj(gv, uv, wv, 1e-5)
+    near(f64(g_u), ru, "f32", "g_u")
+    near(f64(g_w), rw, "f32", "g_w", rms=np.sqrt(rows))
+    near(f64(g_b), rb, "f32", "g_b", rms=np.sqrt(rows))
+
+
 def test_equal_columns_and_no_numbers():
     torch, D = lib()
     x = torch.randn(5, 300, device="cuda")
