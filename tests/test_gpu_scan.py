@@ -7,7 +7,7 @@ import pytest
 
 from gpu_common import say, torch_gpu
 from oracle import seq_oracle as S
-from scan_common import empty, inputs
+from scan_common import SPANS, divided, empty, inputs
 from seq_common import dtype, f64, near, rounded
 
 pytestmark = pytest.mark.gpu
@@ -141,6 +141,51 @@ def test_many_segments_in_place():
         D.dtst_scan(dev["x"], dev["delta"], dev["a"], dev["b"], dev["c"], y, d=dev["d"], o=dev["o"], h0=state, h_out=state)
         near(f64(y), ry, "f32", "y")
         near(f64(state), rh[:, -1], "f32", "h")
+
+
+@pytest.mark.parametrize("case", SPANS, ids=lambda c: "x".join(map(str, c[:4])) + "-" + c[4])
+def test_segments_of_several_spans(case):
+    torch, D = lib()
+    B, T, F, N, t, lengths, segments, _ = case
+    got = divided(D, B, T, F, N)
+    assert got[0] == segments and 2 * segments <= got[2] + 1
+    say(f"[scan] {B} x {T} x {F}, {N} states, {t}: {segments} segments of {got[2]} spans")
+    dev, val = inputs(torch, B, T, F, N, t, 21, lengths)
+    y, h, st = run(torch, D, dev, t, True)
+    some = sorted({0, B // 3, B // 2, B - 1})
+    part = {k: v if k in ("a", "d") or v is None else np.asarray(v)[some] for k, v in val.items()}
+    ry, rh = S.scan(**part)
+    near(f64(y)[some], ry, t, "y")
+    near(f64(h)[some], rh[:, -1], "f32", "h")
+    near(f64(st)[some], rh[:, :-1:D.SCAN_SPAN], "f32", "states")
+    if lengths is not None:
+        for i, n in enumerate(lengths):
+            assert not y[i, n:].any(), i
+    # the states updated in place, with the workspace full of no numbers
+    state, y2 = dev["h0"].clone(), torch.empty_like(y)
+    ws = torch.full((D.dtst_scan_workspace(B, T, F, N),), 255, dtype=torch.uint8, device="cuda")
+    D.dtst_scan(dev["x"], dev["delta"], dev["a"], dev["b"], dev["c"], y2, d=dev["d"], o=dev["o"], h0=state, h_out=state,
+                lengths=dev["lengths"], ws=ws)
+    assert torch.equal(y2, y) and torch.equal(state, h)
+
+
+def test_infinite_states_through_segments_of_several_spans():
+    """As test_infinite_states_and_no_numbers, where a segment's decay comes from the sum
+    of several spans' steps: below the smallest number, though no step's is."""
+    torch, D = lib()
+    B, T, F, N = 8, 300, 4096, 16
+    assert divided(D, B, T, F, N)[0] == 5
+    dev, _ = inputs(torch, B, T, F, N, "f32", 22, gated=False)
+    dev["a"][:, :] = -16.0
+    dev["h0"][2, 0, 3] = float("inf")
+    dev["x"][2, 100, 5] = float("nan")
+    dev["c"][:] = dev["c"].abs() + 0.1
+    y, h, _ = run(torch, D, dev, "f32")
+    assert torch.isinf(h[2, 0, 3]) and torch.isfinite(h[2, 1, 3]) and torch.isinf(y[2, :, 3]).all()
+    assert torch.isnan(h[2, :, 5]).all() and torch.isnan(y[2, 100:, 5]).all() and torch.isfinite(y[2, :100, 5]).all()
+    ok = torch.ones(F, dtype=torch.bool, device="cuda")
+    ok[3] = ok[5] = False
+    assert torch.isfinite(y[2][:, ok]).all() and torch.isfinite(y[:2]).all() and torch.isfinite(y[3:]).all()
 
 
 def test_entries_past_one_segment():

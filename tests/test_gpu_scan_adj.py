@@ -7,7 +7,7 @@ import pytest
 
 from gpu_common import say, torch_gpu
 from oracle import seq_oracle as S
-from scan_common import empty, inputs
+from scan_common import SPANS, divided, empty, inputs
 from seq_common import f64, near, rounded
 
 pytestmark = pytest.mark.gpu
@@ -166,6 +166,42 @@ def test_many_segments():
     g, _, h, _ = gradient(torch, dev, "f32", 6)
     again = run(torch, D, dev, "f32", g, h)
     assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@pytest.mark.parametrize("case", SPANS, ids=lambda c: "x".join(map(str, c[:4])) + "-" + c[4])
+def test_segments_of_several_spans(case):
+    """Some entries have a gradient, so that the sums over all are those of some; the
+    others' are zero."""
+    torch, D = lib()
+    B, T, F, N, t, lengths, _, segments = case
+    got = divided(D, B, T, F, N)
+    assert got[1] == segments and 2 * segments <= got[2] + 1
+    say(f"[scan_adj] {B} x {T} x {F}, {N} states, {t}: {segments} segments of {got[2]} spans")
+    dev, val = inputs(torch, B, T, F, N, t, 31, lengths)
+    g, gv, h, hv = gradient(torch, dev, t, 31, lengths)
+    some = sorted({0, B // 3, B // 2, B - 1})
+    rest = [i for i in range(B) if i not in some]
+    g[rest], h[rest] = 0, 0
+    part = {k: v if k in ("a", "d") or v is None else np.asarray(v)[some] for k, v in val.items()}
+    for v in part.values():
+        if v is not None and np.issubdtype(v.dtype, np.floating):
+            np.nan_to_num(v, copy=False)
+    want = S.scan_adj(*(part[k] for k in OPERANDS), np.nan_to_num(gv[some]), S.scan(**part)[1], part["d"], part["o"],
+                      hv[some], part["lengths"])
+    out = run(torch, D, dev, t, g, h)
+    for k, v in out.items():
+        if k in ("a", "d"):
+            near(f64(v), want[k], "f32", "g_" + k)
+        else:
+            near(f64(v)[some], want[k], "f32" if k == "h0" else t, "g_" + k)
+            assert not v[rest].any(), k
+    if lengths is not None:
+        for i, n in enumerate(lengths):
+            for k in ("x", "delta", "b", "c", "o"):
+                assert not out[k][i, n:].any(), (i, k)
+    ws = torch.full((D.dtst_scan_adj_workspace(B, T, F, N),), 255, dtype=torch.uint8, device="cuda")
+    again = run(torch, D, dev, t, g, h, ws=ws)
+    assert all(torch.equal(out[k], again[k]) for k in out)   # a fixed order of sums
 
 
 def test_added_to_and_in_place():
