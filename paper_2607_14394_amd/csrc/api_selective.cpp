@@ -145,11 +145,14 @@ dtst_status check_scan_desc(const dtst_scan_desc* d) {
                         d->g_delta_stride, d->g_b_stride, d->g_c_stride, d->g_o_stride});
 }
 
-// (workgroups of 256 threads for 256 features of a segment, and for the states)
+// (workgroups of 256 threads for 256 features of a segment; of up to 512 for 64 states
+// that enter segments where there are several, of 256 to copy 256 where there are no steps)
 dtst_status check_scan_grid(const dtst_scan_desc* d, bool adj) {
   const int64_t segments = scan_segments(d->batch, d->steps, d->features, d->states, adj);
+  const int64_t states = d->batch * d->states * d->features;
   DTST_TRY(check_grid((d->features + 255) / 256 * segments * d->batch, 256));
-  return check_grid((d->batch * d->states * d->features + 63) / 64, 512);
+  if (segments > 1) DTST_TRY(check_grid((states + 63) / 64, 512));
+  return d->steps > 0 ? DTST_OK : check_grid((states + 255) / 256, 256);
 }
 
 dtst_status scan_workspace_of(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj, size_t* bytes) {

@@ -188,6 +188,39 @@ def test_infinite_states_through_segments_of_several_spans():
     assert torch.isfinite(y[2][:, ok]).all() and torch.isfinite(y[:2]).all() and torch.isfinite(y[3:]).all()
 
 
+def test_states_past_2_gib():
+    """Single steps of 2^29 values of state, in place, and their backward."""
+    torch, D = lib()
+    B, F, N = 2048, 4096, 64
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(23)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    x, delta, g = rand(B, 1, F), rand(B, 1, F), rand(B, 1, F)
+    b, c, a, d = rand(B, 1, N), rand(B, 1, N), -torch.exp(rand(N, F)), rand(F)
+    h, g_h = rand(B, N, F), rand(B, N, F)
+    y, st = empty(torch, "f32", B, 1, F), empty(torch, "f32", B, 1, N, F)
+    some, cols = [0, 1023, 2047], [0, 77, 4095]
+    val = {k: f64(v[some]) for k, v in dict(x=x, delta=delta, b=b, c=c, h0=h).items()}
+    val.update(a=f64(a), d=f64(d))
+    ry, rh = S.scan(**val)
+    hv, gv = f64(h[:, :, cols]), f64(g_h[:, :, cols])
+    D.dtst_scan(x, delta, a, b, c, y, d=d, h0=h, h_out=h, states=st)
+    near(f64(y[some]), ry, "f32", "y")
+    near(f64(h[some]), rh[:, -1], "f32", "h")
+    near(f64(st[some, 0]), rh[:, 0], "f32", "states")
+    out = [torch.empty_like(v) for v in (x, delta, a, b, c, d)]
+    want = S.scan_adj(val["x"], val["delta"], val["a"], val["b"], val["c"], f64(g[some]), rh, val["d"], None, f64(g_h[some]))
+    D.dtst_scan_adj(x, delta, a, b, c, g, st, *out[:5], d=d, g_d=out[5], g_h=g_h, g_hzero=g_h)
+    for k, v in (("x", out[0]), ("delta", out[1]), ("b", out[3]), ("c", out[4]), ("h0", g_h)):
+        near(f64(v[some]), want[k], "f32", "g_" + k)
+    # the sums over all entries, of some features: relative to the terms' size times the root of their number
+    xv, dv, yv = (f64(v[:, 0, cols]) for v in (x, delta, g))
+    step = np.logaddexp(0.0, dv)[:, None]
+    terms = step * np.exp(step * f64(a)[:, cols]) * (yv[:, None] * f64(c)[:, 0, :, None] + gv) * hv
+    near(f64(out[2][:, cols]), terms.sum(axis=0), "f32", "g_a", rms=np.sqrt((terms ** 2).sum(axis=0).mean()))
+    near(f64(out[5][cols]), (yv * xv).sum(axis=0), "f32", "g_d", rms=np.sqrt(B))
+
+
 def test_entries_past_one_segment():
     """More waves than the card holds: sequences are not divided."""
     torch, D = lib()

@@ -189,6 +189,24 @@ def test_scan_refusals(kw, code, word):
     assert st == code and word in msg, (st, msg)
 
 
+# States of 2^29 values and more that no segments divide: past the checks of a launch's
+# workgroups, to that of the arrays.
+BIG = dict(batch=2048, steps=1, features=4096, states=64, **{k + "_stride": (4096, 4096) for k in
+           ("x", "delta", "o", "y", "g_x", "g_delta", "g_o")}, **{k + "_stride": (64, 64) for k in ("b", "c", "g_b", "g_c")})
+
+
+def test_scan_takes_large_states():
+    st, msg = scan_call(y=P, **BIG)
+    assert st == 1 and "y and x overlap" in msg, (st, msg)
+    st, msg = scan_call("dtst_scan_adj", st=P * 13, nws=1 << 62, gx=P, **BIG)
+    assert st == 1 and "g_x and x overlap" in msg, (st, msg)
+
+
+def test_scan_of_no_steps_and_more_states_than_a_launch_copies():
+    st, msg = scan_call(h0=P, h=P * 2, batch=1 << 20, steps=0, features=1 << 10, states=4)
+    assert st == 2 and "too many" in msg, (st, msg)
+
+
 def test_scan_of_nothing_is_done():
     assert scan_call(batch=0, x=None)[0] == 0 and scan_call(features=0, x=None)[0] == 0
     assert D.scan_states_shape(3, 129, 5, 7) == (3, 9, 7, 5) and D.scan_states_shape(3, 0, 5, 7) == (3, 0, 7, 5)
