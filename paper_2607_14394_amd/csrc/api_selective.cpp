@@ -201,7 +201,7 @@ dtst_status conv(const dtst_conv_desc* d, const void* x, const float* weight, co
   if (state_out) DTST_TRY(check_align(state_out, size, "state_out"));
   if (lengths) DTST_TRY(check_align(lengths, 4, "lengths"));
   DTST_TRY(check_grid(conv_groups(*d, false), 256));
-  DTST_TRY(check_grid((rows * F + 255) / 256, 256));
+  if (T == 0) DTST_TRY(check_grid((rows * F + 255) / 256, 256));  // (the state is copied)
   const Block bw{T > 0 ? weight : nullptr, d->taps * F * 4, "weight"}, bb{bias, F * 4, "bias"}, bn{lengths, B * 4, "lengths"};
   const Block bin{state, rows * F * size, "state"}, bout{state_out, rows * F * size, "state_out"};
   DTST_TRY(check_outputs({&sy}, {&bout}, {&sx}, {&bw, &bb, &bn, &bin}, &bout, &bin));
@@ -234,7 +234,7 @@ dtst_status conv_adj(const dtst_conv_desc* d, const void* x, const float* weight
   const size_t need = conv_adj_workspace(*d);
   DTST_TRY(check_workspace(workspace, workspace_bytes, need));
   DTST_TRY(check_grid(conv_groups(*d, true), 256));
-  DTST_TRY(check_grid((rows * F + 255) / 256, 256));
+  if (!steps) DTST_TRY(check_grid((rows * F + 255) / 256, 256));  // (g_state_out is copied)
   DTST_TRY(check_grid(((d->taps + 1) * F + 31) / 32, 1024));
   const Block bw{steps ? weight : nullptr, d->taps * F * 4, "weight"}, bb{bias, F * 4, "bias"}, bn{lengths, B * 4, "lengths"};
   const Block bin{state, rows * F * size, "state"}, bgo{g_state_out, rows * F * size, "g_state_out"};

@@ -185,6 +185,35 @@ def test_offsets_past_32_bits():
     near(f64(gw), g["w"], "f32", "g_w")
 
 
+def test_states_past_32_bits():
+    """Single steps of 2^32 values of state and more, in place, and their backward."""
+    torch, D = lib()
+    B, F, K, bf = 1 << 20, 640, 8, torch.bfloat16
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(23)
+    rand = lambda *s, dt=bf: torch.randn(*s, generator=gen, device="cuda", dtype=dt)  # noqa: E731
+    x, g, state, last = rand(B, 1, F), rand(B, 1, F), rand(B, K - 1, F), rand(B, K - 1, F)
+    w, bias = rand(K, F, dt=torch.float32), rand(F, dt=torch.float32)
+    some, cols = [0, B // 2 + 1, B - 1], [0, 77, 639]
+    val = dict(x=f64(x[some]), w=f64(w), bias=f64(bias), state=f64(state[some]), g=f64(g[some]), last=f64(last[some]),
+               lengths=None)
+    ry, rl, rg = oracle(val)
+    # the sums over all entries, of some features
+    z = np.concatenate([f64(state[..., cols]), f64(x[..., cols])], axis=1)
+    v = (z * f64(w)[:, cols]).sum(axis=1) + f64(bias)[cols]
+    p = f64(g[:, 0, cols]) * S.logistic(v) * (1 + v * S.logistic(-v))
+    g_x, g_w, g_b, g_s = (torch.empty_like(v) for v in (x, w, bias, last))
+    D.dtst_conv_adj(x, w, g, g_x, g_w, bias=bias, g_bias=g_b, state=state, g_state_out=last, g_state=g_s)
+    near(f64(g_x[some]), rg["x"], "bf16", "g_x")
+    near(f64(g_s[some]), rg["state"], "bf16", "g_state")
+    near(f64(g_w[:, cols]), (p[:, None] * z).sum(axis=0), "f32", "g_w", rms=np.sqrt(((p[:, None] * z) ** 2).sum(axis=0).mean()))
+    near(f64(g_b[cols]), p.sum(axis=0), "f32", "g_bias", rms=np.sqrt((p ** 2).sum(axis=0).mean()))
+    y = torch.empty_like(x)
+    D.dtst_conv(x, w, y, bias=bias, state=state, state_out=state)
+    near(f64(y[some]), ry, "bf16", "y")
+    assert np.array_equal(f64(state[some]), rl)
+
+
 def test_no_numbers_stay_where_they_are():
     """A no number reaches K steps of its feature, and nothing else."""
     torch, D = lib()

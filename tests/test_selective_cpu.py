@@ -316,6 +316,17 @@ def test_conv_adj_refusals(kw, code, word):
     assert st == code and word in msg, (st, msg)
 
 
+def test_conv_takes_large_states():
+    """2^32 values and more of state, which only a call of no steps copies."""
+    big = dict(batch=1 << 20, steps=1, features=1024, taps=8, x_stride=(1024, 1024), y_stride=(1024, 1024), g_x_stride=(1024, 1024))
+    st, msg = conv_call(y=P, **big)
+    assert st == 1 and "y and x overlap" in msg, (st, msg)
+    st, msg = conv_call("dtst_conv_adj", nws=1 << 62, gx=P, **big)
+    assert st == 1 and "g_x and x overlap" in msg, (st, msg)
+    st, msg = conv_call(s=P, so=P * 2, **dict(big, steps=0))
+    assert st == 2 and "too many" in msg, (st, msg)
+
+
 def test_conv_of_nothing_is_done():
     assert conv_call(batch=0, x=None)[0] == 0 and conv_call(features=0, x=None)[0] == 0
     assert conv_call("dtst_conv_adj", features=0, x=None, gw=None)[0] == 0
