@@ -547,7 +547,8 @@ dtst_status dtst_scan_adj(const dtst_scan_desc* desc, const void* x, const void*
 
 /* The norm of n tensors together,
  *   norm = sqrt( sum_i sum_j tensors[i][j]^2 ),
- * in 64 bits and in a fixed order, rounded to fp32 at the end.  tensors[i]:
+ * the squares of two neighbours added in fp32 and these in 64 bits, in a fixed order,
+ * rounded to fp32 at the end: within 2^-23 of itself.  tensors[i]:
  * counts[i] >= 0 values of types[i] (DTST_F32, DTST_BF16 or DTST_F16) without
  * gaps, a device pointer (any where the count is zero); complex values are twice
  * as many real ones.  A tensor listed twice counts twice.  The three arrays are

@@ -7,7 +7,7 @@
 // tensors from a few values to many millions, so a launch takes up to so many
 // tensors as its arguments hold (4 KB), cut into chunks of 8192 values; each of
 // at most 2048 workgroups takes every 2048th, finds its first chunk's tensor and goes
-// on from there.  The sums of eight squares are added up in 64 bits; each workgroup leaves
+// on from there.  The sums of two squares are added up in 64 bits; each workgroup leaves
 // its sum, and one adds those up in a fixed order.  470 MB in bf16: 116 + 5 us (4.1 TB/s)
 // and 161 us (5.8 TB/s, half of what it reads from the last-level cache); 264 tensors of
 // 32 MB in 32 bits 19 and 22 us, where a call takes 95 us on the host.
@@ -81,14 +81,18 @@ __device__ __forceinline__ double group_sum(double s) {
   return s;
 }
 
-// The sum of eight squares: in 32 bits where that neither passes them nor loses what
-// matters (a square below 2^-126 beside a sum of 2^-66), as conversions to 64 bits
-// take longer than the loads (470 MB in bf16: 147 against 120 us).
+// The sum of eight squares: those of two neighbours in 32 bits, as conversions to 64 take
+// long (470 MB in bf16, with the scaling: 284 us; 283 with all eight in 32 bits, 308 with
+// each in 64, or with the roundings of 32 made good).  That is two roundings of 2^-24 of a
+// sum at most, one where 32 bits hold a square (16-bit types), of which the root takes half.
+// All in 64 where 32 pass them or lose what matters (a square below 2^-126 beside a sum of
+// 2^-66).
 __device__ __forceinline__ double squares(const float (&v)[VEC]) {
-  float s = 0.f;
+  float p[VEC / 2];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) s = fmaf(v[j], v[j], s);
-  if (s >= 1e-20f && s <= 1e30f) return s;
+  for (int j = 0; j < VEC / 2; ++j) p[j] = fmaf(v[2 * j + 1], v[2 * j + 1], v[2 * j] * v[2 * j]);
+  const float s = (p[0] + p[1]) + (p[2] + p[3]);
+  if (s >= 1e-20f && s <= 1e30f) return (double(p[0]) + double(p[1])) + (double(p[2]) + double(p[3]));
   double d = 0.0;
 #pragma unroll
   for (int j = 0; j < VEC; ++j) d = fma(double(v[j]), double(v[j]), d);

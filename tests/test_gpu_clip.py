@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 
 from gpu_common import say, torch_gpu
-from seq_common import HALF_STEP, LEAST, dtype, f64
+from seq_common import HALF_STEP, LEAST, dtype, f64, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -120,6 +120,40 @@ def test_values_whose_squares_pass_32_bits():
     n = torch.empty(1, device="cuda")
     D.dtst_global_norm([torch.full((1 << 16,), 3e38, device="cuda")], n)   # beyond 32 bits
     assert math.isinf(float(n))
+
+
+# Eight values whose squares, added one after the other in 32 bits, put the norm 2.7, 3.1
+# and 2.7 units of 2^-24 off.
+EIGHT = {
+    "f32": ["0x1.04e430p-1", "0x1.6ddcd0p+0", "0x1.59e5d0p-1", "0x1.1b8b80p-1", "0x1.0e5008p+0", "0x1.c9a3d4p-2",
+            "0x1.1213f8p-2", "0x1.7ee75ap-3"],
+    "bf16": [0.0308837890625, 0.53125, 0.0257568359375, 0.0252685546875, 0.0308837890625, 0.036865234375, 0.0294189453125,
+             0.013916015625],
+    "f16": [0.744140625, 0.89111328125, 0.94140625, 1.4384765625, 0.30615234375, 0.44189453125, 0.66845703125, 0.25537109375],
+}
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_norm_of_one_group_and_of_equal_values(kind):
+    """The root's rounding to 32 bits, 2^-24, and half of those of two neighbours' squares:
+    two of 2^-24 of their sum (the first square's and the sum's), one of a 16-bit type,
+    whose squares 32 bits hold.  One group of eight, whose own roundings are all there
+    are, and equal values, whose roundings are all alike."""
+    torch, D = lib()
+    rng = np.random.RandomState(3)
+    bar = 2.0 if kind == "f32" else 1.5
+    values = [[float.fromhex(v) if isinstance(v, str) else v for v in EIGHT[kind]]]
+    values += list(rng.uniform(1, 2, (100, 8))) + [np.full(65536 + 8 * i, v) for i, v in enumerate(rng.uniform(1, 2, 100))]
+    values.append(np.full(65536, float.fromhex("0x1.cca210p+0")))
+    ts = [rounded(torch, v, kind)[0] for v in values]
+    n = torch.empty(len(ts), device="cuda")
+    for i, t in enumerate(ts):
+        D.dtst_global_norm([t], n[i])
+    want = np.array([norm64([t]) for t in ts])
+    off = np.abs(f64(n) / want - 1) * 2 ** 24
+    say(f"[clip] {kind}: the norm of eight {off[0]:.3f}, of others up to {off[1:101].max():.3f}, of equal ones up to "
+        f"{off[101:].max():.3f} units of 2^-24 off")
+    assert off.max() <= bar * (1 + 1e-6)
 
 
 def test_no_numbers_and_infinities():
