@@ -91,7 +91,8 @@ __device__ __forceinline__ float rsqrt_of(double m) {
 
 // RW waves a row, V vectors of 8 columns a lane: up to 512 RW V columns.  A
 // workgroup holds max(RW, 4) waves, so four rows with RW = 1.  (8: four registers fewer,
-// where they do not spill, hold one more wave a SIMD: 96.1 -> 94.8 us for the case above.)
+// where they do not spill, hold one more wave a SIMD: 96.1 -> 94.8 us for the case above; the
+// other forms were not timed with it.)
 template <class TX, class TR, bool Q8, int RW, int V, bool MEAN>
 __global__ void __launch_bounds__(RW > 4 ? RW * 64 : 256, MEAN && Q8 && RW == 4 && V == 2 && sizeof(TR) == 2 ? 8 : 1)
 norm_kernel(dtst_norm_desc d, double inv_cols, const TX* x, const TR* res, const float* __restrict__ w,

@@ -102,9 +102,13 @@ int launch_copy_states(const float* in, float* out, int64_t n, void* stream) {
 // 93 us with four a SIMD, 82 and 104 with three; 65536 x 1280 of 16: 589 us with three, 607
 // with four; 8 x 2048 x 1024 of 40: 375 with two, 460 with three), two a SIMD twice over, the
 // backward's (4 x 4096 x 2048 of 16, both directions: 891 us with 4096 waves; 1315, 912, 937
-// and 901 with 1024, 2048, 6144 and 8192).  Whole sequences from 1024 waves on: the second
-// pass over the steps costs more than waves side by side save (32 x 1024 x 4096 of 16: 571 us
-// whole, 908 in two).
+// and 901 with 1024, 2048, 6144 and 8192).  Whole sequences from 1024 waves on, as at 2048 the
+// second pass over the steps costs more than waves side by side save (32 x 1024 x 4096 of 16:
+// 571 us whole, 908 in two).  Between, neither wins: 512 steps x 4096 features, 1024, 1280,
+// 1536 and 1920 waves, whole and in segments, forward 143 184 185 187 and 137 158 185 213 us
+// with 4 states, 211 285 286 287 and 223 318 321 287 with 16, 671 908 911 912 and 756 909 911
+// 915 with 64; both directions 488 572 590 608 and 421 524 676 730, 937 1057 1085 1114 and 775
+// 1044 1287 1313, 3011 5478 5511 5570 and 3732 4858 5029 6250.  Lengths have no say in it.
 int scan_segments(int64_t batch, int64_t steps, int64_t features, int64_t states, bool adj) {
   const int64_t waves = batch * ((features + 63) / 64), spans = (steps + SCAN_SPAN - 1) / SCAN_SPAN;
   if (waves <= 0 || spans <= 1 || waves >= 1024) return 1;

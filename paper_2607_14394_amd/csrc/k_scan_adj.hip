@@ -77,15 +77,15 @@ __global__ void __launch_bounds__(256) scan_adj_lift_kernel(const ScanArgs p, co
 
 // Floats of LDS: e[N][64] | gA[N][64] | the sums' buffer | a span's sums of some states.
 // (Of all 64 states, they leave room for three waves a CU instead of four: 4 x 4096 x 512,
-// both directions, 1387 against 1127 us.)
+// both directions, 1387 against 1114 us.)
 constexpr int TOGETHER = 16;
 __host__ __device__ constexpr int adj_lds(int N, bool ends) {
   return N * 64 + (ends ? 0 : N * 64 + R * PITCH + (N < TOGETHER ? N : TOGETHER) * 2 * R);
 }
 
 // A wave's turn at its SIMD over others': first what ends in loads, stores or LDS, so that
-// the others' arithmetic covers the wait (4 x 4096 x 2048 of 16 states, both directions: 867
-// -> 854 us).
+// the others' arithmetic covers the wait (4 x 4096 x 2048 of 16 states, both directions: 852
+// -> 835 us).
 template <bool ENDS, int P>
 __device__ __forceinline__ void turn() {
   if constexpr (!ENDS) __builtin_amdgcn_s_setprio(P);
