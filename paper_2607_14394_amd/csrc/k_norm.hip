@@ -281,18 +281,18 @@ norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* _
       load_n<VEC>(u + row * d.ld_u + c, cols - c, h[i]);
     }
     if constexpr (MEAN) {
-      // Deviations from the mean in 32 bits, whose rounding they have in common: `low`,
-      // their own mean, is taken off as in the forward, in the sums' one round,
-      //   mean(t h) = r (mean(t v) - low mean t),  h = r (v - low).
+      // Deviations from the mean in 32 bits over the standard deviation, k, have its
+      // rounding in common: `low`, their own mean, is taken off as in the forward, in the
+      // sums' one round,  h = k - low,  mean(t h) = mean(t k) - low mean t.
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int64_t c = first + i * RW * 64 * VEC;
         if (c + VEC <= cols) {
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) h[i][j] -= m;
+          for (int j = 0; j < VEC; ++j) h[i][j] = (h[i][j] - m) * r;
         } else {
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) h[i][j] = c + j < cols ? h[i][j] - m : 0.f;
+          for (int j = 0; j < VEC; ++j) h[i][j] = c + j < cols ? (h[i][j] - m) * r : 0.f;
         }
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
@@ -328,12 +328,12 @@ norm_adj_kernel(dtst_norm_adj_desc d, const TX* g_y, const TR* u, const float* _
       }
       mean_t = sum / float(cols);
       const float low = shift / float(cols);
-      mean = r * (dot / float(cols) - low * mean_t);
+      mean = dot / float(cols) - low * mean_t;
 #pragma unroll
       for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          h[i][j] = (h[i][j] - low) * r;
+          h[i][j] -= low;
           gw[i][j] += g[i][j] * h[i][j];
           g[i][j] *= wv[i][j];
         }

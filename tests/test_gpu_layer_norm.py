@@ -190,6 +190,28 @@ def test_backward_of_a_mean_far_above_the_deviations(cols, t):
     near(f64(g_b), rb, "f32", "g_b", rms=np.sqrt(rows))
 
 
+@pytest.mark.parametrize("cols", [100, 1537, 9000])
+@pytest.mark.parametrize("values,gradients", [(1e-25, 1e-20), (1e25, 1e15), (1e25, 1e-10)])
+def test_backward_of_small_and_large_values(cols, values, gradients):
+    """A row's sums are of its deviations over their own size: products of gradients and
+    values that 32 bits do not hold change nothing.  The bars are the powers of the
+    scales times test_backward's."""
+    torch, D = lib()
+    rng = np.random.RandomState(cols)
+    rows = 7
+    u, uv = rounded(torch, (rng.randn(rows, cols) + 2) * values, "f32")
+    g, gv = rounded(torch, (rng.randn(rows, cols) + 0.5) * gradients, "f32")
+    w, wv = rounded(torch, 1 + 0.3 * rng.randn(cols), "f32")
+    _, mv, rv = S.layer_norm(uv, wv, None, 0.0)
+    mean, rstd = torch.from_numpy(mv).float().cuda(), torch.from_numpy(rv).float().cuda()
+    g_u, g_w, g_b = torch.empty_like(u), torch.empty_like(w), torch.empty_like(w)
+    D.dtst_layer_norm_adj(g, u, w, mean, rstd, g_u, g_w, g_b)
+    ru, rw, rb = S.layer_norm_adj(gv, uv, wv, 0.0)
+    near(f64(g_u) * (values / gradients), ru * (values / gradients), "f32", "g_u")
+    near(f64(g_w) / gradients, rw / gradients, "f32", "g_w", rms=np.sqrt(rows))
+    near(f64(g_b) / gradients, rb / gradients, "f32", "g_b", rms=np.sqrt(rows))
+
+
 def test_equal_columns_and_no_numbers():
     torch, D = lib()
     x = torch.randn(5, 300, device="cuda")
